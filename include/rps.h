@@ -73,8 +73,11 @@ typedef enum {
 #define RPS_DEVERR_WORKSPACE 0x20u /* the workspace was marked unhealthy by an earlier call that gave
                                       up (or holds a stale ticket): the call wrote no statistics;
                                       rps_workspace_init makes the workspace usable again */
+#define RPS_DEVERR_PAGE 0x40u      /* a page id outside the cache, or a length beyond the page table */
+#define RPS_DEVERR_NO_PAGES 0x80u  /* not enough free pages: a sequence was not grown */
+#define RPS_DEVERR_SHARED 0x100u   /* a write into a page that several sequences hold was left out */
 
-typedef enum { RPS_F32 = 0, RPS_BF16 = 1 } rps_dtype;
+typedef enum { RPS_F32 = 0, RPS_BF16 = 1, RPS_F16 = 2 /* K/V cache and its attention only */ } rps_dtype;
 
 /* Per-request state after rps_select_pivots. */
 typedef enum {
@@ -104,6 +107,12 @@ typedef enum {
 #define RPS_MAX_PIVOTS 16   /* P */
 #define RPS_MAX_POS 4096    /* L */
 #define RPS_MAX_SEGMENTS 1024
+#define RPS_KV_MIN_PAGE 16          /* tokens of a cache page: a power of two in this range */
+#define RPS_KV_MAX_PAGE 256
+#define RPS_KV_MAX_LAYERS 1024
+#define RPS_KV_MAX_HEADS 1024       /* heads of the cache */
+#define RPS_KV_MAX_SEQ (1 << 20)    /* n_req * n_branch */
+#define RPS_KV_MAX_GROUP 128        /* query heads per head of the cache */
 
 /* Hyper-parameters (Sec. 4 "Implementation details": k_max = 10, r = 0.1,
  * tau_pivot = 0.9 / 0.95, lambda in [0.1, 0.5]; Appendix C: tau = 0.9). */
@@ -484,6 +493,103 @@ typedef struct {
  * available. A bounded device wait that gives up reports RPS_DEVERR_TIMEOUT
  * (the output is then incomplete). */
 rps_status rps_packed_attention_fwd(const rps_packed_attention *attn, rps_stream_t stream);
+
+/*
+ * Paged K/V cache of the lookahead pass. The paper's packed pass recomputes the
+ * context's keys and values in every step; a denoiser that decodes block by
+ * block keeps them, and every branch of a request reads the same ones. The cache
+ * holds keys and values in pages of page_size tokens. Sequence s = q * n_branch
+ * + b is branch b of request q (b = 0: the base); its tokens 0..len[s]-1 lie in
+ * the pages table[s][0], table[s][1], ...; len[s] < 0: the sequence is absent
+ * and holds no page. page_ref[p] counts the table entries that hold page p; a
+ * page is free when its count is 0 (a caller may pin pages of its own by
+ * counting them once more). The caller starts with page_ref all 0 and len all
+ * -1; the calls below keep the three arrays consistent.
+ * Layout: k, v [n_layers][n_pages][n_heads][page_size][head_dim], head_dim
+ * contiguous, the other strides in elements and multiples of 8 (so either order
+ * of heads and tokens will do), bases 16-byte aligned. head_dim must be 128,
+ * page_size a power of two, 16..256. dtype RPS_BF16 or RPS_F16.
+ */
+typedef struct {
+    void *k, *v;
+    int32_t dtype;
+    int32_t n_layers, n_pages, n_heads, page_size, head_dim;
+    int64_t layer_stride, page_stride, head_stride, token_stride;
+    int32_t *page_ref; /* [n_pages] */
+    int32_t *table;    /* [n_req * n_branch][max_pages] */
+    int32_t *len;      /* [n_req * n_branch] */
+    int32_t n_req, n_branch, max_pages;
+} rps_kv_cache;
+
+/* Workspace bytes of the calls below that take one; 0 for an invalid cache. The
+ * workspace needs no initialisation and keeps nothing between calls. */
+size_t rps_kv_workspace_bytes(const rps_kv_cache *kv);
+
+/*
+ * Forks, moves and frees, all sequences at once (one launch): sequence s takes
+ * the state that sequence d_src[s] had before the call, cut to d_keep[s] tokens
+ * (d_keep NULL: whole; negative: none of it), or becomes absent (d_src[s] = -1).
+ * Pages are shared, not copied. Table entries past a sequence's pages become -1.
+ * d_src[s] outside -1..n_req*n_branch-1 sets RPS_DEVERR_ROW_INDEX and leaves
+ * sequence s as it is.
+ * rps_kv_fork_branches: the branches b >= 1 with d_branch_valid[q][b - 1] != 0
+ * (rps_pivots.branch_valid) take the base of their request, cut to
+ * d_ctx_len[q] tokens (NULL: whole); the others become absent; the base stays.
+ * rps_kv_commit: the base of request q takes the state of branch 1 + d_winner[q]
+ * (rps_commit_out.winner; a negative code keeps the base), every other sequence
+ * becomes absent and its pages are given back. A winner without such a branch
+ * sets RPS_DEVERR_ROW_INDEX and keeps the base.
+ */
+rps_status rps_kv_reorder(const rps_kv_cache *kv, const int32_t *d_src, const int32_t *d_keep, void *d_ws,
+                          size_t ws_bytes, rps_stream_t stream);
+rps_status rps_kv_fork_branches(const rps_kv_cache *kv, const uint8_t *d_branch_valid, const int32_t *d_ctx_len,
+                                void *d_ws, size_t ws_bytes, rps_stream_t stream);
+rps_status rps_kv_commit(const rps_kv_cache *kv, const int32_t *d_winner, void *d_ws, size_t ws_bytes,
+                         rps_stream_t stream);
+
+/*
+ * Every sequence becomes d_new_len[s] tokens long (negative: absent). First the
+ * shorter ones give back the pages past their end. Then the longer ones take
+ * pages, in ascending order of sequences, the lowest free ones first: as many as
+ * they lack, and one more in front where their last page is only partly filled
+ * and has a count above 1, which then gets a copy of that page's filled rows (of
+ * every layer) in its place. (All holders that grow copy it, the last one too.)
+ * A sequence is grown when the pages wanted by it and all sequences before it
+ * are there; otherwise it stays as it is and RPS_DEVERR_NO_PAGES is set. A
+ * length beyond max_pages pages sets RPS_DEVERR_PAGE and leaves its sequence as
+ * it is. The new tokens' rows are unwritten. Two launches.
+ */
+rps_status rps_kv_resize(const rps_kv_cache *kv, const int32_t *d_new_len, void *d_ws, size_t ws_bytes,
+                         rps_stream_t stream);
+
+/*
+ * Moves the live pages (count above 0) to the lowest places: with n_live of
+ * them, the i-th live page from n_live on goes to the i-th free place below
+ * n_live (both ascending; data of every layer, count and table entries). Pages
+ * below n_live stay. d_n_live (optional, device) receives n_live. Two launches.
+ */
+rps_status rps_kv_compact(const rps_kv_cache *kv, int32_t *d_n_live, void *d_ws, size_t ws_bytes, rps_stream_t stream);
+
+/*
+ * Copies page d_src[i] of `from` over page d_dst[i] of `to`, i < n, every layer
+ * (the caches may be the same; dtype, n_layers, n_heads and page_size agree,
+ * strides may differ; the bookkeeping arrays are not looked at). A page that is
+ * a destination twice, or a source and a destination, has unspecified content
+ * afterwards. An id outside its cache sets RPS_DEVERR_PAGE and copies nothing.
+ */
+rps_status rps_kv_copy_pages(const rps_kv_cache *from, const rps_kv_cache *to, const int32_t *d_src,
+                             const int32_t *d_dst, int32_t n, rps_stream_t stream);
+
+/*
+ * Keys and values of each sequence's last n_new tokens into layer `layer`: row i
+ * of sequence s goes to token len[s] - n_new + i (rows before token 0, and those
+ * of absent sequences, have no place and are left out). k_new, v_new
+ * [n_req * n_branch][n_new][n_heads][head_dim], head_dim contiguous, strides in
+ * elements, multiples of 8. A row whose page has a count above 1 is left out and
+ * sets RPS_DEVERR_SHARED (rps_kv_resize gives a growing sequence its own page).
+ */
+rps_status rps_kv_write(const rps_kv_cache *kv, int32_t layer, const void *k_new, const void *v_new, int32_t n_new,
+                        int64_t seq_stride, int64_t token_stride, int64_t head_stride, rps_stream_t stream);
 
 /* Synchronise `stream`, then read and clear the calling device's error word.
  * Returns RPS_OK or RPS_ERR_DEVICE (with the RPS_DEVERR_* bits in *detail when

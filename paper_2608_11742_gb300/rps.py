@@ -29,11 +29,12 @@ if not LIB_PATH.exists():
 _lib = C.CDLL(str(LIB_PATH))
 
 RPS_OK, RPS_ERR_INVALID_ARG, RPS_ERR_UNSUPPORTED, RPS_ERR_CUDA, RPS_ERR_DEVICE, RPS_ERR_TIMEOUT = range(6)
-RPS_F32, RPS_BF16 = 0, 1
+RPS_F32, RPS_BF16, RPS_F16 = 0, 1, 2
 STATE_SEARCH, STATE_DONE, STATE_NO_FEASIBLE, STATE_NO_CANDIDATES = 0, 1, 2, 3
 WIN_ANCHOR, WIN_SKIP, WIN_DONE = -1, -2, -3
 DEVERR_ROW_INDEX, DEVERR_NONFINITE, DEVERR_MASK, DEVERR_TOKEN = 0x1, 0x2, 0x4, 0x8
 DEVERR_TIMEOUT, DEVERR_WORKSPACE = 0x10, 0x20
+DEVERR_PAGE, DEVERR_NO_PAGES, DEVERR_SHARED = 0x40, 0x80, 0x100
 
 _p = C.c_void_p
 
@@ -138,6 +139,23 @@ class RpsPackedAttention(C.Structure):
 
 _lib.rps_packed_attention_fwd.restype = C.c_int
 _lib.rps_packed_attention_fwd.argtypes = [C.POINTER(RpsPackedAttention), _p]
+class RpsKvCache(C.Structure):
+    _fields_ = [("k", _p), ("v", _p), ("dtype", C.c_int32), ("n_layers", C.c_int32), ("n_pages", C.c_int32),
+                ("n_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32),
+                ("layer_stride", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("page_ref", _p), ("table", _p), ("len", _p), ("n_req", C.c_int32),
+                ("n_branch", C.c_int32), ("max_pages", C.c_int32)]
+
+
+# (structs by address, as for rps_run_step)
+_lib.rps_kv_workspace_bytes.restype = C.c_size_t
+_lib.rps_kv_workspace_bytes.argtypes = [_p]
+for _n, _a in (("reorder", [_p, _p, _p, _p, C.c_size_t, _p]), ("fork_branches", [_p, _p, _p, _p, C.c_size_t, _p]),
+               ("commit", [_p, _p, _p, C.c_size_t, _p]), ("resize", [_p, _p, _p, C.c_size_t, _p]),
+               ("compact", [_p, _p, _p, C.c_size_t, _p]), ("copy_pages", [_p, _p, _p, _p, C.c_int32, _p]),
+               ("write", [_p, C.c_int32, _p, _p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _p])):
+    _f = getattr(_lib, "rps_kv_" + _n)
+    _f.restype, _f.argtypes = C.c_int, _a
 _lib.rps_debug_set_ring_wait_ns.restype = C.c_uint64
 _lib.rps_debug_set_ring_wait_ns.argtypes = [C.c_uint64]
 
@@ -495,6 +513,157 @@ def rps_packed_attention_fwd(q: torch.Tensor, k: torch.Tensor, vt: torch.Tensor,
     a = RpsPackedAttention(q.data_ptr(), k.data_ptr(), vt.data_ptr(), out.data_ptr(), n_b, n_h, d, n_context,
                            n_branch, branch_len, scale)
     _check(_lib.rps_packed_attention_fwd(C.byref(a), _stream(stream)), "rps_packed_attention_fwd")
+
+
+# --------------------------------------------------------------------------- K/V cache
+_KV_DTYPES = {torch.bfloat16: RPS_BF16, torch.float16: RPS_F16}
+
+
+def _here(*tensors) -> None:
+    """The library launches on the current device: its tensors have to be there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors must be on the current CUDA device {dev}, got {t.device}")
+
+
+def _ints(name: str, t: torch.Tensor, n: int, dtype=torch.int32) -> int:
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
+    return t.data_ptr()
+
+
+class KvCacheBuf:
+    """Pages of a K/V cache and their bookkeeping (``rps_kv_cache`` of the C ABI).
+
+    ``k``, ``v`` ``[n_layers][n_pages][n_heads][page_size][128]`` (bf16 or fp16, any
+    order of heads and tokens in memory), ``page_ref`` ``[n_pages]``, ``table``
+    ``[n_req][n_branch][max_pages]`` and ``length`` ``[n_req][n_branch]``, int32."""
+
+    def __init__(self, k, v, page_ref=None, table=None, length=None):
+        self.k, self.v, self.page_ref, self.table, self.length = k, v, page_ref, table, length
+        self._key = None
+        self._c()
+
+    @staticmethod
+    def alloc(n_layers: int, n_pages: int, n_heads: int, page_size: int, n_req: int, n_branch: int, max_pages: int,
+              device, dtype=torch.bfloat16) -> "KvCacheBuf":
+        """A cache without sequences: every page free, every length -1."""
+        kv = lambda: torch.empty((n_layers, n_pages, n_heads, page_size, 128), dtype=dtype, device=device)
+        i = lambda v, *s: torch.full(s, v, dtype=torch.int32, device=device)
+        return KvCacheBuf(kv(), kv(), i(0, n_pages), i(-1, n_req, n_branch, max_pages), i(-1, n_req, n_branch))
+
+    @staticmethod
+    def of_pages(k, v) -> "KvCacheBuf":
+        """Pages alone, without bookkeeping (for rps_kv_copy_pages)."""
+        return KvCacheBuf(k, v)
+
+    def _c(self) -> int:
+        """Address of the C struct, built anew when a tensor moved or changed its layout."""
+        k, v, ref, table, length = self.k, self.v, self.page_ref, self.table, self.length
+        key = (k.data_ptr(), v.data_ptr(), k.shape, k.stride(), v.shape, v.stride(), k.dtype, v.dtype,
+               _ptr(ref), _ptr(table), _ptr(length), None if table is None else (ref.shape, table.shape, length.shape))
+        if key == self._key:
+            return self._at
+        if k.dtype not in _KV_DTYPES or v.dtype != k.dtype:
+            raise TypeError(f"k and v must both be bf16 or fp16, got {k.dtype} and {v.dtype}")
+        if k.dim() != 5 or v.shape != k.shape or k.stride(4) != 1 or v.stride() != k.stride():
+            raise ValueError("k and v: [layers][pages][heads][page size][head dim], head dim contiguous, same strides")
+        n_layers, n_pages, n_heads, ps, d = k.shape
+        n_req = n_branch = width = 0
+        if table is not None:
+            if table.dim() != 3 or length is None or ref is None:
+                raise ValueError("table [n_req][n_branch][max_pages] comes with page_ref and length")
+            n_req, n_branch, width = table.shape
+            _ints("page_ref", ref, n_pages)
+            _ints("table", table, n_req * n_branch * width)
+            _ints("length", length, n_req * n_branch)
+        self.n_seq = n_req * n_branch
+        self._struct = RpsKvCache(k.data_ptr(), v.data_ptr(), _KV_DTYPES[k.dtype], n_layers, n_pages, n_heads, ps, d,
+                                  *k.stride()[:4], _ptr(ref), _ptr(table), _ptr(length), n_req, n_branch, width)
+        self._at, self._key = C.addressof(self._struct), key
+        return self._at
+
+    def __getstate__(self):  # a copy or a pickle holds the tensors alone
+        return {n: getattr(self, n) for n in ("k", "v", "page_ref", "table", "length")}
+
+    def __setstate__(self, state):
+        self.__init__(**state)
+
+
+def rps_kv_workspace_bytes(kv: KvCacheBuf) -> int:
+    n = _lib.rps_kv_workspace_bytes(kv._c())
+    if n == 0:
+        raise RPSError(RPS_ERR_INVALID_ARG, "rps_kv_workspace_bytes")
+    return n
+
+
+def _kv_ws(kv: KvCacheBuf, ws: torch.Tensor, *more):
+    at = kv._c()
+    _here(kv.k, kv.table, ws, *more)
+    return at, ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def rps_kv_reorder(kv: KvCacheBuf, src: torch.Tensor, ws: torch.Tensor, keep: Optional[torch.Tensor] = None,
+                   stream=None) -> None:
+    """Every sequence takes the state of sequence ``src[s]`` (-1: none), cut to ``keep[s]`` tokens."""
+    at, p, n = _kv_ws(kv, ws, src, keep)
+    _check(_lib.rps_kv_reorder(at, _ints("src", src, kv.n_seq), None if keep is None else _ints("keep", keep, kv.n_seq),
+                               p, n, _stream(stream)), "rps_kv_reorder")
+
+
+def rps_kv_fork_branches(kv: KvCacheBuf, branch_valid: torch.Tensor, ctx_len: Optional[torch.Tensor], ws: torch.Tensor,
+                         stream=None) -> None:
+    """The valid branches (``PivotsBuf.branch_valid``) take their request's base, cut to ``ctx_len[q]`` tokens."""
+    at, p, n = _kv_ws(kv, ws, branch_valid, ctx_len)
+    n_req, nb = kv.table.shape[:2]
+    _check(_lib.rps_kv_fork_branches(at, _ints("branch_valid", branch_valid, n_req * (nb - 1), torch.uint8),
+                                     None if ctx_len is None else _ints("ctx_len", ctx_len, n_req), p, n,
+                                     _stream(stream)), "rps_kv_fork_branches")
+
+
+def rps_kv_commit(kv: KvCacheBuf, winner: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """Each base takes its winner's state (``CommitBuf.winner``); every branch gives its pages back."""
+    at, p, n = _kv_ws(kv, ws, winner)
+    _check(_lib.rps_kv_commit(at, _ints("winner", winner, kv.table.shape[0]), p, n, _stream(stream)), "rps_kv_commit")
+
+
+def rps_kv_resize(kv: KvCacheBuf, new_len: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """Every sequence becomes ``new_len[s]`` tokens long; a shared last page that grows is copied."""
+    at, p, n = _kv_ws(kv, ws, new_len)
+    _check(_lib.rps_kv_resize(at, _ints("new_len", new_len, kv.n_seq), p, n, _stream(stream)), "rps_kv_resize")
+
+
+def rps_kv_compact(kv: KvCacheBuf, n_live: Optional[torch.Tensor], ws: torch.Tensor, stream=None) -> None:
+    """The live pages move to the lowest places; ``n_live`` (int32[1], optional) receives their number."""
+    at, p, n = _kv_ws(kv, ws, n_live)
+    _check(_lib.rps_kv_compact(at, None if n_live is None else _ints("n_live", n_live, 1), p, n, _stream(stream)),
+           "rps_kv_compact")
+
+
+def rps_kv_copy_pages(src_kv: KvCacheBuf, dst_kv: KvCacheBuf, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """Pages ``src[i]`` of one cache over pages ``dst[i]`` of another (or the same), every layer."""
+    a, b = src_kv._c(), dst_kv._c()
+    _here(src_kv.k, dst_kv.k, src, dst)
+    n = src.numel()
+    _check(_lib.rps_kv_copy_pages(a, b, _ints("src", src, n), _ints("dst", dst, n), n, _stream(stream)),
+           "rps_kv_copy_pages")
+
+
+def rps_kv_write(kv: KvCacheBuf, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, stream=None) -> None:
+    """Keys and values ``[n_req][n_branch][n_new][n_heads][128]`` of each sequence's last ``n_new`` tokens."""
+    at = kv._c()
+    _here(kv.k, kv.table, k_new, v_new)
+    n_req, nb = kv.table.shape[:2]
+    shape, st = k_new.shape, k_new.stride()
+    if len(shape) != 5 or shape[:2] != (n_req, nb) or shape[3:] != (kv.k.shape[2], kv.k.shape[4]) or v_new.shape != shape:
+        raise ValueError("k_new and v_new: [n_req][n_branch][n_new][n_heads][head dim]")
+    if k_new.dtype != kv.k.dtype or v_new.dtype != kv.k.dtype:
+        raise TypeError(f"k_new and v_new must be {kv.k.dtype}, as the cache")
+    if st[4] != 1 or v_new.stride() != st or (n_req > 1 and nb > 1 and st[0] != nb * st[1]):
+        raise ValueError("k_new and v_new: head dim contiguous, the same strides, requests at n_branch sequences' stride")
+    _check(_lib.rps_kv_write(at, layer, k_new.data_ptr(), v_new.data_ptr(), shape[2], st[1] if nb > 1 else st[0], st[2],
+                             st[3], _stream(stream)), "rps_kv_write")
 
 
 # --------------------------------------------------------------------------- one step
