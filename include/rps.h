@@ -591,6 +591,58 @@ rps_status rps_kv_copy_pages(const rps_kv_cache *from, const rps_kv_cache *to, c
 rps_status rps_kv_write(const rps_kv_cache *kv, int32_t layer, const void *k_new, const void *v_new, int32_t n_new,
                         int64_t seq_stride, int64_t token_stride, int64_t head_stride, rps_stream_t stream);
 
+/*
+ * Attention of each sequence's newest tokens over its cached keys and values, the
+ * pages that the sequences of a request share read once for all of them. For query
+ * i of the n_q of sequence s with n = len[s] tokens, and for each query head h
+ * (heads h of the cache: h / (n_heads / kv->n_heads)):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,  lse = log sum_j exp(scale * q . k_j)
+ * over tokens j < n, or with causal != 0 over j <= n - n_q + i (the queries are the
+ * sequence's last tokens). fp32 scores, sums and accumulation; probabilities are
+ * rounded to the cache's type before they weight the values, the output to it at
+ * the end. A query that sees nothing (n = 0, or causal with n < n_q - i), or whose
+ * scores are all -inf, gets out = 0 and lse = -inf. Rows of absent sequences (len <
+ * 0) are left as they are.
+ * shared_len[q] (device, NULL: 0): the leading tokens whose pages all present
+ * sequences of request q hold in common (as after rps_kv_fork_branches with the
+ * same d_ctx_len); whole pages below it, as far as every sequence reaches, are read
+ * through the table row of one sequence. Tokens past a sequence's length, and
+ * pages that no sequence holds, may hold anything; the values of tokens below the
+ * lengths must be finite where several queries share them (a value of inf or NaN
+ * also reaches the queries of its request that share its page, and earlier queries
+ * of its sequence). A page id outside the cache makes the rows that see its keys
+ * NaN and sets RPS_DEVERR_PAGE; a length beyond the table counts as the table's
+ * capacity.
+ * q, out [n_req][n_branch * n_q][n_heads][128] of the cache's dtype, 128
+ * contiguous, other strides in elements, multiples of 8, bases 16-byte aligned;
+ * lse [n_req][n_branch * n_q][n_heads] fp32 or NULL. n_heads a multiple of
+ * kv->n_heads, at most RPS_KV_MAX_GROUP times it. out must not overlap q or the
+ * cache. The lengths and the tables must not change during the call.
+ */
+typedef struct {
+    const void *q;
+    void *out;
+    float *lse;
+    int32_t n_q, n_heads, layer, causal;
+    int64_t q_req_stride, q_token_stride, q_head_stride;
+    int64_t out_req_stride, out_token_stride, out_head_stride;
+    const int32_t *shared_len;
+    float scale;
+} rps_prefix_attention;
+
+/* Workspace bytes of rps_prefix_attention_fwd (0 for invalid arguments). The
+ * workspace needs no initialisation and keeps nothing between calls; one workspace
+ * must not serve two calls that can overlap. */
+size_t rps_prefix_attention_workspace_bytes(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads);
+
+/* Two launches on `stream`. Errors: RPS_ERR_INVALID_ARG for NULL or misaligned
+ * pointers, sizes or strides out of range, or a small workspace;
+ * RPS_ERR_UNSUPPORTED beyond the limits above or 2^23 tokens of a request;
+ * RPS_ERR_CUDA when the tensor-map encoder is not available. A bounded device wait
+ * that gives up reports RPS_DEVERR_TIMEOUT (the output is then incomplete). */
+rps_status rps_prefix_attention_fwd(const rps_prefix_attention *attn, const rps_kv_cache *kv, void *d_ws,
+                                    size_t ws_bytes, rps_stream_t stream);
+
 /* Synchronise `stream`, then read and clear the calling device's error word.
  * Returns RPS_OK or RPS_ERR_DEVICE (with the RPS_DEVERR_* bits in *detail when
  * detail != NULL), or RPS_ERR_CUDA if the synchronisation itself failed. */

@@ -24,7 +24,7 @@ FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcomp
 
 LIBS = {
     "librps.so": ["abi.cu", "rowstats.cu", "decide.cu", "decode.cu", "gather.cu", "static_scratch.cu", "lmhead.cu", "attention.cu",
-                  "kvcache.cu"],
+                  "kvcache.cu", "prefix_attention.cu"],
     "librps_synth.so": ["synth.cu"],
 }
 HEADERS = sorted([*INCLUDE.glob("*.h"), *CSRC.glob("*.h"), *CSRC.glob("*.cuh")])

@@ -1,0 +1,1135 @@
+// prefix_attention.cu -- attention of the sequences' newest tokens over the paged
+// K/V cache, the pages that the sequences of a request share read once for all of
+// them (rps_prefix_attention_fwd).
+//
+// For query i of a sequence, out = sum_j softmax_j(scale q . k_j) v_j over the keys
+// it sees. The softmax over two sets of keys is joined from the sets' maxima m, sums
+// l and weighted sums o: with m = max(m1, m2) both sides are weighted by
+// 2^(m_x - m) and added. So the keys of a row may be taken in any pieces: the
+// sequences of a request, and the query heads that share a cache head, are stacked
+// as the 128 rows of one matrix product with the shared keys; their own keys follow
+// as further key tiles of the same row tile, each 16-key step of the product
+// writing only its sequence's rows; and the key tiles of all row tiles are dealt
+// evenly to the CTAs (prefix_split.h), whose partial (m, l, o) a second launch joins.
+//
+// One persistent CTA per SM takes pieces (row tile, key tiles [j0, j1)). Key tiles
+// are numbered through its pieces; even and odd ones go to two independent halves
+// of the softmax, each with its own S / P buffer, maxima, sums and accumulator:
+//   warp 3      scheduler: finds the pieces from the lengths in device memory and
+//               hands them to the other roles through a ring in shared memory;
+//   warp 0      TMA producer of Q (a box of tokens x heads of the group) and of K,
+//               one box per slot of pages, addresses through the page table;
+//   warp 2      TMA producer of V, in the same way. V lies token by token in the
+//               cache, so it is the MN-major operand of the second product: no
+//               transposed copy of the values is kept;
+//   warp 1      MMA issuer: S = Q K^T into TMEM buffer t % 2, O[t % 2] += P V with P
+//               from TMEM, in the order PV(t), S(t + 2), PV(t + 1), ...; it also
+//               clears the rows of V past a sequence's last key (they may hold
+//               anything, and 0 * NaN would reach the sums);
+//   warps 4-7   softmax of even tiles, 8-11 of odd ones: thread = row. The base-2
+//               reference m is raised only when a score passes it by more than 8.
+//               P is rounded to the cache's type (the product takes no other);
+//   warps 12-15 read-out: the halves' accumulators weighted and added; written as
+//               output rows, or as fp32 partial results where a piece is not all
+//               of its row tile.
+// Every wait is bounded; a role whose wait runs out flags RPS_DEVERR_TIMEOUT and
+// raises the CTA's abort flag, copies and MMAs in flight are drained and TMEM is
+// freed before the CTA exits.
+#include <cuda.h>  // CUtensorMap and the tensor-map encoder's signature (no link against the driver)
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <mutex>
+
+#include "prefix_split.h"
+#include "rps_internal.cuh"
+#include "tc_device.cuh"
+#include "umma_desc.h"
+
+namespace rps {
+namespace {
+
+using prefix::KeySum;
+using prefix::RowTile;
+using prefix::Shape;
+
+constexpr int kD = 128;                // head dimension
+constexpr int kAtom = 64 * 128 * 2;    // one 128-row x 64-column swizzle atom of 16-bit elements: 16 KB
+constexpr int kTileBytes = 2 * kAtom;  // a Q, K or V tile: two atoms along d
+constexpr int kStages = 2;             // of K and of V: a tile's stage, S / P buffer and O go by its parity
+constexpr int kQBufs = 2;
+constexpr int kStageBytes = 32 * 128;  // per read-out warp: 32 rows x 128 bytes on their way out
+constexpr int kSmemBytes = kQBufs * kTileBytes + 2 * kStages * kTileBytes + 4 * kStageBytes + 1024;
+constexpr int kThreads = 512;
+// 128 x 56 + 256 x 176 + 128 x 104 = 65,536 registers of the 512 x 128 of the launch
+constexpr int kCtlRegs = 56, kSoftRegs = 176, kOutRegs = 104;
+static_assert(128 * kCtlRegs + 256 * kSoftRegs + 128 * kOutRegs <= 512 * 128, "the split fits the launch's registers");
+constexpr uint32_t kTmemCols = 512;  // S buffers at columns 0 and 128, O at 256 and 384
+constexpr uint32_t kOCol = 256;
+constexpr int kRing = 4;             // pieces known ahead
+constexpr int kConsumers = 15;       // warps 0, 1, 2 and 4..15
+constexpr int kMaxSeqs = 128;        // sequences with rows in one row tile
+constexpr int kMaxCtas = 160;
+constexpr int kStagedLens = (2 * kStages * kTileBytes) / 4;  // lengths that fit the K and V stages
+constexpr int kCombineThreads = 256;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// A row tile that is cut: the CTA that takes its first key tile writes where its parts are.
+struct Cut {
+    int32_t parts;  // 0: none
+    int32_t q, head, rt;
+};
+
+struct PrefixArgs {
+    Shape s;
+    const int32_t *table, *len, *shared_len;
+    int32_t n_heads;  // query heads
+    void *out;
+    int64_t out_req, out_token, out_head;
+    float *lse;
+    float c;  // scale * log2(e)
+    Cut *cut;       // [kMaxCtas]
+    float2 *part_ml;  // [2 * kMaxCtas][128]: maximum and sum of each row of a partial result
+    float *part_o;    // [2 * kMaxCtas][128][128]
+    uint32_t *err;
+    uint64_t wait_ns;
+};
+
+struct Piece {
+    int32_t q, head, rt;
+    RowTile r;
+    int32_t j0, j1, shared, shared_tiles, shared_row;  // shared slots; whose table row names their pages
+    int32_t part;                                      // -1: the whole row tile, else which partial result
+    int32_t off[kMaxSeqs + 1], len[kMaxSeqs];
+};
+
+struct Ctl {
+    // s_full[t % 2]: S of tile t is computed and the product of tile t - 2 is done, so
+    // K stage t % 2 is free, and Q of the pieces before t's. V stages have a commit of
+    // their own. No wait sees a barrier two phases on: each waits for every phase in turn.
+    uint64_t q_full[kQBufs], k_full[kStages], v_full[kStages], v_empty[kStages];
+    uint64_t s_full[kStages], p_full[kStages], o_ready, o_free, mma_done;
+    uint64_t ring_full[kRing], ring_empty[kRing];
+    // a half's reference and sum of a row at the end of piece n, in slot n % 4: written before
+    // the half's last P of the piece is handed on, read once O is ready, and written again for
+    // piece n + 4, whose P needs the products of piece n + 2 and so the read-out of piece n + 1
+    float2 ml[4][kStages][prefix::kRows];
+    Piece ring[kRing];
+    uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
+    int64_t scan[16];
+    int64_t p0, p1;
+    int32_t find_q, find_rt, find_j;
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+// ---------------------------------------------------------------- the cut
+__device__ __forceinline__ int len_of(const PrefixArgs &a, int64_t s, const int32_t *staged) {
+    return prefix::used_len(a.s, staged ? staged[s] : a.len[s]);
+}
+__device__ __forceinline__ int shared_len_of(const PrefixArgs &a, int q) { return a.shared_len ? a.shared_len[q] : 0; }
+
+// Key tiles of entry e = (request, row tile), by one thread.
+__device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int64_t e, const int32_t *staged) {
+    const int q = static_cast<int>(e / a.s.row_tiles);
+    const RowTile r = prefix::row_tile(a.s, static_cast<int>(e - static_cast<int64_t>(q) * a.s.row_tiles));
+    KeySum k{0, 0, INT32_MAX};
+    const int64_t s0 = static_cast<int64_t>(q) * a.s.n_branch + r.b0;
+    for (int i = 0; i < r.nb; ++i) prefix::add_sequence(a.s, k, len_of(a, s0 + i, staged));
+    return prefix::key_tiles(a.s, k, prefix::shared_slots(a.s, k, shared_len_of(a, q)));
+}
+
+// Exclusive prefix sum over the block's 512 threads; *total: the block's sum.
+__device__ __forceinline__ int64_t scan_block(int v, int64_t *sums, int64_t *total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t u = __shfl_up_sync(kFull, x, o);
+        if (lane >= o) x += u;
+    }
+    __syncthreads();  // (the sums of an earlier scan are read)
+    if (lane == 31) sums[warp] = x;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) before += sums[w];
+        all += sums[w];
+    }
+    *total = all;
+    return before + x - v;
+}
+
+// Where the CTA's range begins: request, cache head, row tile, key tile; and its length.
+struct Start {
+    int32_t q, head, rt, j;
+    int64_t at, end, work;
+    int32_t n;  // CTAs with work
+};
+
+__device__ Start find_start(const PrefixArgs &a, Ctl &c, int32_t *stage) {
+    const int64_t entries = static_cast<int64_t>(a.s.n_req) * a.s.row_tiles;
+    const int64_t n_seq = static_cast<int64_t>(a.s.n_req) * a.s.n_branch;
+    const int32_t *staged = nullptr;
+    if (n_seq <= kStagedLens) {
+        for (int i = threadIdx.x; i < n_seq; i += kThreads) stage[i] = a.len[i];
+        __syncthreads();
+        staged = stage;
+    }
+    // passes over the entries in blocks of 512; of a single block everything stays in registers
+    const bool one = entries <= kThreads;
+    int t0 = 0;
+    int64_t before0 = 0, total = 0, carry = 0;
+    for (int64_t base = 0; base < entries; base += kThreads) {
+        t0 = base + threadIdx.x < entries ? entry_tiles(a, base + threadIdx.x, staged) : 0;
+        before0 = carry + scan_block(t0, c.scan, &total);
+        carry += total;
+    }
+    Start st{};
+    st.work = carry * a.s.heads;
+    // (no more CTAs than key tiles: none in between is without work)
+    st.n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), st.work));
+    if (static_cast<int>(blockIdx.x) >= st.n) return st;
+    st.at = prefix::range_start(blockIdx.x, st.work, st.n);
+    st.end = prefix::range_start(blockIdx.x + 1, st.work, st.n);
+    // Each pass looks at (tiles, tiles before) of every entry. First the last request that
+    // starts at or before the range, then that request's bounds, then the entry in it.
+    for (int pass = 0; pass < 3; ++pass) {
+        __syncthreads();
+        if (threadIdx.x == 0 && pass == 0) c.find_q = 0;
+        const int q_at = pass ? c.find_q : 0;
+        int64_t in_head = 0;
+        if (pass == 2) {
+            const int64_t per_head = c.p1 - c.p0, rem = st.at - a.s.heads * c.p0;
+            st.head = static_cast<int>(rem / per_head);
+            in_head = c.p0 + rem - st.head * per_head;
+        }
+        __syncthreads();
+        carry = 0;
+        for (int64_t base = 0; base < entries; base += kThreads) {
+            const int64_t e = base + threadIdx.x;
+            int t = t0;
+            int64_t before = before0;
+            if (!one) {
+                t = e < entries ? entry_tiles(a, e, staged) : 0;
+                before = carry + scan_block(t, c.scan, &total);
+                carry += total;
+            }
+            if (e >= entries) continue;
+            const int q = static_cast<int>(e / a.s.row_tiles);
+            const int rt = static_cast<int>(e - static_cast<int64_t>(q) * a.s.row_tiles);
+            if (pass == 0) {
+                if (rt == 0 && before * a.s.heads <= st.at) atomicMax(&c.find_q, q);
+            } else if (q == q_at) {
+                if (pass == 1) {
+                    if (rt == 0) c.p0 = before;
+                    if (rt == a.s.row_tiles - 1) c.p1 = before + t;
+                } else if (before <= in_head && in_head < before + t) {
+                    c.find_rt = rt;
+                    c.find_j = static_cast<int>(in_head - before);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    st.q = c.find_q;
+    st.rt = c.find_rt;
+    st.j = c.find_j;
+    return st;
+}
+
+// Row tile rt of request q, by a warp: sequences' lengths and own slots into `p`;
+// returns its number of key tiles (0: no sequence there, `p` is not complete).
+__device__ int fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, Piece &p) {
+    const RowTile r = prefix::row_tile(a.s, rt);
+    const int64_t s0 = static_cast<int64_t>(q) * a.s.n_branch + r.b0;
+    KeySum k{0, 0, INT32_MAX};
+    int first = INT32_MAX, len[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const int i = x * 32 + lane;
+        len[x] = i < r.nb ? len_of(a, s0 + i, nullptr) : -1;
+        prefix::add_sequence(a.s, k, len[x]);
+        if (len[x] >= 0) first = min(first, i);
+    }
+    k.present = warp_sum_int(k.present);
+    k.slots = warp_sum_int(k.slots);
+    k.min_pages = warp_min_int(k.min_pages);
+    first = warp_min_int(first);
+    const int shared = prefix::shared_slots(a.s, k, shared_len_of(a, q));
+    const int tiles = prefix::key_tiles(a.s, k, shared);
+    if (tiles == 0) return 0;
+    int before = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const int i = x * 32 + lane;
+        const int own = len[x] < 0 ? 0 : prefix::ceil_div(len[x], a.s.slot) - shared;
+        int upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(kFull, upto, o);
+            if (lane >= o) upto += u;
+        }
+        if (i < r.nb) {
+            p.len[i] = len[x];
+            p.off[i + 1] = before + upto;
+        }
+        before += __shfl_sync(kFull, upto, 31);
+    }
+    if (lane == 0) {
+        p.off[0] = 0;
+        p.q = q;
+        p.rt = rt;
+        p.r = r;
+        p.shared = shared;
+        p.shared_tiles = prefix::ceil_div(shared, a.s.spt);
+        p.shared_row = static_cast<int>(s0) + first;
+    }
+    return tiles;
+}
+
+// ---------------------------------------------------------------- roles
+// Piece n of the CTA, once the scheduler has it (nullptr: the wait ran out).
+__device__ __forceinline__ const Piece *next_piece(int n, Ctl &c, const PrefixArgs &a) {
+    if (!warp_wait_or_abort(&c.ring_full[n % kRing], (n / kRing) & 1, c, a)) return nullptr;
+    return &c.ring[n % kRing];
+}
+__device__ __forceinline__ void release_piece(int n, int lane, Ctl &c) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&c.ring_empty[n % kRing]);
+}
+
+// The page (id, and first token in it) of slot `lane` of key tile j; an id outside
+// the cache gives n_pages, whose copy is all zeros. `there`: the tile has that slot.
+__device__ __forceinline__ void slot_page(const PrefixArgs &a, const Piece &p, int j, int lane, int &page, int &token,
+                                          bool &there) {
+    int row, x;
+    page = a.s.n_pages;
+    token = 0;
+    if (j < p.shared_tiles) {
+        x = j * a.s.spt + lane;
+        there = x < p.shared;
+        row = p.shared_row;
+    } else {
+        const int o = (j - p.shared_tiles) * a.s.spt + lane;
+        there = o < p.off[p.r.nb];
+        const int i = there ? prefix::slot_owner(p.off, p.r.nb, o) : 0;
+        x = o - p.off[i] + p.shared;
+        row = p.q * a.s.n_branch + p.r.b0 + i;
+    }
+    if (!there) return;
+    const int e = x / a.s.sub;
+    token = (x - e * a.s.sub) * a.s.slot;
+    page = a.table[static_cast<int64_t>(row) * a.s.max_pages + e];
+    if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.s.n_pages)) page = a.s.n_pages;
+}
+
+// The producers of K (with Q) and of V.
+template <bool kIsK>
+__device__ __forceinline__ void produce(const CUtensorMap *tm, const CUtensorMap *tm_q, uint8_t *stages, uint8_t *sq,
+                                        uint32_t tiles, int lane, Ctl &c, const PrefixArgs &a) {
+    uint32_t t = 0;
+    int n = 0, n_q = 0;
+    bool ok = true;
+    const uint32_t q_bytes = 2u * a.s.group * a.s.tokens * 128;
+    for (; t < tiles && ok; ++n) {
+        const Piece *pp = next_piece(n, c, a);
+        if (!pp) break;
+        const Piece &p = *pp;
+        for (int j = p.j0; j < p.j1; ++j, ++t) {
+            const int s = t % kStages;
+            int page, token;
+            bool there = false;
+            if (lane < a.s.spt) slot_page(a, p, j, lane, page, token, there);
+            if (kIsK) {
+                // S of tile t - 2 is computed: its K stage is free, and at a piece's first tile
+                // the Q buffer of piece n - 2, whose last tile is no later
+                if (t >= kStages && !warp_wait_or_abort(&c.s_full[s], (t / kStages - 1) & 1, c, a)) {
+                    ok = false;
+                    break;
+                }
+                if (j == p.j0) ++n_q;
+                const uint32_t bad = __ballot_sync(kFull, there && page == a.s.n_pages);
+                if (lane == 0) {
+                    c.bad[t % 4] = bad;
+                    if (bad) flag_error(a.err, RPS_DEVERR_PAGE);
+                    if (j == p.j0) {
+                        mbar_expect_tx(&c.q_full[n & 1], q_bytes);
+                        uint8_t *dst = sq + (n & 1) * kTileBytes;
+                        tma_load_4d(dst, tm_q, 0, p.head * a.s.group, p.r.tok0, p.q, &c.q_full[n & 1]);
+                        tma_load_4d(dst + kAtom, tm_q, 64, p.head * a.s.group, p.r.tok0, p.q, &c.q_full[n & 1]);
+                    }
+                }
+            } else if (!warp_wait_or_abort(&c.v_empty[s], ((t / kStages) & 1) ^ 1, c, a)) {
+                ok = false;
+                break;
+            }
+            uint64_t *full = kIsK ? &c.k_full[s] : &c.v_full[s];
+            if (lane == 0) mbar_expect_tx(full, kTileBytes);
+            __syncwarp();
+            if (lane < a.s.spt) {  // (slots that are not there: zeros)
+                uint8_t *dst = stages + s * kTileBytes + lane * a.s.slot * 128;
+                tma_load_4d(dst, tm, 0, token, p.head, page, full);
+                tma_load_4d(dst + kAtom, tm, 64, token, p.head, page, full);
+            }
+            __syncwarp();
+        }
+        if (ok) release_piece(n, lane, c);
+    }
+    // every copy issued lands before the CTA leaves
+    if (lane == 0) {
+        for (uint32_t x = t > kStages ? t - kStages : 0; x < t; ++x)
+            wait_drain(kIsK ? &c.k_full[x % kStages] : &c.v_full[x % kStages], (x / kStages) & 1);
+        if (kIsK)
+            for (int x = n_q > kQBufs ? n_q - kQBufs : 0; x < n_q; ++x) wait_drain(&c.q_full[x & 1], (x >> 1) & 1);
+    }
+    __syncwarp();
+}
+
+// The scheduler: the pieces of [st.at, st.end) into the ring.
+__device__ __forceinline__ void schedule(const PrefixArgs &a, const Start &st, int lane, Ctl &c) {
+    int q = st.q, head = st.head, rt = st.rt, j = st.j, n = 0;
+    int64_t at = st.at;
+    bool any = true;  // the request has a key tile at all
+    while (at < st.end) {
+        if (n >= kRing && !warp_wait_or_abort(&c.ring_empty[n % kRing], (n / kRing - 1) & 1, c, a)) return;
+        Piece &p = c.ring[n % kRing];
+        int tiles = 0;
+        for (;;) {
+            tiles = fill_row_tile(a, q, rt, lane, p);
+            any |= tiles > 0;
+            if (tiles > 0) break;
+            if (++rt == a.s.row_tiles) {
+                rt = 0;
+                if (!any || ++head == a.s.heads) {
+                    head = 0;
+                    ++q;
+                }
+                any = false;
+            }
+            if (q >= a.s.n_req) return;  // (not reached while the lengths stay as they are during the call)
+        }
+        if (j >= tiles) return;          // (nor this)
+        const int j1 = static_cast<int>(min(static_cast<int64_t>(tiles), j + (st.end - at)));
+        if (lane == 0) {
+            p.head = head;
+            p.j0 = j;
+            p.j1 = j1;
+            p.part = j == 0 && j1 == tiles ? -1 : j > 0 ? 0 : 1;
+            if (p.part == 1) {
+                const int last = prefix::last_cta(at + tiles, st.work, st.n);
+                a.cut[blockIdx.x] = Cut{last - static_cast<int>(blockIdx.x) + 1, q, head, rt};
+            }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c.ring_full[n % kRing]);
+        at += j1 - j;
+        j = 0;
+        ++n;
+        if (++rt == a.s.row_tiles) {
+            rt = 0;
+            if (++head == a.s.heads) {
+                head = 0;
+                ++q;
+                any = false;
+            }
+        }
+    }
+}
+
+// The MMA issuer (lane 0 issues, the warp stays converged).
+template <bool kF16>
+__device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t *sv, uint32_t tmem, uint32_t tiles,
+                                               int lane, Ctl &c, const PrefixArgs &a) {
+    constexpr uint32_t fmt = kF16 ? umma::kFmtF16 : umma::kFmtBF16;
+    constexpr uint32_t idesc_s = umma::instr_desc_f16(128, 128, fmt, 0);  // K is K-major
+    constexpr uint32_t idesc_o = umma::instr_desc_f16(128, 128, fmt, 1);  // V is MN-major
+    const uint32_t issue = lane == 0;
+    bool ok = true;
+    int sn = 0, sj = 0, sj1 = 0;  // the scores' piece, tile, and the piece's end
+    const auto scores = [&](uint32_t t) -> bool {  // S_t = Q K_t^T into buffer t % 2
+        if (sj == sj1) {
+            const Piece *p = next_piece(sn, c, a);
+            if (!p) return false;
+            sj = p->j0;
+            sj1 = p->j1;
+            if (!warp_wait_or_abort(&c.q_full[sn & 1], (sn >> 1) & 1, c, a)) return false;
+            ++sn;
+        }
+        const int qb = (sn - 1) & 1, s = t % kStages;
+        if (!warp_wait_or_abort(&c.k_full[s], (t / kStages) & 1, c, a)) return false;
+        tc_fence_after();
+        const uint64_t qd = umma::smem_desc_kmajor_sw128(saddr(sq + qb * kTileBytes));
+        const uint64_t qd1 = umma::smem_desc_kmajor_sw128(saddr(sq + qb * kTileBytes + kAtom));
+        const uint64_t kd = umma::smem_desc_kmajor_sw128(saddr(sk + s * kTileBytes));
+        const uint64_t kd1 = umma::smem_desc_kmajor_sw128(saddr(sk + s * kTileBytes + kAtom));
+        const uint32_t sbuf = tmem + s * 128;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            mma_bf16(sbuf, umma::advance_k16(k < 4 ? qd : qd1, k & 3), umma::advance_k16(k < 4 ? kd : kd1, k & 3),
+                     idesc_s, k != 0, issue);
+        mma_commit(&c.s_full[s], issue);
+        ++sj;
+        return true;
+    };
+    uint32_t t = 0;
+    for (uint32_t x = 0; x < min(tiles, static_cast<uint32_t>(kStages)) && ok; ++x) ok = scores(x);
+    for (int n = 0; t < tiles && ok; ++n) {
+        const Piece *pp = next_piece(n, c, a);
+        if (!pp) break;
+        const Piece &p = *pp;
+        for (int j = p.j0; j < p.j1; ++j, ++t) {
+            const int h = t % kStages;
+            prefix::Step st{};
+            if (j >= p.shared_tiles)
+                st = prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane & 7);
+            // the first product of a piece overwrites O: the previous piece's read-out must be done
+            if ((j == p.j0 && !warp_wait_or_abort(&c.o_free, (n & 1) ^ 1, c, a)) ||
+                !warp_wait_or_abort(&c.v_full[h], (t / kStages) & 1, c, a)) {
+                ok = false;
+                break;
+            }
+            uint8_t *vb = sv + h * kTileBytes;
+            if (j >= p.shared_tiles) {  // rows of V past a sequence's last key
+                const uint32_t ragged = __ballot_sync(kFull, lane < 8 && st.keys > 0 && st.keys < 16);
+                if (ragged) {
+                    for (uint32_t m = ragged; m; m &= m - 1) {
+                        const int kk = __ffs(m) - 1, keys = __shfl_sync(kFull, st.keys, kk);
+                        for (int x = lane; x < (16 - keys) * 16; x += 32)  // 8 16-byte units in each of two atoms
+                            st_shared_v4(saddr(vb + (x & 8 ? kAtom : 0) + (kk * 16 + keys + (x >> 4)) * 128 + (x & 7) * 16),
+                                         make_uint4(0, 0, 0, 0));
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+            }
+            if (!warp_wait_or_abort(&c.p_full[h], (t / kStages) & 1, c, a)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            // P of keys 16k..16k+15: columns 8k..8k+7 of S buffer t % 2
+            const uint32_t pcol = tmem + h * 128, ocol = tmem + kOCol + h * 128;
+            const uint64_t vd = umma::smem_desc_mnmajor_sw128(saddr(vb), kAtom);
+            if (j < p.shared_tiles) {
+                const uint32_t more = j - p.j0 >= kStages;  // the half has had a tile of this piece
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    mma_bf16_ts(ocol, pcol + k * 8, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o, more | (k != 0),
+                                issue);
+            } else {
+                for (uint32_t m = __ballot_sync(kFull, lane < 8 && st.keys > 0); m; m &= m - 1) {
+                    const int k = __ffs(m) - 1;
+                    const int r0 = __shfl_sync(kFull, st.r0, k), r1 = __shfl_sync(kFull, st.r1, k);
+                    const uint32_t fresh = __shfl_sync(kFull, st.fresh, k);
+                    uint32_t off[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) off[w] = ~(low_bits(r1 - 32 * w) & ~low_bits(r0 - 32 * w));
+                    mma_bf16_ts_rows(ocol, pcol + k * 8, vd + static_cast<uint64_t>(k) * (2048 >> 4), idesc_o, off,
+                                     fresh ^ 1u, issue);
+                }
+            }
+            mma_commit(&c.v_empty[h], issue);
+            if (j == p.j1 - 1) mma_commit(&c.o_ready, issue);  // the piece's O is complete
+            if (t + kStages < tiles && !(ok = scores(t + kStages))) break;
+        }
+        if (ok) release_piece(n, lane, c);
+    }
+    mma_commit(&c.mma_done, issue);
+    if (lane == 0) wait_drain(&c.mma_done, 0);
+    __syncwarp();
+}
+
+// Softmax of the tiles of half h; this thread's row is TMEM lane r.
+template <bool kF16>
+__device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, uint32_t tiles, Ctl &c,
+                                        const PrefixArgs &a) {
+    const int r = q * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>(q * 32) << 16;
+    const uint32_t sbuf = tmem + lane_off + h * 128, obuf = tmem + lane_off + kOCol + h * 128;
+    const int tok = r / a.s.group;  // the row's token in the tile
+    bool ok = true;
+    uint32_t t0 = 0;  // first tile of the piece
+    for (int n = 0; t0 < tiles && ok; ++n) {
+        const Piece *pp = next_piece(n, c, a);
+        if (!pp) break;
+        const Piece &p = *pp;
+        int limit = 0, own_off = 0, own_end = 0;
+        bool live = false;
+        if (tok < p.r.n_tok) {
+            const int g = p.r.tok0 + tok, b = g / a.s.n_q, i = b - p.r.b0;
+            live = p.len[i] >= 0;
+            limit = prefix::row_limit(a.s, p.len[i], g - b * a.s.n_q);
+            own_off = p.off[i];
+            own_end = p.off[i + 1];
+        }
+        float m = -INFINITY, l = 0.f;
+        const int count = p.j1 - p.j0, x0 = (h ^ static_cast<int>(t0)) & 1;
+        for (int x = x0; x < count; x += kStages) {
+            const uint32_t t = t0 + x;
+            const int j = p.j0 + x;
+            prefix::Columns col = prefix::row_columns(a.s, j, p.shared_tiles, p.shared, own_off, limit);
+            if (!warp_wait_or_abort(&c.s_full[h], (t / kStages) & 1, c, a)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const uint32_t bad = c.bad[t % 4];
+            if (bad && col.lo < col.hi) {  // a page of this row's keys does not exist: NaN
+                const int u0 = col.lo / a.s.slot, u1 = (col.hi - 1) / a.s.slot;
+                if (bad >> u0 & low_bits(u1 - u0 + 1)) {
+                    l = NAN;
+                    col.hi = col.lo;
+                }
+            }
+            // A warp without a row whose P is read has nothing to do: steps of own tiles write the rows
+            // of their sequence only, and what becomes of rows that are not stored does not matter.
+            const int first = (j - p.shared_tiles) * a.s.spt;
+            const bool takes = live && (j < p.shared_tiles || (own_off < first + a.s.spt && own_end > first));
+            if (__any_sync(kFull, takes)) {
+                uint32_t s0[32], s1[32], s2[32], s3[32];  // the row's 128 scores
+                tmem_ld32_async(sbuf, s0);
+                tmem_ld32_async(sbuf + 32, s1);
+                tmem_ld32_async(sbuf + 64, s2);
+                tmem_ld32_async(sbuf + 96, s3);
+                tmem_wait_dep(s0);
+                tmem_wait_dep(s1);
+                tmem_wait_dep(s2);
+                tmem_wait_dep(s3);
+                if (col.lo > 0 || col.hi < 128) {
+                    mask_scores(s0, col.lo, col.hi);
+                    mask_scores(s1, col.lo - 32, col.hi - 32);
+                    mask_scores(s2, col.lo - 64, col.hi - 64);
+                    mask_scores(s3, col.lo - 96, col.hi - 96);
+                }
+                float mx8[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mx8[i] = -INFINITY;
+                max_scores(s0, mx8);
+                max_scores(s1, mx8);
+                max_scores(s2, mx8);
+                max_scores(s3, mx8);
+                const float tm = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
+                                       fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]))) * a.c;
+                float f = 1.f;
+                bool rescale = false;
+                if (m == -INFINITY) {
+                    m = tm;
+                } else if (tm > m + kRescale) {
+                    f = ex2(m - tm);
+                    m = tm;
+                    rescale = true;
+                }
+                // the warp rescales its O together (tcgen05.ld / st are warp-wide), rows without need by
+                // 1. The half's previous product is done: S of this tile was issued after it.
+                if (__any_sync(kFull, rescale)) {
+#pragma unroll 1
+                    for (int ch = 0; ch < 8; ++ch) {
+                        uint32_t o[16];
+                        tmem_ld16_async(obuf + ch * 16, o);
+                        tmem_wait_dep(o);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        tmem_st16(obuf + ch * 16, o);
+                    }
+                }
+                l *= f;
+                // P = 2^(s c - m), pairs of 16 bits over the first 64 columns of S. While all
+                // scores so far are -inf, m is: P = 0 and the sum 0.
+                const float mr = m == -INFINITY ? 0.f : -m;
+                const f2 cc = pack2(a.c, a.c), mm = pack2(mr, mr);
+                f2 lsum[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                uint32_t pk[32];
+                exp_scores<kF16>(s0, cc, mm, lsum, pk, 0);
+                exp_scores<kF16>(s1, cc, mm, lsum, pk, 16);
+                tmem_st32_u(sbuf, pk);
+                uint32_t pk2[32];
+                exp_scores<kF16>(s2, cc, mm, lsum, pk2, 0);
+                exp_scores<kF16>(s3, cc, mm, lsum, pk2, 16);
+                tmem_st32_u(sbuf + 32, pk2);
+                {
+                    float l0, l1;
+                    unpack2(add2(add2(lsum[0], lsum[1]), add2(lsum[2], lsum[3])), l0, l1);
+                    l += l0 + l1;
+                }
+                tmem_wait_st();
+            }
+            if (x + kStages >= count) c.ml[n & 3][h][r] = make_float2(m, l);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.p_full[h]);
+        }
+        t0 += count;
+        if (ok) release_piece(n, lane, c);
+    }
+}
+
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    return kF16 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
+}
+
+// The read-out of the CTA's pieces; this warp's rows are TMEM lanes q * 32 .. + 31.
+// Rows go out through the warp's stage, 128 bytes of each at a time: written a row
+// per thread, read back so that each store instruction covers 128 contiguous bytes
+// of 4 rows. The 16-byte chunk index is XORed with the row's low three bits, so that
+// neither the writes nor the reads put two threads of a quarter-warp in one bank group.
+template <bool kF16>
+__device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_t stage, uint32_t tiles, Ctl &c,
+                                         const PrefixArgs &a) {
+    uint32_t t0 = 0;
+    const uint32_t inv_group = (65536u + a.s.group - 1) / a.s.group;  // (row * it) >> 16 = row / group for row < 128
+    for (int n = 0; t0 < tiles; ++n) {
+        const Piece *pp = next_piece(n, c, a);
+        if (!pp) return;
+        const Piece &p = *pp;
+        const int count = p.j1 - p.j0;
+        if (!warp_wait_or_abort(&c.o_ready, n & 1, c, a)) return;
+        tc_fence_after();
+        const int r = q * 32 + lane;
+        // the rows this lane stores: 4 i + lane / 8
+        int64_t to[8];
+        uint32_t store = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int rr = q * 32 + i * 4 + (lane >> 3), tok = static_cast<int>(rr * inv_group >> 16);
+            to[i] = 0;
+            if (tok < p.r.n_tok && p.len[(p.r.tok0 + tok) / a.s.n_q - p.r.b0] >= 0) {
+                store |= 1u << i;
+                to[i] = p.q * a.out_req + (p.r.tok0 + tok) * a.out_token +
+                        (p.head * a.s.group + rr - tok * a.s.group) * a.out_head;
+            }
+        }
+        const bool both = count > 1;
+        const int only = static_cast<int>(t0) & 1;  // the half of a one-tile piece's tile
+        float2 e = c.ml[n & 3][both ? 0 : only][r];
+        float w0 = 1.f, w1 = 0.f;
+        if (both) {
+            const float2 f = c.ml[n & 3][1][r];
+            const float m = fmaxf(e.x, f.x), mr = m == -INFINITY ? 0.f : m;
+            w0 = e.y == 0.f ? 0.f : ex2(e.x - mr);
+            w1 = f.y == 0.f ? 0.f : ex2(f.x - mr);
+            // (weights of 0 for halves without weight: their accumulators may hold anything)
+            e = make_float2(m, (e.y == 0.f ? 0.f : w0 * e.y) + (f.y == 0.f ? 0.f : w1 * f.y));
+        } else if (e.y == 0.f) {
+            w0 = 0.f;
+        }
+        if (p.part < 0) {
+            const float inv = e.y == 0.f ? 0.f : 1.f / e.y;
+            w0 *= inv;
+            w1 *= inv;
+            if (a.lse) {
+                const int tok = static_cast<int>(r * inv_group >> 16);
+                if (tok < p.r.n_tok && p.len[(p.r.tok0 + tok) / a.s.n_q - p.r.b0] >= 0)
+                    a.lse[(static_cast<int64_t>(p.q) * a.s.n_tokens + p.r.tok0 + tok) * a.n_heads + p.head * a.s.group +
+                          r - tok * a.s.group] = e.y == 0.f ? -INFINITY : (e.x + log2f(e.y)) * kLn2;
+            }
+        } else {
+            a.part_ml[(2 * blockIdx.x + p.part) * prefix::kRows + r] = e;
+        }
+        const uint32_t col = tmem + (static_cast<uint32_t>(q * 32) << 16) + kOCol;
+        float *part = a.part_o + (static_cast<int64_t>(2 * blockIdx.x + max(p.part, 0)) * prefix::kRows + q * 32) * kD;
+#pragma unroll 1
+        for (int ch = 0; ch < 4; ++ch) {  // 32 columns at a time
+            uint32_t o0[32], o1[32];
+            const uint32_t cc = col + ch * 32;
+            tmem_ld32_async(cc + (both ? 0 : only * 128), o0);
+            if (both) {
+                tmem_ld32_async(cc + 128, o1);
+                tmem_wait_dep(o0);
+                tmem_wait_dep(o1);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    o0[i] = __float_as_uint((w0 == 0.f ? 0.f : __uint_as_float(o0[i]) * w0) +
+                                            (w1 == 0.f ? 0.f : __uint_as_float(o1[i]) * w1));
+            } else {
+                tmem_wait_dep(o0);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    o0[i] = __float_as_uint(w0 == 0.f ? 0.f : __uint_as_float(o0[i]) * w0);
+            }
+            if (ch == 3) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&c.o_free);  // O may take the next piece
+            }
+            if (p.part < 0) {  // 64 bytes of each row; a pair of chunks fills the stage
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    uint32_t pk[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        pk[i] = pack16<kF16>(__uint_as_float(o0[8 * u + 2 * i]), __uint_as_float(o0[8 * u + 2 * i + 1]));
+                    st_shared_v4(stage + lane * 128 + ((((ch & 1) * 4 + u) ^ (lane & 7)) << 4),
+                                 make_uint4(pk[0], pk[1], pk[2], pk[3]));
+                }
+                if (ch & 1) {
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int rr = i * 4 + (lane >> 3), x = lane & 7;
+                        const uint4 v = ld_shared_v4(stage + rr * 128 + ((x ^ (rr & 7)) << 4));
+                        if (store >> i & 1)
+                            *reinterpret_cast<uint4 *>(static_cast<char *>(a.out) +
+                                                       (to[i] + (ch >> 1) * 64 + x * 8) * 2) = v;
+                    }
+                    __syncwarp();  // the stage is rewritten next
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    st_shared_v4(stage + lane * 128 + ((u ^ (lane & 7)) << 4),
+                                 make_uint4(o0[4 * u], o0[4 * u + 1], o0[4 * u + 2], o0[4 * u + 3]));
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int rr = i * 4 + (lane >> 3), x = lane & 7;
+                    const uint4 v = ld_shared_v4(stage + rr * 128 + ((x ^ (rr & 7)) << 4));
+                    if (store >> i & 1) *reinterpret_cast<uint4 *>(part + rr * kD + ch * 32 + x * 4) = v;
+                }
+                __syncwarp();
+            }
+        }
+        t0 += count;
+        release_piece(n, lane, c);
+    }
+}
+
+template <bool kF16>
+__global__ void __launch_bounds__(kThreads, 1)
+    prefix_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                            const __grid_constant__ CUtensorMap tm_v, const PrefixArgs a) {
+    extern __shared__ uint8_t dyn_smem[];
+    __shared__ Ctl c;
+    const int warp = __shfl_sync(kFull, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    uint8_t *base = dyn_smem + ((1024u - (saddr(dyn_smem) & 1023u)) & 1023u);
+    uint8_t *sq = base;                          // Q buffers
+    uint8_t *sk = sq + kQBufs * kTileBytes;      // K stages
+    uint8_t *sv = sk + kStages * kTileBytes;     // V stages
+    uint8_t *so = sv + kStages * kTileBytes;     // output stages of the read-out warps
+    if (threadIdx.x == 0) {
+        for (int b = 0; b < kQBufs; ++b) mbar_init(&c.q_full[b], 1);
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&c.k_full[s], 1);
+            mbar_init(&c.v_full[s], 1);
+            mbar_init(&c.v_empty[s], 1);
+            mbar_init(&c.s_full[s], 1);
+            mbar_init(&c.p_full[s], 4);  // a half's four warps
+        }
+        for (int s = 0; s < kRing; ++s) {
+            mbar_init(&c.ring_full[s], 1);
+            mbar_init(&c.ring_empty[s], kConsumers);
+        }
+        mbar_init(&c.o_ready, 1);
+        mbar_init(&c.o_free, 4);
+        mbar_init(&c.mma_done, 1);
+        c.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        tmem_alloc(&c.tmem_base, kTmemCols);
+        tmem_relinquish();
+    }
+    pdl_wait();
+    pdl_launch_next();
+    if (threadIdx.x == 0) a.cut[blockIdx.x].parts = 0;
+    const Start st = find_start(a, c, reinterpret_cast<int32_t *>(sk));
+    // (the K and V stages held the lengths: the copies that follow are ordered after those accesses)
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = c.tmem_base;
+    const uint32_t tiles = static_cast<uint32_t>(st.end - st.at);
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCtlRegs));
+        if (warp == 0)
+            produce<true>(&tm_k, &tm_q, sk, sq, tiles, lane, c, a);
+        else if (warp == 2)
+            produce<false>(&tm_v, nullptr, sv, nullptr, tiles, lane, c, a);
+        else if (warp == 1)
+            issue_products<kF16>(sq, sk, sv, tmem, tiles, lane, c, a);
+        else if (tiles)
+            schedule(a, st, lane, c);
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+        softmax<kF16>(tmem, warp & 3, lane, (warp >> 2) - 1, tiles, c, a);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOutRegs));
+        read_out<kF16>(tmem, warp & 3, lane, saddr(so + (warp - 12) * kStageBytes), tiles, c, a);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, kTmemCols);
+}
+
+// ---------------------------------------------------------------- joining the parts of cut row tiles
+// (m, l, o) of parts first, first + step, ... of a row, this lane's four columns.
+struct Joined {
+    float m, l;
+    float4 o;
+};
+__device__ __forceinline__ void join(Joined &x, float m, float l, float4 o) {
+    const float mm = fmaxf(x.m, m), mr = mm == -INFINITY ? 0.f : mm;
+    const float f = ex2(x.m - mr), g = ex2(m - mr);
+    x.m = mm;
+    x.l = x.l * f + l * g;
+    x.o.x = x.o.x * f + o.x * g;
+    x.o.y = x.o.y * f + o.y * g;
+    x.o.z = x.o.z * f + o.z * g;
+    x.o.w = x.o.w * f + o.w * g;
+}
+__device__ __forceinline__ Joined join_parts(const PrefixArgs &a, int cta, int row, int first, int parts, int step,
+                                             int lane) {
+    Joined x{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    constexpr int kAhead = 4;
+    for (int p = first; p < parts; p += step * kAhead) {
+        float2 ml[kAhead];
+        float4 o[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int pp = p + u * step;
+            ml[u] = make_float2(-INFINITY, 0.f);
+            o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (pp < parts) {
+                // the first part of a row tile ends its CTA's range, the others begin theirs
+                const int64_t at = static_cast<int64_t>(2 * (cta + pp) + (pp == 0 ? 1 : 0)) * prefix::kRows + row;
+                ml[u] = a.part_ml[at];
+                o[u] = *reinterpret_cast<const float4 *>(a.part_o + at * kD + lane * 4);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (p + u * step < parts) join(x, ml[u].x, ml[u].y, o[u]);
+    }
+    return x;
+}
+
+template <bool kF16>
+__device__ __forceinline__ void store_row(const PrefixArgs &a, const Cut &cut, const RowTile &r, int row,
+                                          const Joined &x, int lane) {
+    const int tok = r.tok0 + row / a.s.group, h = cut.head * a.s.group + row % a.s.group;
+    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
+    const uint2 v = make_uint2(pack16<kF16>(x.o.x * inv, x.o.y * inv), pack16<kF16>(x.o.z * inv, x.o.w * inv));
+    *reinterpret_cast<uint2 *>(static_cast<char *>(a.out) +
+                               (cut.q * a.out_req + tok * a.out_token + h * a.out_head + lane * 4) * 2) = v;
+    if (a.lse && lane == 0)
+        a.lse[(static_cast<int64_t>(cut.q) * a.s.n_tokens + tok) * a.n_heads + h] =
+            x.l == 0.f ? -INFINITY : (x.m + log2f(x.l)) * kLn2;
+}
+
+constexpr int kFewParts = 8;  // up to this many parts a warp joins a row, else a block does
+
+template <bool kF16>
+__global__ void __launch_bounds__(kCombineThreads) prefix_combine_kernel(const PrefixArgs a, int ctas) {
+    __shared__ Cut cuts[kMaxCtas];
+    __shared__ int first_unit[kMaxCtas + 1];
+    __shared__ Joined part[kCombineThreads / 32][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_wait();
+    pdl_launch_next();
+    for (int i = threadIdx.x; i < ctas; i += kCombineThreads) cuts[i] = a.cut[i];
+    __syncthreads();
+    // units of the cuts: a row each, or 8 rows
+    if (warp == 0) {
+        int total = 0;
+        for (int base = 0; base < ctas; base += 32) {
+            const int i = base + lane;
+            int units = 0;
+            if (i < ctas && cuts[i].parts > 0) {
+                const int rows = prefix::row_tile(a.s, cuts[i].rt).n_tok * a.s.group;
+                units = cuts[i].parts <= kFewParts ? (rows + 7) / 8 : rows;
+            }
+            int upto = units;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(kFull, upto, o);
+                if (lane >= o) upto += u;
+            }
+            if (i < ctas) first_unit[i] = total + upto - units;
+            total += __shfl_sync(kFull, upto, 31);
+        }
+        if (lane == 0) first_unit[ctas] = total;
+    }
+    __syncthreads();
+    for (int u = blockIdx.x; u < first_unit[ctas]; u += gridDim.x) {
+        const int i = prefix::slot_owner(first_unit, ctas, u);
+        const Cut cut = cuts[i];
+        const RowTile r = prefix::row_tile(a.s, cut.rt);
+        const int rows = r.n_tok * a.s.group;
+        const bool few = cut.parts <= kFewParts;
+        const int row = few ? (u - first_unit[i]) * 8 + warp : u - first_unit[i];
+        const bool there = row < rows && a.len[static_cast<int64_t>(cut.q) * a.s.n_branch +
+                                               (r.tok0 + row / a.s.group) / a.s.n_q] >= 0;
+        if (few) {
+            if (there) store_row<kF16>(a, cut, r, row, join_parts(a, i, row, 0, cut.parts, 1, lane), lane);
+            continue;
+        }
+        if (!there) continue;  // (the same for the whole block)
+        part[warp][lane] = join_parts(a, i, row, warp, cut.parts, kCombineThreads / 32, lane);
+        __syncthreads();
+        if (warp == 0) {
+            Joined x = part[0][lane];
+#pragma unroll
+            for (int w = 1; w < kCombineThreads / 32; ++w) {
+                const Joined y = part[w][lane];
+                join(x, y.m, y.l, y.o);
+            }
+            store_row<kF16>(a, cut, r, row, x, lane);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- host
+std::mutex g_prefix_mutex;
+PFN_cuTensorMapEncodeTiled_v12000 g_prefix_encode = nullptr;
+bool g_prefix_ready[64] = {};
+int g_prefix_sms[64] = {};
+
+rps_status setup(int *sms) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RPS_ERR_CUDA;
+    std::lock_guard<std::mutex> lock(g_prefix_mutex);
+    if (!g_prefix_encode) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) !=
+                cudaSuccess ||
+            q != cudaDriverEntryPointSuccess || !fn)
+            return RPS_ERR_CUDA;
+        g_prefix_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+    }
+    if (!g_prefix_ready[dev]) {
+        if (cudaDeviceGetAttribute(&g_prefix_sms[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+            return RPS_ERR_CUDA;
+        for (auto k : {prefix_attention_kernel<false>, prefix_attention_kernel<true>})
+            if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess)
+                return RPS_ERR_CUDA;
+        g_prefix_ready[dev] = true;
+    }
+    *sms = std::min(g_prefix_sms[dev], kMaxCtas);
+    return RPS_OK;
+}
+
+// A map of 16-bit elements: extents and strides (in elements) from the inner dimension
+// (64-wide boxes of 128 contiguous elements) outwards.
+rps_status map_4d(CUtensorMap *m, const void *base, bool f16, const int64_t (&ext)[3], const int64_t (&stride)[3],
+                  const uint32_t (&box)[3]) {
+    cuuint64_t dims[4] = {kD, 0, 0, 0}, bytes[3];
+    cuuint32_t boxes[4] = {64, 0, 0, 0};
+    const cuuint32_t es[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 3; ++i) {
+        dims[i + 1] = static_cast<cuuint64_t>(ext[i]);
+        // (the stride of a dimension of one is not used, but has to be a valid one)
+        bytes[i] = static_cast<cuuint64_t>(ext[i] > 1 ? stride[i] : kD) * 2;
+        boxes[i + 1] = box[i];
+    }
+    const CUresult r = g_prefix_encode(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                                       const_cast<void *>(base), dims, bytes, boxes, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? RPS_OK : RPS_ERR_CUDA;
+}
+
+// Shape of a call, with the limits that keep its counts in 32 bits.
+rps_status check_shape(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads, int32_t causal, Shape *s) {
+    const rps_status st = check_kv_cache(kv);
+    if (st != RPS_OK) return st;
+    if (n_q < 1 || n_heads < 1 || n_heads % kv->n_heads) return RPS_ERR_INVALID_ARG;
+    if (n_heads / kv->n_heads > RPS_KV_MAX_GROUP) return RPS_ERR_UNSUPPORTED;
+    const int64_t tokens = static_cast<int64_t>(kv->n_branch) * n_q;
+    if (tokens > INT32_MAX / 256 || static_cast<int64_t>(kv->n_req) * tokens > INT32_MAX / 2) return RPS_ERR_UNSUPPORTED;
+    // slots of the sequences of one row tile
+    const int64_t slots = static_cast<int64_t>(kv->max_pages) * std::max(1, kv->page_size / prefix::kRows);
+    if (std::min<int64_t>(kv->n_branch, kMaxSeqs) * slots > INT32_MAX / 256) return RPS_ERR_UNSUPPORTED;
+    *s = prefix::make_shape(kv->n_req, kv->n_branch, n_q, kv->n_heads, n_heads / kv->n_heads, kv->page_size, kv->n_pages,
+                            kv->max_pages, causal);
+    return RPS_OK;
+}
+
+size_t part_bytes(size_t *ml_at, size_t *o_at) {
+    *ml_at = (sizeof(Cut) * kMaxCtas + 255) / 256 * 256;
+    *o_at = *ml_at + sizeof(float2) * 2 * kMaxCtas * prefix::kRows;
+    return *o_at + sizeof(float) * 2 * kMaxCtas * prefix::kRows * kD;
+}
+
+}  // namespace
+}  // namespace rps
+
+using namespace rps;
+
+extern "C" size_t rps_prefix_attention_workspace_bytes(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads) {
+    Shape s;
+    if (check_shape(kv, n_q, n_heads, 0, &s) != RPS_OK) return 0;
+    size_t ml, o;
+    return part_bytes(&ml, &o);
+}
+
+extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, const rps_kv_cache *kv, void *d_ws,
+                                               size_t ws_bytes, rps_stream_t stream) {
+    if (!p || !p->q || !p->out) return RPS_ERR_INVALID_ARG;
+    PrefixArgs a;
+    std::memset(&a, 0, sizeof a);
+    rps_status st = check_shape(kv, p->n_q, p->n_heads, p->causal != 0, &a.s);
+    if (st != RPS_OK) return st;
+    if (p->layer < 0 || p->layer >= kv->n_layers) return RPS_ERR_INVALID_ARG;
+    if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return RPS_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(p->q) % 16 || reinterpret_cast<uintptr_t>(p->out) % 16) return RPS_ERR_INVALID_ARG;
+    const int64_t ext[3] = {p->n_heads, a.s.n_tokens, kv->n_req};
+    const int64_t qs[3] = {p->q_head_stride, p->q_token_stride, p->q_req_stride};
+    const int64_t os[3] = {p->out_head_stride, p->out_token_stride, p->out_req_stride};
+    for (int i = 0; i < 3; ++i)
+        if (ext[i] > 1 && (qs[i] <= 0 || os[i] <= 0 || qs[i] % 8 || os[i] % 8)) return RPS_ERR_INVALID_ARG;
+    size_t ml_at, o_at;
+    if (!d_ws || reinterpret_cast<uintptr_t>(d_ws) % 16 || ws_bytes < part_bytes(&ml_at, &o_at))
+        return RPS_ERR_INVALID_ARG;
+    int sms = 0;
+    if ((st = setup(&sms)) != RPS_OK) return st;
+    if (!(a.err = device_error_word())) return RPS_ERR_CUDA;
+
+    const bool f16 = kv->dtype == RPS_F16;
+    const int64_t kv_at = kv->n_layers > 1 ? p->layer * kv->layer_stride * 2 : 0;
+    const int64_t kext[3] = {kv->page_size, kv->n_heads, kv->n_pages};
+    const int64_t ks[3] = {kv->token_stride, kv->head_stride, kv->page_stride};
+    const uint32_t qbox[3] = {static_cast<uint32_t>(a.s.group), static_cast<uint32_t>(a.s.tokens), 1};
+    const uint32_t kbox[3] = {static_cast<uint32_t>(a.s.slot), 1, 1};
+    CUtensorMap tq, tk, tv;
+    if ((st = map_4d(&tq, p->q, f16, ext, qs, qbox)) != RPS_OK) return st;
+    if ((st = map_4d(&tk, static_cast<char *>(kv->k) + kv_at, f16, kext, ks, kbox)) != RPS_OK) return st;
+    if ((st = map_4d(&tv, static_cast<char *>(kv->v) + kv_at, f16, kext, ks, kbox)) != RPS_OK) return st;
+    a.table = kv->table;
+    a.len = kv->len;
+    a.shared_len = p->shared_len;
+    a.n_heads = p->n_heads;
+    a.out = p->out;
+    a.out_req = kv->n_req > 1 ? os[2] : 0;
+    a.out_token = a.s.n_tokens > 1 ? os[1] : 0;
+    a.out_head = p->n_heads > 1 ? os[0] : 0;
+    a.lse = p->lse;
+    a.c = p->scale * kLog2e;
+    char *ws = static_cast<char *>(d_ws);
+    a.cut = reinterpret_cast<Cut *>(ws);
+    a.part_ml = reinterpret_cast<float2 *>(ws + ml_at);
+    a.part_o = reinterpret_cast<float *>(ws + o_at);
+    a.wait_ns = ring_wait_limit_ns();
+
+    // CTAs: as many as there can be key tiles
+    const int64_t slots = static_cast<int64_t>(a.s.max_pages) * a.s.sub;
+    const int64_t tiles = 2 + (std::min<int64_t>(a.s.n_branch, kMaxSeqs) + 1) * slots / a.s.spt;
+    const int64_t row_tiles = static_cast<int64_t>(a.s.n_req) * a.s.heads * a.s.row_tiles;
+    const int grid = static_cast<int>(std::min<int64_t>(row_tiles * tiles, sms));
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (launch_pdl(f16 ? prefix_attention_kernel<true> : prefix_attention_kernel<false>, dim3(grid), dim3(kThreads),
+                   kSmemBytes, s, tq, tk, tv, a) != cudaSuccess)
+        return RPS_ERR_CUDA;
+    return launch_pdl(f16 ? prefix_combine_kernel<true> : prefix_combine_kernel<false>, dim3(sms * 4),
+                      dim3(kCombineThreads), 0, s, a, grid) == cudaSuccess
+               ? RPS_OK
+               : RPS_ERR_CUDA;
+}

@@ -46,6 +46,11 @@ UMMA_HD inline constexpr uint32_t instr_desc_bf16(uint32_t m, uint32_t n) {
     return (kAccF32 << 4) | (kFmtBF16 << 7) | (kFmtBF16 << 10) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
+// kind::f16 with A and B of one format, f32 accumulator, A K-major; B K-major or MN-major.
+UMMA_HD inline constexpr uint32_t instr_desc_f16(uint32_t m, uint32_t n, uint32_t fmt, uint32_t b_mn_major) {
+    return (kAccF32 << 4) | (fmt << 7) | (fmt << 10) | (b_mn_major << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+
 UMMA_HD inline constexpr uint64_t smem_desc(uint32_t smem_addr, uint32_t lbo_bytes, uint32_t sbo_bytes, uint32_t swizzle) {
     return static_cast<uint64_t>((smem_addr >> 4) & 0x3FFFu) |
            (static_cast<uint64_t>((lbo_bytes >> 4) & 0x3FFFu) << 16) |
@@ -60,6 +65,15 @@ UMMA_HD inline constexpr uint64_t smem_desc_kmajor_sw128(uint32_t smem_addr) {
 
 // The descriptor of the K slice `k16` (16 bf16 = 32 bytes further per slice).
 UMMA_HD inline constexpr uint64_t advance_k16(uint64_t desc, uint32_t k16) { return desc + static_cast<uint64_t>(2 * k16); }
+
+// MN-major tile, 128-byte swizzle: a row holds 64 elements of the M or N
+// dimension of one K index, rows follow each other at 128 bytes, so eight K
+// indexes form a 1024-byte atom and the next eight lie 1024 bytes on (the
+// stride-dimension offset); the next 64 elements of M or N are `chunk` bytes away
+// (the leading-dimension offset). 16 K indexes further: 2048 bytes.
+UMMA_HD inline constexpr uint64_t smem_desc_mnmajor_sw128(uint32_t smem_addr, uint32_t chunk) {
+    return smem_desc(smem_addr, chunk, 1024, kSwizzle128B);
+}
 
 }  // namespace umma
 }  // namespace rps

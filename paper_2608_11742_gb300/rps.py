@@ -147,7 +147,18 @@ class RpsKvCache(C.Structure):
                 ("n_branch", C.c_int32), ("max_pages", C.c_int32)]
 
 
+class RpsPrefixAttention(C.Structure):
+    _fields_ = [("q", _p), ("out", _p), ("lse", _p), ("n_q", C.c_int32), ("n_heads", C.c_int32), ("layer", C.c_int32),
+                ("causal", C.c_int32), ("q_req_stride", C.c_int64), ("q_token_stride", C.c_int64),
+                ("q_head_stride", C.c_int64), ("out_req_stride", C.c_int64), ("out_token_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("shared_len", _p), ("scale", C.c_float)]
+
+
 # (structs by address, as for rps_run_step)
+_lib.rps_prefix_attention_workspace_bytes.restype = C.c_size_t
+_lib.rps_prefix_attention_workspace_bytes.argtypes = [_p, C.c_int32, C.c_int32]
+_lib.rps_prefix_attention_fwd.restype = C.c_int
+_lib.rps_prefix_attention_fwd.argtypes = [_p, _p, _p, C.c_size_t, _p]
 _lib.rps_kv_workspace_bytes.restype = C.c_size_t
 _lib.rps_kv_workspace_bytes.argtypes = [_p]
 for _n, _a in (("reorder", [_p, _p, _p, _p, C.c_size_t, _p]), ("fork_branches", [_p, _p, _p, _p, C.c_size_t, _p]),
@@ -664,6 +675,48 @@ def rps_kv_write(kv: KvCacheBuf, layer: int, k_new: torch.Tensor, v_new: torch.T
         raise ValueError("k_new and v_new: head dim contiguous, the same strides, requests at n_branch sequences' stride")
     _check(_lib.rps_kv_write(at, layer, k_new.data_ptr(), v_new.data_ptr(), shape[2], st[1] if nb > 1 else st[0], st[2],
                              st[3], _stream(stream)), "rps_kv_write")
+
+
+def rps_prefix_attention_workspace_bytes(kv: KvCacheBuf, n_q: int, n_heads: int) -> int:
+    n = _lib.rps_prefix_attention_workspace_bytes(kv._c(), n_q, n_heads)
+    if n == 0:
+        raise RPSError(RPS_ERR_INVALID_ARG, "rps_prefix_attention_workspace_bytes")
+    return n
+
+
+def _token_strides(name: str, t: torch.Tensor):
+    """(request, token, head) strides of ``[n_req][n_branch][n_q][heads][128]``, tokens at one stride through a
+    request."""
+    n_req, nb, n_q, h, _ = t.shape
+    req, branch, token, head, last = t.stride()
+    if n_q == 1:
+        token = branch
+    if last != 1 or (nb > 1 and branch != n_q * token):
+        raise ValueError(f"{name}: head dim contiguous, the tokens of a request at one stride")
+    return req, token, head
+
+
+def rps_prefix_attention_fwd(q: torch.Tensor, kv: KvCacheBuf, layer: int, out: torch.Tensor, ws: torch.Tensor,
+                             shared_len: Optional[torch.Tensor], scale: float, causal: bool = False,
+                             lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of the sequences' last ``n_q`` tokens over their cached keys: q, out
+    ``[n_req][n_branch][n_q][n_heads][128]`` of the cache's dtype, lse (optional) fp32 ``[n_req][n_branch][n_q][n_heads]``;
+    ``shared_len`` (int32 ``[n_req]`` or None): leading tokens whose pages a request's sequences hold in common."""
+    at = kv._c()
+    _here(kv.k, kv.table, q, out, ws, shared_len, lse)
+    n_req, nb = kv.table.shape[:2]
+    shape = q.shape
+    if len(shape) != 5 or shape[:2] != (n_req, nb) or shape[4] != kv.k.shape[4] or out.shape != shape:
+        raise ValueError("q and out: [n_req][n_branch][n_q][n_heads][head dim], as the cache")
+    if q.dtype != kv.k.dtype or out.dtype != kv.k.dtype:
+        raise TypeError(f"q and out must be {kv.k.dtype}, as the cache")
+    a = RpsPrefixAttention(q.data_ptr(), out.data_ptr(),
+                           None if lse is None else _ints("lse", lse, n_req * nb * shape[2] * shape[3], torch.float32),
+                           shape[2], shape[3], layer, 1 if causal else 0, *_token_strides("q", q),
+                           *_token_strides("out", out),
+                           None if shared_len is None else _ints("shared_len", shared_len, n_req), scale)
+    _check(_lib.rps_prefix_attention_fwd(C.addressof(a), at, ws.data_ptr(), ws.numel() * ws.element_size(),
+                                         _stream(stream)), "rps_prefix_attention_fwd")
 
 
 # --------------------------------------------------------------------------- one step

@@ -101,3 +101,33 @@ def test_oracle_keeps_counts_and_order():
     assert c.table[1, :3].tolist() == [0, 3, 4] and c.ref.tolist() == [2, 1, 1, 1, 1, 0, 0, 0]
     c.resize([-1, 40, -1])
     assert c.compact() == 3 and c.table[1, :3].tolist() == [0, 1, 2] and c.err == 0
+
+
+def attention(**kw):
+    base = dict(q=P, out=P, lse=None, n_q=2, n_heads=8, layer=0, causal=0, q_req_stride=6 * 8 * 128, q_token_stride=1024,
+                q_head_stride=128, out_req_stride=6 * 8 * 128, out_token_stride=1024, out_head_stride=128,
+                shared_len=None, scale=0.1)
+    base.update(kw)
+    return rps.RpsPrefixAttention(**base)
+
+
+def test_attention_arguments_that_are_refused():
+    lib, good = rps._lib, cache()
+    need = lib.rps_prefix_attention_workspace_bytes(C.addressof(good), 2, 8)
+    assert need > 0
+    call = lambda a, kv=good, ws=P, n=need: lib.rps_prefix_attention_fwd(C.addressof(a), C.addressof(kv), ws, n, None)
+    for kw in (dict(q=None), dict(out=None), dict(q=P + 8), dict(out=P + 2), dict(n_q=0), dict(n_heads=0), dict(n_heads=6),
+               dict(layer=2), dict(layer=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+               dict(q_head_stride=4), dict(q_token_stride=0), dict(out_req_stride=-8), dict(out_token_stride=100)):
+        assert call(attention(**kw)) == rps.RPS_ERR_INVALID_ARG, kw
+    for kw in (dict(n_heads=4 * 129), dict(n_q=1 << 28)):
+        assert call(attention(**kw)) == rps.RPS_ERR_UNSUPPORTED, kw
+    for ws, n in ((None, need), (P + 4, need), (P, need - 1)):
+        assert call(attention(), ws=ws, n=n) == rps.RPS_ERR_INVALID_ARG
+    for kw in INVALID + BOOK_INVALID:
+        assert call(attention(), cache(**kw)) == rps.RPS_ERR_INVALID_ARG, kw
+    for kw in UNSUPPORTED + BOOK_UNSUPPORTED:
+        assert call(attention(), cache(**kw)) == rps.RPS_ERR_UNSUPPORTED, kw
+        assert lib.rps_prefix_attention_workspace_bytes(C.addressof(cache(**kw)), 2, 8) == 0
+    assert lib.rps_prefix_attention_fwd(None, C.addressof(good), P, need, None) == rps.RPS_ERR_INVALID_ARG
+    assert lib.rps_prefix_attention_fwd(C.addressof(attention()), None, P, need, None) == rps.RPS_ERR_INVALID_ARG
