@@ -125,20 +125,39 @@ struct Ctl {
     int abort_flag;
 };
 
+// ---------------------------------------------------------------- waits
+// Waits for a phase of a barrier, at most a.wait_ns, all lanes; the warp goes on
+// together, on the same answer. A wait that runs out raises the abort flag, which ends
+// the other roles' waits and is reported when the CTA ends. (Short: every role's waits
+// are inlined, and the roles' code has to fit the instruction cache together.)
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl &c, const PrefixArgs &a) {
+    bool ok = a.wait_ns != 0 && mbar_try_wait(bar, parity);
+    if (!__all_sync(kFull, ok)) {
+        const uint64_t start = global_ns();
+#pragma unroll 1
+        while (!(ok = a.wait_ns != 0 && mbar_try_wait(bar, parity)))
+            if (*reinterpret_cast<volatile int *>(&c.abort_flag) || global_ns() - start >= a.wait_ns) break;
+        ok = __all_sync(kFull, ok);
+        if (!ok) *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
+    }
+    return ok;
+}
+
 // ---------------------------------------------------------------- the cut
 __device__ __forceinline__ int len_of(const PrefixArgs &a, int64_t s, const int32_t *staged) {
     return prefix::used_len(a.s, staged ? staged[s] : a.len[s]);
 }
 __device__ __forceinline__ int shared_len_of(const PrefixArgs &a, int q) { return a.shared_len ? a.shared_len[q] : 0; }
 
-// Key tiles of entry e = (request, row tile), by one thread.
-__device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int64_t e, const int32_t *staged) {
-    const int q = static_cast<int>(e / a.s.row_tiles);
-    const RowTile r = prefix::row_tile(a.s, static_cast<int>(e - static_cast<int64_t>(q) * a.s.row_tiles));
+// Key tiles of entry e = (request q, row tile rt), by one thread.
+__device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int q, int rt, const int32_t *staged) {
+    const RowTile r = prefix::row_tile(a.s, rt);
     KeySum k{0, 0, INT32_MAX};
     const int64_t s0 = static_cast<int64_t>(q) * a.s.n_branch + r.b0;
+    const int shared_len = shared_len_of(a, q);
+#pragma unroll 1
     for (int i = 0; i < r.nb; ++i) prefix::add_sequence(a.s, k, len_of(a, s0 + i, staged));
-    return prefix::key_tiles(a.s, k, prefix::shared_slots(a.s, k, shared_len_of(a, q)));
+    return prefix::key_tiles(a.s, k, prefix::shared_slots(a.s, k, shared_len));
 }
 
 // Exclusive prefix sum over the block's 512 threads; *total: the block's sum.
@@ -166,76 +185,77 @@ __device__ __forceinline__ int64_t scan_block(int v, int64_t *sums, int64_t *tot
 // Where the CTA's range begins: request, cache head, row tile, key tile; and its length.
 struct Start {
     int32_t q, head, rt, j;
-    int64_t at, end, work;
-    int32_t n;  // CTAs with work
+    int64_t at, end;
+    prefix::Ranges ranges;
 };
 
-__device__ Start find_start(const PrefixArgs &a, Ctl &c, int32_t *stage) {
-    const int64_t entries = static_cast<int64_t>(a.s.n_req) * a.s.row_tiles;
-    const int64_t n_seq = static_cast<int64_t>(a.s.n_req) * a.s.n_branch;
+__device__ __forceinline__ Start find_start(const PrefixArgs &a, Ctl &c, int32_t *stage) {
+    const int entries = a.s.n_req * a.s.row_tiles, n_seq = a.s.n_req * a.s.n_branch;
     const int32_t *staged = nullptr;
     if (n_seq <= kStagedLens) {
+#pragma unroll 1
         for (int i = threadIdx.x; i < n_seq; i += kThreads) stage[i] = a.len[i];
-        __syncthreads();
         staged = stage;
     }
-    // passes over the entries in blocks of 512; of a single block everything stays in registers
-    const bool one = entries <= kThreads;
-    int t0 = 0;
-    int64_t before0 = 0, total = 0, carry = 0;
-    for (int64_t base = 0; base < entries; base += kThreads) {
-        t0 = base + threadIdx.x < entries ? entry_tiles(a, base + threadIdx.x, staged) : 0;
-        before0 = carry + scan_block(t0, c.scan, &total);
-        carry += total;
-    }
+    if (threadIdx.x == 0) c.find_q = 0;
+    __syncthreads();
+    // Passes over the entries in blocks of 512, each looking at an entry's tiles and the tiles
+    // before it (of a single block they stay in registers): the total; the last request that
+    // starts at or before the range; that request's bounds; the row tile and key tile in it.
     Start st{};
-    st.work = carry * a.s.heads;
-    // (no more CTAs than key tiles: none in between is without work)
-    st.n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), st.work));
-    if (static_cast<int>(blockIdx.x) >= st.n) return st;
-    st.at = prefix::range_start(blockIdx.x, st.work, st.n);
-    st.end = prefix::range_start(blockIdx.x + 1, st.work, st.n);
-    // Each pass looks at (tiles, tiles before) of every entry. First the last request that
-    // starts at or before the range, then that request's bounds, then the entry in it.
-    for (int pass = 0; pass < 3; ++pass) {
-        __syncthreads();
-        if (threadIdx.x == 0 && pass == 0) c.find_q = 0;
-        const int q_at = pass ? c.find_q : 0;
-        int64_t in_head = 0;
-        if (pass == 2) {
-            const int64_t per_head = c.p1 - c.p0, rem = st.at - a.s.heads * c.p0;
-            st.head = static_cast<int>(rem / per_head);
-            in_head = c.p0 + rem - st.head * per_head;
-        }
-        __syncthreads();
-        carry = 0;
-        for (int64_t base = 0; base < entries; base += kThreads) {
-            const int64_t e = base + threadIdx.x;
-            int t = t0;
-            int64_t before = before0;
-            if (!one) {
-                t = e < entries ? entry_tiles(a, e, staged) : 0;
+    int t = 0;
+    int64_t before = 0, in_head = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 4; ++pass) {
+        int64_t carry = 0;
+#pragma unroll 1
+        for (int base = 0; base < entries; base += kThreads) {
+            const int e = base + threadIdx.x;
+            const int q = prefix::quotient(e, a.s.by_row_tiles), rt = e - q * a.s.row_tiles;
+            if (pass == 0 || entries > kThreads) {
+                int64_t total;
+                t = e < entries ? entry_tiles(a, q, rt, staged) : 0;
                 before = carry + scan_block(t, c.scan, &total);
                 carry += total;
             }
             if (e >= entries) continue;
-            const int q = static_cast<int>(e / a.s.row_tiles);
-            const int rt = static_cast<int>(e - static_cast<int64_t>(q) * a.s.row_tiles);
-            if (pass == 0) {
+            if (pass == 1) {
                 if (rt == 0 && before * a.s.heads <= st.at) atomicMax(&c.find_q, q);
-            } else if (q == q_at) {
-                if (pass == 1) {
-                    if (rt == 0) c.p0 = before;
-                    if (rt == a.s.row_tiles - 1) c.p1 = before + t;
-                } else if (before <= in_head && in_head < before + t) {
-                    c.find_rt = rt;
-                    c.find_j = static_cast<int>(in_head - before);
-                }
+            } else if (pass == 2 && q == st.q) {
+                if (rt == 0) c.p0 = before;
+                if (rt == a.s.row_tiles - 1) c.p1 = before + t;
+            } else if (pass == 3 && q == st.q && before <= in_head && in_head < before + t) {
+                c.find_rt = rt;
+                c.find_j = static_cast<int>(in_head - before);
             }
         }
+        if (pass == 0) {
+            const int64_t work = carry * a.s.heads;
+            // (no more CTAs than key tiles: none in between is without work)
+            const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), work));
+            if (static_cast<int>(blockIdx.x) >= n) return st;
+            st.ranges = prefix::make_ranges(work, n);
+            st.at = prefix::range_start(st.ranges, blockIdx.x);
+            st.end = prefix::range_start(st.ranges, blockIdx.x + 1);
+            continue;
+        }
+        __syncthreads();
+        if (pass == 1) st.q = c.find_q;
+        if (pass == 2) {  // (each head of the request has the same key tiles)
+            const int64_t per_head = c.p1 - c.p0, rem = st.at - a.s.heads * c.p0;
+            int lo = 0, hi = a.s.heads;
+#pragma unroll 1
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (mid * per_head <= rem)
+                    lo = mid;
+                else
+                    hi = mid;
+            }
+            st.head = lo;
+            in_head = c.p0 + rem - st.head * per_head;
+        }
     }
-    __syncthreads();
-    st.q = c.find_q;
     st.rt = c.find_rt;
     st.j = c.find_j;
     return st;
@@ -247,36 +267,34 @@ __device__ int fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, Piece
     const RowTile r = prefix::row_tile(a.s, rt);
     const int64_t s0 = static_cast<int64_t>(q) * a.s.n_branch + r.b0;
     KeySum k{0, 0, INT32_MAX};
-    int first = INT32_MAX, len[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        const int i = x * 32 + lane;
-        len[x] = i < r.nb ? len_of(a, s0 + i, nullptr) : -1;
-        prefix::add_sequence(a.s, k, len[x]);
-        if (len[x] >= 0) first = min(first, i);
+    int first = INT32_MAX;
+    const int shared_len = shared_len_of(a, q);
+#pragma unroll 1
+    for (int i = lane; i < r.nb; i += 32) {
+        const int len = len_of(a, s0 + i, nullptr);
+        p.len[i] = len;
+        prefix::add_sequence(a.s, k, len);
+        if (len >= 0) first = min(first, i);
     }
-    k.present = warp_sum_int(k.present);
-    k.slots = warp_sum_int(k.slots);
-    k.min_pages = warp_min_int(k.min_pages);
-    first = warp_min_int(first);
-    const int shared = prefix::shared_slots(a.s, k, shared_len_of(a, q));
+    k.present = __reduce_add_sync(kFull, k.present);
+    k.slots = __reduce_add_sync(kFull, k.slots);
+    k.min_pages = __reduce_min_sync(kFull, k.min_pages);
+    first = __reduce_min_sync(kFull, first);
+    const int shared = prefix::shared_slots(a.s, k, shared_len);
     const int tiles = prefix::key_tiles(a.s, k, shared);
     if (tiles == 0) return 0;
     int before = 0;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        const int i = x * 32 + lane;
-        const int own = len[x] < 0 ? 0 : prefix::ceil_div(len[x], a.s.slot) - shared;
+#pragma unroll 1
+    for (int base = 0; base < r.nb; base += 32) {
+        const int i = base + lane, len = i < r.nb ? p.len[i] : -1;
+        const int own = len < 0 ? 0 : prefix::slots_of(a.s, len) - shared;
         int upto = own;
-#pragma unroll
+#pragma unroll 1
         for (int o = 1; o < 32; o <<= 1) {
             const int u = __shfl_up_sync(kFull, upto, o);
             if (lane >= o) upto += u;
         }
-        if (i < r.nb) {
-            p.len[i] = len[x];
-            p.off[i + 1] = before + upto;
-        }
+        if (i < r.nb) p.off[i + 1] = before + upto;
         before += __shfl_sync(kFull, upto, 31);
     }
     if (lane == 0) {
@@ -285,7 +303,7 @@ __device__ int fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, Piece
         p.rt = rt;
         p.r = r;
         p.shared = shared;
-        p.shared_tiles = prefix::ceil_div(shared, a.s.spt);
+        p.shared_tiles = prefix::tiles_of(a.s, shared);
         p.shared_row = static_cast<int>(s0) + first;
     }
     return tiles;
@@ -294,7 +312,7 @@ __device__ int fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, Piece
 // ---------------------------------------------------------------- roles
 // Piece n of the CTA, once the scheduler has it (nullptr: the wait ran out).
 __device__ __forceinline__ const Piece *next_piece(int n, Ctl &c, const PrefixArgs &a) {
-    if (!warp_wait_or_abort(&c.ring_full[n % kRing], (n / kRing) & 1, c, a)) return nullptr;
+    if (!warp_wait(&c.ring_full[n % kRing], (n / kRing) & 1, c, a)) return nullptr;
     return &c.ring[n % kRing];
 }
 __device__ __forceinline__ void release_piece(int n, int lane, Ctl &c) {
@@ -310,19 +328,19 @@ __device__ __forceinline__ void slot_page(const PrefixArgs &a, const Piece &p, i
     page = a.s.n_pages;
     token = 0;
     if (j < p.shared_tiles) {
-        x = j * a.s.spt + lane;
+        x = (j << a.s.spt_log) + lane;
         there = x < p.shared;
         row = p.shared_row;
     } else {
-        const int o = (j - p.shared_tiles) * a.s.spt + lane;
+        const int o = ((j - p.shared_tiles) << a.s.spt_log) + lane;
         there = o < p.off[p.r.nb];
         const int i = there ? prefix::slot_owner(p.off, p.r.nb, o) : 0;
         x = o - p.off[i] + p.shared;
         row = p.q * a.s.n_branch + p.r.b0 + i;
     }
     if (!there) return;
-    const int e = x / a.s.sub;
-    token = (x - e * a.s.sub) * a.s.slot;
+    const int e = x >> a.s.sub_log;
+    token = (x & (a.s.sub - 1)) << a.s.slot_log;
     page = a.table[static_cast<int64_t>(row) * a.s.max_pages + e];
     if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.s.n_pages)) page = a.s.n_pages;
 }
@@ -347,7 +365,7 @@ __device__ __forceinline__ void produce(const CUtensorMap *tm, const CUtensorMap
             if (kIsK) {
                 // S of tile t - 2 is computed: its K stage is free, and at a piece's first tile
                 // the Q buffer of piece n - 2, whose last tile is no later
-                if (t >= kStages && !warp_wait_or_abort(&c.s_full[s], (t / kStages - 1) & 1, c, a)) {
+                if (t >= kStages && !warp_wait(&c.s_full[s], (t / kStages - 1) & 1, c, a)) {
                     ok = false;
                     break;
                 }
@@ -363,7 +381,7 @@ __device__ __forceinline__ void produce(const CUtensorMap *tm, const CUtensorMap
                         tma_load_4d(dst + kAtom, tm_q, 64, p.head * a.s.group, p.r.tok0, p.q, &c.q_full[n & 1]);
                     }
                 }
-            } else if (!warp_wait_or_abort(&c.v_empty[s], ((t / kStages) & 1) ^ 1, c, a)) {
+            } else if (!warp_wait(&c.v_empty[s], ((t / kStages) & 1) ^ 1, c, a)) {
                 ok = false;
                 break;
             }
@@ -395,7 +413,7 @@ __device__ __forceinline__ void schedule(const PrefixArgs &a, const Start &st, i
     int64_t at = st.at;
     bool any = true;  // the request has a key tile at all
     while (at < st.end) {
-        if (n >= kRing && !warp_wait_or_abort(&c.ring_empty[n % kRing], (n / kRing - 1) & 1, c, a)) return;
+        if (n >= kRing && !warp_wait(&c.ring_empty[n % kRing], (n / kRing - 1) & 1, c, a)) return;
         Piece &p = c.ring[n % kRing];
         int tiles = 0;
         for (;;) {
@@ -420,7 +438,7 @@ __device__ __forceinline__ void schedule(const PrefixArgs &a, const Start &st, i
             p.j1 = j1;
             p.part = j == 0 && j1 == tiles ? -1 : j > 0 ? 0 : 1;
             if (p.part == 1) {
-                const int last = prefix::last_cta(at + tiles, st.work, st.n);
+                const int last = prefix::cta_of(st.ranges, at + tiles - 1);
                 a.cut[blockIdx.x] = Cut{last - static_cast<int>(blockIdx.x) + 1, q, head, rt};
             }
         }
@@ -456,11 +474,11 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             if (!p) return false;
             sj = p->j0;
             sj1 = p->j1;
-            if (!warp_wait_or_abort(&c.q_full[sn & 1], (sn >> 1) & 1, c, a)) return false;
+            if (!warp_wait(&c.q_full[sn & 1], (sn >> 1) & 1, c, a)) return false;
             ++sn;
         }
         const int qb = (sn - 1) & 1, s = t % kStages;
-        if (!warp_wait_or_abort(&c.k_full[s], (t / kStages) & 1, c, a)) return false;
+        if (!warp_wait(&c.k_full[s], (t / kStages) & 1, c, a)) return false;
         tc_fence_after();
         const uint64_t qd = umma::smem_desc_kmajor_sw128(saddr(sq + qb * kTileBytes));
         const uint64_t qd1 = umma::smem_desc_kmajor_sw128(saddr(sq + qb * kTileBytes + kAtom));
@@ -475,20 +493,26 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
         ++sj;
         return true;
     };
-    uint32_t t = 0;
-    for (uint32_t x = 0; x < min(tiles, static_cast<uint32_t>(kStages)) && ok; ++x) ok = scores(x);
-    for (int n = 0; t < tiles && ok; ++n) {
-        const Piece *pp = next_piece(n, c, a);
-        if (!pp) break;
-        const Piece &p = *pp;
-        for (int j = p.j0; j < p.j1; ++j, ++t) {
+    // step x: the product of tile x - 2, then the scores of tile x
+    const Piece *pp = nullptr;
+    int n = -1, j = 0;  // the product's piece and tile
+#pragma unroll 1
+    for (uint32_t x = 0; x < tiles + kStages && ok; ++x) {
+        if (x >= kStages) {
+            const uint32_t t = x - kStages;
+            if (!pp || j == pp->j1) {
+                if (pp) release_piece(n, lane, c);
+                if (!(pp = next_piece(++n, c, a))) break;
+                j = pp->j0;
+            }
+            const Piece &p = *pp;
             const int h = t % kStages;
             prefix::Step st{};
             if (j >= p.shared_tiles)
                 st = prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane & 7);
             // the first product of a piece overwrites O: the previous piece's read-out must be done
-            if ((j == p.j0 && !warp_wait_or_abort(&c.o_free, (n & 1) ^ 1, c, a)) ||
-                !warp_wait_or_abort(&c.v_full[h], (t / kStages) & 1, c, a)) {
+            if ((j == p.j0 && !warp_wait(&c.o_free, (n & 1) ^ 1, c, a)) ||
+                !warp_wait(&c.v_full[h], (t / kStages) & 1, c, a)) {
                 ok = false;
                 break;
             }
@@ -506,7 +530,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                     __syncwarp();
                 }
             }
-            if (!warp_wait_or_abort(&c.p_full[h], (t / kStages) & 1, c, a)) {
+            if (!warp_wait(&c.p_full[h], (t / kStages) & 1, c, a)) {
                 ok = false;
                 break;
             }
@@ -534,10 +558,11 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             }
             mma_commit(&c.v_empty[h], issue);
             if (j == p.j1 - 1) mma_commit(&c.o_ready, issue);  // the piece's O is complete
-            if (t + kStages < tiles && !(ok = scores(t + kStages))) break;
+            ++j;
         }
-        if (ok) release_piece(n, lane, c);
+        if (x < tiles) ok = scores(x);
     }
+    if (pp && ok) release_piece(n, lane, c);
     mma_commit(&c.mma_done, issue);
     if (lane == 0) wait_drain(&c.mma_done, 0);
     __syncwarp();
@@ -550,7 +575,7 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
     const int r = q * 32 + lane;
     const uint32_t lane_off = static_cast<uint32_t>(q * 32) << 16;
     const uint32_t sbuf = tmem + lane_off + h * 128, obuf = tmem + lane_off + kOCol + h * 128;
-    const int tok = r / a.s.group;  // the row's token in the tile
+    const int tok = prefix::quotient(r, a.s.by_group);  // the row's token in the tile
     bool ok = true;
     uint32_t t0 = 0;  // first tile of the piece
     for (int n = 0; t0 < tiles && ok; ++n) {
@@ -560,7 +585,7 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
         int limit = 0, own_off = 0, own_end = 0;
         bool live = false;
         if (tok < p.r.n_tok) {
-            const int g = p.r.tok0 + tok, b = g / a.s.n_q, i = b - p.r.b0;
+            const int g = p.r.tok0 + tok, b = prefix::quotient(g, a.s.by_n_q), i = b - p.r.b0;
             live = p.len[i] >= 0;
             limit = prefix::row_limit(a.s, p.len[i], g - b * a.s.n_q);
             own_off = p.off[i];
@@ -572,14 +597,14 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
             const uint32_t t = t0 + x;
             const int j = p.j0 + x;
             prefix::Columns col = prefix::row_columns(a.s, j, p.shared_tiles, p.shared, own_off, limit);
-            if (!warp_wait_or_abort(&c.s_full[h], (t / kStages) & 1, c, a)) {
+            if (!warp_wait(&c.s_full[h], (t / kStages) & 1, c, a)) {
                 ok = false;
                 break;
             }
             tc_fence_after();
             const uint32_t bad = c.bad[t % 4];
             if (bad && col.lo < col.hi) {  // a page of this row's keys does not exist: NaN
-                const int u0 = col.lo / a.s.slot, u1 = (col.hi - 1) / a.s.slot;
+                const int u0 = col.lo >> a.s.slot_log, u1 = (col.hi - 1) >> a.s.slot_log;
                 if (bad >> u0 & low_bits(u1 - u0 + 1)) {
                     l = NAN;
                     col.hi = col.lo;
@@ -587,7 +612,7 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
             }
             // A warp without a row whose P is read has nothing to do: steps of own tiles write the rows
             // of their sequence only, and what becomes of rows that are not stored does not matter.
-            const int first = (j - p.shared_tiles) * a.s.spt;
+            const int first = (j - p.shared_tiles) << a.s.spt_log;
             const bool takes = live && (j < p.shared_tiles || (own_off < first + a.s.spt && own_end > first));
             if (__any_sync(kFull, takes)) {
                 uint32_t s0[32], s1[32], s2[32], s3[32];  // the row's 128 scores
@@ -681,28 +706,27 @@ template <bool kF16>
 __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_t stage, uint32_t tiles, Ctl &c,
                                          const PrefixArgs &a) {
     uint32_t t0 = 0;
-    const uint32_t inv_group = (65536u + a.s.group - 1) / a.s.group;  // (row * it) >> 16 = row / group for row < 128
     for (int n = 0; t0 < tiles; ++n) {
         const Piece *pp = next_piece(n, c, a);
         if (!pp) return;
         const Piece &p = *pp;
         const int count = p.j1 - p.j0;
-        if (!warp_wait_or_abort(&c.o_ready, n & 1, c, a)) return;
-        tc_fence_after();
         const int r = q * 32 + lane;
         // the rows this lane stores: 4 i + lane / 8
         int64_t to[8];
         uint32_t store = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int rr = q * 32 + i * 4 + (lane >> 3), tok = static_cast<int>(rr * inv_group >> 16);
+            const int rr = q * 32 + i * 4 + (lane >> 3), tok = prefix::quotient(rr, a.s.by_group);
             to[i] = 0;
-            if (tok < p.r.n_tok && p.len[(p.r.tok0 + tok) / a.s.n_q - p.r.b0] >= 0) {
+            if (tok < p.r.n_tok && p.len[prefix::quotient(p.r.tok0 + tok, a.s.by_n_q) - p.r.b0] >= 0) {
                 store |= 1u << i;
                 to[i] = p.q * a.out_req + (p.r.tok0 + tok) * a.out_token +
                         (p.head * a.s.group + rr - tok * a.s.group) * a.out_head;
             }
         }
+        if (!warp_wait(&c.o_ready, n & 1, c, a)) return;
+        tc_fence_after();
         const bool both = count > 1;
         const int only = static_cast<int>(t0) & 1;  // the half of a one-tile piece's tile
         float2 e = c.ml[n & 3][both ? 0 : only][r];
@@ -722,8 +746,8 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
             w0 *= inv;
             w1 *= inv;
             if (a.lse) {
-                const int tok = static_cast<int>(r * inv_group >> 16);
-                if (tok < p.r.n_tok && p.len[(p.r.tok0 + tok) / a.s.n_q - p.r.b0] >= 0)
+                const int tok = prefix::quotient(r, a.s.by_group);
+                if (tok < p.r.n_tok && p.len[prefix::quotient(p.r.tok0 + tok, a.s.by_n_q) - p.r.b0] >= 0)
                     a.lse[(static_cast<int64_t>(p.q) * a.s.n_tokens + p.r.tok0 + tok) * a.n_heads + p.head * a.s.group +
                           r - tok * a.s.group] = e.y == 0.f ? -INFINITY : (e.x + log2f(e.y)) * kLn2;
             }
@@ -865,6 +889,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (threadIdx.x == 0 && c.abort_flag) flag_error(a.err, RPS_DEVERR_TIMEOUT);
     if (warp == 1) tmem_dealloc(tmem, kTmemCols);
 }
 
@@ -913,7 +938,7 @@ __device__ __forceinline__ Joined join_parts(const PrefixArgs &a, int cta, int r
 template <bool kF16>
 __device__ __forceinline__ void store_row(const PrefixArgs &a, const Cut &cut, const RowTile &r, int row,
                                           const Joined &x, int lane) {
-    const int tok = r.tok0 + row / a.s.group, h = cut.head * a.s.group + row % a.s.group;
+    const int t = prefix::quotient(row, a.s.by_group), tok = r.tok0 + t, h = cut.head * a.s.group + row - t * a.s.group;
     const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
     const uint2 v = make_uint2(pack16<kF16>(x.o.x * inv, x.o.y * inv), pack16<kF16>(x.o.z * inv, x.o.w * inv));
     *reinterpret_cast<uint2 *>(static_cast<char *>(a.out) +
@@ -965,7 +990,7 @@ __global__ void __launch_bounds__(kCombineThreads) prefix_combine_kernel(const P
         const bool few = cut.parts <= kFewParts;
         const int row = few ? (u - first_unit[i]) * 8 + warp : u - first_unit[i];
         const bool there = row < rows && a.len[static_cast<int64_t>(cut.q) * a.s.n_branch +
-                                               (r.tok0 + row / a.s.group) / a.s.n_q] >= 0;
+                                               prefix::quotient(r.tok0 + prefix::quotient(row, a.s.by_group), a.s.by_n_q)] >= 0;
         if (few) {
             if (there) store_row<kF16>(a, cut, r, row, join_parts(a, i, row, 0, cut.parts, 1, lane), lane);
             continue;
@@ -1044,7 +1069,7 @@ rps_status check_shape(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads, int
     if (n_q < 1 || n_heads < 1 || n_heads % kv->n_heads) return RPS_ERR_INVALID_ARG;
     if (n_heads / kv->n_heads > RPS_KV_MAX_GROUP) return RPS_ERR_UNSUPPORTED;
     const int64_t tokens = static_cast<int64_t>(kv->n_branch) * n_q;
-    if (tokens > INT32_MAX / 256 || static_cast<int64_t>(kv->n_req) * tokens > INT32_MAX / 2) return RPS_ERR_UNSUPPORTED;
+    if (tokens > INT32_MAX / 256 || static_cast<int64_t>(kv->n_req) * tokens > INT32_MAX / 256) return RPS_ERR_UNSUPPORTED;
     // slots of the sequences of one row tile
     const int64_t slots = static_cast<int64_t>(kv->max_pages) * std::max(1, kv->page_size / prefix::kRows);
     if (std::min<int64_t>(kv->n_branch, kMaxSeqs) * slots > INT32_MAX / 256) return RPS_ERR_UNSUPPORTED;

@@ -10,7 +10,7 @@
 // sequences' own slots, one sequence after another with no gap (a sequence's last
 // slot may be partly filled).
 // Work. Key tiles are numbered through (request, head, row tile, key tile), and
-// CTA c of n <= W takes tiles [c W / n, (c + 1) W / n): equal parts, so a row tile may
+// the n <= W CTAs take equal parts (to one tile) of the W of them, so a row tile may
 // be spread over several CTAs, whose partial results are joined afterwards.
 #pragma once
 
@@ -27,13 +27,34 @@ namespace prefix {
 
 constexpr int kRows = 128;  // rows of a row tile, keys of a key tile
 
+// Division of 0 <= n < 2^31 by a constant d: with l = ceil(log2 d) and mul = ceil(2^(31 + l) / d),
+// n mul / 2^(31 + l) exceeds n / d by less than n / 2^31 / d * (d / 2^l) < 1 / d, so its floor is
+// the quotient. (The compiler's code for a division by a variable is several times as long; the
+// roles' code has to fit the instruction cache together.)
+struct Div {
+    uint32_t mul, shift;
+};
+PREFIX_HD Div make_div(int d) {
+    Div v;
+    uint32_t l = 0;
+    while ((int64_t{1} << l) < d) ++l;
+    v.shift = 31 + l;
+    v.mul = static_cast<uint32_t>(((uint64_t{1} << v.shift) + static_cast<uint64_t>(d) - 1) / static_cast<uint64_t>(d));
+    return v;
+}
+PREFIX_HD int quotient(int n, const Div &v) {
+    return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(n)) * v.mul >> v.shift);
+}
+
 struct Shape {
     int32_t n_req, n_branch, n_q, n_tokens;   // n_tokens = n_branch * n_q
     int32_t heads, group;                     // cache heads, query heads per cache head
     int32_t tokens, row_tiles;                // tokens of a row tile, row tiles of a (request, head)
     int32_t page, slot, sub, spt;             // tokens of a page, of a slot; slots per page, per key tile
+    int32_t page_log, slot_log, sub_log, spt_log;  // all four are powers of two
     int32_t n_pages, max_pages;
     int32_t causal;
+    Div by_n_q, by_group, by_row_tiles;
 };
 
 PREFIX_HD int imin(int a, int b) { return a < b ? a : b; }
@@ -55,11 +76,22 @@ PREFIX_HD Shape make_shape(int n_req, int n_branch, int n_q, int heads, int grou
     s.slot = imin(page, kRows);
     s.sub = page / s.slot;
     s.spt = kRows / s.slot;
+    s.page_log = s.slot_log = s.sub_log = s.spt_log = 0;
+    while ((1 << s.page_log) < s.page) ++s.page_log;
+    while ((1 << s.slot_log) < s.slot) ++s.slot_log;
+    while ((1 << s.sub_log) < s.sub) ++s.sub_log;
+    while ((1 << s.spt_log) < s.spt) ++s.spt_log;
+    s.by_n_q = make_div(n_q);
+    s.by_group = make_div(group);
+    s.by_row_tiles = make_div(s.row_tiles);
     s.n_pages = n_pages;
     s.max_pages = max_pages;
     s.causal = causal;
     return s;
 }
+
+PREFIX_HD int slots_of(const Shape &s, int len) { return (len + s.slot - 1) >> s.slot_log; }
+PREFIX_HD int tiles_of(const Shape &s, int slots) { return (slots + s.spt - 1) >> s.spt_log; }
 
 // A sequence's length as it is used: -1 absent, at most what its table row holds.
 PREFIX_HD int used_len(const Shape &s, int len) { return len < 0 ? -1 : imin(len, s.max_pages * s.page); }
@@ -72,8 +104,8 @@ PREFIX_HD RowTile row_tile(const Shape &s, int rt) {
     RowTile r;
     r.tok0 = rt * s.tokens;
     r.n_tok = imin(s.tokens, s.n_tokens - r.tok0);
-    r.b0 = r.tok0 / s.n_q;
-    r.nb = (r.tok0 + r.n_tok - 1) / s.n_q - r.b0 + 1;
+    r.b0 = quotient(r.tok0, s.by_n_q);
+    r.nb = quotient(r.tok0 + r.n_tok - 1, s.by_n_q) - r.b0 + 1;
     return r;
 }
 
@@ -84,27 +116,61 @@ struct KeySum {
 PREFIX_HD void add_sequence(const Shape &s, KeySum &k, int len) {
     if (len < 0) return;
     ++k.present;
-    k.slots += ceil_div(len, s.slot);
-    k.min_pages = imin(k.min_pages, len / s.page);
+    k.slots += slots_of(s, len);
+    k.min_pages = imin(k.min_pages, len >> s.page_log);
 }
 // Slots that are read once for all: whole pages inside the shared length and inside every sequence.
 PREFIX_HD int shared_slots(const Shape &s, const KeySum &k, int shared_len) {
-    return k.present ? imin(imax(0, shared_len) / s.page, k.min_pages) * s.sub : 0;
+    return k.present ? imin(imax(0, shared_len) >> s.page_log, k.min_pages) << s.sub_log : 0;
 }
 // Key tiles: none where no sequence is there, at least one else (rows that see nothing are written too).
 PREFIX_HD int key_tiles(const Shape &s, const KeySum &k, int shared) {
     if (!k.present) return 0;
     const int own = k.slots - k.present * shared;
-    return imax(1, ceil_div(shared, s.spt) + ceil_div(own, s.spt));
+    return imax(1, tiles_of(s, shared) + tiles_of(s, own));
 }
 
-PREFIX_HD int64_t range_start(int c, int64_t work, int n) { return static_cast<int64_t>(c) * work / n; }
-// The CTA that takes tile x - 1 (x >= 1).
-PREFIX_HD int last_cta(int64_t x, int64_t work, int n) { return static_cast<int>((x * n - 1) / work); }
+// The n CTAs' ranges: `base` tiles each, the first `extra` one more. (By 16-bit digits:
+// n is small.)
+struct Ranges {
+    int64_t base;
+    int32_t extra, n;
+};
+PREFIX_HD Ranges make_ranges(int64_t work, int n) {
+    Ranges r;
+    const uint32_t d = static_cast<uint32_t>(n);  // at most 2^16
+    uint64_t q = 0;
+    uint32_t rem = 0;
+#pragma unroll 1
+    for (int at = 48; at >= 0; at -= 16) {
+        const uint32_t part = (rem << 16) | static_cast<uint32_t>(static_cast<uint64_t>(work) >> at & 0xffffu);
+        q = q << 16 | part / d;
+        rem = part % d;
+    }
+    r.base = static_cast<int64_t>(q);
+    r.extra = static_cast<int32_t>(rem);
+    r.n = n;
+    return r;
+}
+PREFIX_HD int64_t range_start(const Ranges &r, int c) { return c * r.base + imin(c, r.extra); }
+// The CTA that takes tile x.
+PREFIX_HD int cta_of(const Ranges &r, int64_t x) {
+    int lo = 0, hi = r.n;
+#pragma unroll 1
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (range_start(r, mid) <= x)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
 
 // The sequence i of [0, nb) that holds own slot x (off[i] <= x < off[i + 1]; x < off[nb]).
 PREFIX_HD int slot_owner(const int32_t *off, int nb, int x) {
     int lo = 0, hi = nb;
+#pragma unroll 1
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (off[mid] <= x)
@@ -148,9 +214,9 @@ PREFIX_HD Step own_step(const Shape &s, const RowTile &r, const int32_t *off, co
                         int shared, int j0, int j, int kk) {
     Step st;
     st.who = st.keys = st.r0 = st.r1 = st.fresh = 0;
-    const int first = (j - shared_tiles) * s.spt, x = first + kk * 16 / s.slot;
+    const int first = (j - shared_tiles) * s.spt, x = first + (kk * 16 >> s.slot_log);
     if (x >= off[r.nb]) return st;
-    const int i = slot_owner(off, r.nb, x), inner = kk * 16 % s.slot;
+    const int i = slot_owner(off, r.nb, x), inner = kk * 16 & (s.slot - 1);
     const int key = (x - off[i] + shared) * s.slot + inner;
     st.who = i;
     st.keys = imax(0, imin(16, len[i] - key));
@@ -158,7 +224,7 @@ PREFIX_HD Step own_step(const Shape &s, const RowTile &r, const int32_t *off, co
     st.r0 = t0 * s.group;
     st.r1 = t1 * s.group;
     const int begin = imax(off[i], first);  // the sequence's first slot in this tile
-    const int prev = j - 2, from = shared_tiles + off[i] / s.spt, oldest = j0 + ((j - j0) & 1);
+    const int prev = j - 2, from = shared_tiles + (off[i] >> s.spt_log), oldest = j0 + ((j - j0) & 1);
     const bool touched = prev >= j0 && (prev >= from || oldest < shared_tiles);
     st.fresh = x == begin && inner == 0 && !touched;
     return st;

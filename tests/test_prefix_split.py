@@ -22,6 +22,14 @@ using namespace rps::prefix;
 #define CHECK(x) do { if (!(x)) { std::printf("line %d: %s (trial %d)\n", __LINE__, #x, trial); return 1; } } while (0)
 
 int main(int argc, char **argv) {
+    const int trial = -1;
+    for (int d = 1; d < 5000; d += 1 + d / 50) {
+        const Div v = make_div(d);
+        for (int64_t n = 0; n < (int64_t{1} << 31); n += 1 + n / 40 + d / 3)
+            for (int64_t m = n - 1; m <= n + 1; ++m)
+                if (m >= 0 && m < (int64_t{1} << 31)) CHECK(quotient(static_cast<int>(m), v) == m / d);
+        for (int64_t n = d; n < (int64_t{1} << 31); n += d * (1 + n / d / 9)) CHECK(quotient(static_cast<int>(n - 1), v) == (n - 1) / d && quotient(static_cast<int>(n), v) == n / d);
+    }
     std::mt19937 g(std::atoi(argv[1]));
     const auto rnd = [&](int lo, int hi) { return lo + static_cast<int>(g() % static_cast<unsigned>(hi - lo + 1)); };
     for (int trial = 0; trial < 12; ++trial) {
@@ -52,6 +60,11 @@ int main(int argc, char **argv) {
                     work += t;
                 }
         const int n = static_cast<int>(std::min<int64_t>(rnd(1, 160), std::max<int64_t>(1, work)));
+        if (!work) continue;
+        const Ranges ranges = make_ranges(work, n);
+        CHECK(ranges.base == work / n && ranges.extra == work % n);
+        CHECK(make_ranges(work * 1000003 * 4099, n).base == work * 1000003 * 4099 / n);
+        const auto range_start = [&](int c, int64_t, int) { return rps::prefix::range_start(ranges, c); };
         int64_t sum = 0;
         for (int c = 0; c < n; ++c) sum += range_start(c + 1, work, n) - range_start(c, work, n);
         CHECK(sum == work);
@@ -70,7 +83,7 @@ int main(int argc, char **argv) {
                 last = c;
                 pieces.push_back({static_cast<int>(lo - x.start), static_cast<int>(hi - x.start)});
             }
-            CHECK(last_cta(x.start + x.tiles, work, n) == last);
+            CHECK(cta_of(ranges, x.start + x.tiles - 1) == last && cta_of(ranges, x.start) == first);
             if (covered[x.q * s.row_tiles + x.rt]++) continue;  // (another head: the same but for its pieces' ends)
             const RowTile r = row_tile(s, x.rt);
             CHECK(r.nb >= 1 && r.nb <= kRows && r.b0 + r.nb <= nb);
