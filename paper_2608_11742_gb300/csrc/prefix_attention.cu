@@ -94,7 +94,7 @@ struct PrefixArgs {
     float2 *part_ml;  // [2 * kMaxCtas][128]: maximum and sum of each row of a partial result
     float *part_o;    // [2 * kMaxCtas][128][128]
     uint32_t *err;
-    uint64_t wait_ns;
+    uint32_t wait_ns;
 };
 
 struct Piece {
@@ -117,6 +117,8 @@ struct Ctl {
     // piece n + 4, whose P needs the products of piece n + 2 and so the read-out of piece n + 1
     float2 ml[4][kStages][prefix::kRows];
     Piece ring[kRing];
+    uint4 step_off[8];      // own tile at hand: rows that step kk leaves alone
+    int32_t step_fresh[8];  // 1: the step overwrites
     uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
     int64_t p0, p1;
@@ -126,6 +128,11 @@ struct Ctl {
 };
 
 // ---------------------------------------------------------------- waits
+__device__ __forceinline__ uint32_t global_ns_low() {
+    uint32_t t;
+    asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
+    return t;
+}
 // Waits for a phase of a barrier, at most a.wait_ns, all lanes; the warp goes on
 // together, on the same answer. A wait that runs out raises the abort flag, which ends
 // the other roles' waits and is reported when the CTA ends. (Short: every role's waits
@@ -133,10 +140,10 @@ struct Ctl {
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl &c, const PrefixArgs &a) {
     bool ok = a.wait_ns != 0 && mbar_try_wait(bar, parity);
     if (!__all_sync(kFull, ok)) {
-        const uint64_t start = global_ns();
+        const uint32_t start = global_ns_low();
 #pragma unroll 1
         while (!(ok = a.wait_ns != 0 && mbar_try_wait(bar, parity)))
-            if (*reinterpret_cast<volatile int *>(&c.abort_flag) || global_ns() - start >= a.wait_ns) break;
+            if (*reinterpret_cast<volatile int *>(&c.abort_flag) || global_ns_low() - start >= a.wait_ns) break;
         ok = __all_sync(kFull, ok);
         if (!ok) *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
     }
@@ -345,53 +352,49 @@ __device__ __forceinline__ void slot_page(const PrefixArgs &a, const Piece &p, i
     if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.s.n_pages)) page = a.s.n_pages;
 }
 
-// The producers of K (with Q) and of V.
-template <bool kIsK>
-__device__ __forceinline__ void produce(const CUtensorMap *tm, const CUtensorMap *tm_q, uint8_t *stages, uint8_t *sq,
-                                        uint32_t tiles, int lane, Ctl &c, const PrefixArgs &a) {
+// The producers of K (with Q) and of V, in one body: two warps run it.
+__device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const CUtensorMap *tm_q, uint8_t *stages,
+                                        uint8_t *sq, uint32_t tiles, int lane, Ctl &c, const PrefixArgs &a) {
     uint32_t t = 0;
     int n = 0, n_q = 0;
     bool ok = true;
-    const uint32_t q_bytes = 2u * a.s.group * a.s.tokens * 128;
+    uint64_t *full = is_k ? c.k_full : c.v_full;
+    // K: S of tile t - 2 is computed, so its stage is free, and at a piece's first tile the Q
+    // buffer of piece n - 2, whose last tile is no later. V: the product of tile t - 2 is done.
+    uint64_t *empty = is_k ? c.s_full : c.v_empty;
+#pragma unroll 1
     for (; t < tiles && ok; ++n) {
         const Piece *pp = next_piece(n, c, a);
         if (!pp) break;
         const Piece &p = *pp;
+#pragma unroll 1
         for (int j = p.j0; j < p.j1; ++j, ++t) {
             const int s = t % kStages;
-            int page, token;
+            int page = 0, token = 0;
             bool there = false;
             if (lane < a.s.spt) slot_page(a, p, j, lane, page, token, there);
-            if (kIsK) {
-                // S of tile t - 2 is computed: its K stage is free, and at a piece's first tile
-                // the Q buffer of piece n - 2, whose last tile is no later
-                if (t >= kStages && !warp_wait(&c.s_full[s], (t / kStages - 1) & 1, c, a)) {
-                    ok = false;
-                    break;
-                }
-                if (j == p.j0) ++n_q;
+            if (t >= kStages && !(ok = warp_wait(&empty[s], (t / kStages - 1) & 1, c, a))) break;
+            if (is_k) {
                 const uint32_t bad = __ballot_sync(kFull, there && page == a.s.n_pages);
                 if (lane == 0) {
                     c.bad[t % 4] = bad;
                     if (bad) flag_error(a.err, RPS_DEVERR_PAGE);
                     if (j == p.j0) {
-                        mbar_expect_tx(&c.q_full[n & 1], q_bytes);
+                        uint64_t *q_full = &c.q_full[n & 1];
+                        mbar_expect_tx(q_full, 2u * a.s.group * a.s.tokens * 128);
                         uint8_t *dst = sq + (n & 1) * kTileBytes;
-                        tma_load_4d(dst, tm_q, 0, p.head * a.s.group, p.r.tok0, p.q, &c.q_full[n & 1]);
-                        tma_load_4d(dst + kAtom, tm_q, 64, p.head * a.s.group, p.r.tok0, p.q, &c.q_full[n & 1]);
+                        tma_load_4d(dst, tm_q, 0, p.head * a.s.group, p.r.tok0, p.q, q_full);
+                        tma_load_4d(dst + kAtom, tm_q, 64, p.head * a.s.group, p.r.tok0, p.q, q_full);
+                        ++n_q;
                     }
                 }
-            } else if (!warp_wait(&c.v_empty[s], ((t / kStages) & 1) ^ 1, c, a)) {
-                ok = false;
-                break;
             }
-            uint64_t *full = kIsK ? &c.k_full[s] : &c.v_full[s];
-            if (lane == 0) mbar_expect_tx(full, kTileBytes);
+            if (lane == 0) mbar_expect_tx(&full[s], kTileBytes);
             __syncwarp();
             if (lane < a.s.spt) {  // (slots that are not there: zeros)
                 uint8_t *dst = stages + s * kTileBytes + lane * a.s.slot * 128;
-                tma_load_4d(dst, tm, 0, token, p.head, page, full);
-                tma_load_4d(dst + kAtom, tm, 64, token, p.head, page, full);
+                tma_load_4d(dst, tm, 0, token, p.head, page, &full[s]);
+                tma_load_4d(dst + kAtom, tm, 64, token, p.head, page, &full[s]);
             }
             __syncwarp();
         }
@@ -399,10 +402,13 @@ __device__ __forceinline__ void produce(const CUtensorMap *tm, const CUtensorMap
     }
     // every copy issued lands before the CTA leaves
     if (lane == 0) {
-        for (uint32_t x = t > kStages ? t - kStages : 0; x < t; ++x)
-            wait_drain(kIsK ? &c.k_full[x % kStages] : &c.v_full[x % kStages], (x / kStages) & 1);
-        if (kIsK)
-            for (int x = n_q > kQBufs ? n_q - kQBufs : 0; x < n_q; ++x) wait_drain(&c.q_full[x & 1], (x >> 1) & 1);
+#pragma unroll 1
+        for (uint32_t x = t > kStages ? t - kStages : 0; x < t + 2; ++x) {
+            if (x < t)
+                wait_drain(&full[x % kStages], (x / kStages) & 1);
+            else if (n_q > static_cast<int>(x - t))  // Q: the last two
+                wait_drain(&c.q_full[(n_q - 1 - (x - t)) & 1], ((n_q - 1 - (x - t)) >> 1) & 1);
+        }
     }
     __syncwarp();
 }
@@ -507,9 +513,23 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             }
             const Piece &p = *pp;
             const int h = t % kStages;
-            prefix::Step st{};
-            if (j >= p.shared_tiles)
-                st = prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane & 7);
+            const bool own = j >= p.shared_tiles;
+            uint32_t steps = 0, ragged = 0;  // steps with keys; with fewer than 16
+            int keys = 0;
+            if (own) {
+                const prefix::Step st =
+                    prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane & 7);
+                keys = st.keys;
+                steps = __ballot_sync(kFull, lane < 8 && keys > 0);
+                ragged = __ballot_sync(kFull, lane < 8 && keys > 0 && keys < 16);
+                if (lane < 8) {
+                    c.step_off[lane] = make_uint4(
+                        ~(low_bits(st.r1) & ~low_bits(st.r0)), ~(low_bits(st.r1 - 32) & ~low_bits(st.r0 - 32)),
+                        ~(low_bits(st.r1 - 64) & ~low_bits(st.r0 - 64)), ~(low_bits(st.r1 - 96) & ~low_bits(st.r0 - 96)));
+                    c.step_fresh[lane] = st.fresh;
+                }
+                __syncwarp();
+            }
             // the first product of a piece overwrites O: the previous piece's read-out must be done
             if ((j == p.j0 && !warp_wait(&c.o_free, (n & 1) ^ 1, c, a)) ||
                 !warp_wait(&c.v_full[h], (t / kStages) & 1, c, a)) {
@@ -517,18 +537,17 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                 break;
             }
             uint8_t *vb = sv + h * kTileBytes;
-            if (j >= p.shared_tiles) {  // rows of V past a sequence's last key
-                const uint32_t ragged = __ballot_sync(kFull, lane < 8 && st.keys > 0 && st.keys < 16);
-                if (ragged) {
-                    for (uint32_t m = ragged; m; m &= m - 1) {
-                        const int kk = __ffs(m) - 1, keys = __shfl_sync(kFull, st.keys, kk);
-                        for (int x = lane; x < (16 - keys) * 16; x += 32)  // 8 16-byte units in each of two atoms
-                            st_shared_v4(saddr(vb + (x & 8 ? kAtom : 0) + (kk * 16 + keys + (x >> 4)) * 128 + (x & 7) * 16),
-                                         make_uint4(0, 0, 0, 0));
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
+            if (ragged) {  // rows of V past a sequence's last key
+#pragma unroll 1
+                for (uint32_t m = ragged; m; m &= m - 1) {
+                    const int kk = __ffs(m) - 1, filled = __shfl_sync(kFull, keys, kk);
+#pragma unroll 1
+                    for (int y = lane; y < (16 - filled) * 16; y += 32)  // 8 16-byte units in each of two atoms
+                        st_shared_v4(saddr(vb + (y & 8 ? kAtom : 0) + (kk * 16 + filled + (y >> 4)) * 128 + (y & 7) * 16),
+                                     make_uint4(0, 0, 0, 0));
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
             }
             if (!warp_wait(&c.p_full[h], (t / kStages) & 1, c, a)) {
                 ok = false;
@@ -538,23 +557,21 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             // P of keys 16k..16k+15: columns 8k..8k+7 of S buffer t % 2
             const uint32_t pcol = tmem + h * 128, ocol = tmem + kOCol + h * 128;
             const uint64_t vd = umma::smem_desc_mnmajor_sw128(saddr(vb), kAtom);
-            if (j < p.shared_tiles) {
+            if (!own) {
                 const uint32_t more = j - p.j0 >= kStages;  // the half has had a tile of this piece
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     mma_bf16_ts(ocol, pcol + k * 8, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o, more | (k != 0),
                                 issue);
             } else {
-                for (uint32_t m = __ballot_sync(kFull, lane < 8 && st.keys > 0); m; m &= m - 1) {
-                    const int k = __ffs(m) - 1;
-                    const int r0 = __shfl_sync(kFull, st.r0, k), r1 = __shfl_sync(kFull, st.r1, k);
-                    const uint32_t fresh = __shfl_sync(kFull, st.fresh, k);
-                    uint32_t off[4];
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) off[w] = ~(low_bits(r1 - 32 * w) & ~low_bits(r0 - 32 * w));
+#pragma unroll 4
+                for (int k = 0; k < 8; ++k) {
+                    const uint4 o = c.step_off[k];
+                    const uint32_t off[4] = {o.x, o.y, o.z, o.w};
                     mma_bf16_ts_rows(ocol, pcol + k * 8, vd + static_cast<uint64_t>(k) * (2048 >> 4), idesc_o, off,
-                                     fresh ^ 1u, issue);
+                                     c.step_fresh[k] ^ 1, issue & (steps >> k));
                 }
+                __syncwarp();  // (the steps are written again)
             }
             mma_commit(&c.v_empty[h], issue);
             if (j == p.j1 - 1) mma_commit(&c.o_ready, issue);  // the piece's O is complete
@@ -697,126 +714,127 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     return kF16 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
 }
 
-// The read-out of the CTA's pieces; this warp's rows are TMEM lanes q * 32 .. + 31.
-// Rows go out through the warp's stage, 128 bytes of each at a time: written a row
-// per thread, read back so that each store instruction covers 128 contiguous bytes
-// of 4 rows. The 16-byte chunk index is XORed with the row's low three bits, so that
-// neither the writes nor the reads put two threads of a quarter-warp in one bank group.
+// The warp's stage (32 rows x 128 bytes) to the rows' addresses (0: not stored), 4 rows
+// of 128 contiguous bytes per instruction. Written a row per thread with the 16-byte
+// chunk index XORed with the row's low three bits, so that neither the writes nor the
+// reads put two threads of a quarter-warp in one bank group.
+__device__ __forceinline__ void store_stage(uint32_t stage, int lane, uint64_t row, uint32_t at) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int rr = i * 4 + (lane >> 3), x = lane & 7;
+        const uint64_t to = __shfl_sync(kFull, row, rr);
+        const uint4 v = ld_shared_v4(stage + rr * 128 + ((x ^ (rr & 7)) << 4));
+        if (to) *reinterpret_cast<uint4 *>(to + at + x * 16) = v;
+    }
+    __syncwarp();  // (the stage is rewritten next)
+}
+
+// The read-out of the CTA's pieces; this thread's row is TMEM lane q * 32 + lane. O is
+// handed back to the MMA as soon as it is in registers and the stage: the products
+// of the next piece wait for it.
 template <bool kF16>
 __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_t stage, uint32_t tiles, Ctl &c,
                                          const PrefixArgs &a) {
     uint32_t t0 = 0;
+    const int r = q * 32 + lane, tok = prefix::quotient(r, a.s.by_group);
+    const uint32_t col = tmem + (static_cast<uint32_t>(q * 32) << 16) + kOCol;
+#pragma unroll 1
     for (int n = 0; t0 < tiles; ++n) {
         const Piece *pp = next_piece(n, c, a);
         if (!pp) return;
         const Piece &p = *pp;
         const int count = p.j1 - p.j0;
-        const int r = q * 32 + lane;
-        // the rows this lane stores: 4 i + lane / 8
-        int64_t to[8];
-        uint32_t store = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int rr = q * 32 + i * 4 + (lane >> 3), tok = prefix::quotient(rr, a.s.by_group);
-            to[i] = 0;
-            if (tok < p.r.n_tok && p.len[prefix::quotient(p.r.tok0 + tok, a.s.by_n_q) - p.r.b0] >= 0) {
-                store |= 1u << i;
-                to[i] = p.q * a.out_req + (p.r.tok0 + tok) * a.out_token +
-                        (p.head * a.s.group + rr - tok * a.s.group) * a.out_head;
-            }
+        const bool whole = p.part < 0;
+        uint64_t row = 0;  // where this thread's row goes, 0: nowhere
+        float *lse = nullptr;
+        if (tok < p.r.n_tok && p.len[prefix::quotient(p.r.tok0 + tok, a.s.by_n_q) - p.r.b0] >= 0) {
+            const int t = p.r.tok0 + tok, h = p.head * a.s.group + r - tok * a.s.group;
+            row = whole ? reinterpret_cast<uint64_t>(a.out) + 2 * (p.q * a.out_req + t * a.out_token + h * a.out_head)
+                        : reinterpret_cast<uint64_t>(a.part_o + ((2 * blockIdx.x + p.part) * prefix::kRows + r) * kD);
+            if (whole && a.lse) lse = a.lse + (static_cast<int64_t>(p.q) * a.s.n_tokens + t) * a.n_heads + h;
         }
         if (!warp_wait(&c.o_ready, n & 1, c, a)) return;
         tc_fence_after();
         const bool both = count > 1;
         const int only = static_cast<int>(t0) & 1;  // the half of a one-tile piece's tile
         float2 e = c.ml[n & 3][both ? 0 : only][r];
-        float w0 = 1.f, w1 = 0.f;
-        if (both) {
-            const float2 f = c.ml[n & 3][1][r];
-            const float m = fmaxf(e.x, f.x), mr = m == -INFINITY ? 0.f : m;
-            w0 = e.y == 0.f ? 0.f : ex2(e.x - mr);
-            w1 = f.y == 0.f ? 0.f : ex2(f.x - mr);
-            // (weights of 0 for halves without weight: their accumulators may hold anything)
-            e = make_float2(m, (e.y == 0.f ? 0.f : w0 * e.y) + (f.y == 0.f ? 0.f : w1 * f.y));
-        } else if (e.y == 0.f) {
-            w0 = 0.f;
-        }
-        if (p.part < 0) {
-            const float inv = e.y == 0.f ? 0.f : 1.f / e.y;
+        float2 f = both ? c.ml[n & 3][1][r] : make_float2(-INFINITY, 0.f);
+        const float m = fmaxf(e.x, f.x), mr = m == -INFINITY ? 0.f : m;
+        float w0 = e.y == 0.f ? 0.f : ex2(e.x - mr), w1 = f.y == 0.f ? 0.f : ex2(f.x - mr);
+        const float l = w0 * e.y + w1 * f.y;  // (NaN stays)
+        if (whole) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
             w0 *= inv;
             w1 *= inv;
-            if (a.lse) {
-                const int tok = prefix::quotient(r, a.s.by_group);
-                if (tok < p.r.n_tok && p.len[prefix::quotient(p.r.tok0 + tok, a.s.by_n_q) - p.r.b0] >= 0)
-                    a.lse[(static_cast<int64_t>(p.q) * a.s.n_tokens + p.r.tok0 + tok) * a.n_heads + p.head * a.s.group +
-                          r - tok * a.s.group] = e.y == 0.f ? -INFINITY : (e.x + log2f(e.y)) * kLn2;
-            }
-        } else {
-            a.part_ml[(2 * blockIdx.x + p.part) * prefix::kRows + r] = e;
         }
-        const uint32_t col = tmem + (static_cast<uint32_t>(q * 32) << 16) + kOCol;
-        float *part = a.part_o + (static_cast<int64_t>(2 * blockIdx.x + max(p.part, 0)) * prefix::kRows + q * 32) * kD;
+        // (what has no weight may hold anything, NaN too: its bits are cleared)
+        const uint32_t keep0 = w0 == 0.f ? 0u : ~0u, keep1 = w1 == 0.f ? 0u : ~0u;
+        const bool zeros = __any_sync(kFull, (keep0 & keep1) == 0);
+        const f2 ww0 = pack2(w0, w0), ww1 = pack2(w1, w1);
+        const uint32_t at0 = col + (both ? 0 : only * 128), at1 = both ? col + 128 : at0;
+        uint32_t held[16];  // a chunk of the output that does not fit the stage yet
 #pragma unroll 1
         for (int ch = 0; ch < 4; ++ch) {  // 32 columns at a time
             uint32_t o0[32], o1[32];
-            const uint32_t cc = col + ch * 32;
-            tmem_ld32_async(cc + (both ? 0 : only * 128), o0);
-            if (both) {
-                tmem_ld32_async(cc + 128, o1);
-                tmem_wait_dep(o0);
-                tmem_wait_dep(o1);
+            tmem_ld32_async(at0 + ch * 32, o0);
+            tmem_ld32_async(at1 + ch * 32, o1);
+            tmem_wait_dep(o0);
+            tmem_wait_dep(o1);
+            if (zeros) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    o0[i] = __float_as_uint((w0 == 0.f ? 0.f : __uint_as_float(o0[i]) * w0) +
-                                            (w1 == 0.f ? 0.f : __uint_as_float(o1[i]) * w1));
-            } else {
-                tmem_wait_dep(o0);
+                for (int i = 0; i < 32; ++i) {
+                    o0[i] &= keep0;
+                    o1[i] &= keep1;
+                }
+            }
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    o0[i] = __float_as_uint(w0 == 0.f ? 0.f : __uint_as_float(o0[i]) * w0);
+            for (int i = 0; i < 32; i += 2) {
+                const f2 x = pack2(__uint_as_float(o0[i]), __uint_as_float(o0[i + 1]));
+                const f2 y = pack2(__uint_as_float(o1[i]), __uint_as_float(o1[i + 1]));
+                float lo, hi;
+                unpack2(fma2(y, ww1, mul2(x, ww0)), lo, hi);
+                o0[i] = __float_as_uint(lo);
+                o0[i + 1] = __float_as_uint(hi);
             }
             if (ch == 3) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&c.o_free);  // O may take the next piece
             }
-            if (p.part < 0) {  // 64 bytes of each row; a pair of chunks fills the stage
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    uint32_t pk[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        pk[i] = pack16<kF16>(__uint_as_float(o0[8 * u + 2 * i]), __uint_as_float(o0[8 * u + 2 * i + 1]));
-                    st_shared_v4(stage + lane * 128 + ((((ch & 1) * 4 + u) ^ (lane & 7)) << 4),
-                                 make_uint4(pk[0], pk[1], pk[2], pk[3]));
-                }
-                if (ch & 1) {
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int rr = i * 4 + (lane >> 3), x = lane & 7;
-                        const uint4 v = ld_shared_v4(stage + rr * 128 + ((x ^ (rr & 7)) << 4));
-                        if (store >> i & 1)
-                            *reinterpret_cast<uint4 *>(static_cast<char *>(a.out) +
-                                                       (to[i] + (ch >> 1) * 64 + x * 8) * 2) = v;
-                    }
-                    __syncwarp();  // the stage is rewritten next
-                }
-            } else {
+            if (!whole) {
 #pragma unroll
                 for (int u = 0; u < 8; ++u)
                     st_shared_v4(stage + lane * 128 + ((u ^ (lane & 7)) << 4),
                                  make_uint4(o0[4 * u], o0[4 * u + 1], o0[4 * u + 2], o0[4 * u + 3]));
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int rr = i * 4 + (lane >> 3), x = lane & 7;
-                    const uint4 v = ld_shared_v4(stage + rr * 128 + ((x ^ (rr & 7)) << 4));
-                    if (store >> i & 1) *reinterpret_cast<uint4 *>(part + rr * kD + ch * 32 + x * 4) = v;
-                }
-                __syncwarp();
+                store_stage(stage, lane, row, ch * 128);
+                continue;
             }
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                pk[i] = pack16<kF16>(__uint_as_float(o0[2 * i]), __uint_as_float(o0[2 * i + 1]));
+            // chunks 0 and 1 fill the stage; 2 is held; it and 3 follow when the first have left
+            if (ch == 2) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) held[i] = pk[i];
+                continue;
+            }
+            if (ch == 3) {
+                store_stage(stage, lane, row, 0);
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    st_shared_v4(stage + lane * 128 + ((u ^ (lane & 7)) << 4),
+                                 make_uint4(held[4 * u], held[4 * u + 1], held[4 * u + 2], held[4 * u + 3]));
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                st_shared_v4(stage + lane * 128 + ((((ch & 1) * 4 + u) ^ (lane & 7)) << 4),
+                             make_uint4(pk[4 * u], pk[4 * u + 1], pk[4 * u + 2], pk[4 * u + 3]));
         }
+        if (whole) store_stage(stage, lane, row, 128);
+        if (lse) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+        if (!whole) a.part_ml[(2 * blockIdx.x + p.part) * prefix::kRows + r] = make_float2(m, l);
         t0 += count;
         release_piece(n, lane, c);
     }
@@ -871,10 +889,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCtlRegs));
-        if (warp == 0)
-            produce<true>(&tm_k, &tm_q, sk, sq, tiles, lane, c, a);
-        else if (warp == 2)
-            produce<false>(&tm_v, nullptr, sv, nullptr, tiles, lane, c, a);
+        if (warp == 0 || warp == 2)
+            produce(warp == 0, warp == 0 ? &tm_k : &tm_v, &tm_q, warp == 0 ? sk : sv, sq, tiles, lane, c, a);
         else if (warp == 1)
             issue_products<kF16>(sq, sk, sv, tmem, tiles, lane, c, a);
         else if (tiles)
@@ -1142,7 +1158,7 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
     a.cut = reinterpret_cast<Cut *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(ws + ml_at);
     a.part_o = reinterpret_cast<float *>(ws + o_at);
-    a.wait_ns = ring_wait_limit_ns();
+    a.wait_ns = static_cast<uint32_t>(std::min<uint64_t>(ring_wait_limit_ns(), 4000000000u));
 
     // CTAs: as many as there can be key tiles
     const int64_t slots = static_cast<int64_t>(a.s.max_pages) * a.s.sub;
