@@ -637,7 +637,7 @@ size_t rps_prefix_attention_workspace_bytes(const rps_kv_cache *kv, int32_t n_q,
 
 /* Two launches on `stream`. Errors: RPS_ERR_INVALID_ARG for NULL or misaligned
  * pointers, sizes or strides out of range, or a small workspace;
- * RPS_ERR_UNSUPPORTED beyond the limits above or 2^23 tokens of a request;
+ * RPS_ERR_UNSUPPORTED beyond the limits above, 2^23 query tokens or 2^14 requests;
  * RPS_ERR_CUDA when the tensor-map encoder is not available. A bounded device wait
  * that gives up reports RPS_DEVERR_TIMEOUT (the output is then incomplete). */
 rps_status rps_prefix_attention_fwd(const rps_prefix_attention *attn, const rps_kv_cache *kv, void *d_ws,

@@ -72,7 +72,8 @@ constexpr int kRing = 4;             // pieces known ahead
 constexpr int kConsumers = 15;       // warps 0, 1, 2 and 4..15
 constexpr int kMaxSeqs = 128;        // sequences with rows in one row tile
 constexpr int kMaxCtas = 160;
-constexpr int kStagedLens = (2 * kStages * kTileBytes) / 4;  // lengths that fit the K and V stages
+constexpr int kStagedLens = 1024;    // lengths that are kept in shared memory
+constexpr int kMaxReqs = 2 * kStages * kTileBytes / 8;  // requests whose first tiles fit the K and V stages
 constexpr int kCombineThreads = 256;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -121,8 +122,7 @@ struct Ctl {
     int32_t step_fresh[8];  // 1: the step overwrites
     uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
-    int64_t p0, p1;
-    int32_t find_q, find_rt, find_j;
+    int32_t len[kStagedLens];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -151,19 +151,18 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl &c
 }
 
 // ---------------------------------------------------------------- the cut
-__device__ __forceinline__ int len_of(const PrefixArgs &a, int64_t s, const int32_t *staged) {
-    return prefix::used_len(a.s, staged ? staged[s] : a.len[s]);
+__device__ __forceinline__ int len_of(const PrefixArgs &a, int s, const Ctl &c) {
+    return prefix::used_len(a.s, a.s.n_req * a.s.n_branch <= kStagedLens ? c.len[s] : a.len[s]);
 }
 __device__ __forceinline__ int shared_len_of(const PrefixArgs &a, int q) { return a.shared_len ? a.shared_len[q] : 0; }
 
-// Key tiles of entry e = (request q, row tile rt), by one thread.
-__device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int q, int rt, const int32_t *staged) {
+// Key tiles of row tile rt of request q, by one thread.
+__device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int q, int rt, const Ctl &c) {
     const RowTile r = prefix::row_tile(a.s, rt);
     KeySum k{0, 0, INT32_MAX};
-    const int64_t s0 = static_cast<int64_t>(q) * a.s.n_branch + r.b0;
-    const int shared_len = shared_len_of(a, q);
+    const int s0 = q * a.s.n_branch + r.b0, shared_len = shared_len_of(a, q);
 #pragma unroll 1
-    for (int i = 0; i < r.nb; ++i) prefix::add_sequence(a.s, k, len_of(a, s0 + i, staged));
+    for (int i = 0; i < r.nb; ++i) prefix::add_sequence(a.s, k, len_of(a, s0 + i, c));
     return prefix::key_tiles(a.s, k, prefix::shared_slots(a.s, k, shared_len));
 }
 
@@ -189,68 +188,87 @@ __device__ __forceinline__ int64_t scan_block(int v, int64_t *sums, int64_t *tot
     return before + x - v;
 }
 
-// Where the CTA's range begins: request, cache head, row tile, key tile; and its length.
-struct Start {
-    int32_t q, head, rt, j;
+// The CTA's range of key tiles, of those of all (request, head, row tile) in order.
+struct Range {
     int64_t at, end;
-    prefix::Ranges ranges;
+    prefix::Ranges all;
 };
 
-__device__ __forceinline__ Start find_start(const PrefixArgs &a, Ctl &c, int32_t *stage) {
+// By all threads: the lengths into shared memory, and in first[q] the key tiles (of
+// one head: all heads of a request have the same) of the requests before q.
+__device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t *first) {
     const int entries = a.s.n_req * a.s.row_tiles, n_seq = a.s.n_req * a.s.n_branch;
-    const int32_t *staged = nullptr;
-    if (n_seq <= kStagedLens) {
+    if (n_seq <= kStagedLens)
 #pragma unroll 1
-        for (int i = threadIdx.x; i < n_seq; i += kThreads) stage[i] = a.len[i];
-        staged = stage;
-    }
-    if (threadIdx.x == 0) c.find_q = 0;
+        for (int i = threadIdx.x; i < n_seq; i += kThreads) c.len[i] = a.len[i];
     __syncthreads();
-    // Passes over the entries in blocks of 512, each looking at an entry's tiles and the tiles
-    // before it (of a single block they stay in registers): the total; the last request that
-    // starts at or before the range; that request's bounds; the row tile and key tile in it.
+    int64_t carry = 0;
+#pragma unroll 1
+    for (int base = 0; base < entries; base += kThreads) {
+        const int e = base + threadIdx.x;
+        const int q = prefix::quotient(e, a.s.by_row_tiles), rt = e - q * a.s.row_tiles;
+        int64_t total;
+        const int t = e < entries ? entry_tiles(a, q, rt, c) : 0;
+        const int64_t before = carry + scan_block(t, c.scan, &total);
+        if (e < entries && rt == 0) first[q] = before;
+        carry += total;
+    }
+    Range r{};
+    const int64_t work = carry * a.s.heads;
+    // (no more CTAs than key tiles: none in between is without work)
+    const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), work));
+    if (static_cast<int>(blockIdx.x) >= n) return r;
+    r.all = prefix::make_ranges(work, n);
+    r.at = prefix::range_start(r.all, blockIdx.x);
+    r.end = prefix::range_start(r.all, blockIdx.x + 1);
+    return r;
+}
+
+// By a warp: the request, head, row tile and key tile that the range begins with.
+struct Start {
+    int32_t q, head, rt, j;
+};
+__device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &range, const int64_t *first, int lane,
+                                            const Ctl &c) {
     Start st{};
-    int t = 0;
-    int64_t before = 0, in_head = 0;
+    int lo = 0, hi = a.s.n_req;  // the last request that starts at or before the range
 #pragma unroll 1
-    for (int pass = 0; pass < 4; ++pass) {
-        int64_t carry = 0;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] * a.s.heads <= range.at)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    st.q = lo;
+    int64_t rem = range.at - first[lo] * a.s.heads;  // tiles of the request before the range
+    int64_t per_head = 0;
 #pragma unroll 1
-        for (int base = 0; base < entries; base += kThreads) {
-            const int e = base + threadIdx.x;
-            const int q = prefix::quotient(e, a.s.by_row_tiles), rt = e - q * a.s.row_tiles;
-            if (pass == 0 || entries > kThreads) {
-                int64_t total;
-                t = e < entries ? entry_tiles(a, q, rt, staged) : 0;
-                before = carry + scan_block(t, c.scan, &total);
-                carry += total;
+    for (int pass = 0; pass < 2; ++pass) {  // the tiles of a head; then where the rest lies in them
+        int64_t before = 0;
+#pragma unroll 1
+        for (int base = 0; base < a.s.row_tiles; base += 32) {
+            const int t = base + lane < a.s.row_tiles ? entry_tiles(a, st.q, base + lane, c) : 0;
+            int upto = t;
+#pragma unroll 1
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(kFull, upto, o);
+                if (lane >= o) upto += u;
             }
-            if (e >= entries) continue;
             if (pass == 1) {
-                if (rt == 0 && before * a.s.heads <= st.at) atomicMax(&c.find_q, q);
-            } else if (pass == 2 && q == st.q) {
-                if (rt == 0) c.p0 = before;
-                if (rt == a.s.row_tiles - 1) c.p1 = before + t;
-            } else if (pass == 3 && q == st.q && before <= in_head && in_head < before + t) {
-                c.find_rt = rt;
-                c.find_j = static_cast<int>(in_head - before);
+                const uint32_t in = __ballot_sync(kFull, rem < before + upto);
+                if (in) {
+                    const int who = __ffs(in) - 1;
+                    st.rt = base + who;
+                    st.j = static_cast<int>(rem - before) - __shfl_sync(kFull, upto - t, who);
+                    break;
+                }
             }
+            before += __shfl_sync(kFull, upto, 31);
         }
         if (pass == 0) {
-            const int64_t work = carry * a.s.heads;
-            // (no more CTAs than key tiles: none in between is without work)
-            const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), work));
-            if (static_cast<int>(blockIdx.x) >= n) return st;
-            st.ranges = prefix::make_ranges(work, n);
-            st.at = prefix::range_start(st.ranges, blockIdx.x);
-            st.end = prefix::range_start(st.ranges, blockIdx.x + 1);
-            continue;
-        }
-        __syncthreads();
-        if (pass == 1) st.q = c.find_q;
-        if (pass == 2) {  // (each head of the request has the same key tiles)
-            const int64_t per_head = c.p1 - c.p0, rem = st.at - a.s.heads * c.p0;
-            int lo = 0, hi = a.s.heads;
+            per_head = before;
+            lo = 0, hi = a.s.heads;
 #pragma unroll 1
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -260,25 +278,23 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, Ctl &c, int32_t
                     hi = mid;
             }
             st.head = lo;
-            in_head = c.p0 + rem - st.head * per_head;
+            rem -= lo * per_head;
         }
     }
-    st.rt = c.find_rt;
-    st.j = c.find_j;
     return st;
 }
 
 // Row tile rt of request q, by a warp: sequences' lengths and own slots into `p`;
 // returns its number of key tiles (0: no sequence there, `p` is not complete).
-__device__ int fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, Piece &p) {
+__device__ __forceinline__ int fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, const Ctl &c, Piece &p) {
     const RowTile r = prefix::row_tile(a.s, rt);
-    const int64_t s0 = static_cast<int64_t>(q) * a.s.n_branch + r.b0;
+    const int s0 = q * a.s.n_branch + r.b0;
     KeySum k{0, 0, INT32_MAX};
     int first = INT32_MAX;
     const int shared_len = shared_len_of(a, q);
 #pragma unroll 1
     for (int i = lane; i < r.nb; i += 32) {
-        const int len = len_of(a, s0 + i, nullptr);
+        const int len = len_of(a, s0 + i, c);
         p.len[i] = len;
         prefix::add_sequence(a.s, k, len);
         if (len >= 0) first = min(first, i);
@@ -311,7 +327,7 @@ __device__ int fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, Piece
         p.r = r;
         p.shared = shared;
         p.shared_tiles = prefix::tiles_of(a.s, shared);
-        p.shared_row = static_cast<int>(s0) + first;
+        p.shared_row = s0 + first;
     }
     return tiles;
 }
@@ -413,17 +429,20 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
     __syncwarp();
 }
 
-// The scheduler: the pieces of [st.at, st.end) into the ring.
-__device__ __forceinline__ void schedule(const PrefixArgs &a, const Start &st, int lane, Ctl &c) {
+// The scheduler: the pieces of the CTA's range into the ring.
+__device__ __forceinline__ void schedule(const PrefixArgs &a, const Range &range, const int64_t *first, int lane, Ctl &c) {
+    const Start st = find_start(a, range, first, lane, c);
+    // (`first` lies in the K and V stages: the copies that follow the first piece come after its reads)
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     int q = st.q, head = st.head, rt = st.rt, j = st.j, n = 0;
-    int64_t at = st.at;
+    int64_t at = range.at;
     bool any = true;  // the request has a key tile at all
-    while (at < st.end) {
+    while (at < range.end) {
         if (n >= kRing && !warp_wait(&c.ring_empty[n % kRing], (n / kRing - 1) & 1, c, a)) return;
         Piece &p = c.ring[n % kRing];
         int tiles = 0;
         for (;;) {
-            tiles = fill_row_tile(a, q, rt, lane, p);
+            tiles = fill_row_tile(a, q, rt, lane, c, p);
             any |= tiles > 0;
             if (tiles > 0) break;
             if (++rt == a.s.row_tiles) {
@@ -437,14 +456,14 @@ __device__ __forceinline__ void schedule(const PrefixArgs &a, const Start &st, i
             if (q >= a.s.n_req) return;  // (not reached while the lengths stay as they are during the call)
         }
         if (j >= tiles) return;          // (nor this)
-        const int j1 = static_cast<int>(min(static_cast<int64_t>(tiles), j + (st.end - at)));
+        const int j1 = static_cast<int>(min(static_cast<int64_t>(tiles), j + (range.end - at)));
         if (lane == 0) {
             p.head = head;
             p.j0 = j;
             p.j1 = j1;
             p.part = j == 0 && j1 == tiles ? -1 : j > 0 ? 0 : 1;
             if (p.part == 1) {
-                const int last = prefix::cta_of(st.ranges, at + tiles - 1);
+                const int last = prefix::cta_of(range.all, at + tiles - 1);
                 a.cut[blockIdx.x] = Cut{last - static_cast<int>(blockIdx.x) + 1, q, head, rt};
             }
         }
@@ -869,6 +888,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&c.o_free, 4);
         mbar_init(&c.mma_done, 1);
         c.abort_flag = 0;
+        for (const CUtensorMap *m : {&tm_q, &tm_k, &tm_v})
+            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -878,14 +899,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     pdl_wait();
     pdl_launch_next();
     if (threadIdx.x == 0) a.cut[blockIdx.x].parts = 0;
-    const Start st = find_start(a, c, reinterpret_cast<int32_t *>(sk));
-    // (the K and V stages held the lengths: the copies that follow are ordered after those accesses)
+    int64_t *first = reinterpret_cast<int64_t *>(sk);
+    const Range range = find_range(a, c, first);
+    // (`first` lies in the K and V stages: the copies that follow are ordered after its writes)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = c.tmem_base;
-    const uint32_t tiles = static_cast<uint32_t>(st.end - st.at);
+    const uint32_t tiles = static_cast<uint32_t>(range.end - range.at);
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCtlRegs));
@@ -894,7 +916,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         else if (warp == 1)
             issue_products<kF16>(sq, sk, sv, tmem, tiles, lane, c, a);
         else if (tiles)
-            schedule(a, st, lane, c);
+            schedule(a, range, first, lane, c);
     } else if (warp < 12) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         softmax<kF16>(tmem, warp & 3, lane, (warp >> 2) - 1, tiles, c, a);
@@ -1086,6 +1108,7 @@ rps_status check_shape(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads, int
     if (n_heads / kv->n_heads > RPS_KV_MAX_GROUP) return RPS_ERR_UNSUPPORTED;
     const int64_t tokens = static_cast<int64_t>(kv->n_branch) * n_q;
     if (tokens > INT32_MAX / 256 || static_cast<int64_t>(kv->n_req) * tokens > INT32_MAX / 256) return RPS_ERR_UNSUPPORTED;
+    if (kv->n_req > kMaxReqs) return RPS_ERR_UNSUPPORTED;
     // slots of the sequences of one row tile
     const int64_t slots = static_cast<int64_t>(kv->max_pages) * std::max(1, kv->page_size / prefix::kRows);
     if (std::min<int64_t>(kv->n_branch, kMaxSeqs) * slots > INT32_MAX / 256) return RPS_ERR_UNSUPPORTED;
