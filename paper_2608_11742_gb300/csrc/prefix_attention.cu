@@ -74,12 +74,14 @@ constexpr int kMaxSeqs = 128;        // sequences with rows in one row tile
 constexpr int kMaxCtas = 160;
 constexpr int kStagedLens = 1024;    // lengths that are kept in shared memory
 constexpr int kMaxReqs = 2 * kStages * kTileBytes / 8;  // requests whose first tiles fit the K and V stages
-constexpr int kCombineThreads = 256;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// A row tile that is cut: the CTA that takes its first key tile writes where its parts are.
+// A row tile that is cut: the CTA that takes its first key tile writes where its parts
+// are. Entries are by row tile while there are at most kMaxCtas of them, else by CTA (one
+// CTA begins at most one cut row tile, its last).
 struct Cut {
-    int32_t parts;  // 0: none
+    int32_t parts;       // 0: none
+    int32_t cta;         // the first part's
     int32_t q, head, rt;
 };
 
@@ -92,6 +94,7 @@ struct PrefixArgs {
     float *lse;
     float c;  // scale * log2(e)
     Cut *cut;       // [kMaxCtas]
+    int32_t by_tile;  // cuts are listed by row tile
     float2 *part_ml;  // [2 * kMaxCtas][128]: maximum and sum of each row of a partial result
     float *part_o;    // [2 * kMaxCtas][128][128]
     uint32_t *err;
@@ -123,6 +126,7 @@ struct Ctl {
     uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
     int32_t len[kStagedLens];
+    int32_t longest, empty, own;  // key tiles of the longest row tile; one has none; those of the CTA's own
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -188,11 +192,18 @@ __device__ __forceinline__ int64_t scan_block(int v, int64_t *sums, int64_t *tot
     return before + x - v;
 }
 
-// The CTA's range of key tiles, of those of all (request, head, row tile) in order.
+// The CTA's range of key tiles, of those of all (request, head, row tile) in order; or
+// (whole) its one row tile.
 struct Range {
     int64_t at, end;
     prefix::Ranges all;
+    bool whole;
 };
+// Cutting a row tile costs what its parts take to be written and joined, about as much as
+// three key tiles: where every row tile has a CTA of its own and none is longer by more than
+// that than the equal shares, none is cut (one request's 9 branches of 32, 32 heads, context
+// 328: 96 row tiles of 4 to 5 key tiles instead of shares of 3: 25 -> xx us).
+constexpr int kCutTiles = 3;
 
 // By all threads: the lengths into shared memory, and in first[q] the key tiles (of
 // one head: all heads of a request have the same) of the requests before q.
@@ -201,7 +212,11 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
     if (n_seq <= kStagedLens)
 #pragma unroll 1
         for (int i = threadIdx.x; i < n_seq; i += kThreads) c.len[i] = a.len[i];
+    if (threadIdx.x == 0) c.longest = c.empty = 0;
     __syncthreads();
+    const bool few = entries * a.s.heads <= static_cast<int>(gridDim.x);  // (at most one block of entries then)
+    const int mine = few ? prefix::quotient(blockIdx.x, a.s.by_row_tiles) : 0;  // request and head of the CTA's own
+    const int mine_q = mine / a.s.heads;
     int64_t carry = 0;
 #pragma unroll 1
     for (int base = 0; base < entries; base += kThreads) {
@@ -209,6 +224,11 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
         const int q = prefix::quotient(e, a.s.by_row_tiles), rt = e - q * a.s.row_tiles;
         int64_t total;
         const int t = e < entries ? entry_tiles(a, q, rt, c) : 0;
+        if (few && e < entries) {
+            if (t == 0) c.empty = 1;
+            atomicMax(&c.longest, t);
+            if (q == mine_q && rt == static_cast<int>(blockIdx.x) - mine * a.s.row_tiles) c.own = t;
+        }
         const int64_t before = carry + scan_block(t, c.scan, &total);
         if (e < entries && rt == 0) first[q] = before;
         carry += total;
@@ -217,6 +237,11 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
     const int64_t work = carry * a.s.heads;
     // (no more CTAs than key tiles: none in between is without work)
     const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), work));
+    if (few && !c.empty && static_cast<int64_t>(c.longest - kCutTiles) * n <= work) {
+        r.whole = true;
+        r.end = static_cast<int>(blockIdx.x) < entries * a.s.heads ? c.own : 0;
+        return r;
+    }
     if (static_cast<int>(blockIdx.x) >= n) return r;
     r.all = prefix::make_ranges(work, n);
     r.at = prefix::range_start(r.all, blockIdx.x);
@@ -231,6 +256,13 @@ struct Start {
 __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &range, const int64_t *first, int lane,
                                             const Ctl &c) {
     Start st{};
+    if (range.whole) {
+        const int qh = prefix::quotient(blockIdx.x, a.s.by_row_tiles);
+        st.rt = blockIdx.x - qh * a.s.row_tiles;
+        st.q = qh / a.s.heads;
+        st.head = qh - st.q * a.s.heads;
+        return st;
+    }
     int lo = 0, hi = a.s.n_req;  // the last request that starts at or before the range
 #pragma unroll 1
     while (hi - lo > 1) {
@@ -462,9 +494,13 @@ __device__ __forceinline__ void schedule(const PrefixArgs &a, const Range &range
             p.j0 = j;
             p.j1 = j1;
             p.part = j == 0 && j1 == tiles ? -1 : j > 0 ? 0 : 1;
+            const int tile = (q * a.s.heads + head) * a.s.row_tiles + rt;
             if (p.part == 1) {
                 const int last = prefix::cta_of(range.all, at + tiles - 1);
-                a.cut[blockIdx.x] = Cut{last - static_cast<int>(blockIdx.x) + 1, q, head, rt};
+                a.cut[a.by_tile ? tile : static_cast<int>(blockIdx.x)] =
+                    Cut{last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), q, head, rt};
+            } else if (p.part < 0 && a.by_tile) {
+                a.cut[tile].parts = 0;
             }
         }
         __syncwarp();
@@ -898,7 +934,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     pdl_wait();
     pdl_launch_next();
-    if (threadIdx.x == 0) a.cut[blockIdx.x].parts = 0;
+    if (threadIdx.x == 0 && !a.by_tile) a.cut[blockIdx.x].parts = 0;
     int64_t *first = reinterpret_cast<int64_t *>(sk);
     const Range range = find_range(a, c, first);
     // (`first` lies in the K and V stages: the copies that follow are ordered after its writes)
@@ -932,121 +968,92 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // ---------------------------------------------------------------- joining the parts of cut row tiles
-// (m, l, o) of parts first, first + step, ... of a row, this lane's four columns.
+// Half a warp takes a row's parts first, first + step, ..., a lane eight of its columns.
 struct Joined {
     float m, l;
-    float4 o;
+    float4 o[2];
 };
-__device__ __forceinline__ void join(Joined &x, float m, float l, float4 o) {
+__device__ __forceinline__ void weigh(float4 &x, float f, const float4 &y, float g) {
+    x.x = x.x * f + y.x * g;
+    x.y = x.y * f + y.y * g;
+    x.z = x.z * f + y.z * g;
+    x.w = x.w * f + y.w * g;
+}
+__device__ __forceinline__ void join(Joined &x, float m, float l, const float4 (&o)[2]) {
     const float mm = fmaxf(x.m, m), mr = mm == -INFINITY ? 0.f : mm;
     const float f = ex2(x.m - mr), g = ex2(m - mr);
     x.m = mm;
     x.l = x.l * f + l * g;
-    x.o.x = x.o.x * f + o.x * g;
-    x.o.y = x.o.y * f + o.y * g;
-    x.o.z = x.o.z * f + o.z * g;
-    x.o.w = x.o.w * f + o.w * g;
-}
-__device__ __forceinline__ Joined join_parts(const PrefixArgs &a, int cta, int row, int first, int parts, int step,
-                                             int lane) {
-    Joined x{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    constexpr int kAhead = 4;
-    for (int p = first; p < parts; p += step * kAhead) {
-        float2 ml[kAhead];
-        float4 o[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int pp = p + u * step;
-            ml[u] = make_float2(-INFINITY, 0.f);
-            o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (pp < parts) {
-                // the first part of a row tile ends its CTA's range, the others begin theirs
-                const int64_t at = static_cast<int64_t>(2 * (cta + pp) + (pp == 0 ? 1 : 0)) * prefix::kRows + row;
-                ml[u] = a.part_ml[at];
-                o[u] = *reinterpret_cast<const float4 *>(a.part_o + at * kD + lane * 4);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (p + u * step < parts) join(x, ml[u].x, ml[u].y, o[u]);
-    }
-    return x;
+    weigh(x.o[0], f, o[0], g);
+    weigh(x.o[1], f, o[1], g);
 }
 
+constexpr int kJoinThreads = 128, kJoinHalves = kJoinThreads / 16;
+constexpr int kAhead = 4;  // parts in flight
+
+// Block (cut, group of rows): `split` half warps share a row. Most cuts have two or
+// three parts; with few row tiles there are many, and the row's parts are split.
 template <bool kF16>
-__device__ __forceinline__ void store_row(const PrefixArgs &a, const Cut &cut, const RowTile &r, int row,
-                                          const Joined &x, int lane) {
-    const int t = prefix::quotient(row, a.s.by_group), tok = r.tok0 + t, h = cut.head * a.s.group + row - t * a.s.group;
+__global__ void __launch_bounds__(kJoinThreads) prefix_combine_kernel(const PrefixArgs a, int split) {
+    __shared__ Joined others[kJoinHalves][16];
+    const int half = threadIdx.x >> 4, lane = threadIdx.x & 15;
+    pdl_wait();
+    pdl_launch_next();
+    Cut cut = a.cut[blockIdx.x];
+    if (a.by_tile) {  // (the entry of a row tile without a sequence is not written: its lengths say so)
+        const int qh = prefix::quotient(blockIdx.x, a.s.by_row_tiles);
+        cut.rt = blockIdx.x - qh * a.s.row_tiles;
+        cut.q = qh / a.s.heads;
+        cut.head = qh - cut.q * a.s.heads;
+    } else if (cut.parts == 0) {
+        return;
+    }
+    const RowTile r = prefix::row_tile(a.s, cut.rt);
+    const int row = blockIdx.y * (kJoinHalves / split) + half / split, which = half % split;
+    const int t = prefix::quotient(row, a.s.by_group), tok = r.tok0 + t;
+    // (a call that gave up may not have written its entries: the parts are kept inside the workspace)
+    const bool there = t < r.n_tok && a.len[cut.q * a.s.n_branch + prefix::quotient(tok, a.s.by_n_q)] >= 0 &&
+                       cut.parts > 0 && cut.cta >= 0 && cut.cta < kMaxCtas && cut.parts <= kMaxCtas - cut.cta;
+    Joined x{-INFINITY, 0.f, {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}};
+    if (there) {
+#pragma unroll 1
+        for (int p = which; p < cut.parts; p += split * kAhead) {
+            float2 ml[kAhead];
+            float4 o[kAhead][2];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int pp = min(p + u * split, cut.parts - 1);
+                // the first part of a row tile ends its CTA's range, the others begin theirs
+                const int64_t at = static_cast<int64_t>(2 * (cut.cta + pp) + (pp == 0 ? 1 : 0)) * prefix::kRows + row;
+                ml[u] = a.part_ml[at];
+                o[u][0] = *reinterpret_cast<const float4 *>(a.part_o + at * kD + lane * 8);
+                o[u][1] = *reinterpret_cast<const float4 *>(a.part_o + at * kD + lane * 8 + 4);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (p + u * split < cut.parts) join(x, ml[u].x, ml[u].y, o[u]);
+        }
+    }
+    if (split > 1) {
+        others[half][lane] = x;
+        __syncthreads();
+        if (which) return;
+#pragma unroll 1
+        for (int w = 1; w < split; ++w) {
+            const Joined y = others[half + w][lane];
+            join(x, y.m, y.l, y.o);
+        }
+    }
+    if (!there) return;
+    const int h = cut.head * a.s.group + row - t * a.s.group;
     const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
-    const uint2 v = make_uint2(pack16<kF16>(x.o.x * inv, x.o.y * inv), pack16<kF16>(x.o.z * inv, x.o.w * inv));
-    *reinterpret_cast<uint2 *>(static_cast<char *>(a.out) +
-                               (cut.q * a.out_req + tok * a.out_token + h * a.out_head + lane * 4) * 2) = v;
+    const uint4 v = make_uint4(pack16<kF16>(x.o[0].x * inv, x.o[0].y * inv), pack16<kF16>(x.o[0].z * inv, x.o[0].w * inv),
+                               pack16<kF16>(x.o[1].x * inv, x.o[1].y * inv), pack16<kF16>(x.o[1].z * inv, x.o[1].w * inv));
+    *reinterpret_cast<uint4 *>(static_cast<char *>(a.out) +
+                               (cut.q * a.out_req + tok * a.out_token + h * a.out_head + lane * 8) * 2) = v;
     if (a.lse && lane == 0)
         a.lse[(static_cast<int64_t>(cut.q) * a.s.n_tokens + tok) * a.n_heads + h] =
             x.l == 0.f ? -INFINITY : (x.m + log2f(x.l)) * kLn2;
-}
-
-constexpr int kFewParts = 8;  // up to this many parts a warp joins a row, else a block does
-
-template <bool kF16>
-__global__ void __launch_bounds__(kCombineThreads) prefix_combine_kernel(const PrefixArgs a, int ctas) {
-    __shared__ Cut cuts[kMaxCtas];
-    __shared__ int first_unit[kMaxCtas + 1];
-    __shared__ Joined part[kCombineThreads / 32][32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    pdl_wait();
-    pdl_launch_next();
-    for (int i = threadIdx.x; i < ctas; i += kCombineThreads) cuts[i] = a.cut[i];
-    __syncthreads();
-    // units of the cuts: a row each, or 8 rows
-    if (warp == 0) {
-        int total = 0;
-        for (int base = 0; base < ctas; base += 32) {
-            const int i = base + lane;
-            int units = 0;
-            if (i < ctas && cuts[i].parts > 0) {
-                const int rows = prefix::row_tile(a.s, cuts[i].rt).n_tok * a.s.group;
-                units = cuts[i].parts <= kFewParts ? (rows + 7) / 8 : rows;
-            }
-            int upto = units;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int u = __shfl_up_sync(kFull, upto, o);
-                if (lane >= o) upto += u;
-            }
-            if (i < ctas) first_unit[i] = total + upto - units;
-            total += __shfl_sync(kFull, upto, 31);
-        }
-        if (lane == 0) first_unit[ctas] = total;
-    }
-    __syncthreads();
-    for (int u = blockIdx.x; u < first_unit[ctas]; u += gridDim.x) {
-        const int i = prefix::slot_owner(first_unit, ctas, u);
-        const Cut cut = cuts[i];
-        const RowTile r = prefix::row_tile(a.s, cut.rt);
-        const int rows = r.n_tok * a.s.group;
-        const bool few = cut.parts <= kFewParts;
-        const int row = few ? (u - first_unit[i]) * 8 + warp : u - first_unit[i];
-        const bool there = row < rows && a.len[static_cast<int64_t>(cut.q) * a.s.n_branch +
-                                               prefix::quotient(r.tok0 + prefix::quotient(row, a.s.by_group), a.s.by_n_q)] >= 0;
-        if (few) {
-            if (there) store_row<kF16>(a, cut, r, row, join_parts(a, i, row, 0, cut.parts, 1, lane), lane);
-            continue;
-        }
-        if (!there) continue;  // (the same for the whole block)
-        part[warp][lane] = join_parts(a, i, row, warp, cut.parts, kCombineThreads / 32, lane);
-        __syncthreads();
-        if (warp == 0) {
-            Joined x = part[0][lane];
-#pragma unroll
-            for (int w = 1; w < kCombineThreads / 32; ++w) {
-                const Joined y = part[w][lane];
-                join(x, y.m, y.l, y.o);
-            }
-            store_row<kF16>(a, cut, r, row, x, lane);
-        }
-        __syncthreads();
-    }
 }
 
 // ---------------------------------------------------------------- host
@@ -1189,11 +1196,16 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
     const int64_t row_tiles = static_cast<int64_t>(a.s.n_req) * a.s.heads * a.s.row_tiles;
     const int grid = static_cast<int>(std::min<int64_t>(row_tiles * tiles, sms));
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    a.by_tile = row_tiles <= kMaxCtas;
     if (launch_pdl(f16 ? prefix_attention_kernel<true> : prefix_attention_kernel<false>, dim3(grid), dim3(kThreads),
                    kSmemBytes, s, tq, tk, tv, a) != cudaSuccess)
         return RPS_ERR_CUDA;
-    return launch_pdl(f16 ? prefix_combine_kernel<true> : prefix_combine_kernel<false>, dim3(sms * 4),
-                      dim3(kCombineThreads), 0, s, a, grid) == cudaSuccess
+    // a cut row tile has about grid / row_tiles parts: half warps of at most four each
+    int split = 1;
+    while (split < kJoinHalves && row_tiles * kAhead * split < grid) split *= 2;
+    const dim3 cuts(static_cast<unsigned>(std::min<int64_t>(row_tiles, grid)), prefix::kRows / (kJoinHalves / split));
+    return launch_pdl(f16 ? prefix_combine_kernel<true> : prefix_combine_kernel<false>, cuts, dim3(kJoinThreads), 0, s, a,
+                      split) == cudaSuccess
                ? RPS_OK
                : RPS_ERR_CUDA;
 }

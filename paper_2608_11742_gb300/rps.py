@@ -551,9 +551,11 @@ class KvCacheBuf:
     order of heads and tokens in memory), ``page_ref`` ``[n_pages]``, ``table``
     ``[n_req][n_branch][max_pages]`` and ``length`` ``[n_req][n_branch]``, int32."""
 
+    __slots__ = ("k", "v", "page_ref", "table", "length", "n_req", "n_branch", "n_seq", "_kept", "_struct", "_at")
+
     def __init__(self, k, v, page_ref=None, table=None, length=None):
         self.k, self.v, self.page_ref, self.table, self.length = k, v, page_ref, table, length
-        self._key = None
+        self._kept = None
         self._c()
 
     @staticmethod
@@ -570,18 +572,22 @@ class KvCacheBuf:
         return KvCacheBuf(k, v)
 
     def _c(self) -> int:
-        """Address of the C struct, built anew when a tensor moved or changed its layout."""
+        """Address of the C struct, kept while the tensors, their addresses and their strides are the same (built
+        on each call, it took half of a call's time on the host)."""
         k, v, ref, table, length = self.k, self.v, self.page_ref, self.table, self.length
-        key = (k.data_ptr(), v.data_ptr(), k.shape, k.stride(), v.shape, v.stride(), k.dtype, v.dtype,
-               _ptr(ref), _ptr(table), _ptr(length), None if table is None else (ref.shape, table.shape, length.shape))
-        if key == self._key:
+        kept = self._kept
+        if (kept is not None and kept[0] is k and kept[1] is v and kept[2] is ref and kept[3] is table
+                and kept[4] is length and kept[5] == (k.data_ptr(), v.data_ptr(), k.stride(), v.stride())
+                and (table is None or kept[6] == (ref.data_ptr(), table.data_ptr(), length.data_ptr(), table.shape))):
             return self._at
         if k.dtype not in _KV_DTYPES or v.dtype != k.dtype:
             raise TypeError(f"k and v must both be bf16 or fp16, got {k.dtype} and {v.dtype}")
         if k.dim() != 5 or v.shape != k.shape or k.stride(4) != 1 or v.stride() != k.stride():
             raise ValueError("k and v: [layers][pages][heads][page size][head dim], head dim contiguous, same strides")
+        _here(k, v, ref, table, length)
         n_layers, n_pages, n_heads, ps, d = k.shape
         n_req = n_branch = width = 0
+        at = None
         if table is not None:
             if table.dim() != 3 or length is None or ref is None:
                 raise ValueError("table [n_req][n_branch][max_pages] comes with page_ref and length")
@@ -589,17 +595,16 @@ class KvCacheBuf:
             _ints("page_ref", ref, n_pages)
             _ints("table", table, n_req * n_branch * width)
             _ints("length", length, n_req * n_branch)
-        self.n_seq = n_req * n_branch
+            at = (ref.data_ptr(), table.data_ptr(), length.data_ptr(), table.shape)
+        self.n_req, self.n_branch, self.n_seq = n_req, n_branch, n_req * n_branch
         self._struct = RpsKvCache(k.data_ptr(), v.data_ptr(), _KV_DTYPES[k.dtype], n_layers, n_pages, n_heads, ps, d,
                                   *k.stride()[:4], _ptr(ref), _ptr(table), _ptr(length), n_req, n_branch, width)
-        self._at, self._key = C.addressof(self._struct), key
+        self._at = C.addressof(self._struct)
+        self._kept = (k, v, ref, table, length, (k.data_ptr(), v.data_ptr(), k.stride(), v.stride()), at)
         return self._at
 
-    def __getstate__(self):  # a copy or a pickle holds the tensors alone
-        return {n: getattr(self, n) for n in ("k", "v", "page_ref", "table", "length")}
-
-    def __setstate__(self, state):
-        self.__init__(**state)
+    def __reduce__(self):  # a copy or a pickle holds the tensors alone
+        return KvCacheBuf, (self.k, self.v, self.page_ref, self.table, self.length)
 
 
 def rps_kv_workspace_bytes(kv: KvCacheBuf) -> int:
@@ -611,7 +616,7 @@ def rps_kv_workspace_bytes(kv: KvCacheBuf) -> int:
 
 def _kv_ws(kv: KvCacheBuf, ws: torch.Tensor, *more):
     at = kv._c()
-    _here(kv.k, kv.table, ws, *more)
+    _here(kv.k, ws, *more)
     return at, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -627,7 +632,7 @@ def rps_kv_fork_branches(kv: KvCacheBuf, branch_valid: torch.Tensor, ctx_len: Op
                          stream=None) -> None:
     """The valid branches (``PivotsBuf.branch_valid``) take their request's base, cut to ``ctx_len[q]`` tokens."""
     at, p, n = _kv_ws(kv, ws, branch_valid, ctx_len)
-    n_req, nb = kv.table.shape[:2]
+    n_req, nb = kv.n_req, kv.n_branch
     _check(_lib.rps_kv_fork_branches(at, _ints("branch_valid", branch_valid, n_req * (nb - 1), torch.uint8),
                                      None if ctx_len is None else _ints("ctx_len", ctx_len, n_req), p, n,
                                      _stream(stream)), "rps_kv_fork_branches")
@@ -636,7 +641,7 @@ def rps_kv_fork_branches(kv: KvCacheBuf, branch_valid: torch.Tensor, ctx_len: Op
 def rps_kv_commit(kv: KvCacheBuf, winner: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """Each base takes its winner's state (``CommitBuf.winner``); every branch gives its pages back."""
     at, p, n = _kv_ws(kv, ws, winner)
-    _check(_lib.rps_kv_commit(at, _ints("winner", winner, kv.table.shape[0]), p, n, _stream(stream)), "rps_kv_commit")
+    _check(_lib.rps_kv_commit(at, _ints("winner", winner, kv.n_req), p, n, _stream(stream)), "rps_kv_commit")
 
 
 def rps_kv_resize(kv: KvCacheBuf, new_len: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
@@ -664,8 +669,8 @@ def rps_kv_copy_pages(src_kv: KvCacheBuf, dst_kv: KvCacheBuf, src: torch.Tensor,
 def rps_kv_write(kv: KvCacheBuf, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, stream=None) -> None:
     """Keys and values ``[n_req][n_branch][n_new][n_heads][128]`` of each sequence's last ``n_new`` tokens."""
     at = kv._c()
-    _here(kv.k, kv.table, k_new, v_new)
-    n_req, nb = kv.table.shape[:2]
+    _here(kv.k, k_new, v_new)
+    n_req, nb = kv.n_req, kv.n_branch
     shape, st = k_new.shape, k_new.stride()
     if len(shape) != 5 or shape[:2] != (n_req, nb) or shape[3:] != (kv.k.shape[2], kv.k.shape[4]) or v_new.shape != shape:
         raise ValueError("k_new and v_new: [n_req][n_branch][n_new][n_heads][head dim]")
@@ -703,8 +708,8 @@ def rps_prefix_attention_fwd(q: torch.Tensor, kv: KvCacheBuf, layer: int, out: t
     ``[n_req][n_branch][n_q][n_heads][128]`` of the cache's dtype, lse (optional) fp32 ``[n_req][n_branch][n_q][n_heads]``;
     ``shared_len`` (int32 ``[n_req]`` or None): leading tokens whose pages a request's sequences hold in common."""
     at = kv._c()
-    _here(kv.k, kv.table, q, out, ws, shared_len, lse)
-    n_req, nb = kv.table.shape[:2]
+    _here(kv.k, q, out, ws, shared_len, lse)
+    n_req, nb = kv.n_req, kv.n_branch
     shape = q.shape
     if len(shape) != 5 or shape[:2] != (n_req, nb) or shape[4] != kv.k.shape[4] or out.shape != shape:
         raise ValueError("q and out: [n_req][n_branch][n_q][n_heads][head dim], as the cache")
