@@ -98,7 +98,7 @@ struct PrefixArgs {
     float2 *part_ml;  // [2 * kMaxCtas][128]: maximum and sum of each row of a partial result
     float *part_o;    // [2 * kMaxCtas][128][128]
     uint32_t *err;
-    uint32_t wait_ns;
+    uint32_t tries;  // of a wait
 };
 
 struct Piece {
@@ -132,26 +132,29 @@ struct Ctl {
 };
 
 // ---------------------------------------------------------------- waits
-__device__ __forceinline__ uint32_t global_ns_low() {
-    uint32_t t;
-    asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
-    return t;
+// One try of a wait for a phase, which the hardware suspends for about a microsecond at most.
+__device__ __forceinline__ bool try_wait_us(uint64_t *bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(saddr(bar)), "r"(parity), "r"(1000u)
+        : "memory");
+    return done != 0;
 }
-// Waits for a phase of a barrier, at most a.wait_ns, all lanes; the warp goes on
-// together, on the same answer. A wait that runs out raises the abort flag, which ends
-// the other roles' waits and is reported when the CTA ends. (Short: every role's waits
-// are inlined, and the roles' code has to fit the instruction cache together.)
+// Waits for a phase of a barrier, at most a.tries tries, all lanes; the warp goes on
+// together, on the same answer. A wait that runs out raises the abort flag, which is
+// reported when the CTA ends; the other roles' waits then run out too. (Short: every role's
+// waits are inlined, and the roles' code has to fit the instruction cache together.)
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl &c, const PrefixArgs &a) {
-    bool ok = a.wait_ns != 0 && mbar_try_wait(bar, parity);
-    if (!__all_sync(kFull, ok)) {
-        const uint32_t start = global_ns_low();
+    bool ok = false;
 #pragma unroll 1
-        while (!(ok = a.wait_ns != 0 && mbar_try_wait(bar, parity)))
-            if (*reinterpret_cast<volatile int *>(&c.abort_flag) || global_ns_low() - start >= a.wait_ns) break;
-        ok = __all_sync(kFull, ok);
-        if (!ok) *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
-    }
-    return ok;
+    for (uint32_t i = 0; i < a.tries && !ok; ++i) ok = try_wait_us(bar, parity);
+    if (__all_sync(kFull, ok)) return true;
+    *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
+    return false;
 }
 
 // ---------------------------------------------------------------- the cut
@@ -527,6 +530,9 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
     constexpr uint32_t idesc_s = umma::instr_desc_f16(128, 128, fmt, 0);  // K is K-major
     constexpr uint32_t idesc_o = umma::instr_desc_f16(128, 128, fmt, 1);  // V is MN-major
     const uint32_t issue = lane == 0;
+    // (an operand's other buffer, atom or step: its address field moved on)
+    const uint64_t q_desc = umma::smem_desc_kmajor_sw128(saddr(sq)), k_desc = umma::smem_desc_kmajor_sw128(saddr(sk));
+    const uint64_t v_desc = umma::smem_desc_mnmajor_sw128(saddr(sv), kAtom);
     bool ok = true;
     int sn = 0, sj = 0, sj1 = 0;  // the scores' piece, tile, and the piece's end
     const auto scores = [&](uint32_t t) -> bool {  // S_t = Q K_t^T into buffer t % 2
@@ -538,18 +544,16 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             if (!warp_wait(&c.q_full[sn & 1], (sn >> 1) & 1, c, a)) return false;
             ++sn;
         }
-        const int qb = (sn - 1) & 1, s = t % kStages;
+        const uint32_t s = t % kStages;
         if (!warp_wait(&c.k_full[s], (t / kStages) & 1, c, a)) return false;
         tc_fence_after();
-        const uint64_t qd = umma::smem_desc_kmajor_sw128(saddr(sq + qb * kTileBytes));
-        const uint64_t qd1 = umma::smem_desc_kmajor_sw128(saddr(sq + qb * kTileBytes + kAtom));
-        const uint64_t kd = umma::smem_desc_kmajor_sw128(saddr(sk + s * kTileBytes));
-        const uint64_t kd1 = umma::smem_desc_kmajor_sw128(saddr(sk + s * kTileBytes + kAtom));
+        const uint64_t qd = q_desc + (sn & 1 ? 0 : kTileBytes >> 4), kd = k_desc + s * (kTileBytes >> 4);
         const uint32_t sbuf = tmem + s * 128;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            mma_bf16(sbuf, umma::advance_k16(k < 4 ? qd : qd1, k & 3), umma::advance_k16(k < 4 ? kd : kd1, k & 3),
-                     idesc_s, k != 0, issue);
+        for (int k = 0; k < 8; ++k) {  // (16 of the 64 columns of an atom are 32 bytes)
+            const uint32_t at = k / 4 * (kAtom >> 4) + k % 4 * 2;
+            mma_bf16(sbuf, qd + at, kd + at, idesc_s, k != 0, issue);
+        }
         mma_commit(&c.s_full[s], issue);
         ++sj;
         return true;
@@ -567,7 +571,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                 j = pp->j0;
             }
             const Piece &p = *pp;
-            const int h = t % kStages;
+            const uint32_t h = t % kStages;
             const bool own = j >= p.shared_tiles;
             uint32_t steps = 0, ragged = 0;  // steps with keys; with fewer than 16
             int keys = 0;
@@ -611,7 +615,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             tc_fence_after();
             // P of keys 16k..16k+15: columns 8k..8k+7 of S buffer t % 2
             const uint32_t pcol = tmem + h * 128, ocol = tmem + kOCol + h * 128;
-            const uint64_t vd = umma::smem_desc_mnmajor_sw128(saddr(vb), kAtom);
+            const uint64_t vd = v_desc + h * (kTileBytes >> 4);
             if (!own) {
                 const uint32_t more = j - p.j0 >= kStages;  // the half has had a tile of this piece
 #pragma unroll
@@ -619,7 +623,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                     mma_bf16_ts(ocol, pcol + k * 8, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o, more | (k != 0),
                                 issue);
             } else {
-#pragma unroll 4
+#pragma unroll 2
                 for (int k = 0; k < 8; ++k) {
                     const uint4 o = c.step_off[k];
                     const uint32_t off[4] = {o.x, o.y, o.z, o.w};
@@ -687,66 +691,66 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
             const int first = (j - p.shared_tiles) << a.s.spt_log;
             const bool takes = live && (j < p.shared_tiles || (own_off < first + a.s.spt && own_end > first));
             if (__any_sync(kFull, takes)) {
-                uint32_t s0[32], s1[32], s2[32], s3[32];  // the row's 128 scores
-                tmem_ld32_async(sbuf, s0);
-                tmem_ld32_async(sbuf + 32, s1);
-                tmem_ld32_async(sbuf + 64, s2);
-                tmem_ld32_async(sbuf + 96, s3);
-                tmem_wait_dep(s0);
-                tmem_wait_dep(s1);
-                tmem_wait_dep(s2);
-                tmem_wait_dep(s3);
-                if (col.lo > 0 || col.hi < 128) {
-                    mask_scores(s0, col.lo, col.hi);
-                    mask_scores(s1, col.lo - 32, col.hi - 32);
-                    mask_scores(s2, col.lo - 64, col.hi - 64);
-                    mask_scores(s3, col.lo - 96, col.hi - 96);
-                }
-                float mx8[8];
+                // Twice over the scores, 64 at a time: their maximum, then P = 2^(s c - m), pairs
+                // of 16 bits over columns of S that are read. While all scores so far are
+                // -inf, m is: P = 0 and the sum 0. (One body for the four passes instead of all
+                // 128 scores in registers: a third of the code.)
+                float mx8[8], mr = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) mx8[i] = -INFINITY;
-                max_scores(s0, mx8);
-                max_scores(s1, mx8);
-                max_scores(s2, mx8);
-                max_scores(s3, mx8);
-                const float tm = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
-                                       fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]))) * a.c;
-                float f = 1.f;
-                bool rescale = false;
-                if (m == -INFINITY) {
-                    m = tm;
-                } else if (tm > m + kRescale) {
-                    f = ex2(m - tm);
-                    m = tm;
-                    rescale = true;
-                }
-                // the warp rescales its O together (tcgen05.ld / st are warp-wide), rows without need by
-                // 1. The half's previous product is done: S of this tile was issued after it.
-                if (__any_sync(kFull, rescale)) {
-#pragma unroll 1
-                    for (int ch = 0; ch < 8; ++ch) {
-                        uint32_t o[16];
-                        tmem_ld16_async(obuf + ch * 16, o);
-                        tmem_wait_dep(o);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_st16(obuf + ch * 16, o);
-                    }
-                }
-                l *= f;
-                // P = 2^(s c - m), pairs of 16 bits over the first 64 columns of S. While all
-                // scores so far are -inf, m is: P = 0 and the sum 0.
-                const float mr = m == -INFINITY ? 0.f : -m;
-                const f2 cc = pack2(a.c, a.c), mm = pack2(mr, mr);
+                const bool part = col.lo > 0 || col.hi < 128;
+                const f2 cc = pack2(a.c, a.c);
                 f2 lsum[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
-                uint32_t pk[32];
-                exp_scores<kF16>(s0, cc, mm, lsum, pk, 0);
-                exp_scores<kF16>(s1, cc, mm, lsum, pk, 16);
-                tmem_st32_u(sbuf, pk);
-                uint32_t pk2[32];
-                exp_scores<kF16>(s2, cc, mm, lsum, pk2, 0);
-                exp_scores<kF16>(s3, cc, mm, lsum, pk2, 16);
-                tmem_st32_u(sbuf + 32, pk2);
+#pragma unroll 1
+                for (int pass = 0; pass < 4; ++pass) {
+                    const int at = (pass & 1) * 64;
+                    uint32_t s0[32], s1[32];
+                    tmem_ld32_async(sbuf + at, s0);
+                    tmem_ld32_async(sbuf + at + 32, s1);
+                    tmem_wait_dep(s0);
+                    tmem_wait_dep(s1);
+                    if (part) {
+                        mask_scores(s0, col.lo - at, col.hi - at);
+                        mask_scores(s1, col.lo - at - 32, col.hi - at - 32);
+                    }
+                    if (pass >= 2) {
+                        const f2 mm = pack2(mr, mr);
+                        uint32_t pk[32];
+                        exp_scores<kF16>(s0, cc, mm, lsum, pk, 0);
+                        exp_scores<kF16>(s1, cc, mm, lsum, pk, 16);
+                        tmem_st32_u(sbuf + at / 2, pk);
+                        continue;
+                    }
+                    max_scores(s0, mx8);
+                    max_scores(s1, mx8);
+                    if (pass == 0) continue;
+                    const float tm = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
+                                           fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]))) * a.c;
+                    float f = 1.f;
+                    bool rescale = false;
+                    if (m == -INFINITY) {
+                        m = tm;
+                    } else if (tm > m + kRescale) {
+                        f = ex2(m - tm);
+                        m = tm;
+                        rescale = true;
+                    }
+                    // the warp rescales its O together (tcgen05.ld / st are warp-wide), rows without need by
+                    // 1. The half's previous product is done: S of this tile was issued after it.
+                    if (__any_sync(kFull, rescale)) {
+#pragma unroll 1
+                        for (int ch = 0; ch < 8; ++ch) {
+                            uint32_t o[16];
+                            tmem_ld16_async(obuf + ch * 16, o);
+                            tmem_wait_dep(o);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st16(obuf + ch * 16, o);
+                        }
+                    }
+                    l *= f;
+                    mr = m == -INFINITY ? 0.f : -m;
+                }
                 {
                     float l0, l1;
                     unpack2(add2(add2(lsum[0], lsum[1]), add2(lsum[2], lsum[3])), l0, l1);
@@ -819,7 +823,7 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
         float w0 = e.y == 0.f ? 0.f : ex2(e.x - mr), w1 = f.y == 0.f ? 0.f : ex2(f.x - mr);
         const float l = w0 * e.y + w1 * f.y;  // (NaN stays)
         if (whole) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float inv = l == 0.f ? 0.f : __fdividef(1.f, l);
             w0 *= inv;
             w1 *= inv;
         }
@@ -1188,7 +1192,7 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
     a.cut = reinterpret_cast<Cut *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(ws + ml_at);
     a.part_o = reinterpret_cast<float *>(ws + o_at);
-    a.wait_ns = static_cast<uint32_t>(std::min<uint64_t>(ring_wait_limit_ns(), 4000000000u));
+    a.tries = static_cast<uint32_t>(std::min<uint64_t>((ring_wait_limit_ns() + 999) / 1000, 1u << 30));
 
     // CTAs: as many as there can be key tiles
     const int64_t slots = static_cast<int64_t>(a.s.max_pages) * a.s.sub;
