@@ -469,54 +469,73 @@ __device__ __forceinline__ void schedule(const PrefixArgs &a, const Range &range
     const Start st = find_start(a, range, first, lane, c);
     // (`first` lies in the K and V stages: the copies that follow the first piece come after its reads)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    int q = st.q, head = st.head, rt = st.rt, j = st.j, n = 0;
-    int64_t at = range.at;
-    bool any = true;  // the request has a key tile at all
-    while (at < range.end) {
-        if (n >= kRing && !warp_wait(&c.ring_empty[n % kRing], (n / kRing - 1) & 1, c, a)) return;
-        Piece &p = c.ring[n % kRing];
-        int tiles = 0;
-        for (;;) {
-            tiles = fill_row_tile(a, q, rt, lane, c, p);
-            any |= tiles > 0;
-            if (tiles > 0) break;
+    // A range that ends one row tile and begins the next of the same head is taken in the
+    // other order: all CTAs of the head are then near the same keys at the same time,
+    // which L2 holds, instead of all over them (2 requests, 28/4 heads, context 28000: the keys
+    // were read from HBM seven times).
+    int turn = 1, cut_at = 0;
+    if (st.j > 0 && st.rt + 1 < a.s.row_tiles) {
+        const int t = lane < 2 ? entry_tiles(a, st.q, st.rt + lane, c) : 0;
+        cut_at = __shfl_sync(kFull, t, 0) - st.j;  // tiles up to the next row tile
+        const int64_t rest = range.end - range.at - cut_at;
+        if (rest > 0 && rest < __shfl_sync(kFull, t, 1)) turn = 0;
+    }
+    int n = 0;
+#pragma unroll 1
+    for (const bool swapped = turn == 0; turn < 2; ++turn) {
+        const bool second = swapped && turn == 0;
+        int q = st.q, head = st.head, rt = st.rt + second, j = second ? 0 : st.j;
+        int64_t at = range.at + (second ? cut_at : 0);
+        const int64_t end = swapped && turn == 1 ? range.at + cut_at : range.end;
+        bool any = true;  // the request has a key tile at all
+#pragma unroll 1
+        while (at < end) {
+            if (n >= kRing && !warp_wait(&c.ring_empty[n % kRing], (n / kRing - 1) & 1, c, a)) return;
+            Piece &p = c.ring[n % kRing];
+            int tiles = 0;
+#pragma unroll 1
+            for (;;) {
+                tiles = fill_row_tile(a, q, rt, lane, c, p);
+                any |= tiles > 0;
+                if (tiles > 0) break;
+                if (++rt == a.s.row_tiles) {
+                    rt = 0;
+                    if (!any || ++head == a.s.heads) {
+                        head = 0;
+                        ++q;
+                    }
+                    any = false;
+                }
+                if (q >= a.s.n_req) return;  // (not reached while the lengths stay as they are during the call)
+            }
+            if (j >= tiles) return;          // (nor this)
+            const int j1 = static_cast<int>(min(static_cast<int64_t>(tiles), j + (end - at)));
+            if (lane == 0) {
+                p.head = head;
+                p.j0 = j;
+                p.j1 = j1;
+                p.part = j == 0 && j1 == tiles ? -1 : j > 0 ? 0 : 1;
+                const int tile = (q * a.s.heads + head) * a.s.row_tiles + rt;
+                if (p.part == 1) {
+                    const int last = prefix::cta_of(range.all, at + tiles - 1);
+                    a.cut[a.by_tile ? tile : static_cast<int>(blockIdx.x)] =
+                        Cut{last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), q, head, rt};
+                } else if (p.part < 0 && a.by_tile) {
+                    a.cut[tile].parts = 0;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.ring_full[n % kRing]);
+            at += j1 - j;
+            j = 0;
+            ++n;
             if (++rt == a.s.row_tiles) {
                 rt = 0;
-                if (!any || ++head == a.s.heads) {
+                if (++head == a.s.heads) {
                     head = 0;
                     ++q;
+                    any = false;
                 }
-                any = false;
-            }
-            if (q >= a.s.n_req) return;  // (not reached while the lengths stay as they are during the call)
-        }
-        if (j >= tiles) return;          // (nor this)
-        const int j1 = static_cast<int>(min(static_cast<int64_t>(tiles), j + (range.end - at)));
-        if (lane == 0) {
-            p.head = head;
-            p.j0 = j;
-            p.j1 = j1;
-            p.part = j == 0 && j1 == tiles ? -1 : j > 0 ? 0 : 1;
-            const int tile = (q * a.s.heads + head) * a.s.row_tiles + rt;
-            if (p.part == 1) {
-                const int last = prefix::cta_of(range.all, at + tiles - 1);
-                a.cut[a.by_tile ? tile : static_cast<int>(blockIdx.x)] =
-                    Cut{last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), q, head, rt};
-            } else if (p.part < 0 && a.by_tile) {
-                a.cut[tile].parts = 0;
-            }
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&c.ring_full[n % kRing]);
-        at += j1 - j;
-        j = 0;
-        ++n;
-        if (++rt == a.s.row_tiles) {
-            rt = 0;
-            if (++head == a.s.heads) {
-                head = 0;
-                ++q;
-                any = false;
             }
         }
     }
@@ -698,7 +717,8 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
                 float mx8[8], mr = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) mx8[i] = -INFINITY;
-                const bool part = col.lo > 0 || col.hi < 128;
+                // (rows that are not stored need no mask: with 7 heads a group, two rows of every tile)
+                const bool part = live && (col.lo > 0 || col.hi < 128);
                 const f2 cc = pack2(a.c, a.c);
                 f2 lsum[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll 1
