@@ -63,8 +63,8 @@ constexpr int kQBufs = 2;
 constexpr int kStageBytes = 32 * 128;  // per read-out warp: 32 rows x 128 bytes on their way out
 constexpr int kSmemBytes = kQBufs * kTileBytes + 2 * kStages * kTileBytes + 4 * kStageBytes + 1024;
 constexpr int kThreads = 512;
-// 128 x 56 + 256 x 176 + 128 x 104 = 65,536 registers of the 512 x 128 of the launch
-constexpr int kCtlRegs = 56, kSoftRegs = 176, kOutRegs = 104;
+// 128 x 56 + 256 x 144 + 128 x 168 = 65,536 registers of the 512 x 128 of the launch
+constexpr int kCtlRegs = 56, kSoftRegs = 144, kOutRegs = 168;
 static_assert(128 * kCtlRegs + 256 * kSoftRegs + 128 * kOutRegs <= 512 * 128, "the split fits the launch's registers");
 constexpr uint32_t kTmemCols = 512;  // S buffers at columns 0 and 128, O at 256 and 384
 constexpr uint32_t kOCol = 256;
@@ -121,8 +121,10 @@ struct Ctl {
     // piece n + 4, whose P needs the products of piece n + 2 and so the read-out of piece n + 1
     float2 ml[4][kStages][prefix::kRows];
     Piece ring[kRing];
-    uint4 step_off[8];      // own tile at hand: rows that step kk leaves alone
-    int32_t step_fresh[8];  // 1: the step overwrites
+    // own tile in V stage s, from V's producer: rows that step kk leaves alone; 1 where it
+    // overwrites; keys of each step
+    uint4 step_off[kStages][8];
+    int32_t step_fresh[kStages][8], step_keys[kStages][8];
     uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
     int32_t len[kStagedLens];
@@ -164,10 +166,10 @@ __device__ __forceinline__ int len_of(const PrefixArgs &a, int s, const Ctl &c) 
 __device__ __forceinline__ int shared_len_of(const PrefixArgs &a, int q) { return a.shared_len ? a.shared_len[q] : 0; }
 
 // Key tiles of row tile rt of request q, by one thread.
-__device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int q, int rt, const Ctl &c) {
+__device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int q, int rt, int shared_len, const Ctl &c) {
     const RowTile r = prefix::row_tile(a.s, rt);
     KeySum k{0, 0, INT32_MAX};
-    const int s0 = q * a.s.n_branch + r.b0, shared_len = shared_len_of(a, q);
+    const int s0 = q * a.s.n_branch + r.b0;
 #pragma unroll 1
     for (int i = 0; i < r.nb; ++i) prefix::add_sequence(a.s, k, len_of(a, s0 + i, c));
     return prefix::key_tiles(a.s, k, prefix::shared_slots(a.s, k, shared_len));
@@ -216,6 +218,8 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
 #pragma unroll 1
         for (int i = threadIdx.x; i < n_seq; i += kThreads) c.len[i] = a.len[i];
     if (threadIdx.x == 0) c.longest = c.empty = 0;
+    // (loaded while the lengths are)
+    int next_shared = shared_len_of(a, min(prefix::quotient(threadIdx.x, a.s.by_row_tiles), a.s.n_req - 1));
     __syncthreads();
     const bool few = entries * a.s.heads <= static_cast<int>(gridDim.x);  // (at most one block of entries then)
     const int mine = few ? prefix::quotient(blockIdx.x, a.s.by_row_tiles) : 0;  // request and head of the CTA's own
@@ -226,7 +230,9 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
         const int e = base + threadIdx.x;
         const int q = prefix::quotient(e, a.s.by_row_tiles), rt = e - q * a.s.row_tiles;
         int64_t total;
-        const int t = e < entries ? entry_tiles(a, q, rt, c) : 0;
+        const int t = e < entries ? entry_tiles(a, q, rt, next_shared, c) : 0;
+        if (base + kThreads < entries)
+            next_shared = shared_len_of(a, min(prefix::quotient(e + kThreads, a.s.by_row_tiles), a.s.n_req - 1));
         if (few && e < entries) {
             if (t == 0) c.empty = 1;
             atomicMax(&c.longest, t);
@@ -276,6 +282,7 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &ra
             hi = mid;
     }
     st.q = lo;
+    const int shared_len = shared_len_of(a, lo);
     int64_t rem = range.at - first[lo] * a.s.heads;  // tiles of the request before the range
     int64_t per_head = 0;
 #pragma unroll 1
@@ -283,7 +290,7 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &ra
         int64_t before = 0;
 #pragma unroll 1
         for (int base = 0; base < a.s.row_tiles; base += 32) {
-            const int t = base + lane < a.s.row_tiles ? entry_tiles(a, st.q, base + lane, c) : 0;
+            const int t = base + lane < a.s.row_tiles ? entry_tiles(a, st.q, base + lane, shared_len, c) : 0;
             int upto = t;
 #pragma unroll 1
             for (int o = 1; o < 32; o <<= 1) {
@@ -440,6 +447,15 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
                     }
                 }
             }
+            if (!is_k && j >= p.shared_tiles && lane < 8) {
+                const prefix::Step st = prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane);
+                c.step_off[s][lane] = make_uint4(
+                    ~(low_bits(st.r1) & ~low_bits(st.r0)), ~(low_bits(st.r1 - 32) & ~low_bits(st.r0 - 32)),
+                    ~(low_bits(st.r1 - 64) & ~low_bits(st.r0 - 64)), ~(low_bits(st.r1 - 96) & ~low_bits(st.r0 - 96)));
+                c.step_fresh[s][lane] = st.fresh;
+                c.step_keys[s][lane] = st.keys;
+            }
+            __syncwarp();  // (the steps are written before the arrival that hands them on)
             if (lane == 0) mbar_expect_tx(&full[s], kTileBytes);
             __syncwarp();
             if (lane < a.s.spt) {  // (slots that are not there: zeros)
@@ -475,7 +491,7 @@ __device__ __forceinline__ void schedule(const PrefixArgs &a, const Range &range
     // were read from HBM seven times).
     int turn = 1, cut_at = 0;
     if (st.j > 0 && st.rt + 1 < a.s.row_tiles) {
-        const int t = lane < 2 ? entry_tiles(a, st.q, st.rt + lane, c) : 0;
+        const int t = lane < 2 ? entry_tiles(a, st.q, st.rt + lane, shared_len_of(a, st.q), c) : 0;
         cut_at = __shfl_sync(kFull, t, 0) - st.j;  // tiles up to the next row tile
         const int64_t rest = range.end - range.at - cut_at;
         if (rest > 0 && rest < __shfl_sync(kFull, t, 1)) turn = 0;
@@ -592,40 +608,30 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             const Piece &p = *pp;
             const uint32_t h = t % kStages;
             const bool own = j >= p.shared_tiles;
-            uint32_t steps = 0, ragged = 0;  // steps with keys; with fewer than 16
-            int keys = 0;
-            if (own) {
-                const prefix::Step st =
-                    prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane & 7);
-                keys = st.keys;
-                steps = __ballot_sync(kFull, lane < 8 && keys > 0);
-                ragged = __ballot_sync(kFull, lane < 8 && keys > 0 && keys < 16);
-                if (lane < 8) {
-                    c.step_off[lane] = make_uint4(
-                        ~(low_bits(st.r1) & ~low_bits(st.r0)), ~(low_bits(st.r1 - 32) & ~low_bits(st.r0 - 32)),
-                        ~(low_bits(st.r1 - 64) & ~low_bits(st.r0 - 64)), ~(low_bits(st.r1 - 96) & ~low_bits(st.r0 - 96)));
-                    c.step_fresh[lane] = st.fresh;
-                }
-                __syncwarp();
-            }
             // the first product of a piece overwrites O: the previous piece's read-out must be done
             if ((j == p.j0 && !warp_wait(&c.o_free, (n & 1) ^ 1, c, a)) ||
                 !warp_wait(&c.v_full[h], (t / kStages) & 1, c, a)) {
                 ok = false;
                 break;
             }
-            uint8_t *vb = sv + h * kTileBytes;
-            if (ragged) {  // rows of V past a sequence's last key
+            uint32_t steps = 0;  // those with keys
+            if (own) {
+                const int keys = lane < 8 ? c.step_keys[h][lane] : 0;
+                steps = __ballot_sync(kFull, keys > 0);
+                const uint32_t ragged = __ballot_sync(kFull, keys > 0 && keys < 16);
+                uint8_t *vb = sv + h * kTileBytes;
 #pragma unroll 1
-                for (uint32_t m = ragged; m; m &= m - 1) {
+                for (uint32_t m = ragged; m; m &= m - 1) {  // rows of V past a sequence's last key
                     const int kk = __ffs(m) - 1, filled = __shfl_sync(kFull, keys, kk);
 #pragma unroll 1
                     for (int y = lane; y < (16 - filled) * 16; y += 32)  // 8 16-byte units in each of two atoms
                         st_shared_v4(saddr(vb + (y & 8 ? kAtom : 0) + (kk * 16 + filled + (y >> 4)) * 128 + (y & 7) * 16),
                                      make_uint4(0, 0, 0, 0));
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
+                if (ragged) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
             }
             if (!warp_wait(&c.p_full[h], (t / kStages) & 1, c, a)) {
                 ok = false;
@@ -644,12 +650,12 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             } else {
 #pragma unroll 2
                 for (int k = 0; k < 8; ++k) {
-                    const uint4 o = c.step_off[k];
+                    const uint4 o = c.step_off[h][k];
                     const uint32_t off[4] = {o.x, o.y, o.z, o.w};
                     mma_bf16_ts_rows(ocol, pcol + k * 8, vd + static_cast<uint64_t>(k) * (2048 >> 4), idesc_o, off,
-                                     c.step_fresh[k] ^ 1, issue & (steps >> k));
+                                     c.step_fresh[h][k] ^ 1, issue & (steps >> k));
                 }
-                __syncwarp();  // (the steps are written again)
+                __syncwarp();  // (the steps are read: the commit below lets them be written again)
             }
             mma_commit(&c.v_empty[h], issue);
             if (j == p.j1 - 1) mma_commit(&c.o_ready, issue);  // the piece's O is complete
@@ -717,21 +723,49 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
                 float mx8[8], mr = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) mx8[i] = -INFINITY;
-                // (rows that are not stored need no mask: with 7 heads a group, two rows of every tile)
+                // Quarters (32 columns) in which the warp's rows see different keys, and those that no
+                // row sees. (Rows that are not stored need no mask: with 7 heads a group, two of
+                // every tile.)
+                uint32_t mixed = 0, none = 0;
                 const bool part = live && (col.lo > 0 || col.hi < 128);
+                if (__any_sync(kFull, part)) {
+#pragma unroll 1
+                    for (int k = 0; k < 4; ++k) {
+                        const int lo = col.lo - 32 * k, hi = col.hi - 32 * k;
+                        mixed |= (__any_sync(kFull, part && (lo > 0 || hi < 32)) ? 1u : 0u) << k;
+                        none |= (__all_sync(kFull, !live || (part && (hi <= 0 || lo >= 32 || hi <= lo))) ? 1u : 0u) << k;
+                    }
+                }
                 const f2 cc = pack2(a.c, a.c);
                 f2 lsum[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll 1
                 for (int pass = 0; pass < 4; ++pass) {
                     const int at = (pass & 1) * 64;
                     uint32_t s0[32], s1[32];
+                    if ((none >> (at >> 5) & 3u) == 3u && pass != 1) {  // (the maximum is taken in pass 1)
+                        if (pass >= 2) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) s0[i] = 0;
+                            tmem_st32_u(sbuf + at / 2, s0);
+                        }
+                        continue;
+                    }
                     tmem_ld32_async(sbuf + at, s0);
                     tmem_ld32_async(sbuf + at + 32, s1);
                     tmem_wait_dep(s0);
                     tmem_wait_dep(s1);
-                    if (part) {
-                        mask_scores(s0, col.lo - at, col.hi - at);
-                        mask_scores(s1, col.lo - at - 32, col.hi - at - 32);
+                    const uint32_t todo = mixed >> (at >> 5) & 3u;
+                    if (pass < 2 && todo) {  // masked once, and written back
+                        const int lo = part ? col.lo - at : 0, hi = part ? col.hi - at : 64;
+                        if (todo & 1u) {
+                            mask_scores(s0, lo, hi);
+                            tmem_st32_u(sbuf + at, s0);
+                        }
+                        if (todo & 2u) {
+                            mask_scores(s1, lo - 32, hi - 32);
+                            tmem_st32_u(sbuf + at + 32, s1);
+                        }
+                        tmem_wait_st();
                     }
                     if (pass >= 2) {
                         const f2 mm = pack2(mr, mr);
@@ -852,64 +886,58 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
         const bool zeros = __any_sync(kFull, (keep0 & keep1) == 0);
         const f2 ww0 = pack2(w0, w0), ww1 = pack2(w1, w1);
         const uint32_t at0 = col + (both ? 0 : only * 128), at1 = both ? col + 128 : at0;
-        uint32_t held[16];  // a chunk of the output that does not fit the stage yet
 #pragma unroll 1
-        for (int ch = 0; ch < 4; ++ch) {  // 32 columns at a time
-            uint32_t o0[32], o1[32];
-            tmem_ld32_async(at0 + ch * 32, o0);
-            tmem_ld32_async(at1 + ch * 32, o1);
-            tmem_wait_dep(o0);
-            tmem_wait_dep(o1);
+        for (int it = 0; it < 2; ++it) {  // 64 columns at a time
+            uint32_t o[64], o1[64];
+            uint32_t(&oa)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o[0]);
+            uint32_t(&ob)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o[32]);
+            uint32_t(&pa)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o1[0]);
+            uint32_t(&pb)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o1[32]);
+            tmem_ld32_async(at0 + it * 64, oa);
+            tmem_ld32_async(at1 + it * 64, pa);
+            tmem_ld32_async(at0 + it * 64 + 32, ob);
+            tmem_ld32_async(at1 + it * 64 + 32, pb);
+            tmem_wait_dep(oa);
+            tmem_wait_dep(pa);
+            tmem_wait_dep(ob);
+            tmem_wait_dep(pb);
+            if (it == 1) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&c.o_free);  // O may take the next piece
+                if (whole) store_stage(stage, lane, row, 0);  // the first 64 columns
+            }
             if (zeros) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    o0[i] &= keep0;
+                for (int i = 0; i < 64; ++i) {
+                    o[i] &= keep0;
                     o1[i] &= keep1;
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-                const f2 x = pack2(__uint_as_float(o0[i]), __uint_as_float(o0[i + 1]));
+            for (int i = 0; i < 64; i += 2) {
+                const f2 x = pack2(__uint_as_float(o[i]), __uint_as_float(o[i + 1]));
                 const f2 y = pack2(__uint_as_float(o1[i]), __uint_as_float(o1[i + 1]));
                 float lo, hi;
                 unpack2(fma2(y, ww1, mul2(x, ww0)), lo, hi);
-                o0[i] = __float_as_uint(lo);
-                o0[i + 1] = __float_as_uint(hi);
+                if (whole) {
+                    o[i / 2] = pack16<kF16>(lo, hi);
+                } else {
+                    o[i] = __float_as_uint(lo);
+                    o[i + 1] = __float_as_uint(hi);
+                }
             }
-            if (ch == 3) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&c.o_free);  // O may take the next piece
-            }
-            if (!whole) {
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {  // (32 columns of fp32 fill the stage, 64 of 16 bits)
 #pragma unroll
                 for (int u = 0; u < 8; ++u)
                     st_shared_v4(stage + lane * 128 + ((u ^ (lane & 7)) << 4),
-                                 make_uint4(o0[4 * u], o0[4 * u + 1], o0[4 * u + 2], o0[4 * u + 3]));
-                store_stage(stage, lane, row, ch * 128);
-                continue;
+                                 make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]));
+                if (whole) break;
+                store_stage(stage, lane, row, it * 256 + half * 128);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = o[32 + i];
             }
-            uint32_t pk[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                pk[i] = pack16<kF16>(__uint_as_float(o0[2 * i]), __uint_as_float(o0[2 * i + 1]));
-            // chunks 0 and 1 fill the stage; 2 is held; it and 3 follow when the first have left
-            if (ch == 2) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) held[i] = pk[i];
-                continue;
-            }
-            if (ch == 3) {
-                store_stage(stage, lane, row, 0);
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    st_shared_v4(stage + lane * 128 + ((u ^ (lane & 7)) << 4),
-                                 make_uint4(held[4 * u], held[4 * u + 1], held[4 * u + 2], held[4 * u + 3]));
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                st_shared_v4(stage + lane * 128 + ((((ch & 1) * 4 + u) ^ (lane & 7)) << 4),
-                             make_uint4(pk[4 * u], pk[4 * u + 1], pk[4 * u + 2], pk[4 * u + 3]));
         }
         if (whole) store_stage(stage, lane, row, 128);
         if (lse) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
@@ -981,7 +1009,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         softmax<kF16>(tmem, warp & 3, lane, (warp >> 2) - 1, tiles, c, a);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOutRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kOutRegs));
         read_out<kF16>(tmem, warp & 3, lane, saddr(so + (warp - 12) * kStageBytes), tiles, c, a);
     }
     tc_fence_before();
