@@ -72,9 +72,12 @@ constexpr int kRing = 4;             // pieces known ahead
 constexpr int kConsumers = 15;       // warps 0, 1, 2 and 4..15
 constexpr int kMaxSeqs = 128;        // sequences with rows in one row tile
 constexpr int kMaxCtas = 160;
+constexpr int kStepAdds = 32;
 constexpr int kStagedLens = 1024;    // lengths that are kept in shared memory
 constexpr int kMaxReqs = 2 * kStages * kTileBytes / 8;  // requests whose first tiles fit the K and V stages
 constexpr float kLn2 = 0.6931471805599453f;
+// bounds of a tile's sum of P in a row (in units of its reference): P in fp16 stays finite
+constexpr float kMostWeight = 32768.f, kLeastWeight = 1.f / 32768.f;
 
 // A row tile that is cut: the CTA that takes its first key tile writes where its parts
 // are. Entries are by row tile while there are at most kMaxCtas of them, else by CTA (one
@@ -113,7 +116,7 @@ struct Ctl {
     // s_full[t % 2]: S of tile t is computed and the product of tile t - 2 is done, so
     // K stage t % 2 is free, and Q of the pieces before t's. V stages have a commit of
     // their own. No wait sees a barrier two phases on: each waits for every phase in turn.
-    uint64_t q_full[kQBufs], k_full[kStages], v_full[kStages], v_empty[kStages];
+    uint64_t q_full[kQBufs], k_full[kStages], v_full[kStages], v_empty[kStages], v_raw;
     uint64_t s_full[kStages], p_full[kStages], o_ready, o_free, mma_done;
     uint64_t ring_full[kRing], ring_empty[kRing];
     // a half's reference and sum of a row at the end of piece n, in slot n % 4: written before
@@ -121,10 +124,10 @@ struct Ctl {
     // piece n + 4, whose P needs the products of piece n + 2 and so the read-out of piece n + 1
     float2 ml[4][kStages][prefix::kRows];
     Piece ring[kRing];
-    // own tile in V stage s, from V's producer: rows that step kk leaves alone; 1 where it
-    // overwrites; keys of each step
+    // own tile in V stage s, from V's producer: rows that step kk leaves alone; its keys (0: no
+    // step), and kStepAdds unless it overwrites
     uint4 step_off[kStages][8];
-    int32_t step_fresh[kStages][8], step_keys[kStages][8];
+    int32_t step_how[kStages][8];
     uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
     int32_t len[kStagedLens];
@@ -414,8 +417,8 @@ __device__ __forceinline__ void slot_page(const PrefixArgs &a, const Piece &p, i
 __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const CUtensorMap *tm_q, uint8_t *stages,
                                         uint8_t *sq, uint32_t tiles, int lane, Ctl &c, const PrefixArgs &a) {
     uint32_t t = 0;
-    int n = 0, n_q = 0;
-    bool ok = true;
+    int n = 0, n_q = 0, n_ragged = 0;
+    bool ok = true, raw = false;
     uint64_t *full = is_k ? c.k_full : c.v_full;
     // K: S of tile t - 2 is computed, so its stage is free, and at a piece's first tile the Q
     // buffer of piece n - 2, whose last tile is no later. V: the product of tile t - 2 is done.
@@ -447,28 +450,48 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
                     }
                 }
             }
+            int keys = 0;
             if (!is_k && j >= p.shared_tiles && lane < 8) {
                 const prefix::Step st = prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane);
                 c.step_off[s][lane] = make_uint4(
                     ~(low_bits(st.r1) & ~low_bits(st.r0)), ~(low_bits(st.r1 - 32) & ~low_bits(st.r0 - 32)),
                     ~(low_bits(st.r1 - 64) & ~low_bits(st.r0 - 64)), ~(low_bits(st.r1 - 96) & ~low_bits(st.r0 - 96)));
-                c.step_fresh[s][lane] = st.fresh;
-                c.step_keys[s][lane] = st.keys;
+                c.step_how[s][lane] = keys = st.keys > 0 ? st.keys | (st.fresh ? 0 : kStepAdds) : 0;
             }
+            const uint32_t ragged = __ballot_sync(kFull, (keys & 31) > 0 && (keys & 31) < 16);
+            uint64_t *bar = ragged ? &c.v_raw : &full[s];
             __syncwarp();  // (the steps are written before the arrival that hands them on)
-            if (lane == 0) mbar_expect_tx(&full[s], kTileBytes);
+            if (lane == 0) mbar_expect_tx(bar, kTileBytes);
             __syncwarp();
             if (lane < a.s.spt) {  // (slots that are not there: zeros)
                 uint8_t *dst = stages + s * kTileBytes + lane * a.s.slot * 128;
-                tma_load_4d(dst, tm, 0, token, p.head, page, &full[s]);
-                tma_load_4d(dst + kAtom, tm, 64, token, p.head, page, &full[s]);
+                tma_load_4d(dst, tm, 0, token, p.head, page, bar);
+                tma_load_4d(dst + kAtom, tm, 64, token, p.head, page, bar);
             }
             __syncwarp();
+            raw = ragged != 0;
+            if (ragged) {  // rows of V past a sequence's last key: they may hold anything, and 0 * NaN would be added
+                if (!(ok = warp_wait(&c.v_raw, n_ragged & 1, c, a))) break;
+                ++n_ragged;
+                uint8_t *vb = stages + s * kTileBytes;
+#pragma unroll 1
+                for (uint32_t m = ragged; m; m &= m - 1) {
+                    const int kk = __ffs(m) - 1, filled = __shfl_sync(kFull, keys & 31, kk);
+#pragma unroll 1
+                    for (int y = lane; y < (16 - filled) * 16; y += 32)  // 8 16-byte units in each of two atoms
+                        st_shared_v4(saddr(vb + (y & 8 ? kAtom : 0) + (kk * 16 + filled + (y >> 4)) * 128 + (y & 7) * 16),
+                                     make_uint4(0, 0, 0, 0));
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&full[s]);
+            }
         }
         if (ok) release_piece(n, lane, c);
     }
     // every copy issued lands before the CTA leaves
     if (lane == 0) {
+        if (!ok && raw) wait_drain(&c.v_raw, n_ragged & 1);
 #pragma unroll 1
         for (uint32_t x = t > kStages ? t - kStages : 0; x < t + 2; ++x) {
             if (x < t)
@@ -557,115 +580,96 @@ __device__ __forceinline__ void schedule(const PrefixArgs &a, const Range &range
     }
 }
 
-// The MMA issuer (lane 0 issues, the warp stays converged).
+// One thread's wait.
+__device__ __forceinline__ bool lane_wait(uint64_t *bar, uint32_t parity, Ctl &c, const PrefixArgs &a) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < a.tries; ++i)
+        if (try_wait_us(bar, parity)) return true;
+    *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
+    return false;
+}
+
+// The MMA issuer, one thread: S_t = Q K_t^T into TMEM buffer t % 2, O[t % 2] += P_t V_t. The tensor
+// pipe runs them in order, so S of tile t + 2 may overwrite the P that the product of tile t
+// reads without a wait. An issued instruction holds the thread until the pipe takes it, and
+// what the thread does between the batches leaves the pipe idle: so there is one wait for each
+// batch, and one thread without votes.
 template <bool kF16>
 __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t *sv, uint32_t tmem, uint32_t tiles,
                                                int lane, Ctl &c, const PrefixArgs &a) {
-    constexpr uint32_t fmt = kF16 ? umma::kFmtF16 : umma::kFmtBF16;
-    constexpr uint32_t idesc_s = umma::instr_desc_f16(128, 128, fmt, 0);  // K is K-major
-    constexpr uint32_t idesc_o = umma::instr_desc_f16(128, 128, fmt, 1);  // V is MN-major
-    const uint32_t issue = lane == 0;
-    // (an operand's other buffer, atom or step: its address field moved on)
-    const uint64_t q_desc = umma::smem_desc_kmajor_sw128(saddr(sq)), k_desc = umma::smem_desc_kmajor_sw128(saddr(sk));
-    const uint64_t v_desc = umma::smem_desc_mnmajor_sw128(saddr(sv), kAtom);
-    bool ok = true;
-    int sn = 0, sj = 0, sj1 = 0;  // the scores' piece, tile, and the piece's end
-    const auto scores = [&](uint32_t t) -> bool {  // S_t = Q K_t^T into buffer t % 2
-        if (sj == sj1) {
-            const Piece *p = next_piece(sn, c, a);
-            if (!p) return false;
-            sj = p->j0;
-            sj1 = p->j1;
-            if (!warp_wait(&c.q_full[sn & 1], (sn >> 1) & 1, c, a)) return false;
-            ++sn;
-        }
-        const uint32_t s = t % kStages;
-        if (!warp_wait(&c.k_full[s], (t / kStages) & 1, c, a)) return false;
-        tc_fence_after();
-        const uint64_t qd = q_desc + (sn & 1 ? 0 : kTileBytes >> 4), kd = k_desc + s * (kTileBytes >> 4);
-        const uint32_t sbuf = tmem + s * 128;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {  // (16 of the 64 columns of an atom are 32 bytes)
-            const uint32_t at = k / 4 * (kAtom >> 4) + k % 4 * 2;
-            mma_bf16(sbuf, qd + at, kd + at, idesc_s, k != 0, issue);
-        }
-        mma_commit(&c.s_full[s], issue);
-        ++sj;
-        return true;
-    };
-    // step x: the product of tile x - 2, then the scores of tile x
-    const Piece *pp = nullptr;
-    int n = -1, j = 0;  // the product's piece and tile
+    if (lane == 0) {
+        constexpr uint32_t fmt = kF16 ? umma::kFmtF16 : umma::kFmtBF16;
+        constexpr uint32_t idesc_s = umma::instr_desc_f16(128, 128, fmt, 0);  // K is K-major
+        constexpr uint32_t idesc_o = umma::instr_desc_f16(128, 128, fmt, 1);  // V is MN-major
+        // (an operand's other buffer, atom or step: its address field moved on)
+        const uint64_t q_desc = umma::smem_desc_kmajor_sw128(saddr(sq)), k_desc = umma::smem_desc_kmajor_sw128(saddr(sk));
+        const uint64_t v_desc = umma::smem_desc_mnmajor_sw128(saddr(sv), kAtom);
+        int sn = -1, s_left = 0;                        // the scores' piece, and its tiles left
+        int n = -1, j = 0, j0 = 0, j1 = 0, shared_tiles = 0;  // the product's piece and tile
 #pragma unroll 1
-    for (uint32_t x = 0; x < tiles + kStages && ok; ++x) {
-        if (x >= kStages) {
-            const uint32_t t = x - kStages;
-            if (!pp || j == pp->j1) {
-                if (pp) release_piece(n, lane, c);
-                if (!(pp = next_piece(++n, c, a))) break;
-                j = pp->j0;
-            }
-            const Piece &p = *pp;
-            const uint32_t h = t % kStages;
-            const bool own = j >= p.shared_tiles;
-            // the first product of a piece overwrites O: the previous piece's read-out must be done
-            if ((j == p.j0 && !warp_wait(&c.o_free, (n & 1) ^ 1, c, a)) ||
-                !warp_wait(&c.v_full[h], (t / kStages) & 1, c, a)) {
-                ok = false;
-                break;
-            }
-            uint32_t steps = 0;  // those with keys
-            if (own) {
-                const int keys = lane < 8 ? c.step_keys[h][lane] : 0;
-                steps = __ballot_sync(kFull, keys > 0);
-                const uint32_t ragged = __ballot_sync(kFull, keys > 0 && keys < 16);
-                uint8_t *vb = sv + h * kTileBytes;
-#pragma unroll 1
-                for (uint32_t m = ragged; m; m &= m - 1) {  // rows of V past a sequence's last key
-                    const int kk = __ffs(m) - 1, filled = __shfl_sync(kFull, keys, kk);
-#pragma unroll 1
-                    for (int y = lane; y < (16 - filled) * 16; y += 32)  // 8 16-byte units in each of two atoms
-                        st_shared_v4(saddr(vb + (y & 8 ? kAtom : 0) + (kk * 16 + filled + (y >> 4)) * 128 + (y & 7) * 16),
-                                     make_uint4(0, 0, 0, 0));
+        for (uint32_t x = 0; x < tiles + kStages; ++x) {  // the product of tile x - 2, then the scores of tile x
+            const uint32_t h = x % kStages, parity = (x / kStages) & 1;
+            if (x >= kStages) {
+                if (j == j1) {
+                    if (n >= 0) mbar_arrive(&c.ring_empty[n % kRing]);
+                    ++n;
+                    const Piece &p = c.ring[n % kRing];
+                    // the first product of a piece overwrites O: the previous piece's read-out must be done
+                    if (!lane_wait(&c.ring_full[n % kRing], (n / kRing) & 1, c, a) ||
+                        !lane_wait(&c.o_free, (n & 1) ^ 1, c, a))
+                        break;
+                    j = j0 = p.j0;
+                    j1 = p.j1;
+                    shared_tiles = p.shared_tiles;
                 }
-                if (ragged) {
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
-            }
-            if (!warp_wait(&c.p_full[h], (t / kStages) & 1, c, a)) {
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            // P of keys 16k..16k+15: columns 8k..8k+7 of S buffer t % 2
-            const uint32_t pcol = tmem + h * 128, ocol = tmem + kOCol + h * 128;
-            const uint64_t vd = v_desc + h * (kTileBytes >> 4);
-            if (!own) {
-                const uint32_t more = j - p.j0 >= kStages;  // the half has had a tile of this piece
+                if (!lane_wait(&c.p_full[h], parity ^ 1, c, a)) break;  // P, and V (see the softmax)
+                tc_fence_after();
+                // P of keys 16k..16k+15: 8 columns; those of keys 64.. begin where their scores did
+                const uint32_t pcol = tmem + h * 128, ocol = pcol + kOCol;
+                const uint64_t vd = v_desc + h * (kTileBytes >> 4);
+                if (j < shared_tiles) {
+                    const uint32_t more = j - j0 >= kStages;  // the half has had a tile of this piece
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    mma_bf16_ts(ocol, pcol + k * 8, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o, more | (k != 0),
-                                issue);
-            } else {
+                    for (int k = 0; k < 8; ++k)
+                        mma_ts(ocol, pcol + k / 4 * 64 + k % 4 * 8, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o,
+                               k ? 1u : more);
+                } else {
 #pragma unroll 2
-                for (int k = 0; k < 8; ++k) {
-                    const uint4 o = c.step_off[h][k];
-                    const uint32_t off[4] = {o.x, o.y, o.z, o.w};
-                    mma_bf16_ts_rows(ocol, pcol + k * 8, vd + static_cast<uint64_t>(k) * (2048 >> 4), idesc_o, off,
-                                     c.step_fresh[h][k] ^ 1, issue & (steps >> k));
+                    for (int k = 0; k < 8; ++k) {
+                        const uint4 o = c.step_off[h][k];
+                        const int how = c.step_how[h][k];
+                        const uint32_t off[4] = {o.x, o.y, o.z, o.w};
+                        if (how)
+                            mma_ts_rows(ocol, pcol + k / 4 * 64 + k % 4 * 8, vd + static_cast<uint64_t>(k) * (2048 >> 4),
+                                        idesc_o, off, how & kStepAdds);
+                    }
                 }
-                __syncwarp();  // (the steps are read: the commit below lets them be written again)
+                commit(&c.v_empty[h]);
+                if (++j == j1) commit(&c.o_ready);  // the piece's O is complete
             }
-            mma_commit(&c.v_empty[h], issue);
-            if (j == p.j1 - 1) mma_commit(&c.o_ready, issue);  // the piece's O is complete
-            ++j;
+            if (x < tiles) {
+                if (s_left == 0) {
+                    ++sn;
+                    if (!lane_wait(&c.ring_full[sn % kRing], (sn / kRing) & 1, c, a) ||
+                        !lane_wait(&c.q_full[sn & 1], (sn >> 1) & 1, c, a))
+                        break;
+                    s_left = c.ring[sn % kRing].j1 - c.ring[sn % kRing].j0;
+                }
+                if (!lane_wait(&c.k_full[h], parity, c, a)) break;
+                tc_fence_after();
+                const uint64_t qd = q_desc + (sn & 1 ? kTileBytes >> 4 : 0), kd = k_desc + h * (kTileBytes >> 4);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {  // (16 of the 64 columns of an atom are 32 bytes)
+                    const uint32_t at = k / 4 * (kAtom >> 4) + k % 4 * 2;
+                    mma_ss(tmem + h * 128, qd + at, kd + at, idesc_s, k != 0);
+                }
+                commit(&c.s_full[h]);
+                --s_left;
+            }
         }
-        if (x < tiles) ok = scores(x);
+        commit(&c.mma_done);
+        wait_drain(&c.mma_done, 0);
     }
-    if (pp && ok) release_piece(n, lane, c);
-    mma_commit(&c.mma_done, issue);
-    if (lane == 0) wait_drain(&c.mma_done, 0);
     __syncwarp();
 }
 
@@ -692,7 +696,7 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
             own_off = p.off[i];
             own_end = p.off[i + 1];
         }
-        float m = -INFINITY, l = 0.f;
+        float m = kF16 ? -INFINITY : 0.f, l = 0.f;
         const int count = p.j1 - p.j0, x0 = (h ^ static_cast<int>(t0)) & 1;
         for (int x = x0; x < count; x += kStages) {
             const uint32_t t = t0 + x;
@@ -716,103 +720,94 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
             const int first = (j - p.shared_tiles) << a.s.spt_log;
             const bool takes = live && (j < p.shared_tiles || (own_off < first + a.s.spt && own_end > first));
             if (__any_sync(kFull, takes)) {
-                // Twice over the scores, 64 at a time: their maximum, then P = 2^(s c - m), pairs
-                // of 16 bits over columns of S that are read. While all scores so far are
-                // -inf, m is: P = 0 and the sum 0. (One body for the four passes instead of all
-                // 128 scores in registers: a third of the code.)
-                float mx8[8], mr = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) mx8[i] = -INFINITY;
-                // Quarters (32 columns) in which the warp's rows see different keys, and those that no
-                // row sees. (Rows that are not stored need no mask: with 7 heads a group, two of
-                // every tile.)
-                uint32_t mixed = 0, none = 0;
+                // Keys that a row does not see take no weight: quarters (32 columns) in which some
+                // row of the warp has such keys are masked and written back. (Rows that are not
+                // stored need no mask: with 7 heads a group, two of every tile.)
                 const bool part = live && (col.lo > 0 || col.hi < 128);
                 if (__any_sync(kFull, part)) {
 #pragma unroll 1
-                    for (int k = 0; k < 4; ++k) {
-                        const int lo = col.lo - 32 * k, hi = col.hi - 32 * k;
-                        mixed |= (__any_sync(kFull, part && (lo > 0 || hi < 32)) ? 1u : 0u) << k;
-                        none |= (__all_sync(kFull, !live || (part && (hi <= 0 || lo >= 32 || hi <= lo))) ? 1u : 0u) << k;
+                    for (int k = 0; k < 128; k += 32) {
+                        const int lo = part ? col.lo - k : 0, hi = part ? col.hi - k : 32;
+                        if (!__any_sync(kFull, lo > 0 || hi < 32)) continue;
+                        uint32_t s0[32];
+                        tmem_ld32_async(sbuf + k, s0);
+                        tmem_wait_dep(s0);
+                        mask_scores(s0, lo, hi);
+                        tmem_st32_u(sbuf + k, s0);
                     }
+                    tmem_wait_st();
                 }
+                // P = 2^(s c - m) with the row's present reference m, 0 at first; the sum tells whether m
+                // was good enough (P and the sums far from the ends of their types' ranges: for fp16
+                // P, m is within 2^15 of the largest so far). If not, m becomes the tile's largest
+                // score and P is computed again: P is kept in registers until then, for it overwrites scores.
                 const f2 cc = pack2(a.c, a.c);
-                f2 lsum[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                bool raise = kF16 && m == -INFINITY && col.lo < col.hi;
 #pragma unroll 1
-                for (int pass = 0; pass < 4; ++pass) {
-                    const int at = (pass & 1) * 64;
-                    uint32_t s0[32], s1[32];
-                    if ((none >> (at >> 5) & 3u) == 3u && pass != 1) {  // (the maximum is taken in pass 1)
-                        if (pass >= 2) {
+                for (int round = 0; round < 2; ++round) {
+                    if (__any_sync(kFull, raise)) {
+                        float mx8[8];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) s0[i] = 0;
-                            tmem_st32_u(sbuf + at / 2, s0);
+                        for (int i = 0; i < 8; ++i) mx8[i] = -INFINITY;
+#pragma unroll 1
+                        for (int k = 0; k < 128; k += 32) {
+                            uint32_t s0[32];
+                            tmem_ld32_async(sbuf + k, s0);
+                            tmem_wait_dep(s0);
+                            max_scores(s0, mx8);
                         }
-                        continue;
+                        const float tm = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
+                                               fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]))) * a.c;
+                        raise = raise && tm > -INFINITY;
+                        const float f = raise && l != 0.f ? ex2(m - tm) : 1.f;  // (without weight so far: O is 0)
+                        if (raise) m = tm;
+                        l *= f;
+                        // the warp rescales its O together (tcgen05.ld / st are warp-wide), rows without need
+                        // by 1. The half's previous product is done: S of this tile was issued after it.
+                        if (__any_sync(kFull, f != 1.f)) {
+#pragma unroll 1
+                            for (int ch = 0; ch < 8; ++ch) {
+                                uint32_t o[16];
+                                tmem_ld16_async(obuf + ch * 16, o);
+                                tmem_wait_dep(o);
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                tmem_st16(obuf + ch * 16, o);
+                            }
+                        }
                     }
-                    tmem_ld32_async(sbuf + at, s0);
-                    tmem_ld32_async(sbuf + at + 32, s1);
+                    const float mr = m == -INFINITY ? 0.f : -m;
+                    const f2 mm = pack2(mr, mr);
+                    f2 lsum[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                    uint32_t s0[32], s1[32], s2[32], s3[32], pk[32], pk2[32];
+                    tmem_ld32_async(sbuf, s0);
+                    tmem_ld32_async(sbuf + 32, s1);
                     tmem_wait_dep(s0);
                     tmem_wait_dep(s1);
-                    const uint32_t todo = mixed >> (at >> 5) & 3u;
-                    if (pass < 2 && todo) {  // masked once, and written back
-                        const int lo = part ? col.lo - at : 0, hi = part ? col.hi - at : 64;
-                        if (todo & 1u) {
-                            mask_scores(s0, lo, hi);
-                            tmem_st32_u(sbuf + at, s0);
-                        }
-                        if (todo & 2u) {
-                            mask_scores(s1, lo - 32, hi - 32);
-                            tmem_st32_u(sbuf + at + 32, s1);
-                        }
-                        tmem_wait_st();
-                    }
-                    if (pass >= 2) {
-                        const f2 mm = pack2(mr, mr);
-                        uint32_t pk[32];
-                        exp_scores<kF16>(s0, cc, mm, lsum, pk, 0);
-                        exp_scores<kF16>(s1, cc, mm, lsum, pk, 16);
-                        tmem_st32_u(sbuf + at / 2, pk);
-                        continue;
-                    }
-                    max_scores(s0, mx8);
-                    max_scores(s1, mx8);
-                    if (pass == 0) continue;
-                    const float tm = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
-                                           fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]))) * a.c;
-                    float f = 1.f;
-                    bool rescale = false;
-                    if (m == -INFINITY) {
-                        m = tm;
-                    } else if (tm > m + kRescale) {
-                        f = ex2(m - tm);
-                        m = tm;
-                        rescale = true;
-                    }
-                    // the warp rescales its O together (tcgen05.ld / st are warp-wide), rows without need by
-                    // 1. The half's previous product is done: S of this tile was issued after it.
-                    if (__any_sync(kFull, rescale)) {
-#pragma unroll 1
-                        for (int ch = 0; ch < 8; ++ch) {
-                            uint32_t o[16];
-                            tmem_ld16_async(obuf + ch * 16, o);
-                            tmem_wait_dep(o);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st16(obuf + ch * 16, o);
-                        }
-                    }
-                    l *= f;
-                    mr = m == -INFINITY ? 0.f : -m;
-                }
-                {
+                    exp_scores<kF16>(s0, cc, mm, lsum, pk, 0);
+                    tmem_ld32_async(sbuf + 64, s2);
+                    exp_scores<kF16>(s1, cc, mm, lsum, pk, 16);
+                    tmem_ld32_async(sbuf + 96, s3);
+                    tmem_wait_dep(s2);
+                    tmem_wait_dep(s3);
+                    exp_scores<kF16>(s2, cc, mm, lsum, pk2, 0);
+                    exp_scores<kF16>(s3, cc, mm, lsum, pk2, 16);
                     float l0, l1;
                     unpack2(add2(add2(lsum[0], lsum[1]), add2(lsum[2], lsum[3])), l0, l1);
-                    l += l0 + l1;
+                    l0 += l1;
+                    raise = live && col.lo < col.hi && (!(l0 < kMostWeight) || (!kF16 && l == 0.f && l0 < kLeastWeight));
+                    if (round == 0 && __any_sync(kFull, raise)) continue;
+                    l += l0;
+                    tmem_st32_u(sbuf, pk);
+                    tmem_st32_u(sbuf + 64, pk2);
+                    break;
                 }
                 tmem_wait_st();
             }
-            if (x + kStages >= count) c.ml[n & 3][h][r] = make_float2(m, l);
+            if (x + kStages >= count) c.ml[n & 3][h][r] = make_float2(l == 0.f ? -INFINITY : m, l);
+            // (one of the half's warps also waits for V, which is there by now: the issuer then
+            // has one wait less)
+            if (q == 0 && !(ok = warp_wait(&c.v_full[h], (t / kStages) & 1, c, a))) break;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&c.p_full[h]);
@@ -975,6 +970,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&c.o_ready, 1);
         mbar_init(&c.o_free, 4);
         mbar_init(&c.mma_done, 1);
+        mbar_init(&c.v_raw, 1);
         c.abort_flag = 0;
         for (const CUtensorMap *m : {&tm_q, &tm_k, &tm_v})
             asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
