@@ -119,6 +119,11 @@ uint32_t *device_error_word() {
     return device_info(&dev) == RPS_OK ? dev.err : nullptr;
 }
 
+int device_sm_count() {
+    DeviceInfo dev;
+    return device_info(&dev) == RPS_OK ? dev.sm_count : 0;
+}
+
 uint64_t ring_wait_limit_ns() { return g_ring_wait_ns.load(std::memory_order_relaxed); }
 
 }  // namespace rps

@@ -623,10 +623,8 @@ PageData page_data(const rps_kv_cache *kv) {
 rps_status launch_copy(const rps_kv_cache *from, const rps_kv_cache *to, const int32_t *src, const int32_t *dst,
                        const int32_t *used, const CopyHeader *head, int32_t count, int64_t most, uint32_t *err,
                        cudaStream_t stream) {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return RPS_ERR_CUDA;
+    const int sms = device_sm_count();
+    if (sms < 1) return RPS_ERR_CUDA;
     CopyArgs a;
     std::memset(&a, 0, sizeof a);
     a.from = page_data(from);

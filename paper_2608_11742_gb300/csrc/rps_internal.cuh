@@ -140,6 +140,9 @@ cudaError_t launch_score_commit(const ScoreArgs &s, const CommitArgs &c, cudaStr
 // The calling device's sticky error word (nullptr if the device cannot be queried).
 uint32_t *device_error_word();
 
+// The calling device's SM count (0 if it cannot be queried).
+int device_sm_count();
+
 // The current limit of a kernel's wait for an asynchronous copy (rps_debug_set_ring_wait_ns).
 uint64_t ring_wait_limit_ns();
 
