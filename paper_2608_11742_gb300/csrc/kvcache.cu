@@ -6,11 +6,13 @@
 // sequence is absent). A page is free when its count is 0; pages are always
 // taken in ascending order and given to the sequences in ascending order, by
 // prefix sums, so a call's result does not depend on the order of its atomics.
-// Each bookkeeping call is one thread-block cluster: its phases are ordered by
-// the cluster barrier, so a call that reads what it overwrites needs no second
-// launch, and the counts of the blocks' ranges are exchanged through
-// distributed shared memory. The data of copied pages follow in a second
-// launch over the whole device.
+// Forks and commits of a lookahead step need no order between their sequences: a
+// warp each. The other bookkeeping calls are one thread-block cluster (one block of
+// it where there is little): its phases are ordered by the cluster barrier, so a call
+// that reads what it overwrites needs no second launch, and the counts of the blocks'
+// ranges are exchanged through distributed shared memory. The data of copied pages
+// follow in a second launch over the whole device. All of these are bound by the
+// latency of their dependent accesses (0.6 us each from L2), the data by HBM.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -27,6 +29,7 @@ constexpr int kHeadDim = 128;
 constexpr int kBookThreads = 1024;
 constexpr int kBookWarps = kBookThreads / 32;
 constexpr int kCluster = 8;
+constexpr int kOneBlock = 8192;
 constexpr int kCopyThreads = 256;
 constexpr int kTaskRows = 16;  // rows a warp copies at a time: 4 KB, 8 16-byte loads in flight per lane
 constexpr size_t kWsAlign = 256;
@@ -98,43 +101,30 @@ __device__ __forceinline__ bool good_page(const Book &b, int p) {
     return ok;
 }
 
+// Orders the phases of a bookkeeping call.
+__device__ __forceinline__ void book_sync(const cg::cluster_group &cluster) {
+    if (cluster.num_blocks() > 1)
+        cluster.sync();
+    else
+        __syncthreads();
+}
+
 struct ReorderArgs {
     Book b;
-    const int32_t *src_of;  // general form
-    const int32_t *keep;    // tokens kept, nullptr: all
-    const uint8_t *valid;   // fork form: [n_req][n_branch - 1]
-    const int32_t *winner;  // commit form: [n_req]
-    int32_t n_branch;
+    const int32_t *src_of;
+    const int32_t *keep;  // tokens kept, nullptr: all
     KvWorkspace w;
 };
 
 // The sequence whose state sequence s takes (-1: none), and how much of it.
 __device__ __forceinline__ void source_of(const ReorderArgs &a, int s, int &src, int &keep) {
     keep = INT32_MAX;
-    if (a.src_of) {
-        src = a.src_of[s];
-        if (src < -1 || src >= a.b.n_seq) {  // the sequence stays as it is
-            flag_error(a.b.err, RPS_DEVERR_ROW_INDEX);
-            src = s;
-        } else if (a.keep) {
-            keep = a.keep[s];
-        }
-        return;
-    }
-    const int q = s / a.n_branch, b = s - q * a.n_branch;
-    if (a.winner) {
-        int w = b ? -1 : a.winner[q];
-        if (w >= a.n_branch - 1) {  // no such branch: the base stays
-            flag_error(a.b.err, RPS_DEVERR_ROW_INDEX);
-            w = -1;
-        }
-        src = b ? -1 : s + (w >= 0 ? w + 1 : 0);
-        return;
-    }
-    src = s;
-    if (b) {
-        src = a.valid[static_cast<int64_t>(q) * (a.n_branch - 1) + b - 1] ? s - b : -1;
-        if (a.keep) keep = a.keep[q];
+    src = a.src_of[s];
+    if (src < -1 || src >= a.b.n_seq) {  // the sequence stays as it is
+        flag_error(a.b.err, RPS_DEVERR_ROW_INDEX);
+        src = s;
+    } else if (a.keep) {
+        keep = a.keep[s];
     }
 }
 
@@ -164,7 +154,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) reorder_kernel(const ReorderA
         }
         if (lane == 0) a.w.snap_len[s] = len;
     }
-    cluster.sync();
+    book_sync(cluster);
     for (int s = warp; s < b.n_seq; s += warps) {
         int src, keep;
         source_of(a, s, src, keep);
@@ -181,6 +171,71 @@ __global__ void __launch_bounds__(kBookThreads, 1) reorder_kernel(const ReorderA
         for (int i = n + lane; i < b.width; i += 32) own[i] = -1;
         if (lane == 0) b.len[s] = len;
     }
+}
+
+// ---------------------------------------------------------------- a lookahead step's forks and commit
+struct BranchArgs {
+    Book b;
+    const uint8_t *valid;   // fork: [n_req][n_branch - 1]
+    const int32_t *ctx;     // fork: tokens kept, nullptr: all
+    const int32_t *winner;  // commit (fork if nullptr): [n_req]
+    int32_t n_branch;
+};
+
+constexpr int kBranchThreads = 128;
+
+// A warp per sequence. Fork: a branch gives its pages back and takes its base's, which nobody
+// changes. Commit: the base's warp moves the winner's row to the base (the pages' counts
+// stay), the others give their pages back. So no warp reads a row that another writes.
+__global__ void __launch_bounds__(kBranchThreads) branch_kernel(const BranchArgs a) {
+    const Book &b = a.b;
+    const int lane = threadIdx.x & 31, s = blockIdx.x * (kBranchThreads / 32) + (threadIdx.x >> 5);
+    if (s >= b.n_seq) return;
+    const int q = s / a.n_branch, br = s - q * a.n_branch;
+    int32_t *own = b.table + static_cast<int64_t>(s) * b.width;
+    pdl_wait();
+    pdl_launch_next();
+    const int old_len = b.len[s];
+    int src = -1, keep = INT32_MAX;  // -1: the sequence ends, s: it stays
+    if (a.winner) {
+        int w = a.winner[q];
+        if (w >= a.n_branch - 1) {  // no such branch: the base stays
+            if (br == 0) flag_error(b.err, RPS_DEVERR_ROW_INDEX);
+            w = -1;
+        }
+        if (br == 0) src = w >= 0 ? s + w + 1 : s;
+        if (br && br == w + 1) return;  // the base's warp moves it
+    } else if (br == 0) {
+        src = s;
+    } else if (a.valid[static_cast<int64_t>(q) * (a.n_branch - 1) + br - 1]) {
+        src = s - br;
+        if (a.ctx) keep = a.ctx[q];
+    }
+    const int old_n = pages_of(checked_len(b, old_len), b.ps);
+    int32_t *from = b.table + static_cast<int64_t>(src) * b.width;
+    int len = src < 0 ? -1 : checked_len(b, src == s ? old_len : b.len[src]);
+    if (keep < len) len = keep < 0 ? -1 : keep;
+    const int n = pages_of(len, b.ps), most = max(n, old_n);
+    if (src != s) {
+        for (int i = lane; i < most; i += 32) {
+            const int was = i < old_n ? own[i] : -1, is = i < n ? from[i] : -1;
+            if (i < old_n && good_page(b, was)) atomicSub(&b.ref[was], 1);
+            own[i] = is;
+            if (i >= n) continue;
+            const bool good = good_page(b, is);
+            if (a.winner)
+                from[i] = -1;
+            else if (good)
+                atomicAdd(&b.ref[is], 1);
+        }
+        if (lane == 0) {
+            b.len[s] = len;
+            if (a.winner && src >= 0) b.len[src] = -1;
+        }
+    }
+    for (int i = (src == s ? n : most) + lane; i < b.width; i += 32) own[i] = -1;
+    if (a.winner && src >= 0 && src != s)
+        for (int i = n + lane; i < b.width; i += 32) from[i] = -1;
 }
 
 // Inclusive prefix sum over the block in thread order; the block's total in *total.
@@ -209,6 +264,9 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
     __syncthreads();  // (sums may be written again)
     return v;
 }
+
+constexpr int kNearSeqs = 1024;   // sequences of a block whose wishes fit shared memory
+constexpr int kNearPages = 4096;  // free pages that do
 
 struct Counts {
     unsigned long long need;  // of the block's sequences: pages (low 32 bits), copies (high)
@@ -248,6 +306,8 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArg
     cg::cluster_group cluster = cg::this_cluster();
     __shared__ unsigned long long sums[kBookWarps];
     __shared__ Counts mine;
+    __shared__ unsigned long long near_need[kNearSeqs];
+    __shared__ int32_t near_list[kNearPages];
     const Book &b = a.b;
     const int lane = threadIdx.x & 31, rank = cluster.block_rank(), blocks = cluster.num_blocks();
     const int warp = rank * kBookWarps + (threadIdx.x >> 5), warps = blocks * kBookWarps;
@@ -266,12 +326,14 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArg
         __syncwarp();
         if (lane == 0) b.len[s] = new_len;
     }
-    cluster.sync();
-    // 2. what the block's sequences ask for, and the free ones of the block's pages
+    book_sync(cluster);
+    // 2. what the block's sequences ask for, and the free ones of the block's pages (of a block
+    // alone they are counted as they are listed)
     const int per_s = (b.n_seq + blocks - 1) / blocks;
     const int s0 = min(b.n_seq, rank * per_s), s1 = min(b.n_seq, s0 + per_s);
     const int per_p = (b.n_pages + blocks - 1) / blocks;
     const int p0 = min(b.n_pages, rank * per_p), p1 = min(b.n_pages, p0 + per_p);
+    unsigned long long *need_of = per_s <= kNearSeqs ? near_need - s0 : a.w.need;
     unsigned long long carry = 0, total;
     for (int at = s0; at < s1; at += kBookThreads) {
         const int s = at + threadIdx.x;
@@ -281,45 +343,51 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArg
             need = wanted(b, s, old_len, wanted_len(b, a.new_len[s], old_len));
         }
         const unsigned long long upto = block_scan(need, sums, &total);
-        if (s < s1) a.w.need[s] = carry + upto - need;
+        if (s < s1) need_of[s] = carry + upto - need;
         carry += total;
     }
-    int free_here = 0;
-    for (int p = p0 + threadIdx.x; p < p1; p += kBookThreads) free_here += b.ref[p] <= 0;
-    block_scan(free_here, sums, &total);
-    if (threadIdx.x == 0) {
-        mine.need = carry;
-        mine.pages = static_cast<int32_t>(total);
-    }
-    cluster.sync();
-    unsigned long long need_before = 0, need_all = 0;
+    unsigned long long need_before = 0, need_all = carry;
     int free_before = 0, free_all = 0;
-    for (int r = 0; r < blocks; ++r) {
-        const Counts *c = cluster.map_shared_rank(&mine, r);
-        if (r < rank) {
-            need_before += c->need;
-            free_before += c->pages;
+    if (blocks > 1) {
+        int free_here = 0;
+        for (int p = p0 + threadIdx.x; p < p1; p += kBookThreads) free_here += b.ref[p] <= 0;
+        block_scan(free_here, sums, &total);
+        if (threadIdx.x == 0) {
+            mine.need = carry;
+            mine.pages = static_cast<int32_t>(total);
         }
-        need_all += c->need;
-        free_all += c->pages;
+        cluster.sync();
+        need_all = 0;
+        for (int r = 0; r < blocks; ++r) {
+            const Counts *c = cluster.map_shared_rank(&mine, r);
+            if (r < rank) {
+                need_before += c->need;
+                free_before += c->pages;
+            }
+            need_all += c->need;
+            free_all += c->pages;
+        }
     }
     // 3. the lowest free pages, in order, as many as are asked for
     const int wish = static_cast<int>(min(need_all & 0xffffffffull, static_cast<unsigned long long>(INT32_MAX)));
+    int32_t *list = blocks == 1 && wish <= kNearPages ? near_list : a.w.list;
     for (int at = p0; at < p1 && free_before < wish; at += kBookThreads) {
         const int p = at + threadIdx.x;
         const unsigned long long is_free = p < p1 && b.ref[p] <= 0;
         const unsigned long long upto = block_scan(is_free, sums, &total);
-        if (is_free) a.w.list[free_before + static_cast<int>(upto) - 1] = p;
+        const int at_list = free_before + static_cast<int>(upto) - 1;
+        if (is_free && at_list < wish) list[at_list] = p;
         free_before += static_cast<int>(total);
     }
-    cluster.sync();  // (the list is written, and every block has read every count)
+    if (blocks == 1) free_all = free_before;  // (all that there are, or as many as are asked for)
+    book_sync(cluster);  // (the list is written, and every block has read every count)
     // 4. each sequence takes its pages; the copy list
     for (int s = s0 + (threadIdx.x >> 5); s < s1; s += kBookWarps) {
         const int old_len = checked_len(b, b.len[s]), new_len = wanted_len(b, a.new_len[s], old_len);
         if (new_len <= old_len) continue;
         // (counts of pages change while this phase runs: what is wanted is the difference to the next sequence)
-        const unsigned long long off = need_before + a.w.need[s];
-        const unsigned long long next = s + 1 < s1 ? need_before + a.w.need[s + 1] : need_before + carry;
+        const unsigned long long off = need_before + need_of[s];
+        const unsigned long long next = s + 1 < s1 ? need_before + need_of[s + 1] : need_before + carry;
         const bool cow = (next >> 32) != (off >> 32);
         const bool fits = (next & 0xffffffffull) <= static_cast<unsigned long long>(free_all);
         if (!fits) flag_error(b.err, RPS_DEVERR_NO_PAGES);
@@ -328,7 +396,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArg
         if (cow && lane == 0) {
             const int e = static_cast<int>(off >> 32), p = row[n_old - 1];
             a.w.src[e] = fits ? p : -1;
-            a.w.dst[e] = fits ? a.w.list[off & 0xffffffffull] : -1;
+            a.w.dst[e] = fits ? list[off & 0xffffffffull] : -1;
             a.w.used[e] = old_len % b.ps;
             if (fits) atomicSub(&b.ref[p], 1);
         }
@@ -336,7 +404,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArg
         if (!fits) continue;
         const int first = n_old - (cow ? 1 : 0);
         for (int i = first + lane; i < n_new; i += 32) {
-            const int p = a.w.list[(off & 0xffffffffull) + static_cast<unsigned>(i - first)];
+            const int p = list[(off & 0xffffffffull) + static_cast<unsigned>(i - first)];
             row[i] = p;
             b.ref[p] = 1;
         }
@@ -370,13 +438,16 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const CompactA
     int live_here = 0;
     for (int p = p0 + threadIdx.x; p < p1; p += kBookThreads) live_here += b.ref[p] > 0;
     block_scan(live_here, sums, &total);
-    if (threadIdx.x == 0) mine.pages = static_cast<int32_t>(total);
-    cluster.sync();
-    int before = 0, n_live = 0;
-    for (int r = 0; r < blocks; ++r) {
-        const int c = cluster.map_shared_rank(&mine, r)->pages;
-        if (r < rank) before += c;
-        n_live += c;
+    int before = 0, n_live = static_cast<int>(total);
+    if (blocks > 1) {
+        if (threadIdx.x == 0) mine.pages = n_live;
+        cluster.sync();
+        n_live = 0;
+        for (int r = 0; r < blocks; ++r) {
+            const int c = cluster.map_shared_rank(&mine, r)->pages;
+            if (r < rank) before += c;
+            n_live += c;
+        }
     }
     // The i-th free page below n_live takes the i-th live page from n_live on. Live
     // pages go into `list` by their rank among all live ones, so the sources are its
@@ -401,7 +472,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const CompactA
         if (a.n_live) *a.n_live = n_live;
         if (n_live == b.n_pages) a.w.head->src_off = a.w.head->count = 0;
     }
-    cluster.sync();
+    book_sync(cluster);
     const int moved = a.w.head->count, src_off = a.w.head->src_off;
     for (int i = rank * kBookThreads + threadIdx.x; i < moved; i += blocks * kBookThreads) {
         const int src = a.w.list[src_off + i], dst = a.w.dst[i];
@@ -409,7 +480,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const CompactA
         b.ref[dst] = b.ref[src];
         b.ref[src] = 0;
     }
-    cluster.sync();
+    book_sync(cluster);
     for (int s = warp; s < b.n_seq; s += warps) {
         const int n = pages_of(checked_len(b, b.len[s]), b.ps);
         int32_t *row = b.table + static_cast<int64_t>(s) * b.width;
@@ -535,15 +606,12 @@ __global__ void __launch_bounds__(kCopyThreads) write_kernel(const WriteArgs a) 
 }
 
 // ---------------------------------------------------------------- host
-int cluster_blocks(int64_t n_seq, int64_t width, int64_t n_pages) {
-    (void)n_seq, (void)width, (void)n_pages;
-    return kCluster;
-}
-
+// One block while each of its threads has a few entries, else a cluster of eight.
 template <typename Args>
 rps_status launch_book(void (*kernel)(Args), const Args &a, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    const int blocks = cluster_blocks(a.b.n_seq, a.b.width, a.b.n_pages);
+    const int64_t entries = static_cast<int64_t>(a.b.n_seq) * a.b.width + a.b.n_pages;
+    const int blocks = entries <= kOneBlock ? 1 : kCluster;
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(kBookThreads);
     cfg.stream = stream;
@@ -648,18 +716,21 @@ rps_status launch_copy(const rps_kv_cache *from, const rps_kv_cache *to, const i
                : RPS_ERR_CUDA;
 }
 
-rps_status launch_reorder(const rps_kv_cache *kv, const int32_t *src_of, const int32_t *keep, const uint8_t *valid,
-                          const int32_t *winner, void *d_ws, size_t ws_bytes, cudaStream_t stream) {
-    ReorderArgs a;
+rps_status launch_branches(const rps_kv_cache *kv, const uint8_t *valid, const int32_t *ctx, const int32_t *winner,
+                           void *d_ws, size_t ws_bytes, cudaStream_t stream) {
+    BranchArgs a;
     std::memset(&a, 0, sizeof a);
-    const rps_status st = prepare(kv, d_ws, ws_bytes, &a.b, &a.w);
+    KvWorkspace w;  // (taken and checked like the other calls', not used)
+    const rps_status st = prepare(kv, d_ws, ws_bytes, &a.b, &w);
     if (st != RPS_OK) return st;
-    a.src_of = src_of;
-    a.keep = keep;
     a.valid = valid;
+    a.ctx = ctx;
     a.winner = winner;
     a.n_branch = kv->n_branch;
-    return launch_book(reorder_kernel, a, stream);
+    const int per = kBranchThreads / 32;
+    return launch_pdl(branch_kernel, dim3((a.b.n_seq + per - 1) / per), dim3(kBranchThreads), 0, stream, a) == cudaSuccess
+               ? RPS_OK
+               : RPS_ERR_CUDA;
 }
 
 }  // namespace
@@ -681,20 +752,25 @@ size_t rps_kv_workspace_bytes(const rps_kv_cache *kv) {
 rps_status rps_kv_reorder(const rps_kv_cache *kv, const int32_t *d_src, const int32_t *d_keep, void *d_ws,
                           size_t ws_bytes, rps_stream_t stream) {
     if (!d_src) return RPS_ERR_INVALID_ARG;
-    return launch_reorder(kv, d_src, d_keep, nullptr, nullptr, d_ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+    ReorderArgs a;
+    std::memset(&a, 0, sizeof a);
+    const rps_status st = prepare(kv, d_ws, ws_bytes, &a.b, &a.w);
+    if (st != RPS_OK) return st;
+    a.src_of = d_src;
+    a.keep = d_keep;
+    return launch_book(reorder_kernel, a, reinterpret_cast<cudaStream_t>(stream));
 }
 
 rps_status rps_kv_fork_branches(const rps_kv_cache *kv, const uint8_t *d_branch_valid, const int32_t *d_ctx_len,
                                 void *d_ws, size_t ws_bytes, rps_stream_t stream) {
     if (!d_branch_valid || !kv || kv->n_branch < 2) return RPS_ERR_INVALID_ARG;
-    return launch_reorder(kv, nullptr, d_ctx_len, d_branch_valid, nullptr, d_ws, ws_bytes,
-                          reinterpret_cast<cudaStream_t>(stream));
+    return launch_branches(kv, d_branch_valid, d_ctx_len, nullptr, d_ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
 }
 
 rps_status rps_kv_commit(const rps_kv_cache *kv, const int32_t *d_winner, void *d_ws, size_t ws_bytes,
                          rps_stream_t stream) {
     if (!d_winner) return RPS_ERR_INVALID_ARG;
-    return launch_reorder(kv, nullptr, nullptr, nullptr, d_winner, d_ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+    return launch_branches(kv, nullptr, nullptr, d_winner, d_ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
 }
 
 rps_status rps_kv_resize(const rps_kv_cache *kv, const int32_t *d_new_len, void *d_ws, size_t ws_bytes,

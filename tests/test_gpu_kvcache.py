@@ -114,6 +114,7 @@ class Pair:
     (3, 50, 2, 64, 4, 3, 4, torch.float16, False),
     (1, 30, 1, 256, 5, 2, 3, torch.bfloat16, True),
     (1, 700, 1, 16, 37, 9, 7, torch.bfloat16, False),   # 333 sequences: more than a block has warps
+    (1, 3000, 1, 16, 60, 9, 12, torch.float16, False),  # a cluster's share for each of its blocks
 ])
 def test_random_runs(layers, pages, heads, ps, n_req, nb, width, dtype, tokens_first):
     p = Pair(7, layers, pages, heads, ps, n_req, nb, width, dtype, tokens_first)
@@ -137,6 +138,15 @@ def test_random_runs(layers, pages, heads, ps, n_req, nb, width, dtype, tokens_f
             p.write(int(rng.integers(0, layers)), int(rng.integers(1, 2 * ps // 3)), bool(rng.integers(0, 2)))
         else:
             p.compact()
+
+
+def test_more_sequences_than_fit_a_blocks_shared_memory():
+    p = Pair(17, 1, 6000, 1, 16, 3000, 3, 2)
+    rng = np.random.default_rng(18)
+    p.resize(rng.integers(-1, 12, 9000))
+    p.resize(np.where(p.o.length < 6, -1, p.o.length + 9))
+    p.commit(rng.integers(-1, 2, 3000))
+    p.compact()
 
 
 def test_lookahead_cycle():
