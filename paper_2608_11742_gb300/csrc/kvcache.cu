@@ -36,7 +36,7 @@ constexpr size_t kWsAlign = 256;
 
 struct Book {
     int32_t *ref, *table, *len;
-    int32_t n_pages, n_seq, width, ps;  // width: table entries of a sequence
+    int32_t n_pages, n_seq, width, ps, log;  // width: table entries of a sequence; ps = 2^log tokens a page
     uint32_t *err;
 };
 
@@ -83,12 +83,12 @@ size_t ws_layout(int64_t n_pages, int64_t n_seq, int64_t width, char *base, KvWo
 }
 
 // ---------------------------------------------------------------- bookkeeping
-__device__ __forceinline__ int pages_of(int len, int ps) { return len <= 0 ? 0 : (len - 1) / ps + 1; }
+__device__ __forceinline__ int pages_of(const Book &b, int len) { return len <= 0 ? 0 : ((len - 1) >> b.log) + 1; }
 
 // A sequence's length as it may be used: at most what its table row holds.
 __device__ __forceinline__ int checked_len(const Book &b, int len) {
     if (len <= 0) return len < 0 ? -1 : 0;
-    if (pages_of(len, b.ps) > b.width) {
+    if (pages_of(b, len) > b.width) {
         flag_error(b.err, RPS_DEVERR_PAGE);
         return b.width * b.ps;
     }
@@ -140,10 +140,10 @@ __global__ void __launch_bounds__(kBookThreads, 1) reorder_kernel(const ReorderA
     for (int s = warp; s < b.n_seq; s += warps) {
         int src, keep;
         source_of(a, s, src, keep);
-        const int old_n = pages_of(checked_len(b, b.len[s]), b.ps);
+        const int old_n = pages_of(b, checked_len(b, b.len[s]));
         int len = src < 0 ? -1 : checked_len(b, b.len[src]);
         if (keep < len) len = keep < 0 ? -1 : keep;
-        const int n = pages_of(len, b.ps);
+        const int n = pages_of(b, len);
         const int32_t *own = b.table + static_cast<int64_t>(s) * b.width;
         for (int i = (src == s ? n : 0) + lane; i < old_n; i += 32)
             if (good_page(b, own[i])) atomicSub(&b.ref[own[i]], 1);
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) reorder_kernel(const ReorderA
     for (int s = warp; s < b.n_seq; s += warps) {
         int src, keep;
         source_of(a, s, src, keep);
-        const int len = a.w.snap_len[s], n = pages_of(len, b.ps);
+        const int len = a.w.snap_len[s], n = pages_of(b, len);
         int32_t *own = b.table + static_cast<int64_t>(s) * b.width;
         if (src != s) {
             const int32_t *from = a.w.snap + static_cast<int64_t>(s) * b.width;
@@ -211,11 +211,11 @@ __global__ void __launch_bounds__(kBranchThreads) branch_kernel(const BranchArgs
         src = s - br;
         if (a.ctx) keep = a.ctx[q];
     }
-    const int old_n = pages_of(checked_len(b, old_len), b.ps);
+    const int old_n = pages_of(b, checked_len(b, old_len));
     int32_t *from = b.table + static_cast<int64_t>(src) * b.width;
     int len = src < 0 ? -1 : checked_len(b, src == s ? old_len : b.len[src]);
     if (keep < len) len = keep < 0 ? -1 : keep;
-    const int n = pages_of(len, b.ps), most = max(n, old_n);
+    const int n = pages_of(b, len), most = max(n, old_n);
     if (src != s) {
         for (int i = lane; i < most; i += 32) {
             const int was = i < old_n ? own[i] : -1, is = i < n ? from[i] : -1;
@@ -267,6 +267,7 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
 
 constexpr int kNearSeqs = 1024;   // sequences of a block whose wishes fit shared memory
 constexpr int kNearPages = 4096;  // free pages that do
+constexpr int kFewPages = 4;      // pages that a thread hands out alone
 
 struct Counts {
     unsigned long long need;  // of the block's sequences: pages (low 32 bits), copies (high)
@@ -280,14 +281,14 @@ struct ResizeArgs {
 };
 
 // What a sequence asks for: pages wanted in the low 32 bits, 1 << 32 where its
-// shared last page has to be copied first.
-__device__ __forceinline__ unsigned long long wanted(const Book &b, int s, int old_len, int new_len) {
+// shared last page (in `last` then) has to be copied first.
+__device__ __forceinline__ unsigned long long wanted(const Book &b, int s, int old_len, int new_len, int &last) {
     if (new_len <= old_len) return 0;
-    const int n_old = pages_of(old_len, b.ps);
-    unsigned long long need = static_cast<unsigned>(pages_of(new_len, b.ps) - n_old);
-    if (old_len > 0 && old_len % b.ps) {
-        const int p = b.table[static_cast<int64_t>(s) * b.width + n_old - 1];
-        if (good_page(b, p) && b.ref[p] > 1) need += (1ull << 32) + 1;
+    const int n_old = pages_of(b, old_len);
+    unsigned long long need = static_cast<unsigned>(pages_of(b, new_len) - n_old);
+    if (old_len > 0 && (old_len & (b.ps - 1))) {
+        last = b.table[static_cast<int64_t>(s) * b.width + n_old - 1];
+        if (good_page(b, last) && b.ref[last] > 1) need += (1ull << 32) + 1;
     }
     return need;
 }
@@ -295,55 +296,81 @@ __device__ __forceinline__ unsigned long long wanted(const Book &b, int s, int o
 // The length a sequence is to have: one beyond its table row leaves it as it is.
 __device__ __forceinline__ int wanted_len(const Book &b, int new_len, int old_len) {
     if (new_len < 0) return -1;
-    if (pages_of(new_len, b.ps) > b.width) {
+    if (pages_of(b, new_len) > b.width) {
         flag_error(b.err, RPS_DEVERR_PAGE);
         return old_len;
     }
     return new_len;
 }
 
+// A sequence of the block: length at first, length it is to have, the last page that it held.
+struct Near {
+    int32_t old_len, new_len, last;
+};
+
 __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArgs a) {
     cg::cluster_group cluster = cg::this_cluster();
     __shared__ unsigned long long sums[kBookWarps];
     __shared__ Counts mine;
     __shared__ unsigned long long near_need[kNearSeqs];
+    __shared__ Near near_seq[kNearSeqs];
     __shared__ int32_t near_list[kNearPages];
     const Book &b = a.b;
     const int lane = threadIdx.x & 31, rank = cluster.block_rank(), blocks = cluster.num_blocks();
-    const int warp = rank * kBookWarps + (threadIdx.x >> 5), warps = blocks * kBookWarps;
-    pdl_wait();
-    pdl_launch_next();
-    // 1. pages past a shorter sequence's end go back
-    for (int s = warp; s < b.n_seq; s += warps) {
-        const int old_len = checked_len(b, b.len[s]), new_len = wanted_len(b, a.new_len[s], old_len);
-        if (new_len >= old_len) continue;
-        int32_t *row = b.table + static_cast<int64_t>(s) * b.width;
-        const int n_old = pages_of(old_len, b.ps);
-        for (int i = pages_of(new_len, b.ps) + lane; i < n_old; i += 32) {
-            if (good_page(b, row[i])) atomicSub(&b.ref[row[i]], 1);
-            row[i] = -1;
-        }
-        __syncwarp();
-        if (lane == 0) b.len[s] = new_len;
-    }
-    book_sync(cluster);
-    // 2. what the block's sequences ask for, and the free ones of the block's pages (of a block
-    // alone they are counted as they are listed)
     const int per_s = (b.n_seq + blocks - 1) / blocks;
     const int s0 = min(b.n_seq, rank * per_s), s1 = min(b.n_seq, s0 + per_s);
     const int per_p = (b.n_pages + blocks - 1) / blocks;
     const int p0 = min(b.n_pages, rank * per_p), p1 = min(b.n_pages, p0 + per_p);
-    unsigned long long *need_of = per_s <= kNearSeqs ? near_need - s0 : a.w.need;
+    const bool near = per_s <= kNearSeqs;  // the block's sequences are kept in shared memory
+    pdl_wait();
+    pdl_launch_next();
+    const auto lengths = [&](int s) {
+        Near x;
+        x.old_len = checked_len(b, b.len[s]);
+        x.new_len = wanted_len(b, a.new_len[s], x.old_len);
+        x.last = -1;
+        return x;
+    };
+    // 1. pages past a shorter sequence's end go back
+    for (int at = s0; at < s1; at += kBookThreads) {
+        const int s = at + threadIdx.x;
+        Near x{0, 0, -1};
+        if (s < s1) {
+            x = lengths(s);
+            if (near) near_seq[s - s0] = x;
+        }
+        for (uint32_t m = __ballot_sync(kFull, x.new_len < x.old_len); m; m &= m - 1) {  // a warp for each of its threads'
+            const int who = __ffs(m) - 1;
+            const int n_old = pages_of(b, __shfl_sync(kFull, x.old_len, who));
+            const int n_new = pages_of(b, __shfl_sync(kFull, x.new_len, who));
+            int32_t *row = b.table + static_cast<int64_t>(s - lane + who) * b.width;
+            for (int i = n_new + lane; i < n_old; i += 32) {
+                if (good_page(b, row[i])) atomicSub(&b.ref[row[i]], 1);
+                row[i] = -1;
+            }
+        }
+        if (x.new_len < x.old_len) {
+            b.len[s] = x.new_len;
+            if (near) near_seq[s - s0].old_len = x.new_len;
+        }
+    }
+    book_sync(cluster);
+    // 2. what the block's sequences ask for, and the free ones of the block's pages (of a block
+    // alone they are counted as they are listed)
     unsigned long long carry = 0, total;
     for (int at = s0; at < s1; at += kBookThreads) {
         const int s = at + threadIdx.x;
         unsigned long long need = 0;
+        int last = -1;
         if (s < s1) {
-            const int old_len = checked_len(b, b.len[s]);
-            need = wanted(b, s, old_len, wanted_len(b, a.new_len[s], old_len));
+            const Near x = near ? near_seq[s - s0] : lengths(s);
+            need = wanted(b, s, x.old_len, x.new_len, last);
         }
         const unsigned long long upto = block_scan(need, sums, &total);
-        if (s < s1) need_of[s] = carry + upto - need;
+        if (s < s1) {
+            (near ? near_need[s - s0] : a.w.need[s]) = carry + upto - need;
+            if (near) near_seq[s - s0].last = last;
+        }
         carry += total;
     }
     unsigned long long need_before = 0, need_all = carry;
@@ -368,48 +395,69 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArg
             free_all += c->pages;
         }
     }
-    // 3. the lowest free pages, in order, as many as are asked for
+    // 3. the lowest free pages, in order, as many as are asked for; a thread takes four neighbours
     const int wish = static_cast<int>(min(need_all & 0xffffffffull, static_cast<unsigned long long>(INT32_MAX)));
     int32_t *list = blocks == 1 && wish <= kNearPages ? near_list : a.w.list;
-    for (int at = p0; at < p1 && free_before < wish; at += kBookThreads) {
-        const int p = at + threadIdx.x;
-        const unsigned long long is_free = p < p1 && b.ref[p] <= 0;
-        const unsigned long long upto = block_scan(is_free, sums, &total);
-        const int at_list = free_before + static_cast<int>(upto) - 1;
-        if (is_free && at_list < wish) list[at_list] = p;
+    for (int at = p0; at < p1 && free_before < wish; at += 4 * kBookThreads) {
+        const int p = at + 4 * threadIdx.x;
+        uint32_t is_free = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (p + i < p1 && b.ref[p + i] <= 0) is_free |= 1u << i;
+        const int count = __popc(is_free);
+        int to = free_before + static_cast<int>(block_scan(count, sums, &total)) - count;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (is_free >> i & 1u) {
+                if (to < wish) list[to] = p + i;
+                ++to;
+            }
         free_before += static_cast<int>(total);
     }
     if (blocks == 1) free_all = free_before;  // (all that there are, or as many as are asked for)
     book_sync(cluster);  // (the list is written, and every block has read every count)
-    // 4. each sequence takes its pages; the copy list
-    for (int s = s0 + (threadIdx.x >> 5); s < s1; s += kBookWarps) {
-        const int old_len = checked_len(b, b.len[s]), new_len = wanted_len(b, a.new_len[s], old_len);
-        if (new_len <= old_len) continue;
-        // (counts of pages change while this phase runs: what is wanted is the difference to the next sequence)
-        const unsigned long long off = need_before + need_of[s];
-        const unsigned long long next = s + 1 < s1 ? need_before + need_of[s + 1] : need_before + carry;
-        const bool cow = (next >> 32) != (off >> 32);
-        const bool fits = (next & 0xffffffffull) <= static_cast<unsigned long long>(free_all);
-        if (!fits) flag_error(b.err, RPS_DEVERR_NO_PAGES);
-        int32_t *row = b.table + static_cast<int64_t>(s) * b.width;
-        const int n_old = pages_of(old_len, b.ps), n_new = pages_of(new_len, b.ps);
-        if (cow && lane == 0) {
-            const int e = static_cast<int>(off >> 32), p = row[n_old - 1];
-            a.w.src[e] = fits ? p : -1;
-            a.w.dst[e] = fits ? list[off & 0xffffffffull] : -1;
-            a.w.used[e] = old_len % b.ps;
-            if (fits) atomicSub(&b.ref[p], 1);
+    // 4. each sequence takes its pages, a thread's own where they are few; the copy list
+    for (int at = s0; at < s1; at += kBookThreads) {
+        const int s = at + threadIdx.x;
+        int first = 0, count = 0;  // table entries that take pages
+        int64_t from = 0;          // their first page in the list
+        Near x{0, 0, -1};
+        if (s < s1) x = near ? near_seq[s - s0] : lengths(s);
+        if (x.new_len > x.old_len) {
+            // (counts of pages change while this phase runs: what is wanted is the difference to the next sequence)
+            const auto need_of = [&](int i) { return need_before + (i >= s1 ? carry : near ? near_need[i - s0] : a.w.need[i]); };
+            const unsigned long long off = need_of(s), next = need_of(s + 1);
+            const bool cow = (next >> 32) != (off >> 32);
+            const bool fits = (next & 0xffffffffull) <= static_cast<unsigned long long>(free_all);
+            const int n_old = pages_of(b, x.old_len);
+            from = static_cast<int64_t>(off & 0xffffffffull);
+            if (!fits) flag_error(b.err, RPS_DEVERR_NO_PAGES);
+            if (cow) {
+                const int e = static_cast<int>(off >> 32);
+                if (!near) x.last = b.table[static_cast<int64_t>(s) * b.width + n_old - 1];
+                a.w.src[e] = fits ? x.last : -1;
+                a.w.dst[e] = fits ? list[from] : -1;
+                a.w.used[e] = x.old_len & (b.ps - 1);
+                if (fits) atomicSub(&b.ref[x.last], 1);
+            }
+            if (fits) {
+                first = n_old - (cow ? 1 : 0);
+                count = pages_of(b, x.new_len) - first;
+                b.len[s] = x.new_len;
+            }
         }
-        __syncwarp();
-        if (!fits) continue;
-        const int first = n_old - (cow ? 1 : 0);
-        for (int i = first + lane; i < n_new; i += 32) {
-            const int p = list[(off & 0xffffffffull) + static_cast<unsigned>(i - first)];
-            row[i] = p;
+        const auto take = [&](int seq, int entry, int64_t i) {
+            const int p = list[i];
+            b.table[static_cast<int64_t>(seq) * b.width + entry] = p;
             b.ref[p] = 1;
+        };
+        if (count <= kFewPages)
+            for (int i = 0; i < count; ++i) take(s, first + i, from + i);
+        for (uint32_t m = __ballot_sync(kFull, count > kFewPages); m; m &= m - 1) {  // more: the warp together
+            const int who = __ffs(m) - 1, n = __shfl_sync(kFull, count, who), f = __shfl_sync(kFull, first, who);
+            const int64_t l = __shfl_sync(kFull, from, who);
+            for (int i = lane; i < n; i += 32) take(s - lane + who, f + i, l + i);
         }
-        __syncwarp();
-        if (lane == 0) b.len[s] = new_len;
     }
     if (rank == 0 && threadIdx.x == 0) {
         a.w.head->count = static_cast<int32_t>(need_all >> 32);
@@ -482,7 +530,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const CompactA
     }
     book_sync(cluster);
     for (int s = warp; s < b.n_seq; s += warps) {
-        const int n = pages_of(checked_len(b, b.len[s]), b.ps);
+        const int n = pages_of(b, checked_len(b, b.len[s]));
         int32_t *row = b.table + static_cast<int64_t>(s) * b.width;
         for (int i = lane; i < n; i += 32) {
             const int p = row[i];
@@ -508,7 +556,7 @@ struct CopyArgs {
 
 // A warp copies up to 16 rows (a token of a head each, 256 bytes) at a time,
 // half a warp to a row.
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const CopyArgs a) {
+__global__ void __launch_bounds__(kCopyThreads, 3) copy_kernel(const CopyArgs a) {
     const int lane = threadIdx.x & 31;
     pdl_wait();
     pdl_launch_next();
@@ -520,6 +568,17 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const CopyArgs a) {
     int e = static_cast<int>(task / per), t = static_cast<int>(task - static_cast<int64_t>(e) * per);
     const int64_t step_e = step / per;
     const int step_t = static_cast<int>(step - step_e * per);
+    // (the entry of the next task is on its way while a task's rows are)
+    const auto entry = [&](int64_t i, int &src, int &dst, int &used) {
+        src = dst = -1;
+        used = 0;
+        if (i >= count) return;
+        src = a.src[src_off + i];
+        dst = a.dst[i];
+        used = a.used ? a.used[i] : a.ps;
+    };
+    int src, dst, used;
+    entry(e, src, dst, used);
     for (int64_t ee = e; ee < count;) {
         int x = t, head, block;
         if (a.heads_inner) {
@@ -530,31 +589,30 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const CopyArgs a) {
             head = x % a.heads, x /= a.heads;
         }
         const int which = x & 1, layer = x >> 1;
-        const int src = a.src[src_off + ee], dst = a.dst[ee];
-        const int rows = min(kTaskRows, (a.used ? a.used[ee] : a.ps) - block * kTaskRows);
+        const int rows = min(kTaskRows, used - block * kTaskRows);
         const bool skip = a.used && src < 0;  // (a copy that found no page)
         const bool ok = static_cast<unsigned>(src) < static_cast<unsigned>(a.n_from) &&
-                        static_cast<unsigned>(dst) < static_cast<unsigned>(a.n_to);
-        if (!ok && !skip) flag_error(a.err, RPS_DEVERR_PAGE);
-        if (ok && rows > 0) {
-            const uint4 *s = (which ? a.from.v : a.from.k) + layer * a.from.layer + src * a.from.page +
-                             head * a.from.head + (block * kTaskRows + (lane >> 4)) * a.from.token + (lane & 15);
-            uint4 *d = (which ? a.to.v : a.to.k) + layer * a.to.layer + dst * a.to.page + head * a.to.head +
-                       (block * kTaskRows + (lane >> 4)) * a.to.token + (lane & 15);
-            uint4 v[kTaskRows / 2];
+                        static_cast<unsigned>(dst) < static_cast<unsigned>(a.n_to) && rows > 0;
+        if (!ok && !skip && rows > 0) flag_error(a.err, RPS_DEVERR_PAGE);
+        const int row0 = block * kTaskRows + (lane >> 4);
+        const uint4 *s = (which ? a.from.v : a.from.k) + layer * a.from.layer + src * a.from.page + head * a.from.head +
+                         row0 * a.from.token + (lane & 15);
+        uint4 *d = (which ? a.to.v : a.to.k) + layer * a.to.layer + dst * a.to.page + head * a.to.head +
+                   row0 * a.to.token + (lane & 15);
+        uint4 v[kTaskRows / 2];
 #pragma unroll
-            for (int i = 0; i < kTaskRows / 2; ++i)
-                if (2 * i + (lane >> 4) < rows) v[i] = __ldcs(s + 2 * i * a.from.token);
-#pragma unroll
-            for (int i = 0; i < kTaskRows / 2; ++i)
-                if (2 * i + (lane >> 4) < rows) d[2 * i * a.to.token] = v[i];
-        }
+        for (int i = 0; i < kTaskRows / 2; ++i)
+            if (ok && 2 * i + (lane >> 4) < rows) v[i] = __ldcs(s + 2 * i * a.from.token);
         ee += step_e;
         t += step_t;
         if (t >= per) {
             t -= per;
             ++ee;
         }
+        entry(ee, src, dst, used);
+#pragma unroll
+        for (int i = 0; i < kTaskRows / 2; ++i)
+            if (ok && 2 * i + (lane >> 4) < rows) d[2 * i * a.to.token] = v[i];
     }
 }
 
@@ -584,7 +642,7 @@ __global__ void __launch_bounds__(kCopyThreads) write_kernel(const WriteArgs a) 
     const int len = checked_len(a.b, a.b.len[s]);
     if (len < 0) return;
     const int32_t *row = a.b.table + static_cast<int64_t>(s) * a.b.width;
-    const int log = __ffs(a.b.ps) - 1;  // (a power of two)
+    const int log = a.b.log;
     for (int i = threadIdx.x; i < toks; i += kCopyThreads) {
         const int pos = len - a.n_new + tok0 + i;
         int64_t at = -1;
@@ -623,11 +681,10 @@ __global__ void __launch_bounds__(kCopyThreads) write_kernel(const WriteArgs a) 
 }
 
 // ---------------------------------------------------------------- host
-// One block while each of its threads has a few entries, else a cluster of eight.
+// One block while that is enough (`entries`: what it goes through), else a cluster of eight.
 template <typename Args>
-rps_status launch_book(void (*kernel)(Args), const Args &a, cudaStream_t stream) {
+rps_status launch_book(void (*kernel)(Args), const Args &a, int64_t entries, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    const int64_t entries = static_cast<int64_t>(a.b.n_seq) * a.b.width + a.b.n_pages;
     const int blocks = entries <= kOneBlock ? 1 : kCluster;
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(kBookThreads);
@@ -678,6 +735,8 @@ rps_status check_cache(const rps_kv_cache *kv, Book *b) {
         b->n_seq = static_cast<int32_t>(n_seq);
         b->width = kv->max_pages;
         b->ps = kv->page_size;
+        b->log = 0;
+        while ((1 << b->log) < b->ps) ++b->log;
         b->err = nullptr;
     }
     return RPS_OK;
@@ -775,7 +834,7 @@ rps_status rps_kv_reorder(const rps_kv_cache *kv, const int32_t *d_src, const in
     if (st != RPS_OK) return st;
     a.src_of = d_src;
     a.keep = d_keep;
-    return launch_book(reorder_kernel, a, reinterpret_cast<cudaStream_t>(stream));
+    return launch_book(reorder_kernel, a, static_cast<int64_t>(a.b.n_seq) * a.b.width, reinterpret_cast<cudaStream_t>(stream));
 }
 
 rps_status rps_kv_fork_branches(const rps_kv_cache *kv, const uint8_t *d_branch_valid, const int32_t *d_ctx_len,
@@ -799,7 +858,7 @@ rps_status rps_kv_resize(const rps_kv_cache *kv, const int32_t *d_new_len, void 
     if (st != RPS_OK) return st;
     a.new_len = d_new_len;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if ((st = launch_book(resize_kernel, a, s)) != RPS_OK) return st;
+    if ((st = launch_book(resize_kernel, a, std::max(8 * a.b.n_seq, a.b.n_pages), s)) != RPS_OK) return st;
     return launch_copy(kv, kv, a.w.src, a.w.dst, a.w.used, a.w.head, 0, a.b.n_seq, a.b.err, s);
 }
 
@@ -810,7 +869,7 @@ rps_status rps_kv_compact(const rps_kv_cache *kv, int32_t *d_n_live, void *d_ws,
     if (st != RPS_OK) return st;
     a.n_live = d_n_live;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if ((st = launch_book(compact_kernel, a, s)) != RPS_OK) return st;
+    if ((st = launch_book(compact_kernel, a, static_cast<int64_t>(a.b.n_seq) * a.b.width + a.b.n_pages, s)) != RPS_OK) return st;
     return launch_copy(kv, kv, a.w.list, a.w.dst, nullptr, a.w.head, 0, (static_cast<int64_t>(kv->n_pages) + 1) / 2,
                        a.b.err, s);
 }
