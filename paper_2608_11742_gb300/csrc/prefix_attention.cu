@@ -128,6 +128,7 @@ struct Ctl {
     // step), and kStepAdds unless it overwrites
     uint4 step_off[kStages][8];
     int32_t step_how[kStages][8];
+    int2 slot_at[2][8];  // a producer's slots: page, first token
     uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
     int32_t len[kStagedLens];
@@ -160,6 +161,19 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl &c
     if (__all_sync(kFull, ok)) return true;
     *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
     return false;
+}
+
+// One thread of the converged warp, known to the compiler as one.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+// Waits for what is in flight when a role ends, a fifth of a second at most.
+__device__ __forceinline__ void drain(uint64_t *bar, uint32_t parity) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < 200000 && !try_wait_us(bar, parity); ++i) {
+    }
 }
 
 // ---------------------------------------------------------------- the cut
@@ -264,6 +278,7 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
 // By a warp: the request, head, row tile and key tile that the range begins with.
 struct Start {
     int32_t q, head, rt, j;
+    int32_t tiles, next;  // key tiles of the row tile and of the next of the head (0: none, or not known)
 };
 __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &range, const int64_t *first, int lane,
                                             const Ctl &c) {
@@ -306,6 +321,8 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &ra
                     const int who = __ffs(in) - 1;
                     st.rt = base + who;
                     st.j = static_cast<int>(rem - before) - __shfl_sync(kFull, upto - t, who);
+                    st.tiles = __shfl_sync(kFull, t, who);
+                    st.next = who < 31 ? __shfl_sync(kFull, t, who + 1) : 0;
                     break;
                 }
             }
@@ -388,29 +405,21 @@ __device__ __forceinline__ void release_piece(int n, int lane, Ctl &c) {
     if (lane == 0) mbar_arrive(&c.ring_empty[n % kRing]);
 }
 
-// The page (id, and first token in it) of slot `lane` of key tile j; an id outside
-// the cache gives n_pages, whose copy is all zeros. `there`: the tile has that slot.
-__device__ __forceinline__ void slot_page(const PrefixArgs &a, const Piece &p, int j, int lane, int &page, int &token,
-                                          bool &there) {
-    int row, x;
-    page = a.s.n_pages;
-    token = 0;
-    if (j < p.shared_tiles) {
-        x = (j << a.s.spt_log) + lane;
-        there = x < p.shared;
-        row = p.shared_row;
-    } else {
-        const int o = ((j - p.shared_tiles) << a.s.spt_log) + lane;
-        there = o < p.off[p.r.nb];
-        const int i = there ? prefix::slot_owner(p.off, p.r.nb, o) : 0;
-        x = o - p.off[i] + p.shared;
+// The page id (as the table has it: the load is on its way) of slot `lane` of key tile j and the
+// slot's first token in the page; false: the tile has no such slot.
+__device__ __forceinline__ bool slot_page(const PrefixArgs &a, const Piece &p, int j, int lane, int2 &at) {
+    int row = p.shared_row, x, i = 0;
+    const bool own = j >= p.shared_tiles;
+    x = ((own ? j - p.shared_tiles : j) << a.s.spt_log) + lane;
+    if (lane >= a.s.spt || x >= (own ? p.off[p.r.nb] : p.shared)) return false;
+    if (own) {
+        i = prefix::slot_owner(p.off, p.r.nb, x);
+        x += p.shared - p.off[i];
         row = p.q * a.s.n_branch + p.r.b0 + i;
     }
-    if (!there) return;
-    const int e = x >> a.s.sub_log;
-    token = (x & (a.s.sub - 1)) << a.s.slot_log;
-    page = a.table[static_cast<int64_t>(row) * a.s.max_pages + e];
-    if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.s.n_pages)) page = a.s.n_pages;
+    at = make_int2(a.table[static_cast<int64_t>(row) * a.s.max_pages + (x >> a.s.sub_log)],
+                   (x & (a.s.sub - 1)) << a.s.slot_log);
+    return true;
 }
 
 // The producers of K (with Q) and of V, in one body: two warps run it.
@@ -431,23 +440,19 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
 #pragma unroll 1
         for (int j = p.j0; j < p.j1; ++j, ++t) {
             const int s = t % kStages;
-            int page = 0, token = 0;
-            bool there = false;
-            if (lane < a.s.spt) slot_page(a, p, j, lane, page, token, there);
+            int2 at = make_int2(a.s.n_pages, 0);
+            const bool there = slot_page(a, p, j, lane, at);
             if (t >= kStages && !(ok = warp_wait(&empty[s], (t / kStages - 1) & 1, c, a))) break;
+            // (an id outside the cache: n_pages, whose copy is all zeros, as are slots that are not there)
+            const bool bad_page = static_cast<unsigned>(at.x) >= static_cast<unsigned>(a.s.n_pages);
+            if (bad_page) at.x = a.s.n_pages;
+            if (lane < 8) c.slot_at[is_k][lane] = at;
             if (is_k) {
-                const uint32_t bad = __ballot_sync(kFull, there && page == a.s.n_pages);
+                const uint32_t bad = __ballot_sync(kFull, there && bad_page);
+                if (j == p.j0) ++n_q;
                 if (lane == 0) {
                     c.bad[t % 4] = bad;
                     if (bad) flag_error(a.err, RPS_DEVERR_PAGE);
-                    if (j == p.j0) {
-                        uint64_t *q_full = &c.q_full[n & 1];
-                        mbar_expect_tx(q_full, 2u * a.s.group * a.s.tokens * 128);
-                        uint8_t *dst = sq + (n & 1) * kTileBytes;
-                        tma_load_4d(dst, tm_q, 0, p.head * a.s.group, p.r.tok0, p.q, q_full);
-                        tma_load_4d(dst + kAtom, tm_q, 64, p.head * a.s.group, p.r.tok0, p.q, q_full);
-                        ++n_q;
-                    }
                 }
             }
             int keys = 0;
@@ -461,12 +466,22 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
             const uint32_t ragged = __ballot_sync(kFull, (keys & 31) > 0 && (keys & 31) < 16);
             uint64_t *bar = ragged ? &c.v_raw : &full[s];
             __syncwarp();  // (the steps are written before the arrival that hands them on)
-            if (lane == 0) mbar_expect_tx(bar, kTileBytes);
-            __syncwarp();
-            if (lane < a.s.spt) {  // (slots that are not there: zeros)
-                uint8_t *dst = stages + s * kTileBytes + lane * a.s.slot * 128;
-                tma_load_4d(dst, tm, 0, token, p.head, page, bar);
-                tma_load_4d(dst + kAtom, tm, 64, token, p.head, page, bar);
+            if (elect_one()) {  // (operands from shared memory: picked out of lanes a copy took a third longer)
+                mbar_expect_tx(bar, kTileBytes);
+                uint8_t *dst = stages + s * kTileBytes;
+#pragma unroll 1
+                for (int i = 0; i < a.s.spt; ++i, dst += a.s.slot * 128) {
+                    const int2 slot = c.slot_at[is_k][i];
+                    tma_load_4d(dst, tm, 0, slot.y, p.head, slot.x, bar);
+                    tma_load_4d(dst + kAtom, tm, 64, slot.y, p.head, slot.x, bar);
+                }
+                if (is_k && j == p.j0) {  // Q: its buffer's last user, piece n - 2, ended at tile t - 2 or before
+                    uint64_t *q_full = &c.q_full[n & 1];
+                    mbar_expect_tx(q_full, 2u * a.s.group * a.s.tokens * 128);
+                    dst = sq + (n & 1) * kTileBytes;
+                    tma_load_4d(dst, tm_q, 0, p.head * a.s.group, p.r.tok0, p.q, q_full);
+                    tma_load_4d(dst + kAtom, tm_q, 64, p.head * a.s.group, p.r.tok0, p.q, q_full);
+                }
             }
             __syncwarp();
             raw = ragged != 0;
@@ -491,13 +506,13 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
     }
     // every copy issued lands before the CTA leaves
     if (lane == 0) {
-        if (!ok && raw) wait_drain(&c.v_raw, n_ragged & 1);
+        if (!ok && raw) drain(&c.v_raw, n_ragged & 1);
 #pragma unroll 1
         for (uint32_t x = t > kStages ? t - kStages : 0; x < t + 2; ++x) {
             if (x < t)
-                wait_drain(&full[x % kStages], (x / kStages) & 1);
+                drain(&full[x % kStages], (x / kStages) & 1);
             else if (n_q > static_cast<int>(x - t))  // Q: the last two
-                wait_drain(&c.q_full[(n_q - 1 - (x - t)) & 1], ((n_q - 1 - (x - t)) >> 1) & 1);
+                drain(&c.q_full[(n_q - 1 - (x - t)) & 1], ((n_q - 1 - (x - t)) >> 1) & 1);
         }
     }
     __syncwarp();
@@ -513,11 +528,10 @@ __device__ __forceinline__ void schedule(const PrefixArgs &a, const Range &range
     // which L2 holds, instead of all over them (2 requests, 28/4 heads, context 28000: the keys
     // were read from HBM seven times).
     int turn = 1, cut_at = 0;
-    if (st.j > 0 && st.rt + 1 < a.s.row_tiles) {
-        const int t = lane < 2 ? entry_tiles(a, st.q, st.rt + lane, shared_len_of(a, st.q), c) : 0;
-        cut_at = __shfl_sync(kFull, t, 0) - st.j;  // tiles up to the next row tile
+    if (st.j > 0) {
+        cut_at = st.tiles - st.j;  // tiles up to the next row tile
         const int64_t rest = range.end - range.at - cut_at;
-        if (rest > 0 && rest < __shfl_sync(kFull, t, 1)) turn = 0;
+        if (rest > 0 && rest < st.next) turn = 0;
     }
     int n = 0;
 #pragma unroll 1
@@ -668,7 +682,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             }
         }
         commit(&c.mma_done);
-        wait_drain(&c.mma_done, 0);
+        drain(&c.mma_done, 0);
     }
     __syncwarp();
 }
@@ -882,26 +896,29 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
         const f2 ww0 = pack2(w0, w0), ww1 = pack2(w1, w1);
         const uint32_t at0 = col + (both ? 0 : only * 128), at1 = both ? col + 128 : at0;
 #pragma unroll 1
-        for (int it = 0; it < 2; ++it) {  // 64 columns at a time
+        for (int it = 0; it < 3; ++it) {  // 64 columns at a time; what was staged leaves a turn later
             uint32_t o[64], o1[64];
             uint32_t(&oa)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o[0]);
             uint32_t(&ob)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o[32]);
             uint32_t(&pa)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o1[0]);
             uint32_t(&pb)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o1[32]);
-            tmem_ld32_async(at0 + it * 64, oa);
-            tmem_ld32_async(at1 + it * 64, pa);
-            tmem_ld32_async(at0 + it * 64 + 32, ob);
-            tmem_ld32_async(at1 + it * 64 + 32, pb);
-            tmem_wait_dep(oa);
-            tmem_wait_dep(pa);
-            tmem_wait_dep(ob);
-            tmem_wait_dep(pb);
+            if (it < 2) {
+                tmem_ld32_async(at0 + it * 64, oa);
+                tmem_ld32_async(at1 + it * 64, pa);
+                tmem_ld32_async(at0 + it * 64 + 32, ob);
+                tmem_ld32_async(at1 + it * 64 + 32, pb);
+                tmem_wait_dep(oa);
+                tmem_wait_dep(pa);
+                tmem_wait_dep(ob);
+                tmem_wait_dep(pb);
+            }
             if (it == 1) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&c.o_free);  // O may take the next piece
-                if (whole) store_stage(stage, lane, row, 0);  // the first 64 columns
             }
+            if (it > 0 && whole) store_stage(stage, lane, row, (it - 1) * 128);
+            if (it == 2) break;
             if (zeros) {
 #pragma unroll
                 for (int i = 0; i < 64; ++i) {
@@ -934,7 +951,6 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
                 for (int i = 0; i < 32; ++i) o[i] = o[32 + i];
             }
         }
-        if (whole) store_stage(stage, lane, row, 128);
         if (lse) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
         if (!whole) a.part_ml[(2 * blockIdx.x + p.part) * prefix::kRows + r] = make_float2(m, l);
         t0 += count;

@@ -536,12 +536,13 @@ def rps_packed_attention_fwd(q: torch.Tensor, k: torch.Tensor, vt: torch.Tensor,
 _KV_DTYPES = {torch.bfloat16: RPS_BF16, torch.float16: RPS_F16}
 
 
-def _here(*tensors) -> None:
-    """The library launches on the current device: its tensors have to be there."""
+def _here(stream, *tensors) -> Optional[int]:
+    """The stream's handle. The library launches on the current device: the tensors have to be there."""
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors must be on the current CUDA device {dev}, got {t.device}")
+    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 _i32 = torch.int32
@@ -581,19 +582,19 @@ class KvCacheBuf:
         return KvCacheBuf(k, v)
 
     def _c(self) -> int:
-        """Address of the C struct, kept while the tensors, their addresses and their strides are the same (built
-        on each call, it took half of a call's time on the host)."""
+        """Address of the C struct, kept while the tensors, their addresses and the pages' strides are the
+        same (built on each call, it took half of a call's time on the host)."""
         k, v, ref, table, length = self.k, self.v, self.page_ref, self.table, self.length
         kept = self._kept
         if (kept is not None and kept[0] is k and kept[1] is v and kept[2] is ref and kept[3] is table
                 and kept[4] is length and kept[5] == (k.data_ptr(), v.data_ptr(), k.stride(), v.stride())
-                and (table is None or kept[6] == (ref.data_ptr(), table.data_ptr(), length.data_ptr(), table.shape))):
+                and (table is None or kept[6] == (ref.data_ptr(), table.data_ptr(), length.data_ptr()))):
             return self._at
         if k.dtype not in _KV_DTYPES or v.dtype != k.dtype:
             raise TypeError(f"k and v must both be bf16 or fp16, got {k.dtype} and {v.dtype}")
         if k.dim() != 5 or v.shape != k.shape or k.stride(4) != 1 or v.stride() != k.stride():
             raise ValueError("k and v: [layers][pages][heads][page size][head dim], head dim contiguous, same strides")
-        _here(k, v, ref, table, length)
+        _here(None, k, v, ref, table, length)
         n_layers, n_pages, n_heads, ps, d = k.shape
         n_req = n_branch = width = 0
         at = None
@@ -604,7 +605,7 @@ class KvCacheBuf:
             _ints("page_ref", ref, n_pages)
             _ints("table", table, n_req * n_branch * width)
             _ints("length", length, n_req * n_branch)
-            at = (ref.data_ptr(), table.data_ptr(), length.data_ptr(), table.shape)
+            at = (ref.data_ptr(), table.data_ptr(), length.data_ptr())
         self.n_req, self.n_branch, self.n_seq = n_req, n_branch, n_req * n_branch
         self._struct = RpsKvCache(k.data_ptr(), v.data_ptr(), _KV_DTYPES[k.dtype], n_layers, n_pages, n_heads, ps, d,
                                   *k.stride()[:4], _ptr(ref), _ptr(table), _ptr(length), n_req, n_branch, width)
@@ -623,62 +624,53 @@ def rps_kv_workspace_bytes(kv: KvCacheBuf) -> int:
     return n
 
 
-def _kv_ws(kv: KvCacheBuf, ws: torch.Tensor, *more):
-    at = kv._c()
-    _here(kv.k, ws, *more)
-    return at, ws.data_ptr(), ws.nbytes
-
-
 def rps_kv_reorder(kv: KvCacheBuf, src: torch.Tensor, ws: torch.Tensor, keep: Optional[torch.Tensor] = None,
                    stream=None) -> None:
     """Every sequence takes the state of sequence ``src[s]`` (-1: none), cut to ``keep[s]`` tokens."""
-    at, p, n = _kv_ws(kv, ws, src, keep)
+    at, st = kv._c(), _here(stream, kv.k, ws, src, keep)
     _check(_lib.rps_kv_reorder(at, _ints("src", src, kv.n_seq), None if keep is None else _ints("keep", keep, kv.n_seq),
-                               p, n, _stream(stream)), "rps_kv_reorder")
+                               ws.data_ptr(), ws.nbytes, st), "rps_kv_reorder")
 
 
 def rps_kv_fork_branches(kv: KvCacheBuf, branch_valid: torch.Tensor, ctx_len: Optional[torch.Tensor], ws: torch.Tensor,
                          stream=None) -> None:
     """The valid branches (``PivotsBuf.branch_valid``) take their request's base, cut to ``ctx_len[q]`` tokens."""
-    at, p, n = _kv_ws(kv, ws, branch_valid, ctx_len)
-    n_req, nb = kv.n_req, kv.n_branch
-    _check(_lib.rps_kv_fork_branches(at, _ints("branch_valid", branch_valid, n_req * (nb - 1), torch.uint8),
-                                     None if ctx_len is None else _ints("ctx_len", ctx_len, n_req), p, n,
-                                     _stream(stream)), "rps_kv_fork_branches")
+    at, st = kv._c(), _here(stream, kv.k, ws, branch_valid, ctx_len)
+    n_req = kv.n_req
+    _check(_lib.rps_kv_fork_branches(at, _ints("branch_valid", branch_valid, n_req * (kv.n_branch - 1), torch.uint8),
+                                     None if ctx_len is None else _ints("ctx_len", ctx_len, n_req), ws.data_ptr(),
+                                     ws.nbytes, st), "rps_kv_fork_branches")
 
 
 def rps_kv_commit(kv: KvCacheBuf, winner: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """Each base takes its winner's state (``CommitBuf.winner``); every branch gives its pages back."""
-    at, p, n = _kv_ws(kv, ws, winner)
-    _check(_lib.rps_kv_commit(at, _ints("winner", winner, kv.n_req), p, n, _stream(stream)), "rps_kv_commit")
+    at, st = kv._c(), _here(stream, kv.k, ws, winner)
+    _check(_lib.rps_kv_commit(at, _ints("winner", winner, kv.n_req), ws.data_ptr(), ws.nbytes, st), "rps_kv_commit")
 
 
 def rps_kv_resize(kv: KvCacheBuf, new_len: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """Every sequence becomes ``new_len[s]`` tokens long; a shared last page that grows is copied."""
-    at, p, n = _kv_ws(kv, ws, new_len)
-    _check(_lib.rps_kv_resize(at, _ints("new_len", new_len, kv.n_seq), p, n, _stream(stream)), "rps_kv_resize")
+    at, st = kv._c(), _here(stream, kv.k, ws, new_len)
+    _check(_lib.rps_kv_resize(at, _ints("new_len", new_len, kv.n_seq), ws.data_ptr(), ws.nbytes, st), "rps_kv_resize")
 
 
 def rps_kv_compact(kv: KvCacheBuf, n_live: Optional[torch.Tensor], ws: torch.Tensor, stream=None) -> None:
     """The live pages move to the lowest places; ``n_live`` (int32[1], optional) receives their number."""
-    at, p, n = _kv_ws(kv, ws, n_live)
-    _check(_lib.rps_kv_compact(at, None if n_live is None else _ints("n_live", n_live, 1), p, n, _stream(stream)),
+    at, st = kv._c(), _here(stream, kv.k, ws, n_live)
+    _check(_lib.rps_kv_compact(at, None if n_live is None else _ints("n_live", n_live, 1), ws.data_ptr(), ws.nbytes, st),
            "rps_kv_compact")
 
 
 def rps_kv_copy_pages(src_kv: KvCacheBuf, dst_kv: KvCacheBuf, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
     """Pages ``src[i]`` of one cache over pages ``dst[i]`` of another (or the same), every layer."""
-    a, b = src_kv._c(), dst_kv._c()
-    _here(src_kv.k, dst_kv.k, src, dst)
+    a, b, st = src_kv._c(), dst_kv._c(), _here(stream, src_kv.k, dst_kv.k, src, dst)
     n = src.numel()
-    _check(_lib.rps_kv_copy_pages(a, b, _ints("src", src, n), _ints("dst", dst, n), n, _stream(stream)),
-           "rps_kv_copy_pages")
+    _check(_lib.rps_kv_copy_pages(a, b, _ints("src", src, n), _ints("dst", dst, n), n, st), "rps_kv_copy_pages")
 
 
 def rps_kv_write(kv: KvCacheBuf, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, stream=None) -> None:
     """Keys and values ``[n_req][n_branch][n_new][n_heads][128]`` of each sequence's last ``n_new`` tokens."""
-    at = kv._c()
-    _here(kv.k, k_new, v_new)
+    at, handle = kv._c(), _here(stream, kv.k, k_new, v_new)
     n_req, nb = kv.n_req, kv.n_branch
     shape, st, kv_shape, dtype = k_new.shape, k_new.stride(), kv.k.shape, kv.k.dtype
     if (len(shape) != 5 or shape[0] != n_req or shape[1] != nb or shape[3] != kv_shape[2] or shape[4] != kv_shape[4]
@@ -689,7 +681,7 @@ def rps_kv_write(kv: KvCacheBuf, layer: int, k_new: torch.Tensor, v_new: torch.T
     if st[4] != 1 or v_new.stride() != st or (n_req > 1 and nb > 1 and st[0] != nb * st[1]):
         raise ValueError("k_new and v_new: head dim contiguous, the same strides, requests at n_branch sequences' stride")
     _check(_lib.rps_kv_write(at, layer, k_new.data_ptr(), v_new.data_ptr(), shape[2], st[1] if nb > 1 else st[0], st[2],
-                             st[3], _stream(stream)), "rps_kv_write")
+                             st[3], handle), "rps_kv_write")
 
 
 def rps_prefix_attention_workspace_bytes(kv: KvCacheBuf, n_q: int, n_heads: int) -> int:
@@ -717,8 +709,7 @@ def rps_prefix_attention_fwd(q: torch.Tensor, kv: KvCacheBuf, layer: int, out: t
     """Attention of the sequences' last ``n_q`` tokens over their cached keys: q, out
     ``[n_req][n_branch][n_q][n_heads][128]`` of the cache's dtype, lse (optional) fp32 ``[n_req][n_branch][n_q][n_heads]``;
     ``shared_len`` (int32 ``[n_req]`` or None): leading tokens whose pages a request's sequences hold in common."""
-    at = kv._c()
-    _here(kv.k, q, out, ws, shared_len, lse)
+    at, handle = kv._c(), _here(stream, kv.k, q, out, ws, shared_len, lse)
     n_req, nb = kv.n_req, kv.n_branch
     shape, dtype = q.shape, kv.k.dtype
     if len(shape) != 5 or shape[0] != n_req or shape[1] != nb or shape[4] != kv.k.shape[4] or out.shape != shape:
@@ -730,7 +721,7 @@ def rps_prefix_attention_fwd(q: torch.Tensor, kv: KvCacheBuf, layer: int, out: t
                            shape[2], shape[3], layer, 1 if causal else 0, *_token_strides("q", q),
                            *_token_strides("out", out),
                            None if shared_len is None else _ints("shared_len", shared_len, n_req), scale)
-    _check(_lib.rps_prefix_attention_fwd(C.addressof(a), at, ws.data_ptr(), ws.nbytes, _stream(stream)),
+    _check(_lib.rps_prefix_attention_fwd(C.addressof(a), at, ws.data_ptr(), ws.nbytes, handle),
            "rps_prefix_attention_fwd")
 
 

@@ -34,7 +34,7 @@ class Case:
     Everything that no query may see is NaN."""
 
     def __init__(self, seed, lens, shared, n_q, H, Hk, ps, dtype=torch.bfloat16, causal=False, layers=1, layer=0,
-                 tokens_first=False, growth=0.0, spare=3, scale=D ** -0.5):
+                 tokens_first=False, growth=0.0, spare=3, scale=D ** -0.5, wide=False):
         rng = np.random.default_rng(seed)
         lens = np.array(lens)
         self.lens, self.shared, self.n_q, self.H, self.causal, self.layer = lens, shared, n_q, H, causal, layer
@@ -42,6 +42,8 @@ class Case:
         n_req, nb = lens.shape
         pages = lambda n: 0 if n <= 0 else -(-int(n) // ps)
         width = max(1, max(pages(n) for n in lens.ravel())) + 1
+        if wide:  # a table for so many tokens that row tiles get two halves
+            width = max(width, -(-2560 * 128 // (ps * n_req * Hk * -(-nb * n_q // (128 // (H // Hk))))) + 16)
         table, count = np.full((n_req, nb, width), -1), 0
         for r in range(n_req):
             common = max(0, shared[r]) // ps if shared is not None else 0
@@ -143,14 +145,18 @@ CASES = {
     "many small row tiles": dict(lens=[[20 + (i * 7 + j) % 30 for j in range(3)] for i in range(60)], shared=[16] * 60,
                                  n_q=2, H=8, Hk=8, ps=16),
     "group of 128": dict(lens=[[77, 90]], shared=[64], n_q=2, H=128, Hk=1, ps=16),
+    "two halves and one, many heads": dict(lens=[[150, 140, 161, 133, 155], [260, 241, 250, 255, 245]], shared=[128, 240],
+                                           n_q=32, H=6, Hk=6, ps=16),
+    "sequences across the halves": dict(lens=[[400, 390, 380]], shared=[352], n_q=100, H=2, Hk=1, ps=32),
     "shared length beyond the sequences": dict(lens=[[100, 60, 250]], shared=[1000], n_q=3, H=2, Hk=2, ps=32),
 }
 
 
 @pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("name", list(CASES))
-def test_parity(name, causal):
-    c = Case(21, causal=causal, dtype=torch.float16 if len(name) % 2 else torch.bfloat16, **CASES[name])
+def test_parity(name, wide, causal):
+    c = Case(21, causal=causal, dtype=torch.float16 if len(name) % 2 else torch.bfloat16, wide=wide, **CASES[name])
     c.check(*c.run())
 
 
@@ -178,8 +184,24 @@ def test_causal_rows_longer_than_the_sequence():
     assert bool((out[0, 0, :19] == 0).all()) and bool(torch.isinf(lse[0, 0, :19]).all())
 
 
-def test_scores_that_grow_are_rescaled():
-    c = Case(24, [[700, 690]], [640], 4, 2, 1, 64, growth=1.0, scale=0.3)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("scale", [0.3, 3.0, 1e-4])
+def test_scores_that_grow_are_rescaled(dtype, scale):
+    """Scores far above and below the reference that a row starts with."""
+    c = Case(24, [[700, 690]], [640], 4, 2, 1, 64, dtype, growth=1.0, scale=scale)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_scores_that_are_all_far_below_zero(dtype):
+    """Every score about -1400 to -200 in base 2: a weight of 2^score would vanish."""
+    c = Case(31, [[300, 290]], [256], 4, 2, 1, 64, dtype)
+    c.q[..., 0], c.q[..., 1:] = 16.0, c.q[..., 1:] * 0.25
+    for name in ("k",):
+        x = getattr(c, name)
+        x[..., 0] = torch.where(torch.isnan(x[..., 0]), x[..., 0], -20.0 - 2.0 * torch.rand(x[..., 0].shape).to(dtype))
+    c.scale = 1.0
+    c.dq, c.kv.k = c.q.cuda(), c.k.cuda()
     c.check(*c.run())
 
 
