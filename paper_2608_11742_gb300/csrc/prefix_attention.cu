@@ -69,7 +69,7 @@ static_assert(128 * kCtlRegs + 256 * kSoftRegs + 128 * kOutRegs <= 512 * 128, "t
 constexpr uint32_t kTmemCols = 512;  // S buffers at columns 0 and 128, O at 256 and 384
 constexpr uint32_t kOCol = 256;
 constexpr int kRing = 4;             // pieces known ahead
-constexpr int kConsumers = 15;       // warps 0, 1, 2 and 4..15
+constexpr int kConsumers = 16;       // every warp
 constexpr int kMaxSeqs = 128;        // sequences with rows in one row tile
 constexpr int kMaxCtas = 160;
 constexpr int kStepAdds = 32;
@@ -116,7 +116,7 @@ struct Ctl {
     // s_full[t % 2]: S of tile t is computed and the product of tile t - 2 is done, so
     // K stage t % 2 is free, and Q of the pieces before t's. V stages have a commit of
     // their own. No wait sees a barrier two phases on: each waits for every phase in turn.
-    uint64_t q_full[kQBufs], k_full[kStages], v_full[kStages], v_empty[kStages], v_raw;
+    uint64_t q_full[kQBufs], k_full[kStages], v_full[kStages], v_empty[kStages], v_raw[kStages];
     uint64_t s_full[kStages], p_full[kStages], o_ready, o_free, mma_done;
     uint64_t ring_full[kRing], ring_empty[kRing];
     // a half's reference and sum of a row at the end of piece n, in slot n % 4: written before
@@ -124,7 +124,7 @@ struct Ctl {
     // piece n + 4, whose P needs the products of piece n + 2 and so the read-out of piece n + 1
     float2 ml[4][kStages][prefix::kRows];
     Piece ring[kRing];
-    // own tile in V stage s, from V's producer: rows that step kk leaves alone; its keys (0: no
+    // own tile in V stage s, from V's cleaner: rows that step kk leaves alone; its keys (0: no
     // step), and kStepAdds unless it overwrites
     uint4 step_off[kStages][8];
     int32_t step_how[kStages][8];
@@ -426,8 +426,9 @@ __device__ __forceinline__ bool slot_page(const PrefixArgs &a, const Piece &p, i
 __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const CUtensorMap *tm_q, uint8_t *stages,
                                         uint8_t *sq, uint32_t tiles, int lane, Ctl &c, const PrefixArgs &a) {
     uint32_t t = 0;
-    int n = 0, n_q = 0, n_ragged = 0;
-    bool ok = true, raw = false;
+    int n = 0, n_q = 0, raw0 = 0, raw1 = 0;  // V tiles of each stage that went to v_raw
+    uint32_t raw_last = 0;                   // bit s: the last of stage s did
+    bool ok = true;
     uint64_t *full = is_k ? c.k_full : c.v_full;
     // K: S of tile t - 2 is computed, so its stage is free, and at a piece's first tile the Q
     // buffer of piece n - 2, whose last tile is no later. V: the product of tile t - 2 is done.
@@ -455,17 +456,13 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
                     if (bad) flag_error(a.err, RPS_DEVERR_PAGE);
                 }
             }
-            int keys = 0;
-            if (!is_k && j >= p.shared_tiles && lane < 8) {
-                const prefix::Step st = prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane);
-                c.step_off[s][lane] = make_uint4(
-                    ~(low_bits(st.r1) & ~low_bits(st.r0)), ~(low_bits(st.r1 - 32) & ~low_bits(st.r0 - 32)),
-                    ~(low_bits(st.r1 - 64) & ~low_bits(st.r0 - 64)), ~(low_bits(st.r1 - 96) & ~low_bits(st.r0 - 96)));
-                c.step_how[s][lane] = keys = st.keys > 0 ? st.keys | (st.fresh ? 0 : kStepAdds) : 0;
-            }
-            const uint32_t ragged = __ballot_sync(kFull, (keys & 31) > 0 && (keys & 31) < 16);
-            uint64_t *bar = ragged ? &c.v_raw : &full[s];
-            __syncwarp();  // (the steps are written before the arrival that hands them on)
+            // (V of own tiles goes through the cleaner)
+            const bool raw = !is_k && j >= p.shared_tiles;
+            uint64_t *bar = raw ? &c.v_raw[s] : &full[s];
+            raw_last = (raw_last & ~(1u << s)) | (raw ? 1u << s : 0u);
+            raw0 += raw && s == 0;
+            raw1 += raw && s == 1;
+            __syncwarp();
             if (elect_one()) {  // (operands from shared memory: picked out of lanes a copy took a third longer)
                 mbar_expect_tx(bar, kTileBytes);
                 uint8_t *dst = stages + s * kTileBytes;
@@ -484,114 +481,165 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
                 }
             }
             __syncwarp();
-            raw = ragged != 0;
-            if (ragged) {  // rows of V past a sequence's last key: they may hold anything, and 0 * NaN would be added
-                if (!(ok = warp_wait(&c.v_raw, n_ragged & 1, c, a))) break;
-                ++n_ragged;
-                uint8_t *vb = stages + s * kTileBytes;
-#pragma unroll 1
-                for (uint32_t m = ragged; m; m &= m - 1) {
-                    const int kk = __ffs(m) - 1, filled = __shfl_sync(kFull, keys & 31, kk);
-#pragma unroll 1
-                    for (int y = lane; y < (16 - filled) * 16; y += 32)  // 8 16-byte units in each of two atoms
-                        st_shared_v4(saddr(vb + (y & 8 ? kAtom : 0) + (kk * 16 + filled + (y >> 4)) * 128 + (y & 7) * 16),
-                                     make_uint4(0, 0, 0, 0));
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&full[s]);
-            }
         }
         if (ok) release_piece(n, lane, c);
     }
     // every copy issued lands before the CTA leaves
     if (lane == 0) {
-        if (!ok && raw) drain(&c.v_raw, n_ragged & 1);
 #pragma unroll 1
-        for (uint32_t x = t > kStages ? t - kStages : 0; x < t + 2; ++x) {
-            if (x < t)
-                drain(&full[x % kStages], (x / kStages) & 1);
-            else if (n_q > static_cast<int>(x - t))  // Q: the last two
-                drain(&c.q_full[(n_q - 1 - (x - t)) & 1], ((n_q - 1 - (x - t)) >> 1) & 1);
+        for (uint32_t x = t > kStages ? t - kStages : 0; x < t; ++x) {
+            const int s = x % kStages;
+            if (raw_last >> s & 1u)
+                drain(&c.v_raw[s], ((s ? raw1 : raw0) - 1) & 1);
+            else
+                drain(&full[s], (x / kStages) & 1);
         }
+#pragma unroll 1
+        for (int x = n_q > kQBufs ? n_q - kQBufs : 0; x < n_q; ++x) drain(&c.q_full[x & 1], (x >> 1) & 1);
     }
     __syncwarp();
 }
 
-// The scheduler: the pieces of the CTA's range into the ring.
-__device__ __forceinline__ void schedule(const PrefixArgs &a, const Range &range, const int64_t *first, int lane, Ctl &c) {
-    const Start st = find_start(a, range, first, lane, c);
+// The cleaner of V, for own tiles: prepares the product's steps, and clears the rows of V past a
+// sequence's last key before the product may read the tile (they may hold anything, and 0 * NaN
+// would be added). A warp of its own, for the producer has the next tile's copies to issue meanwhile.
+__device__ __forceinline__ void clean(uint8_t *stages, uint32_t tiles, int lane, Ctl &c, const PrefixArgs &a) {
+    uint32_t t0 = 0;
+    int raw0 = 0, raw1 = 0;
+#pragma unroll 1
+    for (int n = 0; t0 < tiles; ++n) {
+        const Piece *pp = next_piece(n, c, a);
+        if (!pp) return;
+        const Piece &p = *pp;
+#pragma unroll 1
+        for (int j = max(p.j0, p.shared_tiles); j < p.j1; ++j) {
+            const int s = (t0 + j - p.j0) % kStages;
+            const prefix::Step st = prefix::own_step(a.s, p.r, p.off, p.len, p.shared_tiles, p.shared, p.j0, j, lane & 7);
+            const int keys = lane < 8 ? st.keys : 0;
+            // (the stage's copies were issued once the product before had read its steps)
+            if (!warp_wait(&c.v_raw[s], (s ? raw1 : raw0) & 1, c, a)) return;
+            raw0 += s == 0;
+            raw1 += s;
+            if (lane < 8) {
+                c.step_off[s][lane] = make_uint4(
+                    ~(low_bits(st.r1) & ~low_bits(st.r0)), ~(low_bits(st.r1 - 32) & ~low_bits(st.r0 - 32)),
+                    ~(low_bits(st.r1 - 64) & ~low_bits(st.r0 - 64)), ~(low_bits(st.r1 - 96) & ~low_bits(st.r0 - 96)));
+                c.step_how[s][lane] = keys > 0 ? keys | (st.fresh ? 0 : kStepAdds) : 0;
+            }
+            uint8_t *vb = stages + s * kTileBytes;
+#pragma unroll 1
+            for (uint32_t m = __ballot_sync(kFull, keys > 0 && keys < 16); m; m &= m - 1) {
+                const int kk = __ffs(m) - 1, filled = __shfl_sync(kFull, keys, kk);
+#pragma unroll 1
+                for (int y = lane; y < (16 - filled) * 16; y += 32)  // 8 16-byte units in each of two atoms
+                    st_shared_v4(saddr(vb + (y & 8 ? kAtom : 0) + (kk * 16 + filled + (y >> 4)) * 128 + (y & 7) * 16),
+                                 make_uint4(0, 0, 0, 0));
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.v_full[s]);
+        }
+        t0 += p.j1 - p.j0;
+        release_piece(n, lane, c);
+    }
+}
+
+// The scheduler: one warp hands out the pieces of the CTA's range, one per call.
+struct Schedule {
+    Start st;
+    int q, head, rt, j, n, cut_at, turn;
+    int64_t at, end;
+    bool swapped, any;  // any: the request has a key tile at all
+};
+
+__device__ __forceinline__ void schedule_part(Schedule &z, const Range &range) {
+    const bool second = z.swapped && z.turn == 0;
+    z.q = z.st.q;
+    z.head = z.st.head;
+    z.rt = z.st.rt + second;
+    z.j = second ? 0 : z.st.j;
+    z.at = range.at + (second ? z.cut_at : 0);
+    z.end = z.swapped && z.turn == 1 ? range.at + z.cut_at : range.end;
+    z.any = true;
+}
+
+__device__ __forceinline__ Schedule schedule_start(const PrefixArgs &a, const Range &range, const int64_t *first, int lane,
+                                                   Ctl &c) {
+    Schedule z;
+    z.st = find_start(a, range, first, lane, c);
     // (`first` lies in the K and V stages: the copies that follow the first piece come after its reads)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     // A range that ends one row tile and begins the next of the same head is taken in the
     // other order: all CTAs of the head are then near the same keys at the same time,
     // which L2 holds, instead of all over them (2 requests, 28/4 heads, context 28000: the keys
     // were read from HBM seven times).
-    int turn = 1, cut_at = 0;
-    if (st.j > 0) {
-        cut_at = st.tiles - st.j;  // tiles up to the next row tile
-        const int64_t rest = range.end - range.at - cut_at;
-        if (rest > 0 && rest < st.next) turn = 0;
+    z.turn = 1;
+    z.cut_at = z.n = 0;
+    if (z.st.j > 0) {
+        z.cut_at = z.st.tiles - z.st.j;  // tiles up to the next row tile
+        const int64_t rest = range.end - range.at - z.cut_at;
+        if (rest > 0 && rest < z.st.next) z.turn = 0;
     }
-    int n = 0;
+    z.swapped = z.turn == 0;
+    schedule_part(z, range);
+    return z;
+}
+
+// The next piece into the ring; false: there is none, or the wait for its slot ran out.
+__device__ __forceinline__ bool schedule_next(Schedule &z, const PrefixArgs &a, const Range &range, int lane, Ctl &c) {
+    if (z.at >= z.end) {
+        if (++z.turn >= 2) return false;
+        schedule_part(z, range);
+    }
+    const int slot = z.n % kRing;
+    if (z.n >= kRing && !warp_wait(&c.ring_empty[slot], (z.n / kRing - 1) & 1, c, a)) return false;
+    Piece &p = c.ring[slot];
+    int tiles = 0;
 #pragma unroll 1
-    for (const bool swapped = turn == 0; turn < 2; ++turn) {
-        const bool second = swapped && turn == 0;
-        int q = st.q, head = st.head, rt = st.rt + second, j = second ? 0 : st.j;
-        int64_t at = range.at + (second ? cut_at : 0);
-        const int64_t end = swapped && turn == 1 ? range.at + cut_at : range.end;
-        bool any = true;  // the request has a key tile at all
-#pragma unroll 1
-        while (at < end) {
-            if (n >= kRing && !warp_wait(&c.ring_empty[n % kRing], (n / kRing - 1) & 1, c, a)) return;
-            Piece &p = c.ring[n % kRing];
-            int tiles = 0;
-#pragma unroll 1
-            for (;;) {
-                tiles = fill_row_tile(a, q, rt, lane, c, p);
-                any |= tiles > 0;
-                if (tiles > 0) break;
-                if (++rt == a.s.row_tiles) {
-                    rt = 0;
-                    if (!any || ++head == a.s.heads) {
-                        head = 0;
-                        ++q;
-                    }
-                    any = false;
-                }
-                if (q >= a.s.n_req) return;  // (not reached while the lengths stay as they are during the call)
+    for (;;) {
+        tiles = fill_row_tile(a, z.q, z.rt, lane, c, p);
+        z.any |= tiles > 0;
+        if (tiles > 0) break;
+        if (++z.rt == a.s.row_tiles) {
+            z.rt = 0;
+            if (!z.any || ++z.head == a.s.heads) {
+                z.head = 0;
+                ++z.q;
             }
-            if (j >= tiles) return;          // (nor this)
-            const int j1 = static_cast<int>(min(static_cast<int64_t>(tiles), j + (end - at)));
-            if (lane == 0) {
-                p.head = head;
-                p.j0 = j;
-                p.j1 = j1;
-                p.part = j == 0 && j1 == tiles ? -1 : j > 0 ? 0 : 1;
-                const int tile = (q * a.s.heads + head) * a.s.row_tiles + rt;
-                if (p.part == 1) {
-                    const int last = prefix::cta_of(range.all, at + tiles - 1);
-                    a.cut[a.by_tile ? tile : static_cast<int>(blockIdx.x)] =
-                        Cut{last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), q, head, rt};
-                } else if (p.part < 0 && a.by_tile) {
-                    a.cut[tile].parts = 0;
-                }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c.ring_full[n % kRing]);
-            at += j1 - j;
-            j = 0;
-            ++n;
-            if (++rt == a.s.row_tiles) {
-                rt = 0;
-                if (++head == a.s.heads) {
-                    head = 0;
-                    ++q;
-                    any = false;
-                }
-            }
+            z.any = false;
+        }
+        if (z.q >= a.s.n_req) return false;  // (not reached while the lengths stay as they are during the call)
+    }
+    if (z.j >= tiles) return false;          // (nor this)
+    const int j1 = static_cast<int>(min(static_cast<int64_t>(tiles), z.j + (z.end - z.at)));
+    if (lane == 0) {
+        p.head = z.head;
+        p.j0 = z.j;
+        p.j1 = j1;
+        p.part = z.j == 0 && j1 == tiles ? -1 : z.j > 0 ? 0 : 1;
+        const int tile = (z.q * a.s.heads + z.head) * a.s.row_tiles + z.rt;
+        if (p.part == 1) {
+            const int last = prefix::cta_of(range.all, z.at + tiles - 1);
+            a.cut[a.by_tile ? tile : static_cast<int>(blockIdx.x)] =
+                Cut{last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), z.q, z.head, z.rt};
+        } else if (p.part < 0 && a.by_tile) {
+            a.cut[tile].parts = 0;
         }
     }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&c.ring_full[slot]);
+    z.at += j1 - z.j;
+    z.j = 0;
+    ++z.n;
+    if (++z.rt == a.s.row_tiles) {
+        z.rt = 0;
+        if (++z.head == a.s.heads) {
+            z.head = 0;
+            ++z.q;
+            z.any = false;
+        }
+    }
+    return true;
 }
 
 // One thread's wait.
@@ -856,13 +904,20 @@ __device__ __forceinline__ void store_stage(uint32_t stage, int lane, uint64_t r
 // handed back to the MMA as soon as it is in registers and the stage: the products
 // of the next piece wait for it.
 template <bool kF16>
-__device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_t stage, uint32_t tiles, Ctl &c,
-                                         const PrefixArgs &a) {
+__device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_t stage, uint32_t tiles, const Range &range,
+                                         const int64_t *first, Ctl &c, const PrefixArgs &a) {
     uint32_t t0 = 0;
+    Schedule z;
+    const bool scheduler = q == 0;
+    if (scheduler) z = schedule_start(a, range, first, lane, c);
     const int r = q * 32 + lane, tok = prefix::quotient(r, a.s.by_group);
     const uint32_t col = tmem + (static_cast<uint32_t>(q * 32) << 16) + kOCol;
 #pragma unroll 1
     for (int n = 0; t0 < tiles; ++n) {
+        if (scheduler)
+#pragma unroll 1
+            while (z.n < n + kRing && schedule_next(z, a, range, lane, c)) {
+            }
         const Piece *pp = next_piece(n, c, a);
         if (!pp) return;
         const Piece &p = *pp;
@@ -976,6 +1031,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(&c.k_full[s], 1);
             mbar_init(&c.v_full[s], 1);
             mbar_init(&c.v_empty[s], 1);
+            mbar_init(&c.v_raw[s], 1);
             mbar_init(&c.s_full[s], 1);
             mbar_init(&c.p_full[s], 4);  // a half's four warps
         }
@@ -986,7 +1042,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&c.o_ready, 1);
         mbar_init(&c.o_free, 4);
         mbar_init(&c.mma_done, 1);
-        mbar_init(&c.v_raw, 1);
         c.abort_flag = 0;
         for (const CUtensorMap *m : {&tm_q, &tm_k, &tm_v})
             asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
@@ -1015,14 +1070,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             produce(warp == 0, warp == 0 ? &tm_k : &tm_v, &tm_q, warp == 0 ? sk : sv, sq, tiles, lane, c, a);
         else if (warp == 1)
             issue_products<kF16>(sq, sk, sv, tmem, tiles, lane, c, a);
-        else if (tiles)
-            schedule(a, range, first, lane, c);
+        else
+            clean(sv, tiles, lane, c, a);
     } else if (warp < 12) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         softmax<kF16>(tmem, warp & 3, lane, (warp >> 2) - 1, tiles, c, a);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kOutRegs));
-        read_out<kF16>(tmem, warp & 3, lane, saddr(so + (warp - 12) * kStageBytes), tiles, c, a);
+        if (tiles) read_out<kF16>(tmem, warp & 3, lane, saddr(so + (warp - 12) * kStageBytes), tiles, range, first, c, a);
     }
     tc_fence_before();
     __syncthreads();
