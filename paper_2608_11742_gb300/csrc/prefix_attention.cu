@@ -73,7 +73,8 @@ constexpr int kConsumers = 16;       // every warp
 constexpr int kMaxSeqs = 128;        // sequences with rows in one row tile
 constexpr int kMaxCtas = 160;
 constexpr int kStepAdds = 32;
-constexpr int kStagedLens = 1024;    // lengths that are kept in shared memory
+constexpr int kStagedLens = 512;     // lengths that are kept in shared memory
+constexpr int kStagedTiles = 512;    // row tiles of a head whose key tiles are (a block of threads' at most)
 constexpr int kMaxReqs = 2 * kStages * kTileBytes / 8;  // requests whose first tiles fit the K and V stages
 constexpr float kLn2 = 0.6931471805599453f;
 // bounds of a tile's sum of P in a row (in units of its reference): P in fp16 stays finite
@@ -131,7 +132,8 @@ struct Ctl {
     int2 slot_at[2][8];  // a producer's slots: page, first token
     uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
-    int32_t len[kStagedLens];
+    int32_t len[kStagedLens];      // as they are used
+    int32_t tiles_of[kStagedTiles];  // key tiles of (request, row tile)
     int32_t longest, empty, own;  // key tiles of the longest row tile; one has none; those of the CTA's own
     uint32_t tmem_base;
     int abort_flag;
@@ -178,7 +180,7 @@ __device__ __forceinline__ void drain(uint64_t *bar, uint32_t parity) {
 
 // ---------------------------------------------------------------- the cut
 __device__ __forceinline__ int len_of(const PrefixArgs &a, int s, const Ctl &c) {
-    return prefix::used_len(a.s, a.s.n_req * a.s.n_branch <= kStagedLens ? c.len[s] : a.len[s]);
+    return a.s.n_req * a.s.n_branch <= kStagedLens ? c.len[s] : prefix::used_len(a.s, a.len[s]);
 }
 __device__ __forceinline__ int shared_len_of(const PrefixArgs &a, int q) { return a.shared_len ? a.shared_len[q] : 0; }
 
@@ -187,9 +189,19 @@ __device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int q, int rt, i
     const RowTile r = prefix::row_tile(a.s, rt);
     KeySum k{0, 0, INT32_MAX};
     const int s0 = q * a.s.n_branch + r.b0;
+    if (a.s.n_req * a.s.n_branch <= kStagedLens) {
+#pragma unroll 4
+        for (int i = 0; i < r.nb; ++i) prefix::add_sequence(a.s, k, c.len[s0 + i]);
+    } else {
 #pragma unroll 1
-    for (int i = 0; i < r.nb; ++i) prefix::add_sequence(a.s, k, len_of(a, s0 + i, c));
+        for (int i = 0; i < r.nb; ++i) prefix::add_sequence(a.s, k, prefix::used_len(a.s, a.len[s0 + i]));
+    }
     return prefix::key_tiles(a.s, k, prefix::shared_slots(a.s, k, shared_len));
+}
+// The same in find_range's wake: looked up where it was kept.
+__device__ __forceinline__ int known_tiles(const PrefixArgs &a, int q, int rt, const Ctl &c) {
+    return a.s.n_req * a.s.row_tiles <= kStagedTiles ? c.tiles_of[q * a.s.row_tiles + rt]
+                                                     : entry_tiles(a, q, rt, shared_len_of(a, q), c);
 }
 
 // Exclusive prefix sum over the block's 512 threads; *total: the block's sum.
@@ -233,7 +245,7 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
     const int entries = a.s.n_req * a.s.row_tiles, n_seq = a.s.n_req * a.s.n_branch;
     if (n_seq <= kStagedLens)
 #pragma unroll 1
-        for (int i = threadIdx.x; i < n_seq; i += kThreads) c.len[i] = a.len[i];
+        for (int i = threadIdx.x; i < n_seq; i += kThreads) c.len[i] = prefix::used_len(a.s, a.len[i]);
     if (threadIdx.x == 0) c.longest = c.empty = 0;
     // (loaded while the lengths are)
     int next_shared = shared_len_of(a, min(prefix::quotient(threadIdx.x, a.s.by_row_tiles), a.s.n_req - 1));
@@ -248,6 +260,7 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
         const int q = prefix::quotient(e, a.s.by_row_tiles), rt = e - q * a.s.row_tiles;
         int64_t total;
         const int t = e < entries ? entry_tiles(a, q, rt, next_shared, c) : 0;
+        if (entries <= kStagedTiles && e < entries) c.tiles_of[e] = t;
         if (base + kThreads < entries)
             next_shared = shared_len_of(a, min(prefix::quotient(e + kThreads, a.s.by_row_tiles), a.s.n_req - 1));
         if (few && e < entries) {
@@ -300,7 +313,6 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &ra
             hi = mid;
     }
     st.q = lo;
-    const int shared_len = shared_len_of(a, lo);
     int64_t rem = range.at - first[lo] * a.s.heads;  // tiles of the request before the range
     int64_t per_head = 0;
 #pragma unroll 1
@@ -308,7 +320,7 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &ra
         int64_t before = 0;
 #pragma unroll 1
         for (int base = 0; base < a.s.row_tiles; base += 32) {
-            const int t = base + lane < a.s.row_tiles ? entry_tiles(a, st.q, base + lane, shared_len, c) : 0;
+            const int t = base + lane < a.s.row_tiles ? known_tiles(a, st.q, base + lane, c) : 0;
             int upto = t;
 #pragma unroll 1
             for (int o = 1; o < 32; o <<= 1) {

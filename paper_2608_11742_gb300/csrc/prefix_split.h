@@ -114,10 +114,9 @@ struct KeySum {
     int32_t present, slots, min_pages;  // sequences there; their slots; whole pages of the shortest
 };
 PREFIX_HD void add_sequence(const Shape &s, KeySum &k, int len) {
-    if (len < 0) return;
-    ++k.present;
+    k.present += len >= 0;  // (an absent one's -1 makes no slot: slots are 16 tokens at least)
     k.slots += slots_of(s, len);
-    k.min_pages = imin(k.min_pages, len >> s.page_log);
+    k.min_pages = imin(k.min_pages, len >= 0 ? len >> s.page_log : INT32_MAX);
 }
 // Slots that are read once for all: whole pages inside the shared length and inside every sequence.
 PREFIX_HD int shared_slots(const Shape &s, const KeySum &k, int shared_len) {
