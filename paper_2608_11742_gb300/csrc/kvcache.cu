@@ -29,7 +29,12 @@ constexpr int kHeadDim = 128;
 constexpr int kBookThreads = 1024;
 constexpr int kBookWarps = kBookThreads / 32;
 constexpr int kCluster = 8;
-constexpr int kOneBlock = 8192;
+// Up to these sizes one block does a call's bookkeeping, beyond them a cluster. A cluster's
+// barriers cost 1 to 2 us, a block alone has an eighth of the loads in flight. In us, block /
+// cluster: reorder (table entries) 234: 3.2 / 3.7, 936: 4.5 / 4.2, 3744: 10.3 / 4.3; growth by two
+// pages (pages, or 8 a sequence) 1944: 4.7 / 7.2, 9792: 6.4 / 8.0, but from nothing 14.1 / 9.6;
+// compaction (entries and pages) 477: 4.7 / 6.7, 3816: 6.8 / 6.4, 7632: 10.1 / 7.3.
+constexpr int kOneReorder = 512, kOneResize = 8192, kOneCompact = 4096;
 constexpr int kCopyThreads = 256;
 constexpr int kTaskRows = 16;  // rows a warp copies at a time: 4 KB, 8 16-byte loads in flight per lane
 constexpr size_t kWsAlign = 256;
@@ -128,6 +133,8 @@ __device__ __forceinline__ void source_of(const ReorderArgs &a, int s, int &src,
     }
 }
 
+// A warp per sequence, the rows to be written staged in the workspace between two barriers, for a
+// sequence's source may be written by the call itself. 576 sequences of 60 pages: 10 us.
 __global__ void __launch_bounds__(kBookThreads, 1) reorder_kernel(const ReorderArgs a) {
     cg::cluster_group cluster = cg::this_cluster();
     const Book &b = a.b;
@@ -265,9 +272,15 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
     return v;
 }
 
-constexpr int kNearSeqs = 1024;   // sequences of a block whose wishes fit shared memory
-constexpr int kNearPages = 4096;  // free pages that do
-constexpr int kFewPages = 4;      // pages that a thread hands out alone
+// What a block's phases hand on stays in shared memory where it fits, else in the workspace (576
+// sequences growing: 15.8 us instead of 16.5).
+constexpr int kNearSeqs = 1024;   // sequences of a block
+constexpr int kNearPages = 4096;  // free pages
+// Up to so many pages a sequence's thread takes or gives back alone, more the warp does together,
+// sequence after sequence. Two pages of each of 72 sequences given back: 4.7 us instead of 11.7
+// by warps; 24 pages each taken and given back, 7.6 instead of 13.5; 60 each of 9216 sequences,
+// alone 107 instead of 79.
+constexpr int kFewPages = 32;
 
 struct Counts {
     unsigned long long need;  // of the block's sequences: pages (low 32 bits), copies (high)
@@ -308,6 +321,11 @@ struct Near {
     int32_t old_len, new_len, last;
 };
 
+// Growth and shrinking: give back, sum up what is asked for, list the lowest free pages, hand them
+// out; the prefix sums give every sequence its part of the list whatever the order of threads. A
+// chain of a dozen accesses to L2 and three barriers: 4.2 us for 9 sequences with the empty copy
+// launch behind it, 8 for 576 (a cluster), where one thread after another would need each
+// sequence's pages to be known before the next.
 __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArgs a) {
     cg::cluster_group cluster = cg::this_cluster();
     __shared__ unsigned long long sums[kBookWarps];
@@ -339,15 +357,18 @@ __global__ void __launch_bounds__(kBookThreads, 1) resize_kernel(const ResizeArg
             x = lengths(s);
             if (near) near_seq[s - s0] = x;
         }
-        for (uint32_t m = __ballot_sync(kFull, x.new_len < x.old_len); m; m &= m - 1) {  // a warp for each of its threads'
-            const int who = __ffs(m) - 1;
-            const int n_old = pages_of(b, __shfl_sync(kFull, x.old_len, who));
-            const int n_new = pages_of(b, __shfl_sync(kFull, x.new_len, who));
-            int32_t *row = b.table + static_cast<int64_t>(s - lane + who) * b.width;
-            for (int i = n_new + lane; i < n_old; i += 32) {
-                if (good_page(b, row[i])) atomicSub(&b.ref[row[i]], 1);
-                row[i] = -1;
-            }
+        const int held = pages_of(b, x.old_len), count = x.new_len < x.old_len ? held - pages_of(b, x.new_len) : 0;
+        const auto give = [&](int seq, int entry) {
+            int32_t *at = b.table + static_cast<int64_t>(seq) * b.width + entry;
+            const int p = *at;
+            if (good_page(b, p)) atomicSub(&b.ref[p], 1);
+            *at = -1;
+        };
+        if (count <= kFewPages)
+            for (int i = 1; i <= count; ++i) give(s, held - i);
+        for (uint32_t m = __ballot_sync(kFull, count > kFewPages); m; m &= m - 1) {
+            const int who = __ffs(m) - 1, n = __shfl_sync(kFull, count, who), h = __shfl_sync(kFull, held, who);
+            for (int i = 1 + lane; i <= n; i += 32) give(s - lane + who, h - i);
         }
         if (x.new_len < x.old_len) {
             b.len[s] = x.new_len;
@@ -471,6 +492,8 @@ struct CompactArgs {
     KvWorkspace w;
 };
 
+// Both lists by one pass of prefix sums over the counts, then the counts move, then the table
+// entries are renamed: 10 us for 8000 pages and 576 sequences, beside 160 for the pages' data.
 __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const CompactArgs a) {
     cg::cluster_group cluster = cg::this_cluster();
     __shared__ unsigned long long sums[kBookWarps];
@@ -550,12 +573,13 @@ struct CopyArgs {
     const int32_t *src, *dst, *used;  // used == nullptr: whole pages
     const CopyHeader *head;           // nullptr: `count` pages from the lists' first entries
     int32_t count, n_from, n_to, layers, heads, ps;
-    int32_t heads_inner;  // heads of a token lie together
     uint32_t *err;
 };
 
-// A warp copies up to 16 rows (a token of a head each, 256 bytes) at a time,
-// half a warp to a row.
+// A warp copies up to 16 rows (a token of a head each, 256 bytes) at a time, half a warp to a
+// row: 8 loads of 16 bytes a lane in flight. Bound by HBM: 1000 pages of 32 tokens, 8 heads, 4
+// layers (524 MB read, as much written) 161 us, 96 % of a plain copy's bandwidth; three blocks an
+// SM (with four, 64 registers a thread, the loads no longer stay together: 168).
 __global__ void __launch_bounds__(kCopyThreads, 3) copy_kernel(const CopyArgs a) {
     const int lane = threadIdx.x & 31;
     pdl_wait();
@@ -580,14 +604,11 @@ __global__ void __launch_bounds__(kCopyThreads, 3) copy_kernel(const CopyArgs a)
     int src, dst, used;
     entry(e, src, dst, used);
     for (int64_t ee = e; ee < count;) {
-        int x = t, head, block;
-        if (a.heads_inner) {
-            head = x % a.heads, x /= a.heads;
-            block = x % blocks, x /= blocks;
-        } else {
-            block = x % blocks, x /= blocks;
-            head = x % a.heads, x /= a.heads;
-        }
+        int x = t;
+        const int block = x % blocks;
+        x /= blocks;
+        const int head = x % a.heads;
+        x /= a.heads;
         const int which = x & 1, layer = x >> 1;
         const int rows = min(kTaskRows, used - block * kTaskRows);
         const bool skip = a.used && src < 0;  // (a copy that found no page)
@@ -681,11 +702,11 @@ __global__ void __launch_bounds__(kCopyThreads) write_kernel(const WriteArgs a) 
 }
 
 // ---------------------------------------------------------------- host
-// One block while that is enough (`entries`: what it goes through), else a cluster of eight.
+// One block, or a cluster of eight.
 template <typename Args>
-rps_status launch_book(void (*kernel)(Args), const Args &a, int64_t entries, cudaStream_t stream) {
+rps_status launch_book(void (*kernel)(Args), const Args &a, bool one_block, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    const int blocks = entries <= kOneBlock ? 1 : kCluster;
+    const int blocks = one_block ? 1 : kCluster;
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(kBookThreads);
     cfg.stream = stream;
@@ -783,7 +804,6 @@ rps_status launch_copy(const rps_kv_cache *from, const rps_kv_cache *to, const i
     a.layers = to->n_layers;
     a.heads = to->n_heads;
     a.ps = to->page_size;
-    a.heads_inner = to->n_heads > 1 && to->head_stride < to->token_stride;
     a.err = err;
     const int64_t tasks = most * a.layers * 2 * a.heads * ((a.ps + kTaskRows - 1) / kTaskRows);
     const int64_t blocks = std::min<int64_t>((tasks + kCopyThreads / 32 - 1) / (kCopyThreads / 32), sms * 8);
@@ -834,7 +854,7 @@ rps_status rps_kv_reorder(const rps_kv_cache *kv, const int32_t *d_src, const in
     if (st != RPS_OK) return st;
     a.src_of = d_src;
     a.keep = d_keep;
-    return launch_book(reorder_kernel, a, static_cast<int64_t>(a.b.n_seq) * a.b.width, reinterpret_cast<cudaStream_t>(stream));
+    return launch_book(reorder_kernel, a, static_cast<int64_t>(a.b.n_seq) * a.b.width <= kOneReorder, reinterpret_cast<cudaStream_t>(stream));
 }
 
 rps_status rps_kv_fork_branches(const rps_kv_cache *kv, const uint8_t *d_branch_valid, const int32_t *d_ctx_len,
@@ -858,7 +878,7 @@ rps_status rps_kv_resize(const rps_kv_cache *kv, const int32_t *d_new_len, void 
     if (st != RPS_OK) return st;
     a.new_len = d_new_len;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if ((st = launch_book(resize_kernel, a, std::max(8 * a.b.n_seq, a.b.n_pages), s)) != RPS_OK) return st;
+    if ((st = launch_book(resize_kernel, a, std::max(8 * a.b.n_seq, a.b.n_pages) <= kOneResize, s)) != RPS_OK) return st;
     return launch_copy(kv, kv, a.w.src, a.w.dst, a.w.used, a.w.head, 0, a.b.n_seq, a.b.err, s);
 }
 
@@ -869,7 +889,7 @@ rps_status rps_kv_compact(const rps_kv_cache *kv, int32_t *d_n_live, void *d_ws,
     if (st != RPS_OK) return st;
     a.n_live = d_n_live;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if ((st = launch_book(compact_kernel, a, static_cast<int64_t>(a.b.n_seq) * a.b.width + a.b.n_pages, s)) != RPS_OK) return st;
+    if ((st = launch_book(compact_kernel, a, static_cast<int64_t>(a.b.n_seq) * a.b.width + a.b.n_pages <= kOneCompact, s)) != RPS_OK) return st;
     return launch_copy(kv, kv, a.w.list, a.w.dst, nullptr, a.w.head, 0, (static_cast<int64_t>(kv->n_pages) + 1) / 2,
                        a.b.err, s);
 }
