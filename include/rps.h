@@ -522,7 +522,8 @@ typedef struct {
 } rps_kv_cache;
 
 /* Workspace bytes of the calls below that take one; 0 for an invalid cache. The
- * workspace needs no initialisation and keeps nothing between calls. */
+ * workspace needs no initialisation and keeps nothing between calls; one workspace
+ * must not serve two calls that can overlap. */
 size_t rps_kv_workspace_bytes(const rps_kv_cache *kv);
 
 /*
@@ -616,8 +617,8 @@ rps_status rps_kv_write(const rps_kv_cache *kv, int32_t layer, const void *k_new
  * q, out [n_req][n_branch * n_q][n_heads][128] of the cache's dtype, 128
  * contiguous, other strides in elements, multiples of 8, bases 16-byte aligned;
  * lse [n_req][n_branch * n_q][n_heads] fp32 or NULL. n_heads a multiple of
- * kv->n_heads, at most RPS_KV_MAX_GROUP times it. out must not overlap q or the
- * cache. The lengths and the tables must not change during the call.
+ * kv->n_heads, at most RPS_KV_MAX_GROUP times it; scale finite and above 0. out must not
+ * overlap q or the cache. The lengths and the tables must not change during the call.
  */
 typedef struct {
     const void *q;

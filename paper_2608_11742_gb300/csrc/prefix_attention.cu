@@ -15,23 +15,41 @@
 // One persistent CTA per SM takes pieces (row tile, key tiles [j0, j1)). Key tiles
 // are numbered through its pieces; even and odd ones go to two independent halves
 // of the softmax, each with its own S / P buffer, maxima, sums and accumulator:
-//   warp 3      scheduler: finds the pieces from the lengths in device memory and
-//               hands them to the other roles through a ring in shared memory;
-//   warp 0      TMA producer of Q (a box of tokens x heads of the group) and of K,
-//               one box per slot of pages, addresses through the page table;
+//   warp 0      TMA producer of K, one box per slot of pages and atom, addresses through
+//               the page table, and of Q (a box of tokens x heads of the group);
 //   warp 2      TMA producer of V, in the same way. V lies token by token in the
 //               cache, so it is the MN-major operand of the second product: no
 //               transposed copy of the values is kept;
-//   warp 1      MMA issuer: S = Q K^T into TMEM buffer t % 2, O[t % 2] += P V with P
-//               from TMEM, in the order PV(t), S(t + 2), PV(t + 1), ...; it also
-//               clears the rows of V past a sequence's last key (they may hold
-//               anything, and 0 * NaN would reach the sums);
-//   warps 4-7   softmax of even tiles, 8-11 of odd ones: thread = row. The base-2
-//               reference m is raised only when a score passes it by more than 8.
-//               P is rounded to the cache's type (the product takes no other);
+//   warp 3      cleaner of own tiles' V: clears the rows past a sequence's last key (they
+//               may hold anything, and 0 * NaN would reach the sums), and lists which
+//               rows each 16-key step of the product writes;
+//   warp 1      MMA issuer, one thread: S = Q K^T into TMEM buffer t % 2, O[t % 2] += P V
+//               with P from TMEM, in the order PV(t), S(t + 2), PV(t + 1), ...;
+//   warps 4-7   softmax of even tiles, 8-11 of odd ones: thread = row. One pass with a
+//               standing base-2 reference, which is changed only where a tile's sum is
+//               far out of range. P is rounded to the cache's type (the product takes
+//               no other); its sum is taken before the rounding, in fp32;
 //   warps 12-15 read-out: the halves' accumulators weighted and added; written as
 //               output rows, or as fp32 partial results where a piece is not all
-//               of its row tile.
+//               of its row tile. Warp 12 also schedules: it finds the pieces from the
+//               lengths in device memory and hands them to the other roles through a
+//               ring in shared memory.
+//
+// What bounds it, at the figures measured (times of both launches):
+//   2 requests, 28 / 4 heads, 9 branches of 32, contexts to 32700, fp16: 178 us, 1310
+//     TFLOP/s. A key tile takes 1740 cycles, 1024 of them the tensor pipe's, about 965
+//     of the issuing thread's time; the clock is the power limit's (1.45 to 1.85 GHz).
+//     Two row tiles sharing K and V stages (195), two issuing warps (240) and unrolled
+//     batches (187) were slower.
+//   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 440
+//     us, 3.1 TB/s of cache, queries and outputs. A tile of such pages is 32 copies of 2
+//     KB (26 cycles each at best in the copy unit, 46 for the thread that issues them);
+//     the ends of pieces, every 5 tiles, and instruction fetches (72 KB of code in
+//     all roles, 6 % of the fetches miss the cache; 158 KB missed 32 %) take the rest. Copies shared out to a second
+//     warp were slower (567).
+//   One request's 9 branches of 32, 32 heads, context 328: 17 us; 64 sequences of one
+//     prompt of 8200: 31. About 5 us pass before a CTA's first copy (lengths, prefix
+//     sums, page table: dependent accesses), 2 in the second launch.
 // Every wait is bounded; a role whose wait runs out flags RPS_DEVERR_TIMEOUT and
 // raises the CTA's abort flag, copies and MMAs in flight are drained and TMEM is
 // freed before the CTA exits.
@@ -73,8 +91,10 @@ constexpr int kConsumers = 16;       // every warp
 constexpr int kMaxSeqs = 128;        // sequences with rows in one row tile
 constexpr int kMaxCtas = 160;
 constexpr int kStepAdds = 32;
-constexpr int kStagedLens = 512;     // lengths that are kept in shared memory
-constexpr int kStagedTiles = 512;    // row tiles of a head whose key tiles are (a block of threads' at most)
+// Lengths, and key tiles of a head's row tiles (a block of threads' at most), are kept in shared
+// memory where they fit (64 sequences of one prompt: 31 us instead of 33.7).
+constexpr int kStagedLens = 512;
+constexpr int kStagedTiles = 512;
 constexpr int kMaxReqs = 2 * kStages * kTileBytes / 8;  // requests whose first tiles fit the K and V stages
 constexpr float kLn2 = 0.6931471805599453f;
 // bounds of a tile's sum of P in a row (in units of its reference): P in fp16 stays finite
@@ -236,7 +256,8 @@ struct Range {
 // Cutting a row tile costs what its parts take to be written and joined, about as much as
 // three key tiles: where every row tile has a CTA of its own and none is longer by more than
 // that than the equal shares, none is cut (one request's 9 branches of 32, 32 heads, context
-// 328: 96 row tiles of 4 to 5 key tiles instead of shares of 3: 25 -> xx us).
+// 328: 96 row tiles of 4 to 5 key tiles instead of shares of 3: 17 us instead of 21; one query of 32
+// heads over 1000 keys, which are worth cutting: 18 instead of 19.6).
 constexpr int kCutTiles = 3;
 
 // By all threads: the lengths into shared memory, and in first[q] the key tiles (of
@@ -250,7 +271,7 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
     // (loaded while the lengths are)
     int next_shared = shared_len_of(a, min(prefix::quotient(threadIdx.x, a.s.by_row_tiles), a.s.n_req - 1));
     __syncthreads();
-    const bool few = entries * a.s.heads <= static_cast<int>(gridDim.x);  // (at most one block of entries then)
+    const bool few = static_cast<int64_t>(entries) * a.s.heads <= gridDim.x;  // (at most one block of entries then)
     const int mine = few ? prefix::quotient(blockIdx.x, a.s.by_row_tiles) : 0;  // request and head of the CTA's own
     const int mine_q = mine / a.s.heads;
     int64_t carry = 0;
@@ -1331,7 +1352,8 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
     if (launch_pdl(f16 ? prefix_attention_kernel<true> : prefix_attention_kernel<false>, dim3(grid), dim3(kThreads),
                    kSmemBytes, s, tq, tk, tv, a) != cudaSuccess)
         return RPS_ERR_CUDA;
-    // a cut row tile has about grid / row_tiles parts: half warps of at most four each
+    // a cut row tile has about grid / row_tiles parts: half warps of at most four each (64 sequences
+    // of one prompt, 16 row tiles: 31 us; one half warp a row, 33.5)
     int split = 1;
     while (split < kJoinHalves && row_tiles * kAhead * split < grid) split *= 2;
     const dim3 cuts(static_cast<unsigned>(std::min<int64_t>(row_tiles, grid)), prefix::kRows / (kJoinHalves / split));

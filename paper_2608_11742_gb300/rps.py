@@ -799,3 +799,43 @@ class Step:
                         stream)
         self.score_branch_rows(dev_logits, stream)
         self.score_and_decide(dev_logits, stream)
+
+
+class BranchCache:
+    """The K/V cache of block decoding, and its calls around one ``Step``.
+
+    Sequence (q, 0) is request q's base, (q, 1 + b) its branch b. One step: ``fork`` the
+    branches that ``PivotsBuf.branch_valid`` lists from their base's context, ``resize``
+    every sequence to its context and block, per layer ``write`` the block's keys and
+    values and ``attend`` over context and block (the context's pages read once for all
+    of a request's branches), then ``commit`` the winner of ``CommitBuf.winner``: its
+    block becomes the base's. Pages, workspaces and bookkeeping are allocated once;
+    every call is asynchronous and reads what it decides by from device memory, so a
+    step can be captured as a CUDA graph."""
+
+    def __init__(self, n_layers: int, n_pages: int, n_heads: int, page_size: int, n_req: int, n_branch: int,
+                 max_pages: int, n_q: int, n_query_heads: int, device, dtype=torch.bfloat16):
+        self.kv = KvCacheBuf.alloc(n_layers, n_pages, n_heads, page_size, n_req, n_branch, max_pages, device, dtype)
+        ws = lambda n: torch.empty(n, dtype=torch.uint8, device=device)
+        self.ws = ws(rps_kv_workspace_bytes(self.kv))
+        self.ws_attn = ws(rps_prefix_attention_workspace_bytes(self.kv, n_q, n_query_heads))
+        self.n_live = torch.zeros(1, dtype=torch.int32, device=device)
+
+    def resize(self, new_len, stream=None):
+        rps_kv_resize(self.kv, new_len, self.ws, stream)
+
+    def fork(self, branch_valid, ctx_len, stream=None):
+        rps_kv_fork_branches(self.kv, branch_valid, ctx_len, self.ws, stream)
+
+    def write(self, layer, k_new, v_new, stream=None):
+        rps_kv_write(self.kv, layer, k_new, v_new, stream)
+
+    def attend(self, layer, q, out, ctx_len, scale, causal=False, lse=None, stream=None):
+        """``ctx_len``: as given to ``fork`` (None: nothing is shared)."""
+        rps_prefix_attention_fwd(q, self.kv, layer, out, self.ws_attn, ctx_len, scale, causal, lse, stream)
+
+    def commit(self, winner, stream=None):
+        rps_kv_commit(self.kv, winner, self.ws, stream)
+
+    def compact(self, stream=None):
+        rps_kv_compact(self.kv, self.n_live, self.ws, stream)
