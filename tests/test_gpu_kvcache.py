@@ -270,3 +270,98 @@ def test_on_a_side_stream_and_replayed_from_a_graph():
         oracle()
     torch.cuda.synchronize()
     p.check("replayed")
+
+
+@pytest.mark.parametrize("n_req,nb", [(2, 3), (70, 4)])  # one block, a cluster
+def test_sequences_of_many_pages(n_req, nb):
+    """Few and many pages taken and given back side by side (a thread alone, a warp together), partial last pages
+    shared and copied on the way."""
+    n, width = n_req * nb, 90
+    p = Pair(31, 1, n * 60, 1, 16, n_req, nb, width)
+    rng = np.random.default_rng(32)
+    for k in range(6):
+        p.resize(rng.choice([-1, 0, 5, 16 * 32, 16 * 33, 16 * 34 - 3, 600, 16 * width], n, p=[.1, .1, .2, .2, .1, .1, .1, .1]))
+        if k % 2 == 0:
+            p.fork(rng.random((n_req, nb - 1)) < 0.7, None)
+            p.resize(np.where(p.o.length > 0, np.minimum(p.o.length + rng.choice([1, 40, 16 * 40], n), 16 * width), p.o.length))
+    p.resize(np.full(n, -1))
+    assert (p.o.ref == 0).all()
+
+
+@pytest.mark.parametrize("heads,n_new,tokens_first", [(3, 171, False), (3, 400, True), (28, 19, True), (1, 1100, False),
+                                                      (600, 2, True), (600, 3, False)])
+def test_writes_of_more_rows_than_a_block_takes(heads, n_new, tokens_first):
+    """512 rows a block: blocks that begin and end inside a token's heads, more heads than rows of a block."""
+    ps, layers = 16, 1
+    width = -(-(n_new + 9) // ps)
+    p = Pair(33, layers, 2 * width, heads, ps, 1, 2, width, tokens_first=tokens_first)
+    p.resize([n_new + 9, n_new - 2])
+    p.write(0, n_new)
+    p.write(0, n_new, heads_first=True)
+
+
+def test_writes_with_one_branch_and_odd_strides():
+    """One branch: sequences lie at the request's stride, whatever the branch's is; rows wider than they are read."""
+    p = Pair(34, 1, 12, 2, 16, 3, 1, 4)
+    p.resize([20, 7, 33])
+    wide = [dev16(bits(p.rng, (3, 5, 2, D + 24))) for _ in range(2)]
+    k, v = (w[:, None, :, :, :D] for w in wide)
+    rps.rps_kv_write(p.kv, 0, k, v)
+    p.o.write(0, *[x[:, 0].contiguous().view(torch.int16).cpu().numpy() for x in (k, v)])
+    p.check("write")
+
+
+def test_refusals_of_the_binding():
+    p = Pair(35, 1, 12, 2, 16, 2, 2, 3)
+    p.resize([16, -1, 16, -1])
+    ok_new = torch.zeros((2, 2, 4, 2, D), dtype=torch.bfloat16, device="cuda")
+    ws, kv = p.ws, p.kv
+    four, two = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.full((2,), -1, dtype=torch.int32, device="cuda")
+    valid = torch.zeros((2, 1), dtype=torch.uint8, device="cuda")
+    refused = [
+        lambda: rps.rps_kv_write(kv, 0, ok_new[:, :, :, :1], ok_new[:, :, :, :1]),              # heads
+        lambda: rps.rps_kv_write(kv, 0, ok_new, ok_new[:, :, :3]),                              # shapes differ
+        lambda: rps.rps_kv_write(kv, 0, ok_new.half(), ok_new.half()),                          # type
+        lambda: rps.rps_kv_write(kv, 0, ok_new.cpu(), ok_new.cpu()),                            # device
+        lambda: rps.rps_kv_write(kv, 0, ok_new, ok_new.transpose(2, 3).contiguous().transpose(2, 3)),  # strides differ
+        lambda: rps.rps_kv_write(kv, 0, ok_new.transpose(0, 1), ok_new.transpose(0, 1)),        # requests inside branches
+        lambda: rps.rps_kv_write(kv, 1, ok_new, ok_new),                                        # layer
+        lambda: rps.rps_kv_write(kv, -1, ok_new, ok_new),
+        lambda: rps.rps_kv_resize(kv, four.long(), ws),
+        lambda: rps.rps_kv_resize(kv, four[:3], ws),
+        lambda: rps.rps_kv_resize(kv, four.cpu(), ws),
+        lambda: rps.rps_kv_resize(kv, four, ws[:-1]),
+        lambda: rps.rps_kv_reorder(kv, four, ws, four[:2]),
+        lambda: rps.rps_kv_fork_branches(kv, valid.int(), None, ws),
+        lambda: rps.rps_kv_fork_branches(kv, valid, four, ws),
+        lambda: rps.rps_kv_commit(kv, four, ws),
+        lambda: rps.rps_kv_compact(kv, two, ws),
+        lambda: rps.rps_kv_copy_pages(kv, kv, four, two),
+        lambda: rps.rps_kv_copy_pages(kv, rps.KvCacheBuf.of_pages(kv.k.half(), kv.v.half()), two, two),
+    ]
+    for i, call in enumerate(refused):
+        with pytest.raises((ValueError, TypeError, rps.RPSError)):
+            call()
+            pytest.fail(f"call {i} was not refused")
+    p.check("refused calls")
+
+
+def test_copies_of_the_buffer_object():
+    """copy.copy shares the tensors, a deep copy and a pickle have their own; replaced tensors are used."""
+    import copy
+    import pickle
+    p = Pair(36, 1, 8, 1, 16, 1, 2, 3)
+    p.resize([20, 3])
+    shared, own, loaded = copy.copy(p.kv), copy.deepcopy(p.kv), pickle.loads(pickle.dumps(p.kv))
+    before = p.kv.length.clone()
+    rps.rps_kv_resize(own, i32([5, -1]), p.ws)
+    rps.rps_kv_resize(loaded, i32([40, 40]), p.ws)
+    p.check("other buffers' calls")
+    assert own.length.tolist() == [[5, -1]] and loaded.length.tolist() == [[40, 40]]
+    assert torch.equal(p.kv.length, before)
+    rps.rps_kv_resize(shared, i32([17, 3]), p.ws)
+    p.o.resize([17, 3])
+    p.check("a shallow copy's call")
+    p.kv.length = p.kv.length.clone()  # the struct is built anew
+    p.resize([1, 30])
+    assert shared.length.tolist() == [[17, 3]]

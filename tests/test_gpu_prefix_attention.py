@@ -42,7 +42,7 @@ class Case:
         n_req, nb = lens.shape
         pages = lambda n: 0 if n <= 0 else -(-int(n) // ps)
         width = max(1, max(pages(n) for n in lens.ravel())) + 1
-        if wide:  # a table for so many tokens that row tiles get two halves
+        if wide:  # a table far wider than the sequences need: more CTAs than key tiles
             width = max(width, -(-2560 * 128 // (ps * n_req * Hk * -(-nb * n_q // (128 // (H // Hk))))) + 16)
         table, count = np.full((n_req, nb, width), -1), 0
         for r in range(n_req):
