@@ -75,7 +75,9 @@ using prefix::Shape;
 
 constexpr int kD = 128;                // head dimension
 constexpr int kAtom = 64 * 128 * 2;    // one 128-row x 64-column swizzle atom of 16-bit elements: 16 KB
-constexpr int kTileBytes = 2 * kAtom;  // a Q, K or V tile: two atoms along d
+constexpr int kTileBytes = 2 * kAtom;  // a Q, K or V tile: Q's two atoms along d
+// A K or V tile goes in groups of 8 tokens: their columns 0..63, then 64..127 (1024 bytes each).
+constexpr int kChunk = 1024, kGroup = 2 * kChunk;
 constexpr int kStages = 2;             // of K and of V: a tile's stage, S / P buffer and O go by its parity
 constexpr int kQBufs = 2;
 constexpr int kStageBytes = 32 * 128;  // per read-out warp: 32 rows x 128 bytes on their way out
@@ -117,6 +119,9 @@ struct PrefixArgs {
     int64_t out_req, out_token, out_head;
     float *lse;
     float c;  // scale * log2(e)
+    // A copy of K or V takes 2^copy_log tokens. by_groups: from a map whose third dimension goes
+    // through the tokens of all pages by eights, page_groups of them a page; else 8 tokens of a page
+    int32_t by_groups, copy_log, page_groups, no_page;  // no_page: a coordinate beyond the pages
     Cut *cut;       // [kMaxCtas]
     int32_t by_tile;  // cuts are listed by row tile
     float2 *part_ml;  // [2 * kMaxCtas][128]: maximum and sum of each row of a partial result
@@ -149,8 +154,8 @@ struct Ctl {
     // step), and kStepAdds unless it overwrites
     uint4 step_off[kStages][8];
     int32_t step_how[kStages][8];
-    int2 slot_at[2][8];  // a producer's slots: page, first token
-    uint32_t bad[4];  // slots of key tile t whose page id is outside the cache (t % 4)
+    int4 copy_at[2][16];  // a producer's copies: their coordinates
+    uint32_t bad[4];  // copies of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
     int32_t len[kStagedLens];      // as they are used
     int32_t tiles_of[kStagedTiles];  // key tiles of (request, row tile)
@@ -438,20 +443,20 @@ __device__ __forceinline__ void release_piece(int n, int lane, Ctl &c) {
     if (lane == 0) mbar_arrive(&c.ring_empty[n % kRing]);
 }
 
-// The page id (as the table has it: the load is on its way) of slot `lane` of key tile j and the
-// slot's first token in the page; false: the tile has no such slot.
-__device__ __forceinline__ bool slot_page(const PrefixArgs &a, const Piece &p, int j, int lane, int2 &at) {
-    int row = p.shared_row, x, i = 0;
+// The page id (as the table has it: the load is on its way) of copy `lane` of key tile j and the
+// copy's first token in the page; false: the tile has no such copy.
+__device__ __forceinline__ bool copy_page(const PrefixArgs &a, const Piece &p, int j, int lane, int2 &at) {
+    const int log = a.s.slot_log - a.copy_log;  // copies of a slot
     const bool own = j >= p.shared_tiles;
-    x = ((own ? j - p.shared_tiles : j) << a.s.spt_log) + lane;
-    if (lane >= a.s.spt || x >= (own ? p.off[p.r.nb] : p.shared)) return false;
+    int row = p.shared_row, x = ((own ? j - p.shared_tiles : j) << a.s.spt_log) + (lane >> log);
+    if (lane >> log >= a.s.spt || x >= (own ? p.off[p.r.nb] : p.shared)) return false;
     if (own) {
-        i = prefix::slot_owner(p.off, p.r.nb, x);
+        const int i = prefix::slot_owner(p.off, p.r.nb, x);
         x += p.shared - p.off[i];
         row = p.q * a.s.n_branch + p.r.b0 + i;
     }
     at = make_int2(a.table[static_cast<int64_t>(row) * a.s.max_pages + (x >> a.s.sub_log)],
-                   (x & (a.s.sub - 1)) << a.s.slot_log);
+                   ((x & (a.s.sub - 1)) << a.s.slot_log) + ((lane & ((1 << log) - 1)) << a.copy_log));
     return true;
 }
 
@@ -474,13 +479,15 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
 #pragma unroll 1
         for (int j = p.j0; j < p.j1; ++j, ++t) {
             const int s = t % kStages;
-            int2 at = make_int2(a.s.n_pages, 0);
-            const bool there = slot_page(a, p, j, lane, at);
+            int2 at = make_int2(-1, 0);
+            const bool there = copy_page(a, p, j, lane, at);
             if (t >= kStages && !(ok = warp_wait(&empty[s], (t / kStages - 1) & 1, c, a))) break;
-            // (an id outside the cache: n_pages, whose copy is all zeros, as are slots that are not there)
+            // (an id outside the cache: a coordinate whose copy is all zeros, as are copies that are not there)
             const bool bad_page = static_cast<unsigned>(at.x) >= static_cast<unsigned>(a.s.n_pages);
-            if (bad_page) at.x = a.s.n_pages;
-            if (lane < 8) c.slot_at[is_k][lane] = at;
+            if (lane < 16)
+                c.copy_at[is_k][lane] =
+                    a.by_groups ? make_int4(0, bad_page ? a.no_page : at.x * a.page_groups + (at.y >> 3), p.head, 0)
+                                : make_int4(at.y, p.head, bad_page ? a.no_page : at.x, 0);
             if (is_k) {
                 const uint32_t bad = __ballot_sync(kFull, there && bad_page);
                 if (j == p.j0) ++n_q;
@@ -496,14 +503,15 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
             raw0 += raw && s == 0;
             raw1 += raw && s == 1;
             __syncwarp();
-            if (elect_one()) {  // (operands from shared memory: picked out of lanes a copy took a third longer)
+            if (elect_one()) {  // (coordinates from shared memory: picked out of lanes a copy took a third longer)
                 mbar_expect_tx(bar, kTileBytes);
                 uint8_t *dst = stages + s * kTileBytes;
+                int4 at = c.copy_at[is_k][0];
 #pragma unroll 1
-                for (int i = 0; i < a.s.spt; ++i, dst += a.s.slot * 128) {
-                    const int2 slot = c.slot_at[is_k][i];
-                    tma_load_4d(dst, tm, 0, slot.y, p.head, slot.x, bar);
-                    tma_load_4d(dst + kAtom, tm, 64, slot.y, p.head, slot.x, bar);
+                for (int i = 1; i <= prefix::kRows >> a.copy_log; ++i, dst += kGroup / 8 << a.copy_log) {
+                    const int4 next = c.copy_at[is_k][i & 15];
+                    tma_load_5d(dst, tm, 0, at.x, 0, at.y, at.z, bar);
+                    at = next;
                 }
                 if (is_k && j == p.j0) {  // Q: its buffer's last user, piece n - 2, ended at tile t - 2 or before
                     uint64_t *q_full = &c.q_full[n & 1];
@@ -564,9 +572,11 @@ __device__ __forceinline__ void clean(uint8_t *stages, uint32_t tiles, int lane,
             for (uint32_t m = __ballot_sync(kFull, keys > 0 && keys < 16); m; m &= m - 1) {
                 const int kk = __ffs(m) - 1, filled = __shfl_sync(kFull, keys, kk);
 #pragma unroll 1
-                for (int y = lane; y < (16 - filled) * 16; y += 32)  // 8 16-byte units in each of two atoms
-                    st_shared_v4(saddr(vb + (y & 8 ? kAtom : 0) + (kk * 16 + filled + (y >> 4)) * 128 + (y & 7) * 16),
+                for (int y = lane; y < (16 - filled) * 16; y += 32) {  // 8 16-byte units in each of two chunks
+                    const int token = kk * 16 + filled + (y >> 4);
+                    st_shared_v4(saddr(vb + token / 8 * kGroup + (y & 8 ? kChunk : 0) + token % 8 * 128 + (y & 7) * 16),
                                  make_uint4(0, 0, 0, 0));
+                }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -697,8 +707,9 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
         constexpr uint32_t idesc_s = umma::instr_desc_f16(128, 128, fmt, 0);  // K is K-major
         constexpr uint32_t idesc_o = umma::instr_desc_f16(128, 128, fmt, 1);  // V is MN-major
         // (an operand's other buffer, atom or step: its address field moved on)
-        const uint64_t q_desc = umma::smem_desc_kmajor_sw128(saddr(sq)), k_desc = umma::smem_desc_kmajor_sw128(saddr(sk));
-        const uint64_t v_desc = umma::smem_desc_mnmajor_sw128(saddr(sv), kAtom);
+        const uint64_t q_desc = umma::smem_desc_kmajor_sw128(saddr(sq));
+        const uint64_t k_desc = umma::smem_desc_kmajor_sw128(saddr(sk), kGroup);
+        const uint64_t v_desc = umma::smem_desc_mnmajor_sw128(saddr(sv), kChunk, kGroup);
         int sn = -1, s_left = 0;                        // the scores' piece, and its tiles left
         int n = -1, j = 0, j0 = 0, j1 = 0, shared_tiles = 0;  // the product's piece and tile
 #pragma unroll 1
@@ -726,7 +737,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                     const uint32_t more = j - j0 >= kStages;  // the half has had a tile of this piece
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        mma_ts(ocol, pcol + k / 4 * 64 + k % 4 * 8, vd + static_cast<uint64_t>(k * (2048 >> 4)), idesc_o,
+                        mma_ts(ocol, pcol + k / 4 * 64 + k % 4 * 8, vd + static_cast<uint64_t>(k * (2 * kGroup >> 4)), idesc_o,
                                k ? 1u : more);
                 } else {
 #pragma unroll 2
@@ -735,7 +746,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                         const int how = c.step_how[h][k];
                         const uint32_t off[4] = {o.x, o.y, o.z, o.w};
                         if (how)
-                            mma_ts_rows(ocol, pcol + k / 4 * 64 + k % 4 * 8, vd + static_cast<uint64_t>(k) * (2048 >> 4),
+                            mma_ts_rows(ocol, pcol + k / 4 * 64 + k % 4 * 8, vd + static_cast<uint64_t>(k) * (2 * kGroup >> 4),
                                         idesc_o, off, how & kStepAdds);
                     }
                 }
@@ -754,10 +765,9 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                 tc_fence_after();
                 const uint64_t qd = q_desc + (sn & 1 ? kTileBytes >> 4 : 0), kd = k_desc + h * (kTileBytes >> 4);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {  // (16 of the 64 columns of an atom are 32 bytes)
-                    const uint32_t at = k / 4 * (kAtom >> 4) + k % 4 * 2;
-                    mma_ss(tmem + h * 128, qd + at, kd + at, idesc_s, k != 0);
-                }
+                for (int k = 0; k < 8; ++k)  // (16 of the 64 columns of an atom are 32 bytes)
+                    mma_ss(tmem + h * 128, qd + k / 4 * (kAtom >> 4) + k % 4 * 2, kd + k / 4 * (kChunk >> 4) + k % 4 * 2,
+                           idesc_s, k != 0);
                 commit(&c.s_full[h]);
                 --s_left;
             }
@@ -804,7 +814,7 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
             tc_fence_after();
             const uint32_t bad = c.bad[t % 4];
             if (bad && col.lo < col.hi) {  // a page of this row's keys does not exist: NaN
-                const int u0 = col.lo >> a.s.slot_log, u1 = (col.hi - 1) >> a.s.slot_log;
+                const int u0 = col.lo >> a.copy_log, u1 = (col.hi - 1) >> a.copy_log;
                 if (bad >> u0 & low_bits(u1 - u0 + 1)) {
                     l = NAN;
                     col.hi = col.lo;
@@ -1239,24 +1249,55 @@ rps_status setup(int *sms) {
     return RPS_OK;
 }
 
-// A map of 16-bit elements: extents and strides (in elements) from the inner dimension
-// (64-wide boxes of 128 contiguous elements) outwards.
-rps_status map_4d(CUtensorMap *m, const void *base, bool f16, const int64_t (&ext)[3], const int64_t (&stride)[3],
-                  const uint32_t (&box)[3]) {
-    cuuint64_t dims[4] = {kD, 0, 0, 0}, bytes[3];
-    cuuint32_t boxes[4] = {64, 0, 0, 0};
-    const cuuint32_t es[4] = {1, 1, 1, 1};
-    for (int i = 0; i < 3; ++i) {
+// A map of 16-bit elements: extents, strides (in elements) and boxes from the inner dimension
+// (64-wide boxes of kD contiguous elements, or 64) outwards.
+template <int n>
+rps_status make_map(CUtensorMap *m, const void *base, bool f16, int64_t inner, const int64_t (&ext)[n],
+                    const int64_t (&stride)[n], const uint32_t (&box)[n]) {
+    cuuint64_t dims[n + 1] = {static_cast<cuuint64_t>(inner)}, bytes[n];
+    cuuint32_t boxes[n + 1] = {64}, es[n + 1] = {1};
+    for (int i = 0; i < n; ++i) {
         dims[i + 1] = static_cast<cuuint64_t>(ext[i]);
         // (the stride of a dimension of one is not used, but has to be a valid one)
         bytes[i] = static_cast<cuuint64_t>(ext[i] > 1 ? stride[i] : kD) * 2;
         boxes[i + 1] = box[i];
+        es[i + 1] = 1;
     }
-    const CUresult r = g_prefix_encode(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+    const CUresult r = g_prefix_encode(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n + 1,
                                        const_cast<void *>(base), dims, bytes, boxes, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? RPS_OK : RPS_ERR_CUDA;
+}
+
+// The maps of K and V: a copy brings whole groups of 8 tokens, both halves of their columns.
+// Where the pages' stride is a multiple of eight tokens', one dimension goes through the groups
+// of all pages, and a copy takes a slot; else a copy is a group of one page.
+rps_status map_pages(CUtensorMap *tk, CUtensorMap *tv, const rps_kv_cache *kv, int64_t layer_at, bool f16, PrefixArgs &a) {
+    const int64_t groups = kv->page_size / 8, token = kv->token_stride, group = 8 * token;
+    const int64_t per_page = kv->n_pages > 1 ? kv->page_stride / group : groups;
+    const int64_t all = (kv->n_pages - 1) * per_page + groups;
+    const void *const base[2] = {static_cast<char *>(kv->k) + layer_at, static_cast<char *>(kv->v) + layer_at};
+    CUtensorMap *const to[2] = {tk, tv};
+    a.by_groups = (kv->n_pages == 1 || kv->page_stride % group == 0) && all <= INT32_MAX;
+    a.copy_log = a.by_groups ? a.s.slot_log : 3;
+    a.page_groups = a.by_groups ? static_cast<int32_t>(per_page) : 0;
+    a.no_page = a.by_groups ? static_cast<int32_t>(all) : kv->n_pages;
+    for (int i = 0; i < 2; ++i) {
+        rps_status st;
+        if (a.by_groups) {
+            const int64_t ext[4] = {8, 2, all, kv->n_heads}, stride[4] = {token, 64, group, kv->head_stride};
+            const uint32_t box[4] = {8, 2, static_cast<uint32_t>(a.s.slot / 8), 1};
+            st = make_map(to[i], base[i], f16, 64, ext, stride, box);
+        } else {
+            const int64_t ext[4] = {kv->page_size, 2, kv->n_heads, kv->n_pages};
+            const int64_t stride[4] = {token, 64, kv->head_stride, kv->page_stride};
+            const uint32_t box[4] = {8, 2, 1, 1};
+            st = make_map(to[i], base[i], f16, 64, ext, stride, box);
+        }
+        if (st != RPS_OK) return st;
+    }
+    return RPS_OK;
 }
 
 // Shape of a call, with the limits that keep its counts in 32 bits.
@@ -1318,14 +1359,10 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
 
     const bool f16 = kv->dtype == RPS_F16;
     const int64_t kv_at = kv->n_layers > 1 ? p->layer * kv->layer_stride * 2 : 0;
-    const int64_t kext[3] = {kv->page_size, kv->n_heads, kv->n_pages};
-    const int64_t ks[3] = {kv->token_stride, kv->head_stride, kv->page_stride};
     const uint32_t qbox[3] = {static_cast<uint32_t>(a.s.group), static_cast<uint32_t>(a.s.tokens), 1};
-    const uint32_t kbox[3] = {static_cast<uint32_t>(a.s.slot), 1, 1};
     CUtensorMap tq, tk, tv;
-    if ((st = map_4d(&tq, p->q, f16, ext, qs, qbox)) != RPS_OK) return st;
-    if ((st = map_4d(&tk, static_cast<char *>(kv->k) + kv_at, f16, kext, ks, kbox)) != RPS_OK) return st;
-    if ((st = map_4d(&tv, static_cast<char *>(kv->v) + kv_at, f16, kext, ks, kbox)) != RPS_OK) return st;
+    if ((st = make_map(&tq, p->q, f16, kD, ext, qs, qbox)) != RPS_OK) return st;
+    if ((st = map_pages(&tk, &tv, kv, kv_at, f16, a)) != RPS_OK) return st;
     a.table = kv->table;
     a.len = kv->len;
     a.shared_len = p->shared_len;

@@ -58,9 +58,9 @@ UMMA_HD inline constexpr uint64_t smem_desc(uint32_t smem_addr, uint32_t lbo_byt
            (static_cast<uint64_t>(swizzle & 7u) << 61);
 }
 
-// K-major tile of 64 bf16 per row, 128-byte swizzle, 8-row groups 1024 bytes apart.
-UMMA_HD inline constexpr uint64_t smem_desc_kmajor_sw128(uint32_t smem_addr) {
-    return smem_desc(smem_addr, 16, 1024, kSwizzle128B);
+// K-major tile of 64 bf16 per row, 128-byte swizzle, 8-row groups 1024 bytes apart (or `group` bytes).
+UMMA_HD inline constexpr uint64_t smem_desc_kmajor_sw128(uint32_t smem_addr, uint32_t group = 1024) {
+    return smem_desc(smem_addr, 16, group, kSwizzle128B);
 }
 
 // The descriptor of the K slice `k16` (16 bf16 = 32 bytes further per slice).
@@ -68,11 +68,11 @@ UMMA_HD inline constexpr uint64_t advance_k16(uint64_t desc, uint32_t k16) { ret
 
 // MN-major tile, 128-byte swizzle: a row holds 64 elements of the M or N
 // dimension of one K index, rows follow each other at 128 bytes, so eight K
-// indexes form a 1024-byte atom and the next eight lie 1024 bytes on (the
-// stride-dimension offset); the next 64 elements of M or N are `chunk` bytes away
-// (the leading-dimension offset). 16 K indexes further: 2048 bytes.
-UMMA_HD inline constexpr uint64_t smem_desc_mnmajor_sw128(uint32_t smem_addr, uint32_t chunk) {
-    return smem_desc(smem_addr, chunk, 1024, kSwizzle128B);
+// indexes form a 1024-byte atom; the next eight lie `group` bytes on (the
+// stride-dimension offset), the next 64 elements of M or N `chunk` bytes (the
+// leading-dimension offset).
+UMMA_HD inline constexpr uint64_t smem_desc_mnmajor_sw128(uint32_t smem_addr, uint32_t chunk, uint32_t group) {
+    return smem_desc(smem_addr, chunk, group, kSwizzle128B);
 }
 
 }  // namespace umma

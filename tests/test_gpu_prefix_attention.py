@@ -176,6 +176,32 @@ def test_types_layers_and_layouts(dtype, tokens_first):
     assert bool((wide[..., 2 * D:] == 7.0).all()) and torch.equal(view(wide, 0).cpu(), c.q)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("ps", [16, 64, 256])
+def test_pages_at_odd_strides(ps, dtype):
+    """Pages whose distance is no multiple of eight tokens', and one that is, with tokens wider than they are read;
+    a page id outside the cache among them."""
+    for pad, extra in ((1, 0), (0, 8), (3, 8)):
+        c = Case(24, [[90, 77, 300], [64, 513, 1]], [64, 0], 3, 6, 3, ps, dtype, True)
+        for name in ("k", "v"):
+            t = getattr(c.kv, name)
+            layers, pages, heads = t.shape[:3]
+            to = torch.full((layers, pages, heads * ps + pad, D + extra), float("nan"), dtype=dtype, device="cuda")
+            view = to[:, :, :heads * ps].view(layers, pages, heads, ps, D + extra)[..., :D] if pad == 0 else to.as_strided(
+                t.shape, (to.stride(0), to.stride(1), ps * (D + extra), D + extra, 1))
+            view.copy_(t)
+            setattr(c.kv, name, view)
+        c.check(*c.run())
+        whole = c.run()
+        c.kv.table[1, 1, 0] = c.kv.k.shape[1] + 5
+        out, lse = c.run()[:2]
+        assert rps.rps_poll_device_status() == (rps.RPS_ERR_DEVICE, rps.DEVERR_PAGE)
+        assert bool(torch.isnan(out[1, 1]).all()) and bool(torch.isnan(lse[1, 1]).all())
+        keep = torch.ones((2, 3), dtype=torch.bool)
+        keep[1, 1] = False
+        assert torch.equal(out[keep], whole[0][keep])
+
+
 def test_causal_rows_longer_than_the_sequence():
     """n_q beyond a sequence's length: the first queries see nothing, their rows are zero."""
     c = Case(23, [[5, 130, 20]], [0], 24, 2, 1, 16, causal=True)
