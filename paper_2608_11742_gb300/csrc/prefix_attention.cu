@@ -72,6 +72,7 @@ namespace {
 using prefix::KeySum;
 using prefix::RowTile;
 using prefix::Shape;
+using prefix::Tiles;
 
 constexpr int kD = 128;                // head dimension
 constexpr int kAtom = 64 * 128 * 2;    // one 128-row x 64-column swizzle atom of 16-bit elements: 16 KB
@@ -97,6 +98,7 @@ constexpr int kStepAdds = 32;
 // memory where they fit (64 sequences of one prompt: 31 us instead of 33.7).
 constexpr int kStagedLens = 512;
 constexpr int kStagedTiles = 512;
+constexpr uint32_t kNoEnd = 1u << 31;  // tiles of the CTA, until its last piece is known
 constexpr int kMaxReqs = 2 * kStages * kTileBytes / 8;  // requests whose first tiles fit the K and V stages
 constexpr float kLn2 = 0.6931471805599453f;
 // bounds of a tile's sum of P in a row (in units of its reference): P in fp16 stays finite
@@ -135,6 +137,7 @@ struct Piece {
     RowTile r;
     int32_t j0, j1, shared, shared_tiles, shared_row;  // shared slots; whose table row names their pages
     int32_t part;                                      // -1: the whole row tile, else which partial result
+    int32_t last;                                      // of the CTA
     int32_t off[kMaxSeqs + 1], len[kMaxSeqs];
 };
 
@@ -158,8 +161,7 @@ struct Ctl {
     uint32_t bad[4];  // copies of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
     int32_t len[kStagedLens];      // as they are used
-    int32_t tiles_of[kStagedTiles];  // key tiles of (request, row tile)
-    int32_t longest, empty, own;  // key tiles of the longest row tile; one has none; those of the CTA's own
+    int32_t longest, empty;  // cost of the most expensive row tile; one has no key tile
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -210,7 +212,7 @@ __device__ __forceinline__ int len_of(const PrefixArgs &a, int s, const Ctl &c) 
 __device__ __forceinline__ int shared_len_of(const PrefixArgs &a, int q) { return a.shared_len ? a.shared_len[q] : 0; }
 
 // Key tiles of row tile rt of request q, by one thread.
-__device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int q, int rt, int shared_len, const Ctl &c) {
+__device__ __forceinline__ Tiles entry_tiles(const PrefixArgs &a, int q, int rt, int shared_len, const Ctl &c) {
     const RowTile r = prefix::row_tile(a.s, rt);
     KeySum k{0, 0, INT32_MAX};
     const int s0 = q * a.s.n_branch + r.b0;
@@ -223,9 +225,14 @@ __device__ __forceinline__ int entry_tiles(const PrefixArgs &a, int q, int rt, i
     }
     return prefix::key_tiles(a.s, k, prefix::shared_slots(a.s, k, shared_len));
 }
-// The same in find_range's wake: looked up where it was kept.
-__device__ __forceinline__ int known_tiles(const PrefixArgs &a, int q, int rt, const Ctl &c) {
-    return a.s.n_req * a.s.row_tiles <= kStagedTiles ? c.tiles_of[q * a.s.row_tiles + rt]
+// What find_range leaves for find_start, in the buffers of Q, K and V, which nothing uses before the
+// first piece is known.
+struct Plan {
+    int64_t *first;  // costs (of one head: all heads of a request have the same) of the requests before q
+    Tiles *tiles;    // of (request, row tile), where they are kept
+};
+__device__ __forceinline__ Tiles known_tiles(const PrefixArgs &a, int q, int rt, const Plan &plan, const Ctl &c) {
+    return a.s.n_req * a.s.row_tiles <= kStagedTiles ? plan.tiles[q * a.s.row_tiles + rt]
                                                      : entry_tiles(a, q, rt, shared_len_of(a, q), c);
 }
 
@@ -251,23 +258,22 @@ __device__ __forceinline__ int64_t scan_block(int v, int64_t *sums, int64_t *tot
     return before + x - v;
 }
 
-// The CTA's range of key tiles, of those of all (request, head, row tile) in order; or
-// (whole) its one row tile.
+// The CTA's range of the costs of all (request, head, row tile) in order (at == end: it has
+// nothing to do); or (whole) its one row tile.
 struct Range {
     int64_t at, end;
     prefix::Ranges all;
     bool whole;
 };
 // Cutting a row tile costs what its parts take to be written and joined, about as much as
-// three key tiles: where every row tile has a CTA of its own and none is longer by more than
-// that than the equal shares, none is cut (one request's 9 branches of 32, 32 heads, context
+// three own tiles: where every row tile has a CTA of its own and none costs by more than
+// that more than the equal shares, none is cut (one request's 9 branches of 32, 32 heads, context
 // 328: 96 row tiles of 4 to 5 key tiles instead of shares of 3: 17 us instead of 21; one query of 32
 // heads over 1000 keys, which are worth cutting: 18 instead of 19.6).
-constexpr int kCutTiles = 3;
+constexpr int kCutCost = 3 * prefix::kOwnCost;
 
-// By all threads: the lengths into shared memory, and in first[q] the key tiles (of
-// one head: all heads of a request have the same) of the requests before q.
-__device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t *first) {
+// By all threads: the lengths into shared memory, and the plan.
+__device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, const Plan &plan) {
     const int entries = a.s.n_req * a.s.row_tiles, n_seq = a.s.n_req * a.s.n_branch;
     if (n_seq <= kStagedLens)
 #pragma unroll 1
@@ -277,34 +283,34 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
     int next_shared = shared_len_of(a, min(prefix::quotient(threadIdx.x, a.s.by_row_tiles), a.s.n_req - 1));
     __syncthreads();
     const bool few = static_cast<int64_t>(entries) * a.s.heads <= gridDim.x;  // (at most one block of entries then)
-    const int mine = few ? prefix::quotient(blockIdx.x, a.s.by_row_tiles) : 0;  // request and head of the CTA's own
-    const int mine_q = mine / a.s.heads;
     int64_t carry = 0;
 #pragma unroll 1
     for (int base = 0; base < entries; base += kThreads) {
         const int e = base + threadIdx.x;
         const int q = prefix::quotient(e, a.s.by_row_tiles), rt = e - q * a.s.row_tiles;
         int64_t total;
-        const int t = e < entries ? entry_tiles(a, q, rt, next_shared, c) : 0;
-        if (entries <= kStagedTiles && e < entries) c.tiles_of[e] = t;
+        Tiles t{0, 0};
+        if (e < entries) t = entry_tiles(a, q, rt, next_shared, c);
+        const int cost = prefix::cost_of(t);
+        if (entries <= kStagedTiles && e < entries) plan.tiles[e] = t;
         if (base + kThreads < entries)
             next_shared = shared_len_of(a, min(prefix::quotient(e + kThreads, a.s.by_row_tiles), a.s.n_req - 1));
         if (few && e < entries) {
-            if (t == 0) c.empty = 1;
-            atomicMax(&c.longest, t);
-            if (q == mine_q && rt == static_cast<int>(blockIdx.x) - mine * a.s.row_tiles) c.own = t;
+            if (cost == 0) c.empty = 1;
+            atomicMax(&c.longest, cost);
         }
-        const int64_t before = carry + scan_block(t, c.scan, &total);
-        if (e < entries && rt == 0) first[q] = before;
+        const int64_t before = carry + scan_block(cost, c.scan, &total);
+        if (e < entries && rt == 0) plan.first[q] = before;
         carry += total;
     }
     Range r{};
     const int64_t work = carry * a.s.heads;
-    // (no more CTAs than key tiles: none in between is without work)
-    const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), work));
-    if (few && !c.empty && static_cast<int64_t>(c.longest - kCutTiles) * n <= work) {
+    // (no more CTAs than have a tile each: none in between is without work)
+    const int64_t most = work / prefix::kWidest;
+    const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), most > 0 ? most : static_cast<int64_t>(work > 0)));
+    if (few && !c.empty && static_cast<int64_t>(c.longest - kCutCost) * n <= work) {
         r.whole = true;
-        r.end = static_cast<int>(blockIdx.x) < entries * a.s.heads ? c.own : 0;
+        r.end = static_cast<int>(blockIdx.x) < entries * a.s.heads ? 1 : 0;
         return r;
     }
     if (static_cast<int>(blockIdx.x) >= n) return r;
@@ -316,10 +322,11 @@ __device__ __forceinline__ Range find_range(const PrefixArgs &a, Ctl &c, int64_t
 
 // By a warp: the request, head, row tile and key tile that the range begins with.
 struct Start {
-    int32_t q, head, rt, j;
-    int32_t tiles, next;  // key tiles of the row tile and of the next of the head (0: none, or not known)
+    int32_t q, head, rt, j;  // (j past the row tile's last tile: the range begins with the next row tile)
+    int64_t base;            // costs before the row tile
+    Tiles tiles, next;       // of the row tile and of the next of the head (none, or not known: 0)
 };
-__device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &range, const int64_t *first, int lane,
+__device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &range, const Plan &plan, int lane,
                                             const Ctl &c) {
     Start st{};
     if (range.whole) {
@@ -333,21 +340,23 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &ra
 #pragma unroll 1
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (first[mid] * a.s.heads <= range.at)
+        if (plan.first[mid] * a.s.heads <= range.at)
             lo = mid;
         else
             hi = mid;
     }
     st.q = lo;
-    int64_t rem = range.at - first[lo] * a.s.heads;  // tiles of the request before the range
+    int64_t rem = range.at - plan.first[lo] * a.s.heads;  // cost of the request before the range
     int64_t per_head = 0;
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {  // the tiles of a head; then where the rest lies in them
+    for (int pass = 0; pass < 2; ++pass) {  // the cost of a head; then where the rest lies in it
         int64_t before = 0;
 #pragma unroll 1
         for (int base = 0; base < a.s.row_tiles; base += 32) {
-            const int t = base + lane < a.s.row_tiles ? known_tiles(a, st.q, base + lane, c) : 0;
-            int upto = t;
+            Tiles t{0, 0};
+            if (base + lane < a.s.row_tiles) t = known_tiles(a, st.q, base + lane, plan, c);
+            const int cost = prefix::cost_of(t);
+            int upto = cost;
 #pragma unroll 1
             for (int o = 1; o < 32; o <<= 1) {
                 const int u = __shfl_up_sync(kFull, upto, o);
@@ -357,10 +366,15 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &ra
                 const uint32_t in = __ballot_sync(kFull, rem < before + upto);
                 if (in) {
                     const int who = __ffs(in) - 1;
+                    const int64_t y = rem - before - __shfl_sync(kFull, upto - cost, who);
                     st.rt = base + who;
-                    st.j = static_cast<int>(rem - before) - __shfl_sync(kFull, upto - t, who);
-                    st.tiles = __shfl_sync(kFull, t, who);
-                    st.next = who < 31 ? __shfl_sync(kFull, t, who + 1) : 0;
+                    st.tiles.shared = __shfl_sync(kFull, t.shared, who);
+                    st.tiles.own = __shfl_sync(kFull, t.own, who);
+                    st.next.shared = __shfl_sync(kFull, t.shared, (who + 1) & 31);
+                    st.next.own = __shfl_sync(kFull, t.own, (who + 1) & 31);
+                    if (who == 31) st.next.shared = st.next.own = 0;
+                    st.j = prefix::reach(st.tiles, y);
+                    st.base = range.at - y;
                     break;
                 }
             }
@@ -385,8 +399,8 @@ __device__ __forceinline__ Start find_start(const PrefixArgs &a, const Range &ra
 }
 
 // Row tile rt of request q, by a warp: sequences' lengths and own slots into `p`;
-// returns its number of key tiles (0: no sequence there, `p` is not complete).
-__device__ __forceinline__ int fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, const Ctl &c, Piece &p) {
+// returns its key tiles (none: no sequence there, `p` is not complete).
+__device__ __forceinline__ Tiles fill_row_tile(const PrefixArgs &a, int q, int rt, int lane, const Ctl &c, Piece &p) {
     const RowTile r = prefix::row_tile(a.s, rt);
     const int s0 = q * a.s.n_branch + r.b0;
     KeySum k{0, 0, INT32_MAX};
@@ -404,8 +418,8 @@ __device__ __forceinline__ int fill_row_tile(const PrefixArgs &a, int q, int rt,
     k.min_pages = __reduce_min_sync(kFull, k.min_pages);
     first = __reduce_min_sync(kFull, first);
     const int shared = prefix::shared_slots(a.s, k, shared_len);
-    const int tiles = prefix::key_tiles(a.s, k, shared);
-    if (tiles == 0) return 0;
+    const Tiles tiles = prefix::key_tiles(a.s, k, shared);
+    if (!k.present) return tiles;
     int before = 0;
 #pragma unroll 1
     for (int base = 0; base < r.nb; base += 32) {
@@ -426,7 +440,7 @@ __device__ __forceinline__ int fill_row_tile(const PrefixArgs &a, int q, int rt,
         p.rt = rt;
         p.r = r;
         p.shared = shared;
-        p.shared_tiles = prefix::tiles_of(a.s, shared);
+        p.shared_tiles = tiles.shared;
         p.shared_row = s0 + first;
     }
     return tiles;
@@ -476,6 +490,7 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
         const Piece *pp = next_piece(n, c, a);
         if (!pp) break;
         const Piece &p = *pp;
+        if (p.last) tiles = t + p.j1 - p.j0;
 #pragma unroll 1
         for (int j = p.j0; j < p.j1; ++j, ++t) {
             const int s = t % kStages;
@@ -552,6 +567,7 @@ __device__ __forceinline__ void clean(uint8_t *stages, uint32_t tiles, int lane,
         const Piece *pp = next_piece(n, c, a);
         if (!pp) return;
         const Piece &p = *pp;
+        if (p.last) tiles = t0 + p.j1 - p.j0;
 #pragma unroll 1
         for (int j = max(p.j0, p.shared_tiles); j < p.j1; ++j) {
             const int s = (t0 + j - p.j0) % kStages;
@@ -590,97 +606,108 @@ __device__ __forceinline__ void clean(uint8_t *stages, uint32_t tiles, int lane,
 // The scheduler: one warp hands out the pieces of the CTA's range, one per call.
 struct Schedule {
     Start st;
-    int q, head, rt, j, n, cut_at, turn;
-    int64_t at, end;
-    bool swapped, any;  // any: the request has a key tile at all
+    int q, head, rt, j, n;
+    int64_t base, end;       // costs before the row tile, and the range's end
+    int cost;                // of the row tile
+    bool swapped, any, done; // swapped: the second of two row tiles comes first; any: the request has a key tile at all
+    bool leave;              // the row tile, at the next call
 };
 
-__device__ __forceinline__ void schedule_part(Schedule &z, const Range &range) {
-    const bool second = z.swapped && z.turn == 0;
-    z.q = z.st.q;
-    z.head = z.st.head;
-    z.rt = z.st.rt + second;
-    z.j = second ? 0 : z.st.j;
-    z.at = range.at + (second ? z.cut_at : 0);
-    z.end = z.swapped && z.turn == 1 ? range.at + z.cut_at : range.end;
-    z.any = true;
-}
-
-__device__ __forceinline__ Schedule schedule_start(const PrefixArgs &a, const Range &range, const int64_t *first, int lane,
+__device__ __forceinline__ Schedule schedule_start(const PrefixArgs &a, const Range &range, const Plan &plan, int lane,
                                                    Ctl &c) {
     Schedule z;
-    z.st = find_start(a, range, first, lane, c);
-    // (`first` lies in the K and V stages: the copies that follow the first piece come after its reads)
+    z.st = find_start(a, range, plan, lane, c);
+    // (the plan lies where Q, K and V go: the copies that follow the first piece come after its reads)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    z.q = z.st.q;
+    z.head = z.st.head;
+    z.rt = z.st.rt;
+    z.j = z.st.j;
+    z.n = 0;
+    z.base = z.st.base;
+    z.end = range.end;
+    z.cost = 0;
+    z.swapped = z.leave = false;
+    z.any = true;
+    z.done = range.at == range.end;
     // A range that ends one row tile and begins the next of the same head is taken in the
     // other order: all CTAs of the head are then near the same keys at the same time,
     // which L2 holds, instead of all over them (2 requests, 28/4 heads, context 28000: the keys
     // were read from HBM seven times).
-    z.turn = 1;
-    z.cut_at = z.n = 0;
-    if (z.st.j > 0) {
-        z.cut_at = z.st.tiles - z.st.j;  // tiles up to the next row tile
-        const int64_t rest = range.end - range.at - z.cut_at;
-        if (rest > 0 && rest < z.st.next) z.turn = 0;
+    const Tiles &t = z.st.tiles, &next = z.st.next;
+    if (z.j > 0 && z.j < t.shared + t.own) {
+        const int64_t after = z.base + prefix::cost_of(t);
+        const int rest = prefix::reach(next, z.end - after);
+        if (rest > 0 && rest < next.shared + next.own) {
+            z.swapped = true;
+            z.base = after;
+            ++z.rt;
+            z.j = 0;
+        }
     }
-    z.swapped = z.turn == 0;
-    schedule_part(z, range);
     return z;
 }
 
 // The next piece into the ring; false: there is none, or the wait for its slot ran out.
 __device__ __forceinline__ bool schedule_next(Schedule &z, const PrefixArgs &a, const Range &range, int lane, Ctl &c) {
-    if (z.at >= z.end) {
-        if (++z.turn >= 2) return false;
-        schedule_part(z, range);
-    }
+    if (z.done) return false;
     const int slot = z.n % kRing;
     if (z.n >= kRing && !warp_wait(&c.ring_empty[slot], (z.n / kRing - 1) & 1, c, a)) return false;
     Piece &p = c.ring[slot];
-    int tiles = 0;
+    Tiles t;
+    int tiles;
 #pragma unroll 1
     for (;;) {
-        tiles = fill_row_tile(a, z.q, z.rt, lane, c, p);
-        z.any |= tiles > 0;
-        if (tiles > 0) break;
-        if (++z.rt == a.s.row_tiles) {
-            z.rt = 0;
-            if (!z.any || ++z.head == a.s.heads) {
-                z.head = 0;
-                ++z.q;
+        if (z.leave) {
+            z.base += z.cost;
+            z.j = 0;
+            if (++z.rt == a.s.row_tiles) {
+                z.rt = 0;
+                if (!z.any || ++z.head == a.s.heads) {
+                    z.head = 0;
+                    ++z.q;
+                }
+                z.any = false;
             }
-            z.any = false;
         }
-        if (z.q >= a.s.n_req) return false;  // (not reached while the lengths stay as they are during the call)
+        z.done = z.q >= a.s.n_req;  // (not reached while the lengths stay as they are during the call)
+        if (z.done) return false;
+        z.leave = true;
+        t = fill_row_tile(a, z.q, z.rt, lane, c, p);
+        z.cost = prefix::cost_of(t);
+        tiles = t.shared + t.own;
+        z.any |= tiles > 0;
+        if (tiles > z.j) break;
     }
-    if (z.j >= tiles) return false;          // (nor this)
-    const int j1 = static_cast<int>(min(static_cast<int64_t>(tiles), z.j + (z.end - z.at)));
+    const int64_t left = z.end - z.base;  // of the range, from the row tile's begin
+    const int j1 = range.whole ? tiles : prefix::reach(t, left);
+    const bool first_of_two = z.swapped && z.rt != z.st.rt;
+    const bool last = !first_of_two && (range.whole || z.swapped || left - z.cost < prefix::kFirstPlace);
+    z.done = last || j1 <= z.j;
+    if (j1 <= z.j) return false;  // (nor this)
     if (lane == 0) {
         p.head = z.head;
         p.j0 = z.j;
         p.j1 = j1;
         p.part = z.j == 0 && j1 == tiles ? -1 : z.j > 0 ? 0 : 1;
+        p.last = last;
         const int tile = (z.q * a.s.heads + z.head) * a.s.row_tiles + z.rt;
         if (p.part == 1) {
-            const int last = prefix::cta_of(range.all, z.at + tiles - 1);
+            const int to = prefix::cta_of(range.all, z.base + prefix::place(t, tiles - 1) - 1);
             a.cut[a.by_tile ? tile : static_cast<int>(blockIdx.x)] =
-                Cut{last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), z.q, z.head, z.rt};
+                Cut{to - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), z.q, z.head, z.rt};
         } else if (p.part < 0 && a.by_tile) {
             a.cut[tile].parts = 0;
         }
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&c.ring_full[slot]);
-    z.at += j1 - z.j;
-    z.j = 0;
     ++z.n;
-    if (++z.rt == a.s.row_tiles) {
-        z.rt = 0;
-        if (++z.head == a.s.heads) {
-            z.head = 0;
-            ++z.q;
-            z.any = false;
-        }
+    if (first_of_two) {
+        z.rt = z.st.rt;
+        z.j = z.st.j;
+        z.base = z.st.base;
+        z.leave = false;
     }
     return true;
 }
@@ -712,12 +739,14 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
         const uint64_t v_desc = umma::smem_desc_mnmajor_sw128(saddr(sv), kChunk, kGroup);
         int sn = -1, s_left = 0;                        // the scores' piece, and its tiles left
         int n = -1, j = 0, j0 = 0, j1 = 0, shared_tiles = 0;  // the product's piece and tile
+        bool s_more = tiles > 0, s_last = false, last = false;
 #pragma unroll 1
-        for (uint32_t x = 0; x < tiles + kStages; ++x) {  // the product of tile x - 2, then the scores of tile x
+        for (uint32_t x = 0; tiles; ++x) {  // the product of tile x - 2, then the scores of tile x
             const uint32_t h = x % kStages, parity = (x / kStages) & 1;
             if (x >= kStages) {
                 if (j == j1) {
                     if (n >= 0) mbar_arrive(&c.ring_empty[n % kRing]);
+                    if (last) break;
                     ++n;
                     const Piece &p = c.ring[n % kRing];
                     // the first product of a piece overwrites O: the previous piece's read-out must be done
@@ -727,6 +756,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                     j = j0 = p.j0;
                     j1 = p.j1;
                     shared_tiles = p.shared_tiles;
+                    last = p.last;
                 }
                 if (!lane_wait(&c.p_full[h], parity ^ 1, c, a)) break;  // P, and V (see the softmax)
                 tc_fence_after();
@@ -753,13 +783,14 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                 commit(&c.v_empty[h]);
                 if (++j == j1) commit(&c.o_ready);  // the piece's O is complete
             }
-            if (x < tiles) {
+            if (s_more) {
                 if (s_left == 0) {
                     ++sn;
                     if (!lane_wait(&c.ring_full[sn % kRing], (sn / kRing) & 1, c, a) ||
                         !lane_wait(&c.q_full[sn & 1], (sn >> 1) & 1, c, a))
                         break;
                     s_left = c.ring[sn % kRing].j1 - c.ring[sn % kRing].j0;
+                    s_last = c.ring[sn % kRing].last;
                 }
                 if (!lane_wait(&c.k_full[h], parity, c, a)) break;
                 tc_fence_after();
@@ -769,7 +800,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                     mma_ss(tmem + h * 128, qd + k / 4 * (kAtom >> 4) + k % 4 * 2, kd + k / 4 * (kChunk >> 4) + k % 4 * 2,
                            idesc_s, k != 0);
                 commit(&c.s_full[h]);
-                --s_left;
+                if (--s_left == 0 && s_last) s_more = false;
             }
         }
         commit(&c.mma_done);
@@ -803,6 +834,7 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
         }
         float m = kF16 ? -INFINITY : 0.f, l = 0.f;
         const int count = p.j1 - p.j0, x0 = (h ^ static_cast<int>(t0)) & 1;
+        if (p.last) tiles = t0 + count;
         for (int x = x0; x < count; x += kStages) {
             const uint32_t t = t0 + x;
             const int j = p.j0 + x;
@@ -948,11 +980,11 @@ __device__ __forceinline__ void store_stage(uint32_t stage, int lane, uint64_t r
 // of the next piece wait for it.
 template <bool kF16>
 __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_t stage, uint32_t tiles, const Range &range,
-                                         const int64_t *first, Ctl &c, const PrefixArgs &a) {
+                                         const Plan &plan, Ctl &c, const PrefixArgs &a) {
     uint32_t t0 = 0;
     Schedule z;
     const bool scheduler = q == 0;
-    if (scheduler) z = schedule_start(a, range, first, lane, c);
+    if (scheduler) z = schedule_start(a, range, plan, lane, c);
     const int r = q * 32 + lane, tok = prefix::quotient(r, a.s.by_group);
     const uint32_t col = tmem + (static_cast<uint32_t>(q * 32) << 16) + kOCol;
 #pragma unroll 1
@@ -965,6 +997,7 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
         if (!pp) return;
         const Piece &p = *pp;
         const int count = p.j1 - p.j0;
+        if (p.last) tiles = t0 + count;
         const bool whole = p.part < 0;
         uint64_t row = 0;  // where this thread's row goes, 0: nowhere
         float *lse = nullptr;
@@ -1097,15 +1130,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     pdl_wait();
     pdl_launch_next();
     if (threadIdx.x == 0 && !a.by_tile) a.cut[blockIdx.x].parts = 0;
-    int64_t *first = reinterpret_cast<int64_t *>(sk);
-    const Range range = find_range(a, c, first);
-    // (`first` lies in the K and V stages: the copies that follow are ordered after its writes)
+    const Plan plan{reinterpret_cast<int64_t *>(sk), reinterpret_cast<Tiles *>(sq)};
+    const Range range = find_range(a, c, plan);
+    // (the copies that follow are ordered after the plan's writes)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = c.tmem_base;
-    const uint32_t tiles = static_cast<uint32_t>(range.end - range.at);
+    const uint32_t tiles = range.at < range.end ? kNoEnd : 0;  // (each role learns the end from its last piece)
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCtlRegs));
@@ -1120,7 +1153,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         softmax<kF16>(tmem, warp & 3, lane, (warp >> 2) - 1, tiles, c, a);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kOutRegs));
-        if (tiles) read_out<kF16>(tmem, warp & 3, lane, saddr(so + (warp - 12) * kStageBytes), tiles, range, first, c, a);
+        if (tiles) read_out<kF16>(tmem, warp & 3, lane, saddr(so + (warp - 12) * kStageBytes), tiles, range, plan, c, a);
     }
     tc_fence_before();
     __syncthreads();

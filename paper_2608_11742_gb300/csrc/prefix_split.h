@@ -9,9 +9,10 @@
 // shared slots (the leading pages that all its sequences hold), then those of its
 // sequences' own slots, one sequence after another with no gap (a sequence's last
 // slot may be partly filled).
-// Work. Key tiles are numbered through (request, head, row tile, key tile), and
-// the n <= W CTAs take equal parts (to one tile) of the W of them, so a row tile may
-// be spread over several CTAs, whose partial results are joined afterwards.
+// Work. Row tiles are numbered through (request, head, row tile) and have costs: so much
+// for the row tile and so much for each of its key tiles. The n CTAs take equal parts
+// (to one tile) of the sum of the costs, so a row tile may be spread over several
+// CTAs, whose partial results are joined afterwards.
 #pragma once
 
 #include <stdint.h>
@@ -123,14 +124,46 @@ PREFIX_HD int shared_slots(const Shape &s, const KeySum &k, int shared_len) {
     return k.present ? imin(imax(0, shared_len) >> s.page_log, k.min_pages) << s.sub_log : 0;
 }
 // Key tiles: none where no sequence is there, at least one else (rows that see nothing are written too).
-PREFIX_HD int key_tiles(const Shape &s, const KeySum &k, int shared) {
-    if (!k.present) return 0;
-    const int own = k.slots - k.present * shared;
-    return imax(1, tiles_of(s, shared) + tiles_of(s, own));
+struct Tiles {
+    int32_t shared, own;
+};
+PREFIX_HD Tiles key_tiles(const Shape &s, const KeySum &k, int shared) {
+    Tiles t;
+    t.shared = t.own = 0;
+    if (!k.present) return t;
+    t.shared = tiles_of(s, shared);
+    t.own = tiles_of(s, k.slots - k.present * shared);
+    if (t.shared + t.own == 0) t.own = 1;
+    return t;
 }
 
-// The n CTAs' ranges: `base` tiles each, the first `extra` one more. (By 16-bit digits:
-// n is small.)
+// Costs, in quarters of a shared tile's 1740 cycles: an own tile takes 2500 (its product writes the
+// rows of one sequence at a time), the change from a row tile to the next 2800 (the product
+// waits for the read-out).
+constexpr int kSharedCost = 4, kOwnCost = 6, kRowCost = 6;
+PREFIX_HD int cost_of(Tiles t) {
+    return t.shared + t.own ? kRowCost + kSharedCost * t.shared + kOwnCost * t.own : 0;
+}
+// Where a row tile's tiles lie in its costs: tile k belongs to the range (y0, y1] that holds place(t, k),
+// the middle of its cost (of the first one's and the row tile's). No two neighbours, of the next row tile
+// too, are more than kWidest apart.
+constexpr int kFirstPlace = 5, kWidest = 12;
+PREFIX_HD int place(Tiles t, int k) {
+    if (k == 0) return kFirstPlace;
+    return kRowCost + (k < t.shared ? kSharedCost * k + kSharedCost / 2
+                                    : kSharedCost * t.shared + kOwnCost * (k - t.shared) + kOwnCost / 2);
+}
+// The tiles whose places are at most y.
+PREFIX_HD int reach(Tiles t, int64_t y) {
+    if (y < kFirstPlace || t.shared + t.own == 0) return 0;
+    if (y >= cost_of(t)) return t.shared + t.own;
+    const int x = static_cast<int>(y) - kRowCost, own = x - kSharedCost * t.shared;
+    const int k = own < 0 ? (x + kSharedCost / 2) / kSharedCost : t.shared + (own + kOwnCost / 2) / kOwnCost;
+    return imax(1, imin(k, t.shared + t.own));
+}
+
+// The n CTAs' ranges of the costs: `base` each, the first `extra` one more. (By 16-bit digits:
+// n is small.) A CTA whose range is at least kWidest long has a tile.
 struct Ranges {
     int64_t base;
     int32_t extra, n;
@@ -152,7 +185,7 @@ PREFIX_HD Ranges make_ranges(int64_t work, int n) {
     return r;
 }
 PREFIX_HD int64_t range_start(const Ranges &r, int c) { return c * r.base + imin(c, r.extra); }
-// The CTA that takes tile x.
+// The CTA in whose range [start, ..) x lies.
 PREFIX_HD int cta_of(const Ranges &r, int64_t x) {
     int lo = 0, hi = r.n;
 #pragma unroll 1

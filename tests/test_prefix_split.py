@@ -23,7 +23,7 @@ using namespace rps::prefix;
 
 int main(int argc, char **argv) {
     const int trial = -1;
-    for (int d = 1; d < 5000; d += 1 + d / 50) {
+    for (int d = 1; d < 5000; d += 1 + d / 9) {
         const Div v = make_div(d);
         for (int64_t n = 0; n < (int64_t{1} << 31); n += 1 + n / 40 + d / 3)
             for (int64_t m = n - 1; m <= n + 1; ++m)
@@ -46,7 +46,7 @@ int main(int argc, char **argv) {
         if (rnd(0, 2) == 0) for (auto &x : len) x = x % 40;
         for (auto &x : len) x = used_len(s, x);
         // the whole work, as the CTAs walk it
-        struct Tile { int q, rt; int64_t start; int tiles; };
+        struct Tile { int q, rt; int64_t start; Tiles t; int tiles; };
         std::vector<Tile> all;
         int64_t work = 0;
         for (int q = 0; q < n_req; ++q)
@@ -55,11 +55,11 @@ int main(int argc, char **argv) {
                     const RowTile r = row_tile(s, rt);
                     KeySum k{0, 0, 1 << 30};
                     for (int i = 0; i < r.nb; ++i) add_sequence(s, k, len[q * nb + r.b0 + i]);
-                    const int t = key_tiles(s, k, shared_slots(s, k, shared_len[q]));
-                    all.push_back({q, rt, work, t});
-                    work += t;
+                    const Tiles t = key_tiles(s, k, shared_slots(s, k, shared_len[q]));
+                    all.push_back({q, rt, work, t, t.shared + t.own});
+                    work += cost_of(t);
                 }
-        const int n = static_cast<int>(std::min<int64_t>(rnd(1, 160), std::max<int64_t>(1, work)));
+        const int n = static_cast<int>(std::min<int64_t>(rnd(1, 160), std::max<int64_t>(1, work / kWidest)));
         if (!work) continue;
         const Ranges ranges = make_ranges(work, n);
         CHECK(ranges.base == work / n && ranges.extra == work % n);
@@ -69,21 +69,35 @@ int main(int argc, char **argv) {
         for (int c = 0; c < n; ++c) sum += range_start(c + 1, work, n) - range_start(c, work, n);
         CHECK(sum == work);
         for (int c = 0; c < n && work; ++c) CHECK(range_start(c + 1, work, n) > range_start(c, work, n));
-        std::vector<int> covered(n_req * s.row_tiles, 0);
+        std::vector<int> covered(n_req * s.row_tiles, 0), taken(n, 0);
+        int64_t before = -1;  // place of the tile before
         for (const Tile &x : all) {
+            CHECK(cost_of(x.t) == (x.tiles ? kRowCost + kSharedCost * x.t.shared + kOwnCost * x.t.own : 0));
             if (!x.tiles) continue;
+            for (int k = 0; k < x.tiles; ++k) {
+                const int64_t at = x.start + place(x.t, k);
+                CHECK(at > before && at - before <= kWidest && place(x.t, k) < cost_of(x.t));
+                CHECK(reach(x.t, place(x.t, k)) == k + 1 && reach(x.t, place(x.t, k) - 1) == k);
+                before = at;
+            }
+            CHECK(reach(x.t, -1000) == 0 && reach(x.t, 0) == 0 && reach(x.t, cost_of(x.t)) == x.tiles);
+            CHECK(reach(x.t, int64_t{1} << 60) == x.tiles);
             // pieces of this row tile: cut at the CTAs' range ends
             std::vector<std::pair<int, int>> pieces;
             int first = -1, last = -1;
             for (int c = 0; c < n; ++c) {
-                const int64_t a = range_start(c, work, n), b = range_start(c + 1, work, n);
-                const int64_t lo = a > x.start ? a : x.start, hi = b < x.start + x.tiles ? b : x.start + x.tiles;
+                const int lo = reach(x.t, range_start(c, work, n) - x.start), hi = reach(x.t, range_start(c + 1, work, n) - x.start);
+                CHECK(lo <= hi);
                 if (lo >= hi) continue;
+                CHECK(pieces.empty() ? lo == 0 : lo == pieces.back().second);
+                CHECK(first < 0 || c == last + 1);  // the parts of a cut row tile are neighbours
                 if (first < 0) first = c;
                 last = c;
-                pieces.push_back({static_cast<int>(lo - x.start), static_cast<int>(hi - x.start)});
+                taken[c] += hi - lo;
+                pieces.push_back({lo, hi});
             }
-            CHECK(cta_of(ranges, x.start + x.tiles - 1) == last && cta_of(ranges, x.start) == first);
+            CHECK(pieces.back().second == x.tiles);
+            CHECK(cta_of(ranges, x.start + place(x.t, x.tiles - 1) - 1) == last && cta_of(ranges, x.start + place(x.t, 0) - 1) == first);
             if (covered[x.q * s.row_tiles + x.rt]++) continue;  // (another head: the same but for its pieces' ends)
             const RowTile r = row_tile(s, x.rt);
             CHECK(r.nb >= 1 && r.nb <= kRows && r.b0 + r.nb <= nb);
@@ -149,6 +163,7 @@ int main(int argc, char **argv) {
                 }
             }
         }
+        if (n > 1) for (int c = 0; c < n; ++c) CHECK(taken[c] > 0);  // each CTA has a tile
     }
     std::printf("ok\n");
     return 0;
