@@ -9,14 +9,14 @@
 // sequences of a request, and the query heads that share a cache head, are stacked
 // as the 128 rows of one matrix product with the shared keys; their own keys follow
 // as further key tiles of the same row tile, each 16-key step of the product
-// writing only its sequence's rows; and the key tiles of all row tiles are dealt
-// evenly to the CTAs (prefix_split.h), whose partial (m, l, o) a second launch joins.
+// writing only its sequence's rows; and the key tiles of all row tiles are dealt to
+// the CTAs by equal costs (prefix_split.h), whose partial (m, l, o) a second launch joins.
 //
 // One persistent CTA per SM takes pieces (row tile, key tiles [j0, j1)). Key tiles
 // are numbered through its pieces; even and odd ones go to two independent halves
 // of the softmax, each with its own S / P buffer, maxima, sums and accumulator:
-//   warp 0      TMA producer of K, one box per slot of pages and atom, addresses through
-//               the page table, and of Q (a box of tokens x heads of the group);
+//   warp 0      TMA producer of K, one box per slot of pages, addresses through the
+//               page table, and of Q (a box of tokens x heads of the group);
 //   warp 2      TMA producer of V, in the same way. V lies token by token in the
 //               cache, so it is the MN-major operand of the second product: no
 //               transposed copy of the values is kept;
@@ -36,20 +36,22 @@
 //               ring in shared memory.
 //
 // What bounds it, at the figures measured (times of both launches):
-//   2 requests, 28 / 4 heads, 9 branches of 32, contexts to 32700, fp16: 178 us, 1310
-//     TFLOP/s. A key tile takes 1740 cycles, 1024 of them the tensor pipe's, about 965
-//     of the issuing thread's time; the clock is the power limit's (1.45 to 1.85 GHz).
-//     Two row tiles sharing K and V stages (195), two issuing warps (240) and unrolled
-//     batches (187) were slower.
-//   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 440
-//     us, 3.1 TB/s of cache, queries and outputs. A tile of such pages is 32 copies of 2
-//     KB (26 cycles each at best in the copy unit, 46 for the thread that issues them);
-//     the ends of pieces, every 5 tiles, and instruction fetches (72 KB of code in
-//     all roles, 6 % of the fetches miss the cache; 158 KB missed 32 %) take the rest. Copies shared out to a second
-//     warp were slower (567).
+//   2 requests, 28 / 4 heads, 9 branches of 32, contexts to 32700, fp16: 174 us, 1340
+//     TFLOP/s. A key tile takes 1740 cycles: the chain of one half (S 500, softmax 1660,
+//     PV 460, the way between them 800) is as long as two tiles, and about 965 cycles of
+//     a tile are the issuing thread's, 1024 the tensor pipe's; the clock is the power
+//     limit's (1.45 to 1.9 GHz). Two row tiles sharing K and V stages (195), two issuing
+//     warps (240), unrolled batches (187) and K awaited before the products (194) were slower.
+//   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 397
+//     us, 3.4 TB/s of cache, queries and outputs. A row tile has 6 shared tiles and 1.6 own
+//     ones: the change to the next takes 2800 cycles (the read-out hands O back after 1900;
+//     half of O at once, in 128 registers, was slower), own tiles half as much again
+//     as shared ones, and a stage of K is free only 2600 cycles before its next use, of which
+//     the copies take 2200. Instruction fetches: 78 KB of code in all roles, 7 % of the
+//     fetches miss the cache (158 KB missed 32 %).
 //   One request's 9 branches of 32, 32 heads, context 328: 17 us; 64 sequences of one
-//     prompt of 8200: 31. About 5 us pass before a CTA's first copy (lengths, prefix
-//     sums, page table: dependent accesses), 2 in the second launch.
+//     prompt of 8200: 29. About 6 us pass before a CTA's first copy (lengths, prefix
+//     sums, the range's begin, the page table: dependent accesses), 2 in the second launch.
 // Every wait is bounded; a role whose wait runs out flags RPS_DEVERR_TIMEOUT and
 // raises the CTA's abort flag, copies and MMAs in flight are drained and TMEM is
 // freed before the CTA exits.
@@ -99,7 +101,7 @@ constexpr int kStepAdds = 32;
 constexpr int kStagedLens = 512;
 constexpr int kStagedTiles = 512;
 constexpr uint32_t kNoEnd = 1u << 31;  // tiles of the CTA, until its last piece is known
-constexpr int kMaxReqs = 2 * kStages * kTileBytes / 8;  // requests whose first tiles fit the K and V stages
+constexpr int kMaxReqs = 2 * kStages * kTileBytes / 8;  // requests whose first costs fit the K and V stages
 constexpr float kLn2 = 0.6931471805599453f;
 // bounds of a tile's sum of P in a row (in units of its reference): P in fp16 stays finite
 constexpr float kMostWeight = 32768.f, kLeastWeight = 1.f / 32768.f;
@@ -1423,7 +1425,7 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
                    kSmemBytes, s, tq, tk, tv, a) != cudaSuccess)
         return RPS_ERR_CUDA;
     // a cut row tile has about grid / row_tiles parts: half warps of at most four each (64 sequences
-    // of one prompt, 16 row tiles: 31 us; one half warp a row, 33.5)
+    // of one prompt, 16 row tiles: 2.4 us faster than with one half warp a row)
     int split = 1;
     while (split < kJoinHalves && row_tiles * kAhead * split < grid) split *= 2;
     const dim3 cuts(static_cast<unsigned>(std::min<int64_t>(row_tiles, grid)), prefix::kRows / (kJoinHalves / split));
