@@ -1013,6 +1013,19 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
         tc_fence_after();
         const bool both = count > 1;
         const int only = static_cast<int>(t0) & 1;  // the half of a one-tile piece's tile
+        const uint32_t at0 = col + (both ? 0 : only * 128), at1 = both ? col + 128 : at0;
+        uint32_t o[64], o1[64];  // 64 columns at a time, the first on their way while the weights are computed
+        uint32_t(&oa)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o[0]);
+        uint32_t(&ob)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o[32]);
+        uint32_t(&pa)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o1[0]);
+        uint32_t(&pb)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o1[32]);
+        const auto load = [&](int from) {
+            tmem_ld32_async(at0 + from, oa);
+            tmem_ld32_async(at1 + from, pa);
+            tmem_ld32_async(at0 + from + 32, ob);
+            tmem_ld32_async(at1 + from + 32, pb);
+        };
+        load(0);
         float2 e = c.ml[n & 3][both ? 0 : only][r];
         float2 f = both ? c.ml[n & 3][1][r] : make_float2(-INFINITY, 0.f);
         const float m = fmaxf(e.x, f.x), mr = m == -INFINITY ? 0.f : m;
@@ -1027,19 +1040,9 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
         const uint32_t keep0 = w0 == 0.f ? 0u : ~0u, keep1 = w1 == 0.f ? 0u : ~0u;
         const bool zeros = __any_sync(kFull, (keep0 & keep1) == 0);
         const f2 ww0 = pack2(w0, w0), ww1 = pack2(w1, w1);
-        const uint32_t at0 = col + (both ? 0 : only * 128), at1 = both ? col + 128 : at0;
 #pragma unroll 1
-        for (int it = 0; it < 3; ++it) {  // 64 columns at a time; what was staged leaves a turn later
-            uint32_t o[64], o1[64];
-            uint32_t(&oa)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o[0]);
-            uint32_t(&ob)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o[32]);
-            uint32_t(&pa)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o1[0]);
-            uint32_t(&pb)[32] = *reinterpret_cast<uint32_t(*)[32]>(&o1[32]);
+        for (int it = 0; it < 3; ++it) {  // what was staged leaves a turn later
             if (it < 2) {
-                tmem_ld32_async(at0 + it * 64, oa);
-                tmem_ld32_async(at1 + it * 64, pa);
-                tmem_ld32_async(at0 + it * 64 + 32, ob);
-                tmem_ld32_async(at1 + it * 64 + 32, pb);
                 tmem_wait_dep(oa);
                 tmem_wait_dep(pa);
                 tmem_wait_dep(ob);
@@ -1083,6 +1086,7 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = o[32 + i];
             }
+            if (it == 0) load(64);
         }
         if (lse) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
         if (!whole) a.part_ml[(2 * blockIdx.x + p.part) * prefix::kRows + r] = make_float2(m, l);
