@@ -727,11 +727,12 @@ __device__ __forceinline__ bool lane_wait(uint64_t *bar, uint32_t parity, Ctl &c
 // pipe runs them in order, so S of tile t + 2 may overwrite the P that the product of tile t
 // reads without a wait. An issued instruction holds the thread until the pipe takes it, and
 // what the thread does between the batches leaves the pipe idle: so there is one wait for each
-// batch, and one thread without votes.
+// batch, and one thread without votes, elected (so the compiler knows that it is alone and keeps the
+// operands in uniform registers: 353 -> 341 us against lane 0, 64 requests, context 704).
 template <bool kF16>
 __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t *sv, uint32_t tmem, uint32_t tiles,
                                                int lane, Ctl &c, const PrefixArgs &a) {
-    if (lane == 0) {
+    if (elect_one()) {
         constexpr uint32_t fmt = kF16 ? umma::kFmtF16 : umma::kFmtBF16;
         constexpr uint32_t idesc_s = umma::instr_desc_f16(128, 128, fmt, 0);  // K is K-major
         constexpr uint32_t idesc_o = umma::instr_desc_f16(128, 128, fmt, 1);  // V is MN-major
