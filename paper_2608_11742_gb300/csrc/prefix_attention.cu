@@ -36,21 +36,21 @@
 //               ring in shared memory.
 //
 // What bounds it, at the figures measured (times of both launches):
-//   2 requests, 28 / 4 heads, 9 branches of 32, contexts to 32700, fp16: 174 us, 1340
-//     TFLOP/s. A key tile takes 1740 cycles: the chain of one half (S 500, softmax 1660,
-//     PV 460, the way between them 800) is as long as two tiles, and about 965 cycles of
-//     a tile are the issuing thread's, 1024 the tensor pipe's; the clock is the power
+//   2 requests, 28 / 4 heads, 9 branches of 32, contexts to 32700, fp16: 169 us, 1390
+//     TFLOP/s. A key tile takes 1690 cycles: the chain of one half (S 500, softmax 1660,
+//     PV 460, the way between them 750) is as long as two tiles, and of a tile the issuing
+//     thread waits some 900 cycles for MMAs to be taken, which execute in 1024; the clock is the power
 //     limit's (1.45 to 1.9 GHz). Two row tiles sharing K and V stages (195), two issuing
 //     warps (240), unrolled batches (187) and K awaited before the products (194) were slower.
-//   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 397
-//     us, 3.4 TB/s of cache, queries and outputs. A row tile has 6 shared tiles and 1.6 own
+//   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 388
+//     us, 3.45 TB/s of cache, queries and outputs. A row tile has 6 shared tiles and 1.6 own
 //     ones: the change to the next takes 2800 cycles (the read-out hands O back after 1900;
 //     half of O at once, in 128 registers, was slower), own tiles half as much again
 //     as shared ones, and a stage of K is free only 2600 cycles before its next use, of which
 //     the copies take 2200. Instruction fetches: 78 KB of code in all roles, 7 % of the
 //     fetches miss the cache (158 KB missed 32 %).
 //   One request's 9 branches of 32, 32 heads, context 328: 17 us; 64 sequences of one
-//     prompt of 8200: 29. About 6 us pass before a CTA's first copy (lengths, prefix
+//     prompt of 8200: 28. About 6 us pass before a CTA's first copy (lengths, prefix
 //     sums, the range's begin, the page table: dependent accesses), 2 in the second launch.
 // Every wait is bounded; a role whose wait runs out flags RPS_DEVERR_TIMEOUT and
 // raises the CTA's abort flag, copies and MMAs in flight are drained and TMEM is

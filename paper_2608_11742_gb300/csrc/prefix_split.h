@@ -137,7 +137,7 @@ PREFIX_HD Tiles key_tiles(const Shape &s, const KeySum &k, int shared) {
     return t;
 }
 
-// Costs, in quarters of a shared tile's 1740 cycles: an own tile takes 2500 (its product writes the
+// Costs, in quarters of a shared tile's 1700 cycles: an own tile takes 2500 (its product writes the
 // rows of one sequence at a time); the change from a row tile to the next 2800 (the product waits for
 // the read-out), and a cut one's parts are written and joined. With row tiles at 6 instead of 10, 64
 // sequences of one prompt took 30.2 us instead of 28.8, 64 requests of 9 branches 396 instead of 399.
