@@ -42,8 +42,8 @@
 //     thread waits some 900 cycles for MMAs to be taken, which execute in 1024; the clock is the power
 //     limit's (1.45 to 1.9 GHz). Two row tiles sharing K and V stages (195), two issuing
 //     warps (240), unrolled batches (187) and K awaited before the products (194) were slower.
-//   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 388
-//     us, 3.45 TB/s of cache, queries and outputs. A row tile has 6 shared tiles and 1.6 own
+//   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 382
+//     us, 3.5 TB/s of cache, queries and outputs. A row tile has 6 shared tiles and 1.6 own
 //     ones: the change to the next takes 2800 cycles (the read-out hands O back after 1900;
 //     half of O at once, in 128 registers, was slower), own tiles half as much again
 //     as shared ones, and a stage of K is free only 2600 cycles before its next use, of which
@@ -159,7 +159,7 @@ struct Ctl {
     // step), and kStepAdds unless it overwrites
     uint4 step_off[kStages][8];
     int32_t step_how[kStages][8];
-    int4 copy_at[2][16];  // a producer's copies: their coordinates
+    int4 copy_at[2][32];  // a producer's copies: their coordinates, of two tiles
     uint32_t bad[4];  // copies of key tile t whose page id is outside the cache (t % 4)
     int64_t scan[16];
     int32_t len[kStagedLens];      // as they are used
@@ -476,6 +476,15 @@ __device__ __forceinline__ bool copy_page(const PrefixArgs &a, const Piece &p, i
     return true;
 }
 
+// One thread's wait.
+__device__ __forceinline__ bool lane_wait(uint64_t *bar, uint32_t parity, Ctl &c, const PrefixArgs &a) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < a.tries; ++i)
+        if (try_wait_us(bar, parity)) return true;
+    *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
+    return false;
+}
+
 // The producers of K (with Q) and of V, in one body: two warps run it.
 __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const CUtensorMap *tm_q, uint8_t *stages,
                                         uint8_t *sq, uint32_t tiles, int lane, Ctl &c, const PrefixArgs &a) {
@@ -494,51 +503,61 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
         const Piece &p = *pp;
         if (p.last) tiles = t + p.j1 - p.j0;
 #pragma unroll 1
-        for (int j = p.j0; j < p.j1; ++j, ++t) {
-            const int s = t % kStages;
+        for (int j = p.j0; ok && j < p.j1; j += 2) {
+            // two tiles are looked up at a time, half a warp each: with votes and shared memory it takes as
+            // long as a tile's copies (64 requests, contexts 200 to 1200: 387 us with one, 382 with two)
+            const int two = min(2, p.j1 - j), half = lane >> 4;
             int2 at = make_int2(-1, 0);
-            const bool there = copy_page(a, p, j, lane, at);
-            if (t >= kStages && !(ok = warp_wait(&empty[s], (t / kStages - 1) & 1, c, a))) break;
+            const bool there = half < two && copy_page(a, p, j + half, lane & 15, at);
             // (an id outside the cache: a coordinate whose copy is all zeros, as are copies that are not there)
             const bool bad_page = static_cast<unsigned>(at.x) >= static_cast<unsigned>(a.s.n_pages);
-            if (lane < 16)
-                c.copy_at[is_k][lane] =
-                    a.by_groups ? make_int4(0, bad_page ? a.no_page : at.x * a.page_groups + (at.y >> 3), p.head, 0)
-                                : make_int4(at.y, p.head, bad_page ? a.no_page : at.x, 0);
-            if (is_k) {
-                const uint32_t bad = __ballot_sync(kFull, there && bad_page);
-                if (j == p.j0) ++n_q;
-                if (lane == 0) {
-                    c.bad[t % 4] = bad;
-                    if (bad) flag_error(a.err, RPS_DEVERR_PAGE);
-                }
-            }
-            // (V of own tiles goes through the cleaner)
-            const bool raw = !is_k && j >= p.shared_tiles;
-            uint64_t *bar = raw ? &c.v_raw[s] : &full[s];
-            raw_last = (raw_last & ~(1u << s)) | (raw ? 1u << s : 0u);
-            raw0 += raw && s == 0;
-            raw1 += raw && s == 1;
+            c.copy_at[is_k][lane] =
+                a.by_groups ? make_int4(0, bad_page ? a.no_page : at.x * a.page_groups + (at.y >> 3), p.head, 0)
+                            : make_int4(at.y, p.head, bad_page ? a.no_page : at.x, 0);
+            const uint32_t bad = __ballot_sync(kFull, there && bad_page);
+            if (bad && is_k && lane == 0) flag_error(a.err, RPS_DEVERR_PAGE);
             __syncwarp();
-            if (elect_one()) {  // (coordinates from shared memory: picked out of lanes a copy took a third longer)
-                mbar_expect_tx(bar, kTileBytes);
-                uint8_t *dst = stages + s * kTileBytes;
-                int4 at = c.copy_at[is_k][0];
+            int done = 0;
+            if (elect_one()) {
 #pragma unroll 1
-                for (int i = 1; i <= prefix::kRows >> a.copy_log; ++i, dst += kGroup / 8 << a.copy_log) {
-                    const int4 next = c.copy_at[is_k][i & 15];
-                    tma_load_5d(dst, tm, 0, at.x, 0, at.y, at.z, bar);
-                    at = next;
-                }
-                if (is_k && j == p.j0) {  // Q: its buffer's last user, piece n - 2, ended at tile t - 2 or before
-                    uint64_t *q_full = &c.q_full[n & 1];
-                    mbar_expect_tx(q_full, 2u * a.s.group * a.s.tokens * 128);
-                    dst = sq + (n & 1) * kTileBytes;
-                    tma_load_4d(dst, tm_q, 0, p.head * a.s.group, p.r.tok0, p.q, q_full);
-                    tma_load_4d(dst + kAtom, tm_q, 64, p.head * a.s.group, p.r.tok0, p.q, q_full);
+                for (; done < two; ++done) {
+                    const uint32_t x = t + done;
+                    const int s = x % kStages;
+                    if (x >= kStages && !lane_wait(&empty[s], (x / kStages - 1) & 1, c, a)) break;
+                    // (V of own tiles goes through the cleaner)
+                    uint64_t *bar = !is_k && j + done >= p.shared_tiles ? &c.v_raw[s] : &full[s];
+                    mbar_expect_tx(bar, kTileBytes);
+                    if (is_k) c.bad[x % 4] = bad >> done * 16 & 0xffffu;
+                    // (coordinates from shared memory: picked out of lanes a copy took a third longer)
+                    uint8_t *dst = stages + s * kTileBytes;
+                    const int4 *from = &c.copy_at[is_k][done * 16];
+                    int4 at = from[0];
+#pragma unroll 1
+                    for (int i = 1; i <= prefix::kRows >> a.copy_log; ++i, dst += kGroup / 8 << a.copy_log) {
+                        const int4 next = from[i & 15];
+                        tma_load_5d(dst, tm, 0, at.x, 0, at.y, at.z, bar);
+                        at = next;
+                    }
+                    if (is_k && j + done == p.j0) {  // Q: its buffer's last user, piece n - 2, ended at tile x - 2 or before
+                        uint64_t *q_full = &c.q_full[n & 1];
+                        mbar_expect_tx(q_full, 2u * a.s.group * a.s.tokens * 128);
+                        dst = sq + (n & 1) * kTileBytes;
+                        tma_load_4d(dst, tm_q, 0, p.head * a.s.group, p.r.tok0, p.q, q_full);
+                        tma_load_4d(dst + kAtom, tm_q, 64, p.head * a.s.group, p.r.tok0, p.q, q_full);
+                    }
                 }
             }
-            __syncwarp();
+            done = __reduce_max_sync(kFull, done);
+            ok = done == two;
+            n_q += is_k && j == p.j0 && done > 0;
+#pragma unroll 1
+            for (int u = 0; u < done; ++u, ++t) {
+                const int s = t % kStages;
+                const bool raw = !is_k && j + u >= p.shared_tiles;
+                raw_last = (raw_last & ~(1u << s)) | (raw ? 1u << s : 0u);
+                raw0 += raw && s == 0;
+                raw1 += raw && s == 1;
+            }
         }
         if (ok) release_piece(n, lane, c);
     }
@@ -712,15 +731,6 @@ __device__ __forceinline__ bool schedule_next(Schedule &z, const PrefixArgs &a, 
         z.leave = false;
     }
     return true;
-}
-
-// One thread's wait.
-__device__ __forceinline__ bool lane_wait(uint64_t *bar, uint32_t parity, Ctl &c, const PrefixArgs &a) {
-#pragma unroll 1
-    for (uint32_t i = 0; i < a.tries; ++i)
-        if (try_wait_us(bar, parity)) return true;
-    *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
-    return false;
 }
 
 // The MMA issuer, one thread: S_t = Q K_t^T into TMEM buffer t % 2, O[t % 2] += P_t V_t. The tensor
