@@ -202,6 +202,26 @@ def test_pages_at_odd_strides(ps, dtype):
         assert torch.equal(out[keep], whole[0][keep])
 
 
+@pytest.mark.parametrize("causal", [False, True])
+def test_more_row_tiles_than_a_block_has_threads(causal):
+    """700 requests of two sequences, some absent: the plan goes through two blocks of row tiles, lengths and key tiles
+    are read again instead of kept."""
+    rng = np.random.default_rng(27)
+    lens = rng.integers(1, 60, (700, 2))
+    lens[rng.random((700, 2)) < 0.15] = -1
+    lens[300:310] = -1
+    c = Case(27, lens, [int(x) for x in rng.integers(0, 40, 700)], 1, 2, 2, 16, causal=causal)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("group,n_q", [(2, 64), (128, 1)])
+def test_many_row_tiles_of_a_request(group, n_q):
+    """70 row tiles of a head: the range's begin is found in more than a warp's width of them."""
+    nb = 70
+    c = Case(28, [[200 + 5 * (i % 9) for i in range(nb)], [66] * nb], [192, 64], n_q, 2 * group, 2, 32, causal=True)
+    c.check(*c.run())
+
+
 def test_causal_rows_longer_than_the_sequence():
     """n_q beyond a sequence's length: the first queries see nothing, their rows are zero."""
     c = Case(23, [[5, 130, 20]], [0], 24, 2, 1, 16, causal=True)
