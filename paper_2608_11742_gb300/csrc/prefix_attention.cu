@@ -47,7 +47,7 @@
 //     ones: the change to the next takes 2800 cycles (the read-out hands O back after 1900;
 //     half of O at once, in 128 registers, was slower), own tiles half as much again
 //     as shared ones, and a stage of K is free only 2600 cycles before its next use, of which
-//     the copies take 2200. Instruction fetches: 78 KB of code in all roles, 7 % of the
+//     the copies take 2200. Instruction fetches: 76 KB of code in all roles, 5 % of the
 //     fetches miss the cache (158 KB missed 32 %).
 //   One request's 9 branches of 32, 32 heads, context 328: 17 us; 64 sequences of one
 //     prompt of 8200: 28. About 6 us pass before a CTA's first copy (lengths, prefix
