@@ -37,9 +37,10 @@
 //
 // What bounds it, at the figures measured (times of both launches):
 //   2 requests, 28 / 4 heads, 9 branches of 32, contexts to 32700, fp16: 169 us, 1390
-//     TFLOP/s. A key tile takes 1690 cycles: the chain of one half (S 500, softmax 1660,
-//     PV 460, the way between them 750) is as long as two tiles, and of a tile the issuing
-//     thread waits some 900 cycles for MMAs to be taken, which execute in 1024; the clock is the power
+//     TFLOP/s. A key tile takes 1600 to 1690 cycles, of which MMAs execute in 1024: two tiles
+//     take as long as the chain of one half (softmax 1730, P handed on 90, PV issued 150,
+//     its commit and K's wait 420, S issued 220, S executed and seen 580);
+//     the clock is the power
 //     limit's (1.45 to 1.9 GHz). Two row tiles sharing K and V stages (195), two issuing
 //     warps (240), unrolled batches (187) and K awaited before the products (194) were slower.
 //   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 382
