@@ -39,10 +39,9 @@
 //   2 requests, 28 / 4 heads, 9 branches of 32, contexts to 32700, fp16: 169 us, 1390
 //     TFLOP/s. A key tile takes 1600 to 1690 cycles, of which MMAs execute in 1024: two tiles
 //     take as long as the chain of one half (softmax 1730, P handed on 90, PV issued 150,
-//     its commit and K's wait 420, S issued 220, S executed and seen 580);
-//     the clock is the power
-//     limit's (1.45 to 1.9 GHz). Two row tiles sharing K and V stages (195), two issuing
-//     warps (240), unrolled batches (187) and K awaited before the products (194) were slower.
+//     its commit and K's wait 420, S issued 220, S executed and seen 580). The clock is the
+//     power limit's (1.45 to 1.9 GHz). Slower: two row tiles sharing K and V stages (195), two
+//     issuing warps (240), unrolled batches (187), K awaited before the products (194).
 //   64 requests, 32 heads, 9 branches of 32, contexts 200 to 1200 in pages of 16: 382
 //     us, 3.5 TB/s of cache, queries and outputs. A row tile has 6 shared tiles and 1.6 own
 //     ones: the change to the next takes 2800 cycles (the read-out hands O back after 1900;
