@@ -71,6 +71,7 @@
 namespace rps {
 namespace {
 
+using prefix::kMaxCtas;
 using prefix::KeySum;
 using prefix::RowTile;
 using prefix::Shape;
@@ -94,7 +95,6 @@ constexpr uint32_t kOCol = 256;
 constexpr int kRing = 4;             // pieces known ahead
 constexpr int kConsumers = 16;       // every warp
 constexpr int kMaxSeqs = 128;        // sequences with rows in one row tile
-constexpr int kMaxCtas = 160;
 constexpr int kStepAdds = 32;
 // Lengths, and key tiles of a head's row tiles (a block of threads' at most), are kept in shared
 // memory where they fit (64 sequences of one prompt: 31 us instead of 33.7).
@@ -107,8 +107,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kMostWeight = 32768.f, kLeastWeight = 1.f / 32768.f;
 
 // A row tile that is cut: the CTA that takes its first key tile writes where its parts
-// are. Entries are by row tile while there are at most kMaxCtas of them, else by CTA (one
-// CTA begins at most one cut row tile, its last).
+// are, into the row tile's entry or its own (prefix::cut_list).
 struct Cut {
     int32_t parts;       // 0: none
     int32_t cta;         // the first part's
@@ -1435,7 +1434,8 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
     const int64_t row_tiles = static_cast<int64_t>(a.s.n_req) * a.s.heads * a.s.row_tiles;
     const int grid = static_cast<int>(std::min<int64_t>(row_tiles * tiles, sms));
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    a.by_tile = row_tiles <= kMaxCtas;
+    const prefix::CutList list = prefix::cut_list(row_tiles, grid);
+    a.by_tile = list.by_tile;
     if (launch_pdl(f16 ? prefix_attention_kernel<true> : prefix_attention_kernel<false>, dim3(grid), dim3(kThreads),
                    kSmemBytes, s, tq, tk, tv, a) != cudaSuccess)
         return RPS_ERR_CUDA;
@@ -1443,7 +1443,7 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
     // of one prompt, 16 row tiles: 2.4 us faster than with one half warp a row)
     int split = 1;
     while (split < kJoinHalves && row_tiles * kAhead * split < grid) split *= 2;
-    const dim3 cuts(static_cast<unsigned>(std::min<int64_t>(row_tiles, grid)), prefix::kRows / (kJoinHalves / split));
+    const dim3 cuts(static_cast<unsigned>(list.blocks), prefix::kRows / (kJoinHalves / split));
     return launch_pdl(f16 ? prefix_combine_kernel<true> : prefix_combine_kernel<false>, cuts, dim3(kJoinThreads), 0, s, a,
                       split) == cudaSuccess
                ? RPS_OK

@@ -26,7 +26,8 @@
 namespace rps {
 namespace prefix {
 
-constexpr int kRows = 128;  // rows of a row tile, keys of a key tile
+constexpr int kRows = 128;     // rows of a row tile, keys of a key tile
+constexpr int kMaxCtas = 160;  // CTAs of a call, and cut row tiles that are listed
 
 // Division of 0 <= n < 2^31 by a constant d: with l = ceil(log2 d) and mul = ceil(2^(31 + l) / d),
 // n mul / 2^(31 + l) exceeds n / d by less than n / 2^31 / d * (d / 2^l) < 1 / d, so its floor is
@@ -198,6 +199,20 @@ PREFIX_HD int cta_of(const Ranges &r, int64_t x) {
             hi = mid;
     }
     return lo;
+}
+
+// The list of cut row tiles, and the blocks that join their parts, one an entry. Entries are by
+// row tile while there are at most kMaxCtas of them (more than the CTAs of a card with fewer SMs:
+// each row tile has a block, not each CTA), else by the CTA that takes the first part: one CTA
+// begins at most one cut row tile, its last.
+struct CutList {
+    int32_t by_tile, blocks;
+};
+PREFIX_HD CutList cut_list(int64_t row_tiles, int ctas) {
+    CutList l;
+    l.by_tile = row_tiles <= kMaxCtas;
+    l.blocks = l.by_tile ? static_cast<int32_t>(row_tiles) : ctas;
+    return l;
 }
 
 // The sequence i of [0, nb) that holds own slot x (off[i] <= x < off[i + 1]; x < off[nb]).
