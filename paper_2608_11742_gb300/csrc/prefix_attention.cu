@@ -525,8 +525,9 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
                     if (x >= kStages && !lane_wait(&empty[s], (x / kStages - 1) & 1, c, a)) break;
                     // (V of own tiles goes through the cleaner)
                     uint64_t *bar = !is_k && j + done >= p.shared_tiles ? &c.v_raw[s] : &full[s];
-                    mbar_expect_tx(bar, kTileBytes);
+                    // (before the arrival, which hands it on to the softmax of tile x; that of tile x - 4 has read its own)
                     if (is_k) c.bad[x % 4] = bad >> done * 16 & 0xffffu;
+                    mbar_expect_tx(bar, kTileBytes);
                     // (coordinates from shared memory: picked out of lanes a copy took a third longer)
                     uint8_t *dst = stages + s * kTileBytes;
                     const int4 *from = &c.copy_at[is_k][done * 16];
