@@ -503,8 +503,9 @@ rps_status rps_packed_attention_fwd(const rps_packed_attention *attn, rps_stream
  * the pages table[s][0], table[s][1], ...; len[s] < 0: the sequence is absent
  * and holds no page. page_ref[p] counts the table entries that hold page p; a
  * page is free when its count is 0 (a caller may pin pages of its own by
- * counting them once more). The caller starts with page_ref all 0 and len all
- * -1; the calls below keep the three arrays consistent.
+ * counting them once more; rps_kv_compact moves them like the others). The
+ * caller starts with page_ref all 0 and len all -1; the calls below keep the
+ * three arrays consistent.
  * Layout: k, v [n_layers][n_pages][n_heads][page_size][head_dim], head_dim
  * contiguous, the other strides in elements and multiples of 8 (so either order
  * of heads and tokens will do), bases 16-byte aligned. head_dim must be 128,
@@ -568,6 +569,10 @@ rps_status rps_kv_resize(const rps_kv_cache *kv, const int32_t *d_new_len, void 
  * them, the i-th live page from n_live on goes to the i-th free place below
  * n_live (both ascending; data of every layer, count and table entries). Pages
  * below n_live stay. d_n_live (optional, device) receives n_live. Two launches.
+ * A page that is live by a caller's own count alone moves too, with its count; the
+ * table's entries are the only ids that are renamed. A moved page's id that the caller
+ * keeps elsewhere names a free place after the call, and another page later: the caller
+ * finds the new place by the rule above from page_ref as it was before.
  */
 rps_status rps_kv_compact(const rps_kv_cache *kv, int32_t *d_n_live, void *d_ws, size_t ws_bytes, rps_stream_t stream);
 

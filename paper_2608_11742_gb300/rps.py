@@ -655,7 +655,9 @@ def rps_kv_resize(kv: KvCacheBuf, new_len: torch.Tensor, ws: torch.Tensor, strea
 
 
 def rps_kv_compact(kv: KvCacheBuf, n_live: Optional[torch.Tensor], ws: torch.Tensor, stream=None) -> None:
-    """The live pages move to the lowest places; ``n_live`` (int32[1], optional) receives their number."""
+    """The live pages move to the lowest places; ``n_live`` (int32[1], optional) receives their number. Page ids kept
+    outside ``kv.table`` (pages pinned in ``page_ref``) are not renamed: the i-th live page from n_live on goes to the
+    i-th free place below it."""
     at, st = kv._c(), _here(stream, kv.k, ws, n_live)
     _check(_lib.rps_kv_compact(at, None if n_live is None else _ints("n_live", n_live, 1), ws.data_ptr(), ws.nbytes, st),
            "rps_kv_compact")
