@@ -539,8 +539,9 @@ size_t rps_kv_workspace_bytes(const rps_kv_cache *kv);
  * d_ctx_len[q] tokens (NULL: whole); the others become absent; the base stays.
  * rps_kv_commit: the base of request q takes the state of branch 1 + d_winner[q]
  * (rps_commit_out.winner; a negative code keeps the base), every other sequence
- * becomes absent and its pages are given back. A winner without such a branch
- * sets RPS_DEVERR_ROW_INDEX and keeps the base.
+ * becomes absent and its pages are given back. A winner beyond n_branch - 2 sets
+ * RPS_DEVERR_ROW_INDEX and keeps the base; that of an absent branch leaves the
+ * base absent. (These two check their workspace like the others and do not use it.)
  */
 rps_status rps_kv_reorder(const rps_kv_cache *kv, const int32_t *d_src, const int32_t *d_keep, void *d_ws,
                           size_t ws_bytes, rps_stream_t stream);
@@ -599,7 +600,8 @@ rps_status rps_kv_write(const rps_kv_cache *kv, int32_t layer, const void *k_new
 
 /*
  * Attention of each sequence's newest tokens over its cached keys and values, the
- * pages that the sequences of a request share read once for all of them. For query
+ * pages that the sequences of a request share read once for 128 query rows (query
+ * tokens times the query heads of a cache head) instead of for each sequence. For query
  * i of the n_q of sequence s with n = len[s] tokens, and for each query head h
  * (heads h of the cache: h / (n_heads / kv->n_heads)):
  *   out = sum_j softmax_j(scale * q . k_j) v_j,  lse = log sum_j exp(scale * q . k_j)
@@ -612,7 +614,7 @@ rps_status rps_kv_write(const rps_kv_cache *kv, int32_t layer, const void *k_new
  * shared_len[q] (device, NULL: 0): the leading tokens whose pages all present
  * sequences of request q hold in common (as after rps_kv_fork_branches with the
  * same d_ctx_len); whole pages below it, as far as every sequence reaches, are read
- * through the table row of one sequence. Tokens past a sequence's length, and
+ * through the table row of one sequence of those 128 rows. Tokens past a sequence's length, and
  * pages that no sequence holds, may hold anything; the values of tokens below the
  * lengths must be finite where several queries share them (a value of inf or NaN
  * also reaches the queries of its request that share its page, and earlier queries

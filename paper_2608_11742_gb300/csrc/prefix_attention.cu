@@ -1,6 +1,6 @@
 // prefix_attention.cu -- attention of the sequences' newest tokens over the paged
-// K/V cache, the pages that the sequences of a request share read once for all of
-// them (rps_prefix_attention_fwd).
+// K/V cache, the pages that the sequences of a request share read once for a tile of
+// 128 query rows of all of them (rps_prefix_attention_fwd).
 //
 // For query i of a sequence, out = sum_j softmax_j(scale q . k_j) v_j over the keys
 // it sees. The softmax over two sets of keys is joined from the sets' maxima m, sums

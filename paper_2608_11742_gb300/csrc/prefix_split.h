@@ -120,7 +120,7 @@ PREFIX_HD void add_sequence(const Shape &s, KeySum &k, int len) {
     k.slots += slots_of(s, len);
     k.min_pages = imin(k.min_pages, len >= 0 ? len >> s.page_log : INT32_MAX);
 }
-// Slots that are read once for all: whole pages inside the shared length and inside every sequence.
+// Slots that are read once for the row tile's sequences: whole pages inside the shared length and inside each of them.
 PREFIX_HD int shared_slots(const Shape &s, const KeySum &k, int shared_len) {
     return k.present ? imin(imax(0, shared_len) >> s.page_log, k.min_pages) << s.sub_log : 0;
 }

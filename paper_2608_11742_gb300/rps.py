@@ -809,8 +809,8 @@ class BranchCache:
     Sequence (q, 0) is request q's base, (q, 1 + b) its branch b. One step: ``fork`` the
     branches that ``PivotsBuf.branch_valid`` lists from their base's context, ``resize``
     every sequence to its context and block, per layer ``write`` the block's keys and
-    values and ``attend`` over context and block (the context's pages read once for all
-    of a request's branches), then ``commit`` the winner of ``CommitBuf.winner``: its
+    values and ``attend`` over context and block (the context's pages read once for 128
+    query rows of a request's branches), then ``commit`` the winner of ``CommitBuf.winner``: its
     block becomes the base's. Pages, workspaces and bookkeeping are allocated once;
     every call is asynchronous and reads what it decides by from device memory, so a
     step can be captured as a CUDA graph."""
