@@ -55,14 +55,12 @@
 // Every wait is bounded; a role whose wait runs out flags RPS_DEVERR_TIMEOUT and
 // raises the CTA's abort flag, copies and MMAs in flight are drained and TMEM is
 // freed before the CTA exits.
-#include <cuda.h>  // CUtensorMap and the tensor-map encoder's signature (no link against the driver)
-#include <cudaTypedefs.h>
-
 #include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <mutex>
 
+#include "kv_maps.cuh"
 #include "prefix_split.h"
 #include "rps_internal.cuh"
 #include "tc_device.cuh"
@@ -122,9 +120,7 @@ struct PrefixArgs {
     int64_t out_req, out_token, out_head;
     float *lse;
     float c;  // scale * log2(e)
-    // A copy of K or V takes 2^copy_log tokens. by_groups: from a map whose third dimension goes
-    // through the tokens of all pages by eights, page_groups of them a page; else 8 tokens of a page
-    int32_t by_groups, copy_log, page_groups, no_page;  // no_page: a coordinate beyond the pages
+    PageCopies copies;
     Cut *cut;       // [kMaxCtas]
     int32_t by_tile;  // cuts are listed by row tile
     float2 *part_ml;  // [2 * kMaxCtas][128]: maximum and sum of each row of a partial result
@@ -166,45 +162,6 @@ struct Ctl {
     uint32_t tmem_base;
     int abort_flag;
 };
-
-// ---------------------------------------------------------------- waits
-// One try of a wait for a phase, which the hardware suspends for about a microsecond at most.
-__device__ __forceinline__ bool try_wait_us(uint64_t *bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(saddr(bar)), "r"(parity), "r"(1000u)
-        : "memory");
-    return done != 0;
-}
-// Waits for a phase of a barrier, at most a.tries tries, all lanes; the warp goes on
-// together, on the same answer. A wait that runs out raises the abort flag, which is
-// reported when the CTA ends; the other roles' waits then run out too. (Short: every role's
-// waits are inlined, and the roles' code has to fit the instruction cache together.)
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl &c, const PrefixArgs &a) {
-    bool ok = false;
-#pragma unroll 1
-    for (uint32_t i = 0; i < a.tries && !ok; ++i) ok = try_wait_us(bar, parity);
-    if (__all_sync(kFull, ok)) return true;
-    *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
-    return false;
-}
-
-// One thread of the converged warp, known to the compiler as one.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t one;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-    return one != 0;
-}
-// Waits for what is in flight when a role ends, a fifth of a second at most.
-__device__ __forceinline__ void drain(uint64_t *bar, uint32_t parity) {
-#pragma unroll 1
-    for (uint32_t i = 0; i < 200000 && !try_wait_us(bar, parity); ++i) {
-    }
-}
 
 // ---------------------------------------------------------------- the cut
 __device__ __forceinline__ int len_of(const PrefixArgs &a, int s, const Ctl &c) {
@@ -461,7 +418,7 @@ __device__ __forceinline__ void release_piece(int n, int lane, Ctl &c) {
 // The page id (as the table has it: the load is on its way) of copy `lane` of key tile j and the
 // copy's first token in the page; false: the tile has no such copy.
 __device__ __forceinline__ bool copy_page(const PrefixArgs &a, const Piece &p, int j, int lane, int2 &at) {
-    const int log = a.s.slot_log - a.copy_log;  // copies of a slot
+    const int log = a.s.slot_log - a.copies.copy_log;  // copies of a slot
     const bool own = j >= p.shared_tiles;
     int row = p.shared_row, x = ((own ? j - p.shared_tiles : j) << a.s.spt_log) + (lane >> log);
     if (lane >> log >= a.s.spt || x >= (own ? p.off[p.r.nb] : p.shared)) return false;
@@ -471,17 +428,8 @@ __device__ __forceinline__ bool copy_page(const PrefixArgs &a, const Piece &p, i
         row = p.q * a.s.n_branch + p.r.b0 + i;
     }
     at = make_int2(a.table[static_cast<int64_t>(row) * a.s.max_pages + (x >> a.s.sub_log)],
-                   ((x & (a.s.sub - 1)) << a.s.slot_log) + ((lane & ((1 << log) - 1)) << a.copy_log));
+                   ((x & (a.s.sub - 1)) << a.s.slot_log) + ((lane & ((1 << log) - 1)) << a.copies.copy_log));
     return true;
-}
-
-// One thread's wait.
-__device__ __forceinline__ bool lane_wait(uint64_t *bar, uint32_t parity, Ctl &c, const PrefixArgs &a) {
-#pragma unroll 1
-    for (uint32_t i = 0; i < a.tries; ++i)
-        if (try_wait_us(bar, parity)) return true;
-    *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
-    return false;
 }
 
 // The producers of K (with Q) and of V, in one body: two warps run it.
@@ -511,8 +459,8 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
             // (an id outside the cache: a coordinate whose copy is all zeros, as are copies that are not there)
             const bool bad_page = static_cast<unsigned>(at.x) >= static_cast<unsigned>(a.s.n_pages);
             c.copy_at[is_k][lane] =
-                a.by_groups ? make_int4(0, bad_page ? a.no_page : at.x * a.page_groups + (at.y >> 3), p.head, 0)
-                            : make_int4(at.y, p.head, bad_page ? a.no_page : at.x, 0);
+                a.copies.by_groups ? make_int4(0, bad_page ? a.copies.no_page : at.x * a.copies.page_groups + (at.y >> 3), p.head, 0)
+                            : make_int4(at.y, p.head, bad_page ? a.copies.no_page : at.x, 0);
             const uint32_t bad = __ballot_sync(kFull, there && bad_page);
             if (bad && is_k && lane == 0) flag_error(a.err, RPS_DEVERR_PAGE);
             __syncwarp();
@@ -533,7 +481,7 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
                     const int4 *from = &c.copy_at[is_k][done * 16];
                     int4 at = from[0];
 #pragma unroll 1
-                    for (int i = 1; i <= prefix::kRows >> a.copy_log; ++i, dst += kGroup / 8 << a.copy_log) {
+                    for (int i = 1; i <= prefix::kRows >> a.copies.copy_log; ++i, dst += kGroup / 8 << a.copies.copy_log) {
                         const int4 next = from[i & 15];
                         tma_load_5d(dst, tm, 0, at.x, 0, at.y, at.z, bar);
                         at = next;
@@ -859,7 +807,7 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
             tc_fence_after();
             const uint32_t bad = c.bad[t % 4];
             if (bad && col.lo < col.hi) {  // a page of this row's keys does not exist: NaN
-                const int u0 = col.lo >> a.copy_log, u1 = (col.hi - 1) >> a.copy_log;
+                const int u0 = col.lo >> a.copies.copy_log, u1 = (col.hi - 1) >> a.copies.copy_log;
                 if (bad >> u0 & low_bits(u1 - u0 + 1)) {
                     l = NAN;
                     col.hi = col.lo;
@@ -965,11 +913,6 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, int h, u
         t0 += count;
         if (ok) release_piece(n, lane, c);
     }
-}
-
-template <bool kF16>
-__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
-    return kF16 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
 }
 
 // The warp's stage (32 rows x 128 bytes) to the rows' addresses (0: not stored), 4 rows
@@ -1270,7 +1213,6 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_combine_kernel(const Pref
 
 // ---------------------------------------------------------------- host
 std::mutex g_prefix_mutex;
-PFN_cuTensorMapEncodeTiled_v12000 g_prefix_encode = nullptr;
 bool g_prefix_ready[64] = {};
 int g_prefix_sms[64] = {};
 
@@ -1278,15 +1220,6 @@ rps_status setup(int *sms) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return RPS_ERR_CUDA;
     std::lock_guard<std::mutex> lock(g_prefix_mutex);
-    if (!g_prefix_encode) {
-        void *fn = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) !=
-                cudaSuccess ||
-            q != cudaDriverEntryPointSuccess || !fn)
-            return RPS_ERR_CUDA;
-        g_prefix_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
-    }
     if (!g_prefix_ready[dev]) {
         if (cudaDeviceGetAttribute(&g_prefix_sms[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
             return RPS_ERR_CUDA;
@@ -1296,57 +1229,6 @@ rps_status setup(int *sms) {
         g_prefix_ready[dev] = true;
     }
     *sms = std::min(g_prefix_sms[dev], kMaxCtas);
-    return RPS_OK;
-}
-
-// A map of 16-bit elements: extents, strides (in elements) and boxes from the inner dimension
-// (64-wide boxes of kD contiguous elements, or 64) outwards.
-template <int n>
-rps_status make_map(CUtensorMap *m, const void *base, bool f16, int64_t inner, const int64_t (&ext)[n],
-                    const int64_t (&stride)[n], const uint32_t (&box)[n]) {
-    cuuint64_t dims[n + 1] = {static_cast<cuuint64_t>(inner)}, bytes[n];
-    cuuint32_t boxes[n + 1] = {64}, es[n + 1] = {1};
-    for (int i = 0; i < n; ++i) {
-        dims[i + 1] = static_cast<cuuint64_t>(ext[i]);
-        // (the stride of a dimension of one is not used, but has to be a valid one)
-        bytes[i] = static_cast<cuuint64_t>(ext[i] > 1 ? stride[i] : kD) * 2;
-        boxes[i + 1] = box[i];
-        es[i + 1] = 1;
-    }
-    const CUresult r = g_prefix_encode(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n + 1,
-                                       const_cast<void *>(base), dims, bytes, boxes, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? RPS_OK : RPS_ERR_CUDA;
-}
-
-// The maps of K and V: a copy brings whole groups of 8 tokens, both halves of their columns.
-// Where the pages' stride is a multiple of eight tokens', one dimension goes through the groups
-// of all pages, and a copy takes a slot; else a copy is a group of one page.
-rps_status map_pages(CUtensorMap *tk, CUtensorMap *tv, const rps_kv_cache *kv, int64_t layer_at, bool f16, PrefixArgs &a) {
-    const int64_t groups = kv->page_size / 8, token = kv->token_stride, group = 8 * token;
-    const int64_t per_page = kv->n_pages > 1 ? kv->page_stride / group : groups;
-    const int64_t all = (kv->n_pages - 1) * per_page + groups;
-    const void *const base[2] = {static_cast<char *>(kv->k) + layer_at, static_cast<char *>(kv->v) + layer_at};
-    CUtensorMap *const to[2] = {tk, tv};
-    a.by_groups = (kv->n_pages == 1 || kv->page_stride % group == 0) && all <= INT32_MAX;
-    a.copy_log = a.by_groups ? a.s.slot_log : 3;
-    a.page_groups = a.by_groups ? static_cast<int32_t>(per_page) : 0;
-    a.no_page = a.by_groups ? static_cast<int32_t>(all) : kv->n_pages;
-    for (int i = 0; i < 2; ++i) {
-        rps_status st;
-        if (a.by_groups) {
-            const int64_t ext[4] = {8, 2, all, kv->n_heads}, stride[4] = {token, 64, group, kv->head_stride};
-            const uint32_t box[4] = {8, 2, static_cast<uint32_t>(a.s.slot / 8), 1};
-            st = make_map(to[i], base[i], f16, 64, ext, stride, box);
-        } else {
-            const int64_t ext[4] = {kv->page_size, 2, kv->n_heads, kv->n_pages};
-            const int64_t stride[4] = {token, 64, kv->head_stride, kv->page_stride};
-            const uint32_t box[4] = {8, 2, 1, 1};
-            st = make_map(to[i], base[i], f16, 64, ext, stride, box);
-        }
-        if (st != RPS_OK) return st;
-    }
     return RPS_OK;
 }
 
@@ -1408,11 +1290,12 @@ extern "C" rps_status rps_prefix_attention_fwd(const rps_prefix_attention *p, co
     if (!(a.err = device_error_word())) return RPS_ERR_CUDA;
 
     const bool f16 = kv->dtype == RPS_F16;
-    const int64_t kv_at = kv->n_layers > 1 ? p->layer * kv->layer_stride * 2 : 0;
+    const Encoder encode = tensor_map_encoder();
+    if (!encode) return RPS_ERR_CUDA;
     const uint32_t qbox[3] = {static_cast<uint32_t>(a.s.group), static_cast<uint32_t>(a.s.tokens), 1};
     CUtensorMap tq, tk, tv;
-    if ((st = make_map(&tq, p->q, f16, kD, ext, qs, qbox)) != RPS_OK) return st;
-    if ((st = map_pages(&tk, &tv, kv, kv_at, f16, a)) != RPS_OK) return st;
+    if ((st = make_map(encode, &tq, p->q, f16, kD, ext, qs, qbox)) != RPS_OK) return st;
+    if ((st = map_pages(encode, &tk, &tv, kv, p->layer, a.s.slot_log, a.copies)) != RPS_OK) return st;
     a.table = kv->table;
     a.len = kv->len;
     a.shared_len = p->shared_len;

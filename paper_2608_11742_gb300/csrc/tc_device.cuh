@@ -255,6 +255,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    return kF16 ? pack_f16(lo, hi) : pack_bf16(lo, hi);
+}
+
 // ---------------------------------------------------------------- waits
 // Waits for a phase of a barrier, at most a.wait_ns; a wait that runs out flags the
 // error word and raises the CTA's abort flag, which ends the other roles' waits.
@@ -284,6 +289,56 @@ __device__ void wait_drain(uint64_t *bar, uint32_t parity) {
     const uint64_t start = global_ns();
     while (global_ns() - start < kDrainNs)
         if (mbar_try_wait(bar, parity)) return;
+}
+
+// The same in tries instead of nanoseconds (shorter code, for kernels of many roles).
+// One try of a wait for a phase, which the hardware suspends for about a microsecond at most.
+__device__ __forceinline__ bool try_wait_us(uint64_t *bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(saddr(bar)), "r"(parity), "r"(1000u)
+        : "memory");
+    return done != 0;
+}
+// Waits for a phase of a barrier, at most a.tries tries, all lanes; the warp goes on
+// together, on the same answer. A wait that runs out raises the abort flag, which is
+// reported when the CTA ends; the other roles' waits then run out too. (Short: every role's
+// waits are inlined, and the roles' code has to fit the instruction cache together.)
+template <typename Ctl_, typename Args_>
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl_ &c, const Args_ &a) {
+    bool ok = false;
+#pragma unroll 1
+    for (uint32_t i = 0; i < a.tries && !ok; ++i) ok = try_wait_us(bar, parity);
+    if (__all_sync(kFull, ok)) return true;
+    *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
+    return false;
+}
+
+// One thread of the converged warp, known to the compiler as one.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+// Waits for what is in flight when a role ends, a fifth of a second at most.
+__device__ __forceinline__ void drain(uint64_t *bar, uint32_t parity) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < 200000 && !try_wait_us(bar, parity); ++i) {
+    }
+}
+
+// One thread's wait.
+template <typename Ctl_, typename Args_>
+__device__ __forceinline__ bool lane_wait(uint64_t *bar, uint32_t parity, Ctl_ &c, const Args_ &a) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < a.tries; ++i)
+        if (try_wait_us(bar, parity)) return true;
+    *reinterpret_cast<volatile int *>(&c.abort_flag) = 1;
+    return false;
 }
 
 // ---------------------------------------------------------------- softmax
