@@ -113,6 +113,7 @@ typedef enum {
 #define RPS_KV_MAX_HEADS 1024       /* heads of the cache */
 #define RPS_KV_MAX_SEQ (1 << 20)    /* n_req * n_branch */
 #define RPS_KV_MAX_GROUP 128        /* query heads per head of the cache */
+#define RPS_TREE_MAX_TOKENS 1024    /* drafted tokens of a sequence */
 
 /* Hyper-parameters (Sec. 4 "Implementation details": k_max = 10, r = 0.1,
  * tau_pivot = 0.9 / 0.95, lambda in [0.1, 0.5]; Appendix C: tau = 0.9). */
@@ -650,6 +651,140 @@ size_t rps_prefix_attention_workspace_bytes(const rps_kv_cache *kv, int32_t n_q,
  * that gives up reports RPS_DEVERR_TIMEOUT (the output is then incomplete). */
 rps_status rps_prefix_attention_fwd(const rps_prefix_attention *attn, const rps_kv_cache *kv, void *d_ws,
                                     size_t ws_bytes, rps_stream_t stream);
+
+/*
+ * Positions and norms of queries and keys. For a head x of D elements: where its side
+ * (queries or keys) has weights w, y = x w / sqrt(mean(x^2) + eps), else y = x. Then the
+ * first rotary_dim elements are turned in pairs, (i, i + rotary_dim / 2), or with
+ * interleaved != 0 (2i, 2i + 1): by the angle a = position * frequency of pair i,
+ *   (y0, y1) -> amplitude * (y0 cos a - y1 sin a, y1 cos a + y0 sin a).
+ * The elements past rotary_dim stay as they are. Sums, angles and products in fp32 and
+ * more, rounded once at the end. Frequencies are given as turns[i]: the turns that a
+ * position makes, in units of 2^-64 (rps_rope_turns of the radians), so that far positions
+ * lose nothing. Scaled contexts come as scaled frequencies and an amplitude.
+ * rotary_dim: 0 (no rotation, turns may be NULL) or a multiple of 16 up to D; weights: NULL
+ * or [D] of the heads' dtype, 16-byte aligned.
+ */
+typedef struct {
+    const uint64_t *turns; /* [rotary_dim / 2], device */
+    int32_t rotary_dim, interleaved;
+    float amplitude, eps;
+    const void *q_weight, *k_weight;
+} rps_rope;
+
+/* Heads [n_seq][n_tok][n_heads][D], D contiguous, the other strides in elements, multiples
+ * of 8, bases 16-byte aligned; strides of dimensions of one are not used. dst may be src
+ * itself with the same strides, and must not overlap it otherwise. */
+typedef struct {
+    const void *src;
+    void *dst;
+    int32_t n_heads;
+    int64_t src_seq, src_token, src_head, dst_seq, dst_token, dst_head;
+} rps_heads;
+
+/* The fraction of a turn that `radians` makes, in units of 2^-64 (0 for what is not finite). Host only. */
+uint64_t rps_rope_turns(double radians);
+
+/*
+ * Queries and keys (k may be NULL) with their norms and positions. d_pos [n_seq][n_tok]
+ * (NULL: token i of its sequence is at position i). dtype RPS_BF16 or RPS_F16, head_dim a
+ * multiple of 16 up to 256. One launch. Errors: RPS_ERR_INVALID_ARG for NULL or misaligned
+ * pointers, sizes, strides or parameters out of range; RPS_ERR_UNSUPPORTED beyond the
+ * limits above.
+ */
+rps_status rps_rope_heads(const rps_rope *rope, const rps_heads *q, const rps_heads *k, int32_t dtype, int32_t head_dim,
+                          int32_t n_seq, int32_t n_tok, const int32_t *d_pos, rps_stream_t stream);
+
+/*
+ * rps_kv_write with norms and positions on the way, and those of the same tokens'
+ * queries in the same launch. Sequence s brings its last m = d_n_tok[s] tokens (NULL:
+ * n_new; what is outside 0..n_new counts as the nearest), rows i < m of k_new, v_new and
+ * q [n_req * n_branch][n_new][heads][head_dim]: row i is token len[s] - m + i, at position
+ * d_pos[s][i] (NULL: the token's index). Keys are written with norm and rotation, values as they
+ * are; q->dst (q may be NULL) takes the queries. Rows before token 0, those of absent
+ * sequences and rows i >= m are left out, of q too. A row whose page has a count above 1 is not
+ * written and sets RPS_DEVERR_SHARED, a page id outside the cache or a length beyond the
+ * table RPS_DEVERR_PAGE (the length counts as the table's capacity). rope NULL: rows as they are. dst of k_new and
+ * v_new is not used; rows and cache must not overlap. One launch; errors as for rps_rope_heads.
+ */
+rps_status rps_kv_append(const rps_kv_cache *kv, int32_t layer, const rps_rope *rope, const rps_heads *q,
+                         const rps_heads *k_new, const rps_heads *v_new, int32_t n_new, const int32_t *d_n_tok,
+                         const int32_t *d_pos, rps_stream_t stream);
+
+/*
+ * Drafted tokens: several continuations of a sequence as a tree of its last tokens, so
+ * that one pass checks them all and their common beginnings are computed once. Sequence s
+ * has m = d_n_tok[s] of them (NULL: n_tok; what is outside 0..n_tok counts as the nearest).
+ * d_parent [n_seq][n_tok]: the drafted token that token i follows (before it: below i), -1: the
+ * context's last. Written for i < m: d_mask [n_seq][n_tok][ceil(n_tok / 32)], bit j % 32 of word
+ * j / 32 set for i itself and its ancestors; d_pos [n_seq][n_tok] (or NULL), the number of i's
+ * ancestors, plus d_len[s] - m where d_len (the sequences' lengths, the drafted tokens among them)
+ * is not NULL: its position. A parent out of range sets RPS_DEVERR_ROW_INDEX and counts as -1.
+ * n_tok at most RPS_TREE_MAX_TOKENS. One launch.
+ */
+rps_status rps_tree_masks(const int32_t *d_parent, const int32_t *d_n_tok, const int32_t *d_len, int32_t n_seq, int32_t n_tok,
+                          uint32_t *d_mask, int32_t *d_pos, rps_stream_t stream);
+
+/*
+ * The accepted path of each sequence's drafted tokens moves to their front: with m =
+ * d_n_tok[s] drafted tokens (NULL: n_q; clamped to 0..n_q), the keys and values of token len - m + d_path[s][d] go to
+ * token len - m + d, d < d_n_keep[s], in every layer. d_path [n_req * n_branch][n_path] ascends.
+ * d_new_len (or NULL) takes len - m + n_keep, -1 for absent sequences: the lengths for
+ * rps_kv_resize, which gives the other tokens' pages back; len itself stays. A path that does not
+ * ascend or leaves 0..m-1, and more kept tokens than n_path or m, set RPS_DEVERR_ROW_INDEX,
+ * move nothing of their sequence and keep its length. A row whose new page has a count above 1
+ * is left out and sets RPS_DEVERR_SHARED, a page id outside the cache RPS_DEVERR_PAGE. n_path and n_q at most
+ * RPS_TREE_MAX_TOKENS, at most 65535 sequences. One launch.
+ */
+rps_status rps_kv_keep_path(const rps_kv_cache *kv, const int32_t *d_path, const int32_t *d_n_keep, int32_t n_path,
+                            const int32_t *d_n_tok, int32_t n_q, int32_t *d_new_len, rps_stream_t stream);
+
+/*
+ * Attention of each sequence's newest tokens over its cached keys and values, each with a
+ * mask of its own over those tokens: for query i < m of sequence s (m = d_n_tok[s] as above) with
+ * n = len[s] tokens, and each query head h (head h / (n_heads / kv->n_heads) of the cache):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,  lse = log sum_j exp(scale * q . k_j)
+ * over the tokens j < n - m and the drafted ones j = n - m + t whose bit t is set in
+ * mask[s][i] ([ceil(n_q / 32)] words, as rps_tree_masks writes them; nothing is implied, also
+ * not i itself). mask NULL: a chain, bits 0..i (with n_q = 1 the form for single tokens). fp32
+ * scores, sums and accumulation; probabilities are rounded to the cache's type before they
+ * weight the values, the output to it at the end. A query that sees nothing, or whose scores are
+ * all -inf, gets out = 0 and lse = -inf. Rows i >= m and rows of absent sequences are left as
+ * they are. Tokens past a sequence's length may hold anything, keys that a row does not see
+ * anything too; the values of tokens below the length must be finite (one of inf or NaN makes
+ * rows of its sequence that do not see it NaN as well). A page id outside the cache makes
+ * the rows that see its keys NaN and sets RPS_DEVERR_PAGE; a length beyond the table counts
+ * as the table's capacity.
+ * q, out [n_req * n_branch][n_q][n_heads][128] of the cache's dtype, 128 contiguous, other strides
+ * in elements, multiples of 8, bases 16-byte aligned; lse [n_req * n_branch][n_q][n_heads] fp32 or
+ * NULL. n_heads a multiple of kv->n_heads, at most RPS_KV_MAX_GROUP times it; n_q at most
+ * RPS_TREE_MAX_TOKENS; scale finite and above 0. out must not overlap q or the cache. The
+ * lengths and the tables must not change during the call. (Sequences that share pages read them
+ * once each; rps_prefix_attention_fwd reads them once for all.)
+ */
+typedef struct {
+    const void *q;
+    void *out;
+    float *lse;
+    int32_t n_q, n_heads, layer;
+    int64_t q_seq_stride, q_token_stride, q_head_stride;
+    int64_t out_seq_stride, out_token_stride, out_head_stride;
+    const int32_t *n_tok;
+    const uint32_t *mask;
+    float scale;
+} rps_tree_attention;
+
+/* Workspace bytes of rps_tree_attention_fwd (0 for invalid arguments). The workspace needs
+ * no initialisation and keeps nothing between calls; one workspace must not serve two calls
+ * that can overlap. */
+size_t rps_tree_attention_workspace_bytes(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads);
+
+/* Two launches on `stream`. Errors: RPS_ERR_INVALID_ARG for NULL or misaligned pointers,
+ * sizes or strides out of range, or a small workspace; RPS_ERR_UNSUPPORTED beyond the limits
+ * above; RPS_ERR_CUDA when the tensor-map encoder is not available. A bounded device
+ * wait that gives up reports RPS_DEVERR_TIMEOUT (the output is then incomplete). */
+rps_status rps_tree_attention_fwd(const rps_tree_attention *attn, const rps_kv_cache *kv, void *d_ws, size_t ws_bytes,
+                                  rps_stream_t stream);
 
 /* Synchronise `stream`, then read and clear the calling device's error word.
  * Returns RPS_OK or RPS_ERR_DEVICE (with the RPS_DEVERR_* bits in *detail when

@@ -13,6 +13,7 @@ one decoding step together on preallocated buffers.
 from __future__ import annotations
 
 import ctypes as C
+import math
 from dataclasses import dataclass
 from operator import attrgetter
 from pathlib import Path
@@ -35,6 +36,7 @@ WIN_ANCHOR, WIN_SKIP, WIN_DONE = -1, -2, -3
 DEVERR_ROW_INDEX, DEVERR_NONFINITE, DEVERR_MASK, DEVERR_TOKEN = 0x1, 0x2, 0x4, 0x8
 DEVERR_TIMEOUT, DEVERR_WORKSPACE = 0x10, 0x20
 DEVERR_PAGE, DEVERR_NO_PAGES, DEVERR_SHARED = 0x40, 0x80, 0x100
+RPS_TREE_MAX_TOKENS = 1024
 
 _p = C.c_void_p
 
@@ -154,7 +156,34 @@ class RpsPrefixAttention(C.Structure):
                 ("out_head_stride", C.c_int64), ("shared_len", _p), ("scale", C.c_float)]
 
 
+class RpsRope(C.Structure):
+    _fields_ = [("turns", _p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_float),
+                ("eps", C.c_float), ("q_weight", _p), ("k_weight", _p)]
+
+
+class RpsHeads(C.Structure):
+    _fields_ = [("src", _p), ("dst", _p), ("n_heads", C.c_int32)] + [
+        (n, C.c_int64) for n in ("src_seq", "src_token", "src_head", "dst_seq", "dst_token", "dst_head")]
+
+
+class RpsTreeAttention(C.Structure):
+    _fields_ = [("q", _p), ("out", _p), ("lse", _p), ("n_q", C.c_int32), ("n_heads", C.c_int32), ("layer", C.c_int32),
+                ("q_seq_stride", C.c_int64), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out_seq_stride", C.c_int64), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64),
+                ("n_tok", _p), ("mask", _p), ("scale", C.c_float)]
+
+
 # (structs by address, as for rps_run_step)
+_lib.rps_rope_turns.restype = C.c_uint64
+_lib.rps_rope_turns.argtypes = [C.c_double]
+_lib.rps_rope_heads.restype = C.c_int
+_lib.rps_rope_heads.argtypes = [_p, _p, _p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _p, _p]
+_lib.rps_tree_masks.restype = C.c_int
+_lib.rps_tree_masks.argtypes = [_p, _p, _p, C.c_int32, C.c_int32, _p, _p, _p]
+_lib.rps_tree_attention_workspace_bytes.restype = C.c_size_t
+_lib.rps_tree_attention_workspace_bytes.argtypes = [_p, C.c_int32, C.c_int32]
+_lib.rps_tree_attention_fwd.restype = C.c_int
+_lib.rps_tree_attention_fwd.argtypes = [_p, _p, _p, C.c_size_t, _p]
 _lib.rps_prefix_attention_workspace_bytes.restype = C.c_size_t
 _lib.rps_prefix_attention_workspace_bytes.argtypes = [_p, C.c_int32, C.c_int32]
 _lib.rps_prefix_attention_fwd.restype = C.c_int
@@ -164,7 +193,9 @@ _lib.rps_kv_workspace_bytes.argtypes = [_p]
 for _n, _a in (("reorder", [_p, _p, _p, _p, C.c_size_t, _p]), ("fork_branches", [_p, _p, _p, _p, C.c_size_t, _p]),
                ("commit", [_p, _p, _p, C.c_size_t, _p]), ("resize", [_p, _p, _p, C.c_size_t, _p]),
                ("compact", [_p, _p, _p, C.c_size_t, _p]), ("copy_pages", [_p, _p, _p, _p, C.c_int32, _p]),
-               ("write", [_p, C.c_int32, _p, _p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _p])):
+               ("write", [_p, C.c_int32, _p, _p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _p]),
+               ("append", [_p, C.c_int32, _p, _p, _p, _p, C.c_int32, _p, _p, _p]),
+               ("keep_path", [_p, _p, _p, C.c_int32, _p, C.c_int32, _p, _p])):
     _f = getattr(_lib, "rps_kv_" + _n)
     _f.restype, _f.argtypes = C.c_int, _a
 _lib.rps_debug_set_ring_wait_ns.restype = C.c_uint64
@@ -727,6 +758,183 @@ def rps_prefix_attention_fwd(q: torch.Tensor, kv: KvCacheBuf, layer: int, out: t
            "rps_prefix_attention_fwd")
 
 
+# --------------------------------------------------------------------------- positions, drafted tokens
+def rope_inv_freq(rotary_dim: int, base: float = 10000.0, linear: float = 1.0, parts=None):
+    """Radians per position of each pair, and the amplitude of the rotated elements: ``base ** (-2 i / rotary_dim)``,
+    divided by ``linear``, or scaled by parts (``parts = (factor, trained_length, fast, slow)``, arXiv 2309.00071): pairs
+    that make more than ``fast`` turns over the trained length stay, those below ``slow`` are divided by the factor,
+    a ramp lies between, and the amplitude is ``0.1 ln(factor) + 1``."""
+    freq = [base ** (-2.0 * i / rotary_dim) / linear for i in range(rotary_dim // 2)]
+    if parts is None:
+        return freq, 1.0
+    factor, trained, fast, slow = parts
+    if not (factor >= 1.0 and trained > 0 and fast > slow):
+        raise ValueError("parts: a factor of 1 or more, a trained length above 0, fast above slow")
+    for i, f in enumerate(freq):
+        keep = min(1.0, max(0.0, (trained * f / (2.0 * math.pi) - slow) / (fast - slow)))
+        freq[i] = f * keep + f / factor * (1.0 - keep)
+    return freq, 0.1 * math.log(factor) + 1.0
+
+
+class Rope:
+    """Rotation and norms of queries and keys (``rps_rope`` of the C ABI), made once and kept.
+
+    ``inv_freq``: radians per position of each pair (``rope_inv_freq``; empty or None: no rotation), as Python or
+    numpy doubles; ``interleaved``: pairs side by side instead of in two halves; ``amplitude``: factor of the
+    rotated elements; ``q_weight``, ``k_weight``: ``[head_dim]`` CUDA tensors of the heads' dtype, or None (no norm)."""
+
+    def __init__(self, inv_freq, device, interleaved: bool = False, amplitude: float = 1.0, q_weight=None, k_weight=None,
+                 eps: float = 1e-6):
+        turns = [_lib.rps_rope_turns(float(f)) for f in (() if inv_freq is None else inv_freq)]
+        self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device=device)
+        self.q_weight, self.k_weight, self.rotary_dim = q_weight, k_weight, 2 * len(turns)
+        for w in (q_weight, k_weight):
+            if w is not None and (w.dim() != 1 or not w.is_contiguous() or w.dtype not in _KV_DTYPES):
+                raise ValueError("norm weights: contiguous [head dim] tensors, bf16 or fp16")
+        self._struct = RpsRope(self.turns.data_ptr() if turns else None, 2 * len(turns), 1 if interleaved else 0, amplitude,
+                               eps, _ptr(q_weight), _ptr(k_weight))
+
+    def _c(self, head_dim: int, dtype) -> int:
+        for w in (self.q_weight, self.k_weight):
+            if w is not None and (w.shape[0] != head_dim or w.dtype is not dtype):
+                raise ValueError(f"norm weights: [{head_dim}] of {dtype}, as the heads")
+        return C.addressof(self._struct)
+
+
+def _heads(name: str, src: torch.Tensor, dst: Optional[torch.Tensor] = None) -> RpsHeads:
+    """``[n_seq][n_tok][heads][D]`` rows, and where they go."""
+    st, h = src.stride(), src.shape[2]
+    if st[3] != 1:
+        raise ValueError(f"{name}: head dim contiguous")
+    if dst is None:
+        return RpsHeads(src.data_ptr(), None, h, st[0], st[1], st[2], 0, 0, 0)
+    to = dst.stride()
+    if dst.shape != src.shape or to[3] != 1:
+        raise ValueError(f"{name}: source and destination of one shape, head dim contiguous")
+    if dst.dtype is not src.dtype:
+        raise TypeError(f"{name}: source and destination of one dtype")
+    return RpsHeads(src.data_ptr(), dst.data_ptr(), h, st[0], st[1], st[2], to[0], to[1], to[2])
+
+
+def rps_rope_heads(rope: Rope, q: torch.Tensor, q_out: torch.Tensor, k: Optional[torch.Tensor] = None,
+                   k_out: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Queries (and keys) ``[n_seq][n_tok][heads][D]`` with their norms and positions; ``q_out`` may be ``q``. ``pos``:
+    int32 ``[n_seq][n_tok]`` (None: token i of its sequence is at position i)."""
+    handle = _here(stream, q, q_out, k, k_out, pos, rope.turns if rope.rotary_dim else None, rope.q_weight, rope.k_weight)
+    if q.dim() != 4 or q.dtype not in _KV_DTYPES:
+        raise ValueError("q: [n_seq][n_tok][heads][head dim], bf16 or fp16")
+    if (k is None) != (k_out is None):
+        raise ValueError("k comes with k_out")
+    if k is not None and (k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3] or k.dtype is not q.dtype):
+        raise ValueError("k: [n_seq][n_tok][heads][head dim], as q")
+    n_seq, n_tok, _, d = q.shape
+    a = _heads("q", q, q_out)
+    b = None if k is None else _heads("k", k, k_out)
+    _check(_lib.rps_rope_heads(rope._c(d, q.dtype), C.addressof(a), None if b is None else C.addressof(b),
+                               _KV_DTYPES[q.dtype], d, n_seq, n_tok, None if pos is None else _ints("pos", pos, n_seq * n_tok),
+                               handle), "rps_rope_heads")
+
+
+def _as_seqs(name: str, t: torch.Tensor, kv: KvCacheBuf) -> torch.Tensor:
+    """``[n_req][n_branch][...]`` as ``[n_seq][...]``, without a copy."""
+    if t.dim() != 5 or t.shape[0] != kv.n_req or t.shape[1] != kv.n_branch or t.shape[4] != kv.k.shape[4]:
+        raise ValueError(f"{name}: [n_req][n_branch][n_tok][heads][head dim]")
+    if t.dtype is not kv.k.dtype:
+        raise TypeError(f"{name} must be {kv.k.dtype}, as the cache")
+    if kv.n_branch == 1:
+        return t[:, 0]
+    if kv.n_req == 1:
+        return t[0]
+    st = t.stride()
+    if st[0] != kv.n_branch * st[1]:
+        raise ValueError(f"{name}: requests at n_branch sequences' stride")
+    return t.flatten(0, 1) if t.is_contiguous() else t.as_strided((kv.n_seq, *t.shape[2:]), st[1:])
+
+
+def rps_kv_append(kv: KvCacheBuf, layer: int, rope: Optional[Rope], k_new: torch.Tensor, v_new: torch.Tensor,
+                  q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, n_tok: Optional[torch.Tensor] = None,
+                  pos: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rps_kv_write with norms and positions on the way: keys and values ``[n_req][n_branch][n_new][n_heads][128]`` of each
+    sequence's last ``n_tok[s]`` tokens (None: ``n_new``) into its pages, the same tokens' queries ``q`` into ``q_out`` (which
+    may be ``q``). ``pos``: int32 ``[n_req][n_branch][n_new]`` (None: a token's index in its sequence)."""
+    at = kv._c()
+    handle = _here(stream, kv.k, k_new, v_new, q, q_out, n_tok, pos, rope.turns if rope is not None and rope.rotary_dim else None,
+                   None if rope is None else rope.q_weight, None if rope is None else rope.k_weight)
+    if (q is None) != (q_out is None):
+        raise ValueError("q comes with q_out")
+    k1, v1 = _as_seqs("k_new", k_new, kv), _as_seqs("v_new", v_new, kv)
+    n_new = k1.shape[1]
+    if k1.shape[2] != kv.k.shape[2] or v1.shape != k1.shape:
+        raise ValueError("k_new and v_new: [n_req][n_branch][n_new][n_heads][head dim]")
+    a = None
+    if q is not None:
+        q1 = _as_seqs("q", q, kv)
+        if q1.shape[1] != n_new:
+            raise ValueError("q: as many tokens as k_new")
+        a = _heads("q", q1, _as_seqs("q_out", q_out, kv))
+    b, c = _heads("k_new", k1), _heads("v_new", v1)
+    _check(_lib.rps_kv_append(at, layer, None if rope is None else rope._c(k1.shape[3], k1.dtype),
+                              None if a is None else C.addressof(a), C.addressof(b), C.addressof(c), n_new,
+                              None if n_tok is None else _ints("n_tok", n_tok, kv.n_seq),
+                              None if pos is None else _ints("pos", pos, kv.n_seq * n_new), handle), "rps_kv_append")
+
+
+def rps_tree_masks(parent: torch.Tensor, mask: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                   n_tok: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None, stream=None) -> None:
+    """From the parents ``[..., n_tok]`` of drafted tokens (int32; -1: the context's last token) the masks of what they see,
+    ``[..., n_tok, ceil(n_tok / 32)]`` int32 words, and their positions like ``parent`` (with ``length``, the
+    sequences' lengths; without, their depths)."""
+    handle = _here(stream, parent, mask, pos, n_tok, length)
+    if parent.dim() < 1 or parent.numel() == 0:
+        raise ValueError("parent: [..., n_tok]")
+    n = parent.shape[-1]
+    n_seq = parent.numel() // n
+    _check(_lib.rps_tree_masks(_ints("parent", parent, n_seq * n), None if n_tok is None else _ints("n_tok", n_tok, n_seq),
+                               None if length is None else _ints("length", length, n_seq), n_seq, n,
+                               _ints("mask", mask, n_seq * n * -(-n // 32)), None if pos is None else _ints("pos", pos, n_seq * n),
+                               handle), "rps_tree_masks")
+
+
+def rps_kv_keep_path(kv: KvCacheBuf, path: torch.Tensor, n_keep: torch.Tensor, new_len: Optional[torch.Tensor], n_q: int,
+                     n_tok: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The accepted path of each sequence's last ``n_tok[s]`` tokens (None: ``n_q``) to their front, every layer: drafted
+    token ``path[s][d]`` (int32 ``[..., n_path]``, ascending) becomes the d-th, d < ``n_keep[s]``. ``new_len`` takes the
+    lengths for ``rps_kv_resize``."""
+    at, handle = kv._c(), _here(stream, kv.k, path, n_keep, new_len, n_tok)
+    n_path = path.shape[-1] if path.dim() else 0
+    _check(_lib.rps_kv_keep_path(at, _ints("path", path, kv.n_seq * n_path), _ints("n_keep", n_keep, kv.n_seq), n_path,
+                                 None if n_tok is None else _ints("n_tok", n_tok, kv.n_seq), n_q,
+                                 None if new_len is None else _ints("new_len", new_len, kv.n_seq), handle), "rps_kv_keep_path")
+
+
+def rps_tree_attention_workspace_bytes(kv: KvCacheBuf, n_q: int, n_heads: int) -> int:
+    n = _lib.rps_tree_attention_workspace_bytes(kv._c(), n_q, n_heads)
+    if n == 0:
+        raise RPSError(RPS_ERR_INVALID_ARG, "rps_tree_attention_workspace_bytes")
+    return n
+
+
+def rps_tree_attention_fwd(q: torch.Tensor, kv: KvCacheBuf, layer: int, out: torch.Tensor, ws: torch.Tensor,
+                           mask: Optional[torch.Tensor], scale: float, n_tok: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of the sequences' last ``n_tok[s]`` tokens (None: all ``n_q``) over their cached keys, each seeing the
+    context and the drafted tokens of its mask (``rps_tree_masks``; None: a chain): q, out
+    ``[n_req][n_branch][n_q][n_heads][128]`` of the cache's dtype, lse (optional) fp32 ``[n_req][n_branch][n_q][n_heads]``."""
+    at, handle = kv._c(), _here(stream, kv.k, q, out, ws, mask, n_tok, lse)
+    q1, o1 = _as_seqs("q", q, kv), _as_seqs("out", out, kv)
+    _, n_q, h, _ = q1.shape
+    if o1.shape != q1.shape:
+        raise ValueError("q and out: [n_req][n_branch][n_q][n_heads][head dim], as the cache")
+    st, to = q1.stride(), o1.stride()
+    if st[3] != 1 or to[3] != 1:
+        raise ValueError("q and out: head dim contiguous")
+    a = RpsTreeAttention(q1.data_ptr(), o1.data_ptr(),
+                         None if lse is None else _ints("lse", lse, kv.n_seq * n_q * h, torch.float32), n_q, h, layer,
+                         st[0], st[1], st[2], to[0], to[1], to[2], None if n_tok is None else _ints("n_tok", n_tok, kv.n_seq),
+                         None if mask is None else _ints("mask", mask, kv.n_seq * n_q * -(-n_q // 32)), scale)
+    _check(_lib.rps_tree_attention_fwd(C.addressof(a), at, ws.data_ptr(), ws.nbytes, handle), "rps_tree_attention_fwd")
+
+
 # --------------------------------------------------------------------------- one step
 class Step:
     """Preallocated buffers and the ABI calls of one RPS decoding step.
@@ -811,17 +1019,21 @@ class BranchCache:
     every sequence to its context and block, per layer ``write`` the block's keys and
     values and ``attend`` over context and block (the context's pages read once for 128
     query rows of a request's branches), then ``commit`` the winner of ``CommitBuf.winner``: its
-    block becomes the base's. Pages, workspaces and bookkeeping are allocated once;
+    block becomes the base's. Drafted tokens of a sequence, as a tree instead of branches:
+    ``resize`` to its context and tokens, ``append`` and ``attend_tree`` per layer, then
+    ``keep_path`` of what was accepted (``tree=True`` allocates its workspace). Pages, workspaces and bookkeeping are allocated once;
     every call is asynchronous and reads what it decides by from device memory, so a
     step can be captured as a CUDA graph."""
 
     def __init__(self, n_layers: int, n_pages: int, n_heads: int, page_size: int, n_req: int, n_branch: int,
-                 max_pages: int, n_q: int, n_query_heads: int, device, dtype=torch.bfloat16):
+                 max_pages: int, n_q: int, n_query_heads: int, device, dtype=torch.bfloat16, tree: bool = False):
         self.kv = KvCacheBuf.alloc(n_layers, n_pages, n_heads, page_size, n_req, n_branch, max_pages, device, dtype)
         ws = lambda n: torch.empty(n, dtype=torch.uint8, device=device)
         self.ws = ws(rps_kv_workspace_bytes(self.kv))
         self.ws_attn = ws(rps_prefix_attention_workspace_bytes(self.kv, n_q, n_query_heads))
+        self.ws_tree = ws(rps_tree_attention_workspace_bytes(self.kv, n_q, n_query_heads)) if tree else None
         self.n_live = torch.zeros(1, dtype=torch.int32, device=device)
+        self.new_len = torch.zeros((n_req, n_branch), dtype=torch.int32, device=device)
 
     def resize(self, new_len, stream=None):
         rps_kv_resize(self.kv, new_len, self.ws, stream)
@@ -835,6 +1047,21 @@ class BranchCache:
     def attend(self, layer, q, out, ctx_len, scale, causal=False, lse=None, stream=None):
         """``ctx_len``: as given to ``fork`` (None: nothing is shared)."""
         rps_prefix_attention_fwd(q, self.kv, layer, out, self.ws_attn, ctx_len, scale, causal, lse, stream)
+
+    def append(self, layer, rope, k_new, v_new, q=None, q_out=None, n_tok=None, pos=None, stream=None):
+        """``write`` with the rotation and norms of keys (and of the same tokens' queries) on the way."""
+        rps_kv_append(self.kv, layer, rope, k_new, v_new, q, q_out, n_tok, pos, stream)
+
+    def attend_tree(self, layer, q, out, mask, scale, n_tok=None, lse=None, stream=None):
+        """Drafted tokens: each sequence's last tokens under the masks of ``rps_tree_masks`` (None: a chain)."""
+        if self.ws_tree is None or self.ws_tree.device != q.device:
+            raise ValueError("attend_tree needs a cache made with tree=True")
+        rps_tree_attention_fwd(q, self.kv, layer, out, self.ws_tree, mask, scale, n_tok, lse, stream)
+
+    def keep_path(self, path, n_keep, n_q, n_tok=None, stream=None):
+        """The accepted path's tokens stay, in their order, the other drafted tokens' pages go back."""
+        rps_kv_keep_path(self.kv, path, n_keep, self.new_len, n_q, n_tok, stream)
+        rps_kv_resize(self.kv, self.new_len, self.ws, stream)
 
     def commit(self, winner, stream=None):
         rps_kv_commit(self.kv, winner, self.ws, stream)
