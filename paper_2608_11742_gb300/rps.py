@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 from dataclasses import dataclass
 from operator import attrgetter
 from pathlib import Path
@@ -785,70 +786,81 @@ class Rope:
 
     def __init__(self, inv_freq, device, interleaved: bool = False, amplitude: float = 1.0, q_weight=None, k_weight=None,
                  eps: float = 1e-6):
-        turns = [_lib.rps_rope_turns(float(f)) for f in (() if inv_freq is None else inv_freq)]
+        freq = [float(f) for f in (() if inv_freq is None else inv_freq)]
+        self._made_of = (freq, device, interleaved, amplitude, q_weight, k_weight, eps)
+        turns = [_lib.rps_rope_turns(f) for f in freq]
         self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device=device)
         self.q_weight, self.k_weight, self.rotary_dim = q_weight, k_weight, 2 * len(turns)
-        for w in (q_weight, k_weight):
-            if w is not None and (w.dim() != 1 or not w.is_contiguous() or w.dtype not in _KV_DTYPES):
-                raise ValueError("norm weights: contiguous [head dim] tensors, bf16 or fp16")
+        self._weights = [w for w in (q_weight, k_weight) if w is not None]
+        for w in self._weights:
+            if w.dim() != 1 or not w.is_contiguous() or w.dtype not in _KV_DTYPES or w.device != self.turns.device:
+                raise ValueError(f"norm weights: contiguous [head dim] tensors on {self.turns.device}, bf16 or fp16")
+        if any((w.shape, w.dtype) != (self._weights[0].shape, self._weights[0].dtype) for w in self._weights):
+            raise ValueError("norm weights: of one size and dtype")
+        self._kind = (self._weights[0].shape[0], self._weights[0].dtype) if self._weights else None
+        self.any = self.turns  # (a tensor on the device that all of them are on)
         self._struct = RpsRope(self.turns.data_ptr() if turns else None, 2 * len(turns), 1 if interleaved else 0, amplitude,
                                eps, _ptr(q_weight), _ptr(k_weight))
+        self._at = C.addressof(self._struct)
 
     def _c(self, head_dim: int, dtype) -> int:
-        for w in (self.q_weight, self.k_weight):
-            if w is not None and (w.shape[0] != head_dim or w.dtype is not dtype):
-                raise ValueError(f"norm weights: [{head_dim}] of {dtype}, as the heads")
-        return C.addressof(self._struct)
+        if self._kind is not None and self._kind != (head_dim, dtype):
+            raise ValueError(f"norm weights: [{head_dim}] of {dtype}, as the heads")
+        return self._at
+
+    def __reduce__(self):  # a copy or a pickle is made anew
+        return Rope, self._made_of
 
 
-def _heads(name: str, src: torch.Tensor, dst: Optional[torch.Tensor] = None) -> RpsHeads:
+# (the structs of these calls as packed bytes: a ctypes struct field by field takes four times as long)
+_HEADS = struct.Struct("@PPi6q")
+_TREE_ATTENTION = struct.Struct("@PPPiii6qPPf4x")
+assert _HEADS.size == C.sizeof(RpsHeads) and _TREE_ATTENTION.size == C.sizeof(RpsTreeAttention)
+
+
+def _heads(name: str, src: torch.Tensor, dst: torch.Tensor) -> bytes:
     """``[n_seq][n_tok][heads][D]`` rows, and where they go."""
-    st, h = src.stride(), src.shape[2]
-    if st[3] != 1:
-        raise ValueError(f"{name}: head dim contiguous")
-    if dst is None:
-        return RpsHeads(src.data_ptr(), None, h, st[0], st[1], st[2], 0, 0, 0)
-    to = dst.stride()
-    if dst.shape != src.shape or to[3] != 1:
+    shape, st, to = src.shape, src.stride(), dst.stride()
+    if dst.shape != shape or st[3] != 1 or to[3] != 1:
         raise ValueError(f"{name}: source and destination of one shape, head dim contiguous")
     if dst.dtype is not src.dtype:
         raise TypeError(f"{name}: source and destination of one dtype")
-    return RpsHeads(src.data_ptr(), dst.data_ptr(), h, st[0], st[1], st[2], to[0], to[1], to[2])
+    return _HEADS.pack(src.data_ptr(), dst.data_ptr(), shape[2], st[0], st[1], st[2], to[0], to[1], to[2])
 
 
 def rps_rope_heads(rope: Rope, q: torch.Tensor, q_out: torch.Tensor, k: Optional[torch.Tensor] = None,
                    k_out: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, stream=None) -> None:
     """Queries (and keys) ``[n_seq][n_tok][heads][D]`` with their norms and positions; ``q_out`` may be ``q``. ``pos``:
     int32 ``[n_seq][n_tok]`` (None: token i of its sequence is at position i)."""
-    handle = _here(stream, q, q_out, k, k_out, pos, rope.turns if rope.rotary_dim else None, rope.q_weight, rope.k_weight)
-    if q.dim() != 4 or q.dtype not in _KV_DTYPES:
+    handle = _here(stream, q, q_out, k, k_out, pos, rope.any)
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 4 or dtype not in _KV_DTYPES:
         raise ValueError("q: [n_seq][n_tok][heads][head dim], bf16 or fp16")
     if (k is None) != (k_out is None):
         raise ValueError("k comes with k_out")
-    if k is not None and (k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3] or k.dtype is not q.dtype):
-        raise ValueError("k: [n_seq][n_tok][heads][head dim], as q")
-    n_seq, n_tok, _, d = q.shape
-    a = _heads("q", q, q_out)
-    b = None if k is None else _heads("k", k, k_out)
-    _check(_lib.rps_rope_heads(rope._c(d, q.dtype), C.addressof(a), None if b is None else C.addressof(b),
-                               _KV_DTYPES[q.dtype], d, n_seq, n_tok, None if pos is None else _ints("pos", pos, n_seq * n_tok),
-                               handle), "rps_rope_heads")
+    n_seq, n_tok, _, d = shape
+    b = None
+    if k is not None:
+        if len(k.shape) != 4 or k.shape[:2] != shape[:2] or k.shape[3] != d or k.dtype is not dtype:
+            raise ValueError("k: [n_seq][n_tok][heads][head dim], as q")
+        b = _heads("k", k, k_out)
+    _check(_lib.rps_rope_heads(rope._c(d, dtype), _heads("q", q, q_out), b, _KV_DTYPES[dtype], d, n_seq, n_tok,
+                               None if pos is None else _ints("pos", pos, n_seq * n_tok), handle), "rps_rope_heads")
 
 
-def _as_seqs(name: str, t: torch.Tensor, kv: KvCacheBuf) -> torch.Tensor:
-    """``[n_req][n_branch][...]`` as ``[n_seq][...]``, without a copy."""
-    if t.dim() != 5 or t.shape[0] != kv.n_req or t.shape[1] != kv.n_branch or t.shape[4] != kv.k.shape[4]:
-        raise ValueError(f"{name}: [n_req][n_branch][n_tok][heads][head dim]")
-    if t.dtype is not kv.k.dtype:
-        raise TypeError(f"{name} must be {kv.k.dtype}, as the cache")
-    if kv.n_branch == 1:
-        return t[:, 0]
-    if kv.n_req == 1:
-        return t[0]
-    st = t.stride()
-    if st[0] != kv.n_branch * st[1]:
+def _seq_rows(name: str, t: torch.Tensor, kv: KvCacheBuf):
+    """Shape and (sequence, token, head) strides of ``[n_req][n_branch][n_tok][heads][128]``, sequences at one stride."""
+    shape, st, cache = t.shape, t.stride(), kv.k
+    n_req, nb = kv.n_req, kv.n_branch
+    if len(shape) != 5 or shape[0] != n_req or shape[1] != nb or shape[4] != cache.shape[4] or st[4] != 1:
+        raise ValueError(f"{name}: [n_req][n_branch][n_tok][heads][head dim], head dim contiguous")
+    if t.dtype is not cache.dtype:
+        raise TypeError(f"{name} must be {cache.dtype}, as the cache")
+    if nb == 1:
+        return shape, st[0], st[2], st[3]
+    if n_req > 1 and st[0] != nb * st[1]:
         raise ValueError(f"{name}: requests at n_branch sequences' stride")
-    return t.flatten(0, 1) if t.is_contiguous() else t.as_strided((kv.n_seq, *t.shape[2:]), st[1:])
+    return shape, st[1], st[2], st[3]
 
 
 def rps_kv_append(kv: KvCacheBuf, layer: int, rope: Optional[Rope], k_new: torch.Tensor, v_new: torch.Tensor,
@@ -858,23 +870,24 @@ def rps_kv_append(kv: KvCacheBuf, layer: int, rope: Optional[Rope], k_new: torch
     sequence's last ``n_tok[s]`` tokens (None: ``n_new``) into its pages, the same tokens' queries ``q`` into ``q_out`` (which
     may be ``q``). ``pos``: int32 ``[n_req][n_branch][n_new]`` (None: a token's index in its sequence)."""
     at = kv._c()
-    handle = _here(stream, kv.k, k_new, v_new, q, q_out, n_tok, pos, rope.turns if rope is not None and rope.rotary_dim else None,
-                   None if rope is None else rope.q_weight, None if rope is None else rope.k_weight)
+    handle = _here(stream, kv.k, k_new, v_new, q, q_out, n_tok, pos, None if rope is None else rope.any)
+    ks, k0, k1, k2 = _seq_rows("k_new", k_new, kv)
+    vs, v0, v1, v2 = _seq_rows("v_new", v_new, kv)
+    n_new, h = ks[2], kv.k.shape[2]
+    if ks[3] != h or vs != ks:
+        raise ValueError("k_new and v_new: [n_req][n_branch][n_new][n_heads][head dim]")
     if (q is None) != (q_out is None):
         raise ValueError("q comes with q_out")
-    k1, v1 = _as_seqs("k_new", k_new, kv), _as_seqs("v_new", v_new, kv)
-    n_new = k1.shape[1]
-    if k1.shape[2] != kv.k.shape[2] or v1.shape != k1.shape:
-        raise ValueError("k_new and v_new: [n_req][n_branch][n_new][n_heads][head dim]")
     a = None
     if q is not None:
-        q1 = _as_seqs("q", q, kv)
-        if q1.shape[1] != n_new:
-            raise ValueError("q: as many tokens as k_new")
-        a = _heads("q", q1, _as_seqs("q_out", q_out, kv))
-    b, c = _heads("k_new", k1), _heads("v_new", v1)
-    _check(_lib.rps_kv_append(at, layer, None if rope is None else rope._c(k1.shape[3], k1.dtype),
-                              None if a is None else C.addressof(a), C.addressof(b), C.addressof(c), n_new,
+        qs, q0, q1, q2 = _seq_rows("q", q, kv)
+        os, o0, o1, o2 = _seq_rows("q_out", q_out, kv)
+        if qs[2] != n_new or os != qs:
+            raise ValueError("q and q_out: of one shape, as many tokens as k_new")
+        a = _HEADS.pack(q.data_ptr(), q_out.data_ptr(), qs[3], q0, q1, q2, o0, o1, o2)
+    _check(_lib.rps_kv_append(at, layer, None if rope is None else rope._c(128, k_new.dtype), a,
+                              _HEADS.pack(k_new.data_ptr(), 0, h, k0, k1, k2, 0, 0, 0),
+                              _HEADS.pack(v_new.data_ptr(), 0, h, v0, v1, v2, 0, 0, 0), n_new,
                               None if n_tok is None else _ints("n_tok", n_tok, kv.n_seq),
                               None if pos is None else _ints("pos", pos, kv.n_seq * n_new), handle), "rps_kv_append")
 
@@ -921,18 +934,16 @@ def rps_tree_attention_fwd(q: torch.Tensor, kv: KvCacheBuf, layer: int, out: tor
     context and the drafted tokens of its mask (``rps_tree_masks``; None: a chain): q, out
     ``[n_req][n_branch][n_q][n_heads][128]`` of the cache's dtype, lse (optional) fp32 ``[n_req][n_branch][n_q][n_heads]``."""
     at, handle = kv._c(), _here(stream, kv.k, q, out, ws, mask, n_tok, lse)
-    q1, o1 = _as_seqs("q", q, kv), _as_seqs("out", out, kv)
-    _, n_q, h, _ = q1.shape
-    if o1.shape != q1.shape:
+    shape, q0, q1, q2 = _seq_rows("q", q, kv)
+    to, o0, o1, o2 = _seq_rows("out", out, kv)
+    if to != shape:
         raise ValueError("q and out: [n_req][n_branch][n_q][n_heads][head dim], as the cache")
-    st, to = q1.stride(), o1.stride()
-    if st[3] != 1 or to[3] != 1:
-        raise ValueError("q and out: head dim contiguous")
-    a = RpsTreeAttention(q1.data_ptr(), o1.data_ptr(),
-                         None if lse is None else _ints("lse", lse, kv.n_seq * n_q * h, torch.float32), n_q, h, layer,
-                         st[0], st[1], st[2], to[0], to[1], to[2], None if n_tok is None else _ints("n_tok", n_tok, kv.n_seq),
-                         None if mask is None else _ints("mask", mask, kv.n_seq * n_q * -(-n_q // 32)), scale)
-    _check(_lib.rps_tree_attention_fwd(C.addressof(a), at, ws.data_ptr(), ws.nbytes, handle), "rps_tree_attention_fwd")
+    n_q, h, n_seq = shape[2], shape[3], kv.n_seq
+    a = _TREE_ATTENTION.pack(q.data_ptr(), out.data_ptr(),
+                             0 if lse is None else _ints("lse", lse, n_seq * n_q * h, torch.float32), n_q, h, layer, q0, q1, q2,
+                             o0, o1, o2, 0 if n_tok is None else _ints("n_tok", n_tok, n_seq),
+                             0 if mask is None else _ints("mask", mask, n_seq * n_q * -(-n_q // 32)), scale)
+    _check(_lib.rps_tree_attention_fwd(a, at, ws.data_ptr(), ws.nbytes, handle), "rps_tree_attention_fwd")
 
 
 # --------------------------------------------------------------------------- one step
