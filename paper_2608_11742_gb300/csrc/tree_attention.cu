@@ -60,6 +60,7 @@ constexpr int kSmemBytes = kQBufs * kTileBytes + 2 * kStages * kTileBytes + 1024
 constexpr int kThreads = 384;
 constexpr uint32_t kTmemCols = 512;  // S buffers at columns 0 and 128, O at 256 and 384
 constexpr uint32_t kOCol = 256;
+constexpr int kStagedSeqs = 1024;    // sequences whose lengths are kept in shared memory
 constexpr float kLn2 = 0.6931471805599453f;
 // bounds of a tile's sum of P in a row (in units of its reference): P in fp16 stays finite
 constexpr float kMostWeight = 32768.f, kLeastWeight = 1.f / 32768.f;
@@ -82,6 +83,7 @@ struct TreeArgs {
     float c;  // scale * log2(e)
     PageCopies copies;
     int32_t paired;   // units may have two row tiles
+    int32_t sectors;  // output rows begin on 32-byte bounds
     Cut *cut;         // [grid]
     float2 *part_ml;  // [2 * grid][2][128]: maximum and sum of each row of a partial result
     float *part_o;    // [2 * grid][2][128][128]
@@ -98,6 +100,7 @@ struct Ctl {
     float2 ml[2][2][tree::kRows];
     int4 copy_at[2][32];  // a producer's copies: their coordinates, of two tiles
     uint32_t bad[4];      // copies of key tile t whose page id is outside the cache (t % 4)
+    Seq seq[kStagedSeqs];  // as they are used
     int64_t scan[kThreads / 32];
     Walk walk;
     int64_t range_end;
@@ -147,6 +150,7 @@ __device__ __forceinline__ void find_range(const TreeArgs &a, Ctl &c) {
     int longest = 0;
     const auto look = [&](int e) {
         q = e < n_seq ? seq_of(a, e) : Seq{-1, 0};
+        if (e < n_seq && n_seq <= kStagedSeqs) c.seq[e] = q;
         places = tree::places_of(a.s, q, &longest);
         units = static_cast<int64_t>(tree::pairs_of(a.s, q)) * a.s.heads;
     };
@@ -163,12 +167,12 @@ __device__ __forceinline__ void find_range(const TreeArgs &a, Ctl &c) {
     __syncthreads();
     if (work == 0) return;
     const int grid = gridDim.x, me = blockIdx.x;
-    const int n = static_cast<int>(min(static_cast<int64_t>(grid), work));
-    if (n_seq <= kThreads && all_units <= grid && c.longest <= work / grid + tree::kCutCost) {
+    const int n = work < static_cast<int64_t>(grid) * tree::kPairCost ? max(1, static_cast<int>(work) / tree::kPairCost) : grid;
+    if (n_seq <= kThreads && all_units <= grid && c.longest <= tree::divide(work, grid) + tree::kCutCost) {
         const int64_t first = scan_block(units, c.scan, &all_units);
         if (me >= first && me < first + units) {
             const int pairs = tree::pairs_of(a.s, q), u = me - static_cast<int>(first), h = u / pairs, p = u - h * pairs;
-            c.walk = Walk{static_cast<int>(threadIdx.x), h, p, 0, tree::tiles_of(a.s, q, p) + tree::kUnitCost};
+            c.walk = Walk{static_cast<int>(threadIdx.x), h, p, 0, tree::cost_of(a.s, q, p)};
         }
     } else {
         const tree::Ranges r = tree::make_ranges(work, n);
@@ -192,31 +196,42 @@ __device__ __forceinline__ void find_range(const TreeArgs &a, Ctl &c) {
 }
 
 // ---------------------------------------------------------------- roles
-__device__ __forceinline__ bool next(const TreeArgs &a, Walk &w, Piece &x) {
-    return tree::next_piece(a.s, w, x, [&](int s) { return seq_of(a, s); });
+__device__ __forceinline__ bool next(const TreeArgs &a, const Ctl &c, Walk &w, Piece &x) {
+    return tree::next_piece(a.s, w, x, [&](int s) { return a.s.n_seq <= kStagedSeqs ? c.seq[s] : seq_of(a, s); });
 }
 
 // The producers of K (with Q) and of V, in one body: two warps run it.
 __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const CUtensorMap *tm_q, uint8_t *stages,
                                         uint8_t *sq, int lane, Ctl &c, const TreeArgs &a) {
     Walk w = c.walk;
-    Piece p{};
+    Piece p{}, following{};
     uint32_t t = 0;
     int n_q = 0;
     bool ok = true;
     uint64_t *full = is_k ? c.k_full : c.v_full, *empty = is_k ? c.k_empty : c.v_empty;
     const int copies = tree::kRows >> a.copies.copy_log;  // of a tile, 16 at most
     const int half = lane >> 4;
-    // the page of copy lane % 16 of key tile j (-1: not a token of the sequence)
-    const auto page_of = [&](int j, int &token) {
+    // the page of copy lane % 16 of key tile j of a piece (-1: not a token of the sequence)
+    const auto page_of = [&](const Piece &x, int j, int &token) {
         token = j * tree::kRows + ((lane & 15) << a.copies.copy_log);
-        if ((lane & 15) >= copies || j >= p.j1 || token >= p.q.len) return -1;
+        if ((lane & 15) >= copies || j >= x.j1 || token >= x.q.len) return -1;
         // (a negative id is told from a token that is not there)
-        return a.table[static_cast<int64_t>(p.s) * a.s.max_pages + (token >> a.s.page_log)] & 0x7fffffff;
+        return a.table[static_cast<int64_t>(x.s) * a.s.max_pages + (token >> a.s.page_log)] & 0x7fffffff;
     };
+    // A piece ahead: its first pages' ids are on their way while the piece before is copied, and its
+    // queries in L2 (a change of units took 4.5 us, of which the lookups were 2).
+    bool some = next(a, c, w, following);
+    int token = 0, id = some ? page_of(following, following.j0 + half, token) : -1;
 #pragma unroll 1
-    for (int n = 0; ok && next(a, w, p); ++n) {
-        int token, id = page_of(p.j0 + half, token);
+    for (int n = 0; ok && some; ++n) {
+        p = following;
+        some = next(a, c, w, following);
+        int first_token = 0;
+        const int first_id = some ? page_of(following, following.j0 + half, first_token) : -1;
+        if (is_k && some && elect_one())
+#pragma unroll 1
+            for (int r = 0; r < 2 * following.rt; ++r)
+                tma_prefetch_4d(tm_q, r & 1 ? 64 : 0, following.h * a.s.group, (2 * following.p + (r >> 1)) * a.s.tokens, following.s);
 #pragma unroll 1
         for (int j = p.j0; ok && j < p.j1; j += 2) {
             const int two = min(2, p.j1 - j);
@@ -229,7 +244,12 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
             const uint32_t bad = __ballot_sync(kFull, there && bad_page);
             if (bad && is_k && lane == 0) flag_error(a.err, RPS_DEVERR_PAGE);
             __syncwarp();
-            id = page_of(j + 2 + half, token);  // (on its way while these copies wait for their stages)
+            if (j + 2 < p.j1) {
+                id = page_of(p, j + 2 + half, token);  // (on its way while these copies wait for their stages)
+            } else {
+                id = first_id;
+                token = first_token;
+            }
             int done = 0;
             if (elect_one()) {
 #pragma unroll 1
@@ -313,7 +333,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
             const uint32_t h = x & 1, parity = (x >> 1) & 1;
             if (x >= 2) {
                 if (at == items) {
-                    if (!next(a, wp, p)) break;
+                    if (!next(a, c, wp, p)) break;
                     ++n;
                     two = p.rt - 1;
                     items = (p.j1 - p.j0) << two;
@@ -339,7 +359,7 @@ __device__ __forceinline__ void issue_products(uint8_t *sq, uint8_t *sk, uint8_t
                 if (at == items) commit(&c.o_ready);  // the piece's O is complete
             }
             if (more && s_at == s_items) {
-                more = next(a, ws, p);
+                more = next(a, c, ws, p);
                 if (more) {
                     ++sn;
                     s_two = p.rt - 1;
@@ -395,6 +415,27 @@ __device__ __forceinline__ void store_out(uint64_t to, const float (&o)[8]) {
     *reinterpret_cast<uint4 *>(to) = make_uint4(pack16<kF16>(o[0], o[1]), pack16<kF16>(o[2], o[3]), pack16<kF16>(o[4], o[5]),
                                                 pack16<kF16>(o[6], o[7]));
 }
+// Columns [ch, ch + 32) of row r: to the output row, whole sectors where rows lie on their bounds, or to a partial result.
+template <bool kF16>
+__device__ __forceinline__ void store_columns(const TreeArgs &a, int64_t slot, uint64_t row, int r, int ch, bool whole,
+                                              const uint32_t (&o)[32]) {
+    if (!whole) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) st_global_v8(part_at(a, slot, ch / 8 + u, r), o + 8 * u);
+        return;
+    }
+    uint32_t y[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) y[u] = pack16<kF16>(__uint_as_float(o[2 * u]), __uint_as_float(o[2 * u + 1]));
+    if (a.sectors) {
+        st_global_v8(reinterpret_cast<float *>(row + 2 * ch), y);
+        st_global_v8(reinterpret_cast<float *>(row + 2 * ch + 32), y + 8);
+    } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            *reinterpret_cast<uint4 *>(row + 2 * ch + 16 * u) = make_uint4(y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]);
+    }
+}
 
 // Softmax and read-out of half h; this thread's row is TMEM lane r of its item's row tile.
 template <bool kF16>
@@ -408,7 +449,7 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, uint32_t
     uint32_t x0 = 0, kt0 = 0;  // items and key tiles of the pieces before
     bool ok = true;
 #pragma unroll 1
-    for (int n = 0; ok && next(a, w, p); ++n) {
+    for (int n = 0; ok && next(a, c, w, p); ++n) {
         const int two = p.rt - 1, items = (p.j1 - p.j0) << two;
         const int first = (h ^ x0) & 1;                       // the half's first item
         const int i = (2 * p.p + (two ? first : 0)) * a.s.tokens + tok;  // the row's query
@@ -588,35 +629,33 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, uint32_t
             // (what has no weight may hold anything, NaN too: its bits are cleared)
             const uint32_t keep0 = w0 == 0.f ? 0u : ~0u, keep1 = w1 == 0.f ? 0u : ~0u;
             const uint32_t at0 = tmem + lane_off + kOCol + (both ? 0 : only * 128), at1 = tmem + lane_off + kOCol + 128;
-            const int from = two ? 0 : static_cast<int>(h) * 64, to = two ? 128 : from + 64;
+            // 32 columns at a time, the next on their way: of a pair all four quarters, else two with both halves' sums
+            uint32_t o[32], o1[32];
+            const int from = two ? 0 : static_cast<int>(h) * 64;
+            tmem_ld32_async(at0 + from, o);
+            tmem_ld32_async(two ? at0 + 32 : at1 + from, o1);
 #pragma unroll 1
-            for (int ch = from; ch < to; ch += 32) {
-                uint32_t o[32], o1[32];
-                tmem_ld32_async(at0 + ch, o);
-                if (both) {
-                    tmem_ld32_async(at1 + ch, o1);
-                    tmem_wait_dep(o1);
-                }
+            for (int ch = from;; ch += 32) {
                 tmem_wait_dep(o);
+                tmem_wait_dep(o1);
+                if (both) {
 #pragma unroll
-                for (int b = 0; b < 32; ++b) {
-                    float y = __uint_as_float(o[b] & keep0) * w0;
-                    if (both) y += __uint_as_float(o1[b] & keep1) * w1;
-                    o[b] = __float_as_uint(y);
+                    for (int b = 0; b < 32; ++b)
+                        o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0 + __uint_as_float(o1[b] & keep1) * w1);
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 32; ++b) o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0);
                 }
-                if (live) {
+                if (live) store_columns<kF16>(a, slot, row, r, ch, whole, o);
+                if (two) {
+                    ch += 32;
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if (whole) {
-                            float y[8];
-#pragma unroll
-                            for (int b = 0; b < 8; ++b) y[b] = __uint_as_float(o[8 * u + b]);
-                            store_out<kF16>(row + 2 * ch + 16 * u, y);
-                        } else {
-                            st_global_v8(part_at(a, slot, ch / 8 + u, r), o + 8 * u);
-                        }
-                    }
+                    for (int b = 0; b < 32; ++b) o[b] = __float_as_uint(__uint_as_float(o1[b] & keep0) * w0);
+                    if (live) store_columns<kF16>(a, slot, row, r, ch, whole, o);
                 }
+                if (ch + 32 >= (two ? 128 : from + 64)) break;
+                tmem_ld32_async(at0 + ch + 32, o);
+                tmem_ld32_async(two ? at0 + ch + 64 : at1 + ch + 32, o1);
             }
             if (live && (two || h == 0)) {
                 if (!whole)
@@ -627,8 +666,8 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, uint32_t
             }
         }
         if (p.part == 1 && h == 0 && q == 0 && lane == 0) {
-            // the unit's other tiles follow the range's end, place by place
-            const int last = tree::cta_of(c.ranges, c.range_end + (p.tiles - p.j1) - 1);
+            // the unit's other tiles follow the range's end
+            const int last = tree::cta_of(c.ranges, c.range_end + p.to_last);
             a.cut[blockIdx.x] = Cut{last - static_cast<int>(blockIdx.x) + 1, p.s, p.h, p.p};
         }
         tc_fence_before();
@@ -715,7 +754,7 @@ __device__ __forceinline__ void join(Joined &x, float m, float l, const float (&
 // have parts, in order: there are no more than units, so no block is started in vain for each CTA
 // (2 sequences, 16 units, context 28000: 19456 blocks, most of them empty, took 20 us).
 template <bool kF16>
-__global__ void __launch_bounds__(kJoinThreads) tree_combine_kernel(const TreeArgs a, int ctas, int split) {
+__global__ void __launch_bounds__(kJoinThreads, 4) tree_combine_kernel(const TreeArgs a, int ctas, int split) {
     __shared__ Joined others[kJoinWarps][32];
     __shared__ int found[kJoinWarps + 1], at_cta;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -876,6 +915,7 @@ extern "C" rps_status rps_tree_attention_fwd(const rps_tree_attention *p, const 
     a.lse = p->lse;
     a.c = p->scale * kLog2e;
     a.paired = p->n_q > a.s.tokens;
+    a.sectors = (reinterpret_cast<uintptr_t>(p->out) | static_cast<uintptr_t>(2 * (a.out_seq | a.out_token | a.out_head))) % 32 == 0;
     char *ws = static_cast<char *>(d_ws);
     a.cut = reinterpret_cast<Cut *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(ws + ml_at);
@@ -893,7 +933,7 @@ extern "C" rps_status rps_tree_attention_fwd(const rps_tree_attention *p, const 
     // a cut unit has about grid / units parts, and there are no more cuts than units: a block for each,
     // and for each 32 rows and 8 columns a warp, or several where the parts are many
     int split = 1;
-    while (split < kJoinWarps && units * kAhead * split < grid) split *= 2;
+    while (split < kJoinWarps && units * 2 * kAhead * split < grid) split *= 2;
     const int rows = a.paired ? 2 * tree::kRows : a.s.tokens * a.s.group;
     const int tasks = (rows + 31) / 32 * (kD / 8), per = kJoinWarps / split;
     return launch_pdl(f16 ? tree_combine_kernel<true> : tree_combine_kernel<false>,

@@ -7,9 +7,10 @@
 // neighbouring row tiles, or a last one alone: a pair reads the keys once.
 // Keys. A key tile is 128 tokens of the sequence. A unit takes the key tiles up to the
 // last key that one of its rows sees; at least one (rows that see nothing are written too).
-// Work. Units are numbered through (sequence, head, pair); one stands for its key tiles
-// and kUnitCost places more. The n CTAs take equal parts of all places, so a unit may be
-// spread over several CTAs, whose partial results are joined afterwards.
+// Work. Units are numbered through (sequence, head, pair) and have places: kTileCost or
+// kPairCost for each of their key tiles, and kUnitCost behind them. The n CTAs take equal parts
+// of all places, a key tile goes where its first place is; so a unit may be spread over
+// several CTAs, whose partial results are joined afterwards.
 #pragma once
 
 #include <stdint.h>
@@ -27,10 +28,13 @@ using prefix::quotient;
 
 constexpr int kRows = 128;     // rows of a row tile, keys of a key tile
 constexpr int kMaxCtas = 160;  // CTAs of a call
-constexpr int kUnitCost = 1;   // the change from a unit to the next, in key tiles
-// Cutting a unit costs what its parts take to be written and joined, in key tiles: where every
-// unit has a CTA of its own and none is longer by more than that than the equal shares, none is cut.
-constexpr int kCutCost = 3;
+// Costs, in thirds of a key tile of one row tile, which takes 1.1 us: one of a pair takes 1.85, the
+// change from a unit to the next 1.5 and more. (By numbers of key tiles, 64 sequences of 1 to 32 drafted
+// tokens, 32/4 heads: the first CTA ended after 45 us, the last after 80.)
+constexpr int kTileCost = 3, kPairCost = 5, kUnitCost = 5;
+// Cutting a unit costs what its parts take to be written and joined, as much as three key tiles: where
+// every unit has a CTA of its own and none costs by more than that more than the equal shares, none is cut.
+constexpr int kCutCost = 3 * kTileCost;
 
 struct Shape {
     int32_t n_seq, n_q, heads, group;  // heads of the cache, query heads of each
@@ -82,6 +86,11 @@ PREFIX_HD int tiles_of(const Shape &s, const Seq &q, int p) {
     return imax(1, (q.len - q.count + last + kRows - 1) >> 7);
 }
 
+PREFIX_HD int tile_cost(int row_tiles) { return row_tiles > 1 ? kPairCost : kTileCost; }
+PREFIX_HD int cost_of(const Shape &s, const Seq &q, int p) {
+    return tiles_of(s, q, p) * tile_cost(row_tiles_of(s, q, p)) + kUnitCost;
+}
+
 // The bits of keys [key, key + 32) that query i of the sequence sees, for a chain.
 PREFIX_HD uint32_t low_ones(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
 PREFIX_HD uint32_t chain_bits(const Seq &q, int i, int key) {
@@ -103,14 +112,19 @@ PREFIX_HD uint32_t mask_bits(const Seq &q, int key, Word word) {
     return shift ? lo >> shift | at(w + 1) << (32 - shift) : lo;
 }
 
-// The n CTAs' ranges of the places: `base` each, the first `extra` one more.
+// The n CTAs' ranges of the places: `base` each, the first `extra` one more. With kPairCost places and
+// more in each, one that lies inside a unit's key tiles has a tile.
 struct Ranges {
     int64_t base;
     int32_t extra, n;
 };
+// (A division of 32 bits where they are enough: one of 64 takes several times as long.)
+PREFIX_HD int64_t divide(int64_t x, int64_t d) {
+    return (x | d) >> 32 ? x / d : static_cast<int64_t>(static_cast<uint32_t>(x) / static_cast<uint32_t>(d));
+}
 PREFIX_HD Ranges make_ranges(int64_t work, int n) {
     Ranges r;
-    r.base = work / n;
+    r.base = divide(work, n);
     r.extra = static_cast<int32_t>(work - r.base * n);
     r.n = n;
     return r;
@@ -119,7 +133,7 @@ PREFIX_HD int64_t range_start(const Ranges &r, int c) { return c * r.base + imin
 // The CTA in whose range place x lies (base > 0).
 PREFIX_HD int cta_of(const Ranges &r, int64_t x) {
     const int64_t wide = r.extra * (r.base + 1);
-    return static_cast<int>(x < wide ? x / (r.base + 1) : r.extra + (x - wide) / r.base);
+    return static_cast<int>(x < wide ? divide(x, r.base + 1) : r.extra + divide(x - wide, r.base));
 }
 
 // A walk through the units of a CTA's range, piece by piece.
@@ -131,6 +145,7 @@ struct Piece {
     int32_t s, h, p, rt;        // rt: row tiles
     int32_t j0, j1, tiles;      // its key tiles, of the unit's
     int32_t part;               // -1: the whole unit; 1: its first tiles; 0: later ones
+    int32_t to_last;            // places from the range's end to the unit's last tile, of its first tiles
     Seq q;
 };
 // The next piece (false: there is none). seq(s) gives a sequence as used.
@@ -149,11 +164,12 @@ PREFIX_HD bool next_piece(const Shape &s, Walk &w, Piece &x, SeqOf seq) {
         x.p = w.p;
         x.rt = row_tiles_of(s, x.q, w.p);
         x.tiles = tiles_of(s, x.q, w.p);
-        const int cost = x.tiles + kUnitCost, rest = cost - w.j;
-        const int take = w.left < rest ? static_cast<int>(w.left) : rest;
-        x.j0 = w.j;
-        x.j1 = imin(x.tiles, w.j + take);
+        const int each = tile_cost(x.rt), cost = x.tiles * each + kUnitCost, rest = cost - w.j;
+        const int take = w.left < rest ? static_cast<int>(w.left) : rest, end = w.j + take;
+        x.j0 = imin(x.tiles, ceil_div(w.j, each));
+        x.j1 = imin(x.tiles, ceil_div(end, each));
         x.part = x.j0 > 0 ? 0 : x.j1 < x.tiles ? 1 : -1;
+        x.to_last = (x.tiles - 1) * each - end;
         w.left -= take;
         w.j += take;
         if (w.j == cost) {
@@ -176,14 +192,14 @@ PREFIX_HD Walk begin_walk(const Shape &s, int at, const Seq &q, int64_t rem, int
     const int pairs = pairs_of(s, q);
     int64_t head = 0;
 #pragma unroll 1
-    for (int p = 0; p < pairs; ++p) head += tiles_of(s, q, p) + kUnitCost;
+    for (int p = 0; p < pairs; ++p) head += cost_of(s, q, p);
     w.s = at;
-    w.h = static_cast<int>(rem / head);
+    w.h = static_cast<int>(divide(rem, head));
     rem -= w.h * head;
     w.p = 0;
 #pragma unroll 1
     for (;;) {
-        const int cost = tiles_of(s, q, w.p) + kUnitCost;
+        const int cost = cost_of(s, q, w.p);
         if (rem < cost) break;
         rem -= cost;
         ++w.p;
@@ -197,9 +213,9 @@ PREFIX_HD int64_t places_of(const Shape &s, const Seq &q, int *longest) {
     int64_t head = 0;
 #pragma unroll 1
     for (int p = 0; p < pairs; ++p) {
-        const int t = tiles_of(s, q, p);
-        *longest = imax(*longest, t);
-        head += t + kUnitCost;
+        const int cost = cost_of(s, q, p);
+        *longest = imax(*longest, cost);
+        head += cost;
     }
     return head * s.heads;
 }

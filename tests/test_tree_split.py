@@ -51,7 +51,8 @@ int main(int argc, char **argv) {
                     const int last = std::min((2 * p + 2) * s.tokens, seq[i].count);
                     const int keys = s.chain ? std::max(0, seq[i].len - seq[i].count + last) : seq[i].len;
                     CHECK(t >= 1 && t * kRows >= keys && (t == 1 || (t - 1) * kRows < keys));
-                    sum += t + kUnitCost;
+                    sum += cost_of(s, seq[i], p);
+                    CHECK(cost_of(s, seq[i], p) == t * (row_tiles_of(s, seq[i], p) == 2 ? kPairCost : kTileCost) + kUnitCost);
                     if (h == 0) rows += std::min(row_tiles_of(s, seq[i], p) * s.tokens, seq[i].count - 2 * p * s.tokens);
                 }
             CHECK(sum == places && rows == seq[i].count);
@@ -59,7 +60,7 @@ int main(int argc, char **argv) {
             longest = std::max<int64_t>(longest, most);
         }
         if (!work) continue;
-        const int n = static_cast<int>(std::min<int64_t>(rnd(1, 160), work));
+        const int n = static_cast<int>(std::min<int64_t>(rnd(1, 160), std::max<int64_t>(1, work / kPairCost)));
         const Ranges r = make_ranges(work, n);
         std::map<std::tuple<int, int, int>, int> at;        // tiles taken of each unit
         std::map<std::tuple<int, int, int>, int> first, parts;
@@ -90,7 +91,8 @@ int main(int argc, char **argv) {
                 CHECK(cut_first == (x.part == 1));  // one that begins a cut unit comes last
                 if (x.part == 1) {
                     first[u] = c;
-                    parts[u] = cta_of(r, hi + (x.tiles - x.j1) - 1) - c + 1;
+                    CHECK(x.to_last >= 0);
+                    parts[u] = cta_of(r, hi + x.to_last) - c + 1;
                     CHECK(parts[u] >= 2 && c + parts[u] <= n);
                 } else if (x.part == 0) {
                     CHECK(c - first[u] < parts[u] && (x.j1 < x.tiles || c == first[u] + parts[u] - 1));
