@@ -9,11 +9,15 @@
 // t f modulo 2^64 is the fraction of a turn exactly, whatever the position: what is
 // left to fp32 is half a turn at most. All in fp32, rounded once at the end.
 //
-// Bound by HBM: 4 D bytes a row (16-bit elements read and written once). A lane holds
-// 16 elements of a row in two 16-byte units, chosen so that both elements of its
-// pairs are its own: in the half layout units l and l + R / 16, else 2l and 2l + 1. A
-// warp takes rows of one token, so its 32 lanes compute the token's sines and cosines
-// once, and share them through shared memory.
+// Bound by HBM: 4 D bytes a row (16-bit elements read and written once), as long as a pass
+// of a warp over 1024 bytes takes less than about 170 instructions (at twice as many, 576 x 32
+// tokens of 96 rows, half of them there, took 106 us). A lane holds 16 elements of a row
+// in two 16-byte units, chosen so that both elements of its pairs are its own: in the half
+// layout units l and l + R / 16, else 2l and 2l + 1. A warp takes rows of one token and one
+// side, so its lanes compute the token's sines and cosines once, share them through shared
+// memory, and multiply them with the weights once:
+//   z0 = r ((w0 cos) y0 - (w1 sin) y1),  z1 = r ((w1 cos) y1 + (w0 sin) y0),  r = 1 / sqrt(..),
+// two pairs to an instruction (packed fp32).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -22,13 +26,20 @@
 #include <cstring>
 
 #include "rps_internal.cuh"
+#include "tc_device.cuh"
 
 namespace rps {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kPasses = 4;  // rows of a lane in flight
+constexpr int kAhead = 4;     // rows of a lane in flight
+constexpr int kPasses = 8;    // rows of a lane in a task, at most
 constexpr int kMaxDim = 256;
+
+// (A division of 32 bits where they are enough.)
+__device__ __forceinline__ int64_t divide(int64_t x, int32_t d) {
+    return x >> 32 ? x / d : static_cast<int64_t>(static_cast<uint32_t>(x) / static_cast<uint32_t>(d));
+}
 
 struct Side {
     const char *src;
@@ -45,7 +56,7 @@ struct RotateArgs {
     float amplitude, eps, inv_d;
     int32_t D, n_tok;
     const int32_t *pos;
-    int32_t rows, passes, chunks;  // rows of a token (queries, keys, values), passes of a task, tasks of a token
+    int32_t passes, chunks_q, chunks_k, chunks;  // passes of a task; tasks of a token's queries, of its keys, of all
     int64_t tasks;
     // append: the values, and where keys and values go
     Side v;
@@ -55,43 +66,55 @@ struct RotateArgs {
     uint32_t *err;
 };
 
+// Two 16-bit elements as fp32.
 template <bool kF16>
 __device__ __forceinline__ float2 widen(uint32_t x) {
     if (kF16) return __half22float2(*reinterpret_cast<const __half2 *>(&x));
-    return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&x));
+    return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
 }
+// A lane's 16 elements as the first and the second ones of its eight pairs, two pairs to an f2:
+// unit by unit, or (interleaved) the even and the odd ones of both units.
 template <bool kF16>
-__device__ __forceinline__ uint32_t narrow(float lo, float hi) {
-    if (kF16) {
-        const __half2 h = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t *>(&h);
+__device__ __forceinline__ void widen16(const uint4 &u, const uint4 &v, bool interleaved, f2 (&y0)[4], f2 (&y1)[4]) {
+    const uint32_t a[4] = {u.x, u.y, u.z, u.w}, b[4] = {v.x, v.y, v.z, v.w};
+    if (interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = widen<kF16>(i < 2 ? a[2 * i] : b[2 * i - 4]), g = widen<kF16>(i < 2 ? a[2 * i + 1] : b[2 * i - 3]);
+            y0[i] = pack2(f.x, g.x);
+            y1[i] = pack2(f.y, g.y);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = widen<kF16>(a[i]), g = widen<kF16>(b[i]);
+            y0[i] = pack2(f.x, f.y);
+            y1[i] = pack2(g.x, g.y);
+        }
     }
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
 }
-// Eight elements of a 16-byte unit.
 template <bool kF16>
-__device__ __forceinline__ void widen8(const uint4 &u, float *x) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void narrow16(const f2 (&y0)[4], const f2 (&y1)[4], bool interleaved, uint4 &u, uint4 &v) {
+    uint32_t a[4], b[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 f = widen<kF16>(w[i]);
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
+        float p, q, r, s;
+        unpack2(y0[i], p, q);
+        unpack2(y1[i], r, s);
+        a[i] = interleaved ? pack16<kF16>(p, r) : pack16<kF16>(p, q);
+        b[i] = interleaved ? pack16<kF16>(q, s) : pack16<kF16>(r, s);
+    }
+    if (interleaved) {
+        u = make_uint4(a[0], b[0], a[1], b[1]);
+        v = make_uint4(a[2], b[2], a[3], b[3]);
+    } else {
+        u = make_uint4(a[0], a[1], a[2], a[3]);
+        v = make_uint4(b[0], b[1], b[2], b[3]);
     }
 }
-template <bool kF16>
-__device__ __forceinline__ uint4 narrow8(const float *x) {
-    return make_uint4(narrow<kF16>(x[0], x[1]), narrow<kF16>(x[2], x[3]), narrow<kF16>(x[4], x[5]), narrow<kF16>(x[6], x[7]));
-}
 
-__device__ __forceinline__ void turn(float &y0, float &y1, float cs, float sn) {
-    const float z0 = y0 * cs - y1 * sn;
-    y1 = y1 * cs + y0 * sn;
-    y0 = z0;
-}
-
-// kLanes lanes to a row (16 elements each), 32 / kLanes rows of a token at a time.
+// kLanes lanes to a row (16 elements each), 32 / kLanes rows of a token's side at a time, up to eight
+// such passes a task, four of them in flight.
 template <bool kF16, int kLanes, bool kPaged>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
     __shared__ float2 turned[kWarps][kMaxDim / 2];
@@ -101,59 +124,76 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
     pdl_wait();
     pdl_launch_next();
     if (task >= a.tasks) return;
-    const int64_t x = task / a.chunks;
-    const int row0 = static_cast<int>(task - x * a.chunks) * a.passes * kAt + lane / kLanes;
-    const int64_t s = x / a.n_tok;
+    const int64_t x = divide(task, a.chunks);
+    int chunk = static_cast<int>(task - x * a.chunks);
+    const int64_t s = divide(x, a.n_tok);
     const int i = static_cast<int>(x - s * a.n_tok);
-    int len = 0, count = a.n_tok;
+    int token = i;
     if (kPaged) {
-        len = a.len[s];
-        if (a.count) count = min(max(a.count[s], 0), a.n_tok);
+        int len = a.len[s];
+        const int count = a.count ? min(max(a.count[s], 0), a.n_tok) : a.n_tok;
         if (len < 0 || i >= count) return;
         if (len > 0 && (len - 1) >> a.page_log >= a.width) {
             if (lane == 0) flag_error(a.err, RPS_DEVERR_PAGE);
             len = a.width << a.page_log;
         }
+        token = len - count + i;
+        if (token < 0) return;  // (a row without a place)
     }
-    const int token = kPaged ? len - count + i : i;
-    if (token < 0) return;  // (a row without a place)
+    const bool is_q = chunk < a.chunks_q, is_v = kPaged && chunk >= a.chunks_q + a.chunks_k;
+    const Side &d = is_q ? a.q : is_v ? a.v : a.k;
+    chunk -= is_q ? 0 : is_v ? a.chunks_q + a.chunks_k : a.chunks_q;
+    const int row0 = chunk * a.passes * kAt, end = min(d.heads, row0 + a.passes * kAt);  // the task's rows
 
     // this lane's 16-byte units of a row
-    const int l = lane % kLanes;
+    const int l = lane % kLanes, mine = row0 + lane / kLanes;
     const bool rotates = l < a.R / 16, there = l < a.D / 16;
     const bool halves = rotates && !a.interleaved;
     const int u0 = (halves ? l : 2 * l) * 16, u1 = (halves ? l + a.R / 16 : 2 * l + 1) * 16;
-    uint4 raw0[kPasses], raw1[kPasses];
-    const auto side_of = [&](int row, int &head) -> const Side & {
-        head = row;
-        if (row < a.q.heads) return a.q;
-        head -= a.q.heads;
-        if (!kPaged || head < a.k.heads) return a.k;
-        head -= a.k.heads;
-        return a.v;
+    const char *from = d.src + s * d.src_seq + i * d.src_token + mine * d.src_head;
+    uint4 raw0[kAhead], raw1[kAhead];
+    const auto load = [&](int p, int u) {
+        if (!there || mine + p * kAt >= end) return;
+        const char *at = from + p * (kAt * d.src_head);
+        raw0[u] = __ldcs(reinterpret_cast<const uint4 *>(at + u0));
+        raw1[u] = __ldcs(reinterpret_cast<const uint4 *>(at + u1));
     };
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int row = row0 + p * kAt;
-        if (p >= a.passes || row >= a.rows || !there) continue;
-        int head;
-        const Side &d = side_of(row, head);
-        const char *from = d.src + s * d.src_seq + i * d.src_token + head * d.src_head;
-        raw0[p] = __ldcs(reinterpret_cast<const uint4 *>(from + u0));
-        raw1[p] = __ldcs(reinterpret_cast<const uint4 *>(from + u1));
-    }
-    // the token's place, and its sines and cosines while the rows are on their way
-    int64_t place = -1;
-    if (kPaged) {
+    for (int u = 0; u < kAhead; ++u) load(u, u);
+    char *to = d.dst + mine * (kPaged && !is_q ? a.head_stride : d.dst_head);
+    int64_t step = kAt * d.dst_head;
+    if (kPaged && !is_q) {
         const int page = a.table[s * a.width + (token >> a.page_log)];
         if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
             if (lane == 0) flag_error(a.err, RPS_DEVERR_PAGE);
-        } else if (a.ref[page] > 1) {  // others read this page too
-            if (lane == 0) flag_error(a.err, RPS_DEVERR_SHARED);
-        } else {
-            place = page * a.page_stride + (token & ((1 << a.page_log) - 1)) * a.token_stride;
+            return;
         }
+        if (a.ref[page] > 1) {  // others read this page too
+            if (lane == 0) flag_error(a.err, RPS_DEVERR_SHARED);
+            return;
+        }
+        to += page * a.page_stride + (token & ((1 << a.page_log) - 1)) * a.token_stride;
+        step = kAt * a.head_stride;
+    } else {
+        to += s * d.dst_seq + i * d.dst_token;
     }
+    const auto store = [&](int p, int u) {
+        if (!there || mine + p * kAt >= end) return;
+        char *at = to + p * step;
+        *reinterpret_cast<uint4 *>(at + u0) = raw0[u];
+        *reinterpret_cast<uint4 *>(at + u1) = raw1[u];
+    };
+    if (is_v) {
+#pragma unroll 1
+        for (int p0 = 0; row0 + p0 * kAt < end; p0 += kAhead)
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                store(p0 + u, u);
+                load(p0 + u + kAhead, u);
+            }
+        return;
+    }
+    // the token's sines and cosines, and this lane's with its weights, while the rows are on their way
     if (a.R) {
         const int64_t t = a.pos ? a.pos[x] : token;
         for (int p = lane; p < a.R / 2; p += 32) {
@@ -164,68 +204,58 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
         }
         __syncwarp();
     }
-    float cs[8], sn[8];
+    const f2 one = pack2(1.f, 1.f), minus = pack2(-1.f, -1.f);
+    f2 c0[4], c1[4], s0[4], s1[4];  // w0 cos, w1 cos, w0 sin, -w1 sin
+    {
+        f2 w0[4] = {one, one, one, one}, w1[4] = {one, one, one, one};
+        if (d.weight && there)
+            widen16<kF16>(*reinterpret_cast<const uint4 *>(static_cast<const char *>(d.weight) + u0),
+                          *reinterpret_cast<const uint4 *>(static_cast<const char *>(d.weight) + u1), !halves, w0, w1);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float2 f = rotates ? turned[warp][8 * l + j] : make_float2(1.f, 0.f);
-        cs[j] = f.x;
-        sn[j] = f.y;
+        for (int j = 0; j < 4; ++j) {
+            const float4 f = rotates ? *reinterpret_cast<const float4 *>(&turned[warp][8 * l + 2 * j]) : make_float4(1.f, 0.f, 1.f, 0.f);
+            const f2 cs = pack2(f.x, f.z), sn = pack2(f.y, f.w);
+            c0[j] = mul2(w0[j], cs);
+            c1[j] = mul2(w1[j], cs);
+            s0[j] = mul2(w0[j], sn);
+            s1[j] = mul2(mul2(w1[j], sn), minus);
+        }
     }
+    const bool normed = d.weight != nullptr;
+#pragma unroll 1
+    for (int p0 = 0; row0 + p0 * kAt < end; p0 += kAhead) {
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        if (p >= a.passes) break;  // (the same for the whole warp)
-        const int row = row0 + p * kAt;
-        const bool live = row < a.rows && there;
-        int head;
-        const Side &d = side_of(row, head);
-        const bool value = kPaged && row >= a.q.heads + a.k.heads;
-        if (!value) {
-            float y[16];
-            if (live) {
-                widen8<kF16>(raw0[p], y);
-                widen8<kF16>(raw1[p], y + 8);
-            } else {
+        for (int u = 0; u < kAhead; ++u) {
+            if (row0 + (p0 + u) * kAt >= end) break;  // (the same for the whole warp)
+            f2 y0[4], y1[4];
+            widen16<kF16>(raw0[u], raw1[u], !halves, y0, y1);
+            float r = 1.f;
+            if (normed) {
+                f2 sum = pack2(0.f, 0.f);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) y[j] = 0.f;
+                for (int j = 0; j < 4; ++j) sum = fma2(y1[j], y1[j], fma2(y0[j], y0[j], sum));
+                float lo, hi;
+                unpack2(sum, lo, hi);
+                lo = there ? lo + hi : 0.f;
+#pragma unroll
+                for (int o = kLanes / 2; o > 0; o >>= 1) lo += __shfl_xor_sync(kFull, lo, o);
+                r = rsqrtf(lo * a.inv_d + a.eps);
             }
-            if (d.weight) {
-                float sum = 0.f;
+            const f2 rr = pack2(r, r);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sum += y[j] * y[j];
-                // (the lanes of a row agree on its side)
-                const unsigned mask = (kLanes == 32 ? kFull : (1u << kLanes) - 1) << (lane / kLanes * kLanes);
-#pragma unroll
-                for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(mask, sum, o);
-                const float r = rsqrtf(sum * a.inv_d + a.eps);
-                if (live) {
-                    float w[16];
-                    widen8<kF16>(*reinterpret_cast<const uint4 *>(static_cast<const char *>(d.weight) + u0), w);
-                    widen8<kF16>(*reinterpret_cast<const uint4 *>(static_cast<const char *>(d.weight) + u1), w + 8);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) y[j] *= r * w[j];
+            for (int j = 0; j < 4; ++j) {
+                f2 z0 = fma2(s1[j], y1[j], mul2(c0[j], y0[j])), z1 = fma2(s0[j], y0[j], mul2(c1[j], y1[j]));
+                if (normed) {
+                    z0 = mul2(z0, rr);
+                    z1 = mul2(z1, rr);
                 }
+                y0[j] = z0;
+                y1[j] = z1;
             }
-            // (a loop for each layout: one that picked its elements would put them into local memory)
-            if (halves) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) turn(y[j], y[j + 8], cs[j], sn[j]);
-            } else if (rotates) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) turn(y[2 * j], y[2 * j + 1], cs[j], sn[j]);
-            }
-            raw0[p] = narrow8<kF16>(y);
-            raw1[p] = narrow8<kF16>(y + 8);
+            narrow16<kF16>(y0, y1, !halves, raw0[u], raw1[u]);
+            store(p0 + u, u);
+            load(p0 + u + kAhead, u);
         }
-        if (!live) continue;
-        char *to;
-        if (kPaged && row >= a.q.heads) {
-            if (place < 0) continue;
-            to = d.dst + place + head * a.head_stride;
-        } else {
-            to = d.dst + s * d.dst_seq + i * d.dst_token + head * d.dst_head;
-        }
-        *reinterpret_cast<uint4 *>(to + u0) = raw0[p];
-        *reinterpret_cast<uint4 *>(to + u1) = raw1[p];
     }
 }
 
@@ -280,12 +310,15 @@ rps_status launch_rotate(RotateArgs &a, int32_t n_seq, bool f16, cudaStream_t st
     if (sms < 1) return RPS_ERR_CUDA;
     const int lanes = a.D <= 64 ? 4 : a.D <= 128 ? 8 : 16, at = 32 / lanes;
     const int64_t tokens = static_cast<int64_t>(n_seq) * a.n_tok;
-    // Few rows are spread over more warps: a warp's rows come one after another.
-    const auto chunks = [&](int passes) { return (a.rows + passes * at - 1) / (passes * at); };
-    a.passes = kPasses;
-    while (a.passes > 1 && tokens * chunks(a.passes) < sms * 8) a.passes /= 2;
-    a.chunks = chunks(a.passes);
-    a.tasks = tokens * a.chunks;
+    // Few rows are spread over more warps: a warp's passes come one after another.
+    const auto chunks = [&](int heads) { return (heads + a.passes * at - 1) / (a.passes * at); };
+    for (a.passes = kPasses;; a.passes /= 2) {
+        a.chunks_q = chunks(a.q.heads);
+        a.chunks_k = chunks(a.k.heads);
+        a.chunks = a.chunks_q + a.chunks_k + (kPaged ? chunks(a.v.heads) : 0);
+        a.tasks = tokens * a.chunks;
+        if (a.passes == 1 || a.tasks >= sms * (a.passes > kAhead ? 64 : 8)) break;
+    }
     const int64_t blocks = (a.tasks + kWarps - 1) / kWarps;
     if (blocks > INT32_MAX) return RPS_ERR_UNSUPPORTED;
     const auto kernel = lanes == 4   ? (f16 ? rotate_kernel<true, 4, kPaged> : rotate_kernel<false, 4, kPaged>)
@@ -322,7 +355,6 @@ rps_status rps_rope_heads(const rps_rope *rope, const rps_heads *q, const rps_he
     if (k && (st = check_side(k, n_seq, n_tok, true, &a.k)) != RPS_OK) return st;
     a.n_tok = n_tok;
     a.pos = d_pos;
-    a.rows = a.q.heads + a.k.heads;
     return launch_rotate<false>(a, n_seq, dtype == RPS_F16, reinterpret_cast<cudaStream_t>(stream));
 }
 
@@ -345,7 +377,6 @@ rps_status rps_kv_append(const rps_kv_cache *kv, int32_t layer, const rps_rope *
     a.v.dst = static_cast<char *>(kv->v) + at;
     a.n_tok = n_new;
     a.pos = d_pos;
-    a.rows = a.q.heads + 2 * kv->n_heads;
     a.table = kv->table;
     a.len = kv->len;
     a.ref = kv->page_ref;
