@@ -8,7 +8,7 @@
 // Keys. A key tile is 128 tokens of the sequence. A unit takes the key tiles up to the
 // last key that one of its rows sees; at least one (rows that see nothing are written too).
 // Work. Units are numbered through (sequence, head, pair) and have places: kTileCost or
-// kPairCost for each of their key tiles, and kUnitCost behind them. The n CTAs take equal parts
+// kPairCost for each of their key tiles, and kUnitCost or kPairUnitCost behind them. The n CTAs take equal parts
 // of all places, a key tile goes where its first place is; so a unit may be spread over
 // several CTAs, whose partial results are joined afterwards.
 #pragma once
@@ -28,10 +28,11 @@ using prefix::quotient;
 
 constexpr int kRows = 128;     // rows of a row tile, keys of a key tile
 constexpr int kMaxCtas = 160;  // CTAs of a call
-// Costs, in thirds of a key tile of one row tile, which takes 1.1 us: one of a pair takes 1.85, the
-// change from a unit to the next 1.5 and more. (By numbers of key tiles, 64 sequences of 1 to 32 drafted
-// tokens, 32/4 heads: the first CTA ended after 45 us, the last after 80.)
-constexpr int kTileCost = 3, kPairCost = 5, kUnitCost = 5;
+// Costs, in thirds of a key tile of one row tile: fitted to the times of 152 CTAs, which take 1.07 us for
+// such a tile, 1.65 for one of a pair, 2.0 to 2.5 for a unit's begin and end, 4.1 for a pair's. (By
+// numbers of key tiles, 64 sequences of 1 to 32 drafted tokens, 32/4 heads: the first CTA ended after
+// 45 us, the last after 80.)
+constexpr int kTileCost = 3, kPairCost = 5, kUnitCost = 6, kPairUnitCost = 11;
 // Cutting a unit costs what its parts take to be written and joined, as much as three key tiles: where
 // every unit has a CTA of its own and none costs by more than that more than the equal shares, none is cut.
 constexpr int kCutCost = 3 * kTileCost;
@@ -87,8 +88,10 @@ PREFIX_HD int tiles_of(const Shape &s, const Seq &q, int p) {
 }
 
 PREFIX_HD int tile_cost(int row_tiles) { return row_tiles > 1 ? kPairCost : kTileCost; }
+PREFIX_HD int unit_cost(int row_tiles) { return row_tiles > 1 ? kPairUnitCost : kUnitCost; }
 PREFIX_HD int cost_of(const Shape &s, const Seq &q, int p) {
-    return tiles_of(s, q, p) * tile_cost(row_tiles_of(s, q, p)) + kUnitCost;
+    const int rt = row_tiles_of(s, q, p);
+    return tiles_of(s, q, p) * tile_cost(rt) + unit_cost(rt);
 }
 
 // The bits of keys [key, key + 32) that query i of the sequence sees, for a chain.
@@ -164,7 +167,7 @@ PREFIX_HD bool next_piece(const Shape &s, Walk &w, Piece &x, SeqOf seq) {
         x.p = w.p;
         x.rt = row_tiles_of(s, x.q, w.p);
         x.tiles = tiles_of(s, x.q, w.p);
-        const int each = tile_cost(x.rt), cost = x.tiles * each + kUnitCost, rest = cost - w.j;
+        const int each = tile_cost(x.rt), cost = x.tiles * each + unit_cost(x.rt), rest = cost - w.j;
         const int take = w.left < rest ? static_cast<int>(w.left) : rest, end = w.j + take;
         x.j0 = imin(x.tiles, ceil_div(w.j, each));
         x.j1 = imin(x.tiles, ceil_div(end, each));

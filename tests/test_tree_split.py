@@ -52,7 +52,7 @@ int main(int argc, char **argv) {
                     const int keys = s.chain ? std::max(0, seq[i].len - seq[i].count + last) : seq[i].len;
                     CHECK(t >= 1 && t * kRows >= keys && (t == 1 || (t - 1) * kRows < keys));
                     sum += cost_of(s, seq[i], p);
-                    CHECK(cost_of(s, seq[i], p) == t * (row_tiles_of(s, seq[i], p) == 2 ? kPairCost : kTileCost) + kUnitCost);
+                    CHECK(cost_of(s, seq[i], p) == (row_tiles_of(s, seq[i], p) == 2 ? t * kPairCost + kPairUnitCost : t * kTileCost + kUnitCost));
                     if (h == 0) rows += std::min(row_tiles_of(s, seq[i], p) * s.tokens, seq[i].count - 2 * p * s.tokens);
                 }
             CHECK(sum == places && rows == seq[i].count);
