@@ -85,7 +85,8 @@ struct TreeArgs {
     float c;  // scale * log2(e)
     PageCopies copies;
     int32_t paired;   // units may have two row tiles
-    int32_t whole;    // no unit is cut: a CTA takes one
+    int32_t few;      // no more units than CTAs, and a thread for each sequence
+    int32_t whole;    // and none is cut: a CTA takes one
     int32_t sectors;  // output rows begin on 32-byte bounds
     Cut *cut;         // [grid]
     float2 *part_ml;  // [2 * grid][2][128]: maximum and sum of each row of a partial result
@@ -146,55 +147,55 @@ __device__ __forceinline__ void find_range(const TreeArgs &a, Ctl &c) {
         c.longest = 0;
         c.walk = Walk{0, 0, 0, 0, 0};
     }
-    __syncthreads();
-    // the places of the sequences, and how many units there are
-    int64_t places = 0, units = 0, work = 0, all_units = 0;
+    // the places of the sequences
+    int64_t places = 0, work = 0, before = 0, total;
     Seq q{-1, 0};
     int longest = 0;
     const auto look = [&](int e) {
         q = e < n_seq ? seq_of(a, e) : Seq{-1, 0};
         if (e < n_seq && n_seq <= kStagedSeqs) c.seq[e] = q;
         places = tree::places_of(a.s, q, &longest);
-        units = static_cast<int64_t>(tree::pairs_of(a.s, q)) * a.s.heads;
     };
-    int64_t before = 0, total;
 #pragma unroll 1
     for (int base = 0; base < n_seq; base += kThreads) {
         look(base + threadIdx.x);
         before = scan_block(places, c.scan, &total);
         work += total;
     }
-    const int most = __reduce_max_sync(kFull, longest);
-    if ((threadIdx.x & 31) == 0 && most) atomicMax(&c.longest, most);
-    if (n_seq <= kThreads) scan_block(units, c.scan, &all_units);
-    __syncthreads();
-    if (work == 0) return;
     const int grid = gridDim.x, me = blockIdx.x;
-    const int n = work < static_cast<int64_t>(grid) * tree::kPairCost ? max(1, static_cast<int>(work) / tree::kPairCost) : grid;
-    if (a.whole || (n_seq <= kThreads && all_units <= grid && c.longest <= tree::divide(work, grid) + tree::kCutCost)) {
-        const int64_t first = scan_block(units, c.scan, &all_units);
-        if (me >= first && me < first + units) {
-            const int pairs = tree::pairs_of(a.s, q), u = me - static_cast<int>(first), h = u / pairs, p = u - h * pairs;
-            c.walk = Walk{static_cast<int>(threadIdx.x), h, p, 0, tree::cost_of(a.s, q, p)};
-        }
-    } else {
-        const tree::Ranges r = tree::make_ranges(work, n);
-        const int64_t at = tree::range_start(r, me), end = tree::range_start(r, me + 1);
-        if (threadIdx.x == 0) {
-            c.ranges = r;
-            c.range_end = end;
-        }
-        int64_t carry = 0;
-#pragma unroll 1
-        for (int base = 0; base < n_seq && me < n; base += kThreads) {
-            if (n_seq > kThreads) {
-                look(base + threadIdx.x);
-                before = carry + scan_block(places, c.scan, &total);
-                carry += total;
+    if (a.few) {  // (a thread has its sequence)
+        const int most = __reduce_max_sync(kFull, longest);
+        if ((threadIdx.x & 31) == 0 && most) atomicMax(&c.longest, most);
+        __syncthreads();
+        if (a.whole || c.longest <= tree::divide(work, grid) + tree::kCutCost) {
+            const int pairs = tree::pairs_of(a.s, q), units = pairs * a.s.heads;
+            const int first = static_cast<int>(scan_block(units, c.scan, &total));
+            if (me >= first && me < first + units) {
+                const int u = me - first, h = u / pairs, p = u - h * pairs;
+                c.walk = Walk{static_cast<int>(threadIdx.x), h, p, 0, tree::cost_of(a.s, q, p)};
             }
-            if (before <= at && at < before + places)
-                c.walk = tree::begin_walk(a.s, base + threadIdx.x, q, at - before, end - at);
+            return;
         }
+    }
+    if (work == 0) return;
+    const int n = work < static_cast<int64_t>(grid) * tree::kPairCost ? max(1, static_cast<int>(work) / tree::kPairCost) : grid;
+    if (me >= n) return;
+    const tree::Ranges r = tree::make_ranges(work, n);
+    const int64_t at = tree::range_start(r, me), end = tree::range_start(r, me + 1);
+    if (threadIdx.x == 0) {
+        c.ranges = r;
+        c.range_end = end;
+    }
+    int64_t carry = 0;
+#pragma unroll 1
+    for (int base = 0; base < n_seq; base += kThreads) {
+        if (n_seq > kThreads) {
+            look(base + threadIdx.x);
+            before = carry + scan_block(places, c.scan, &total);
+            carry += total;
+        }
+        if (before <= at && at < before + places)
+            c.walk = tree::begin_walk(a.s, base + threadIdx.x, q, at - before, end - at);
     }
 }
 
@@ -937,7 +938,8 @@ extern "C" rps_status rps_tree_attention_fwd(const rps_tree_attention *p, const 
     const int64_t units = static_cast<int64_t>(a.s.n_seq) * a.s.heads * a.s.pairs;
     // Where units are no more than CTAs and cannot be long, none is cut, and there is nothing to join: one launch
     // (one sequence, 32 heads, 344 tokens: 11.5 us with two, 9 with one).
-    a.whole = units <= std::min(sms, kThreads) && tiles <= kWholeTiles;
+    a.few = units <= std::min(sms, kThreads);  // (so there are no more sequences)
+    a.whole = a.few && tiles <= kWholeTiles;
     const int grid = static_cast<int>(std::min<int64_t>(a.whole ? units : units * tiles, sms));
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (launch_pdl(f16 ? tree_attention_kernel<true> : tree_attention_kernel<false>, dim3(grid), dim3(kThreads), kSmemBytes, s,
