@@ -61,6 +61,7 @@ constexpr int kThreads = 384;
 constexpr uint32_t kTmemCols = 512;  // S buffers at columns 0 and 128, O at 256 and 384
 constexpr uint32_t kOCol = 256;
 constexpr int kWholeTiles = 4;       // key tiles of units that are never cut
+constexpr int kMlSlots = 3;
 constexpr int kStagedSeqs = 1024;    // sequences whose lengths are kept in shared memory
 constexpr float kLn2 = 0.6931471805599453f;
 // bounds of a tile's sum of P in a row (in units of its reference): P in fp16 stays finite
@@ -95,13 +96,20 @@ struct TreeArgs {
     uint32_t tries;  // of a wait
 };
 
+// A piece, and the items before it.
+struct Noted {
+    Piece p;
+    uint32_t x0;
+};
+
 struct Ctl {
     uint64_t q_full[kQBufs], q_empty[kQBufs], k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
     uint64_t s_full[2], p_full[2], o_ready, o_free, mma_done;
-    // a half's reference and sum of a row at the end of piece n, in slot n % 2: written before the
-    // half's last P of the piece is handed on, read once O is ready, and written again for piece
-    // n + 2 by warps that have seen O of piece n + 1 ready, whose products wait for the read-out of n
-    float2 ml[2][2][tree::kRows];
+    // a half's reference and sum of a row at the end of piece n, in slot n % 3: written before the half's last
+    // P of the piece is handed on, read once O is ready, and written again for piece n + 3 by warps that have
+    // seen O of piece n + 1 ready, whose products wait for the read-out of n
+    float2 ml[kMlSlots][2][tree::kRows];
+    Noted noted[8];  // of each warp of the softmax: the piece that it has to read out
     int4 copy_at[2][32];  // a producer's copies: their coordinates, of two tiles
     uint32_t bad[4];      // copies of key tile t whose page id is outside the cache (t % 4)
     Seq seq[kStagedSeqs];  // as they are used
@@ -441,244 +449,289 @@ __device__ __forceinline__ void store_columns(const TreeArgs &a, int64_t slot, u
     }
 }
 
-// Softmax and read-out of half h; this thread's row is TMEM lane r of its item's row tile.
+// Read-out of piece n, as its half's warps noted it (d): of a pair each half its own row tile, else each half
+// 64 columns of both accumulators.
+template <bool kF16>
+__device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_t h, int n, const Noted &d, Ctl &c, const TreeArgs &a) {
+    const int r = q * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>(q * 32) << 16;
+    const int tok = prefix::quotient(r, a.s.by_group), g = r - tok * a.s.group;
+    const Piece &p = d.p;
+    const uint32_t x0 = d.x0;
+    const int two = p.rt - 1, items = (p.j1 - p.j0) << two, first = (h ^ x0) & 1;
+    const int i = (2 * p.p + (two ? first : 0)) * a.s.tokens + tok;
+    const bool live = tok < a.s.tokens && i < p.q.count, any = __any_sync(kFull, live);
+    const bool both = !two && items > 1;
+    const int only = two ? h : x0 & 1;  // the half that has the (other) sums
+    if (any) {
+        const bool whole = p.part < 0;
+        const int head = p.h * a.s.group + g;
+        const int64_t slot = (2ll * blockIdx.x + max(p.part, 0)) * 2 + (two ? first : 0);
+        const uint64_t row = reinterpret_cast<uint64_t>(a.out) + 2 * (p.s * a.out_seq + i * a.out_token + head * a.out_head);
+        const float2 e = c.ml[n % kMlSlots][both ? 0 : only][r];
+        const float2 f = both ? c.ml[n % kMlSlots][1][r] : make_float2(-INFINITY, 0.f);
+        const float mx = fmaxf(e.x, f.x), mr = mx == -INFINITY ? 0.f : mx;
+        float w0 = e.y == 0.f ? 0.f : ex2(e.x - mr), w1 = f.y == 0.f ? 0.f : ex2(f.x - mr);
+        const float total = w0 * e.y + w1 * f.y;  // (NaN stays)
+        if (whole) {
+            const float inv = total == 0.f ? 0.f : __fdividef(1.f, total);
+            w0 *= inv;
+            w1 *= inv;
+        }
+        // (what has no weight may hold anything, NaN too: its bits are cleared)
+        const uint32_t keep0 = w0 == 0.f ? 0u : ~0u, keep1 = w1 == 0.f ? 0u : ~0u;
+        const uint32_t at0 = tmem + lane_off + kOCol + (both ? 0 : only * 128), at1 = tmem + lane_off + kOCol + 128;
+        // 32 columns at a time, the next on their way: of a pair all four quarters, else two with both halves' sums
+        uint32_t o[32], o1[32];
+        const int from = two ? 0 : static_cast<int>(h) * 64;
+        tmem_ld32_async(at0 + from, o);
+        tmem_ld32_async(two ? at0 + 32 : at1 + from, o1);
+#pragma unroll 1
+        for (int ch = from;; ch += 32) {
+            tmem_wait_dep(o);
+            tmem_wait_dep(o1);
+            if (both) {
+#pragma unroll
+                for (int b = 0; b < 32; ++b)
+                    o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0 + __uint_as_float(o1[b] & keep1) * w1);
+            } else {
+#pragma unroll
+                for (int b = 0; b < 32; ++b) o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0);
+            }
+            if (live) store_columns<kF16>(a, slot, row, r, ch, whole, o);
+            if (two) {
+                ch += 32;
+#pragma unroll
+                for (int b = 0; b < 32; ++b) o[b] = __float_as_uint(__uint_as_float(o1[b] & keep0) * w0);
+                if (live) store_columns<kF16>(a, slot, row, r, ch, whole, o);
+            }
+            if (ch + 32 >= (two ? 128 : from + 64)) break;
+            tmem_ld32_async(at0 + ch + 32, o);
+            tmem_ld32_async(two ? at0 + ch + 64 : at1 + ch + 32, o1);
+        }
+        if (live && (two || h == 0)) {
+            if (!whole)
+                a.part_ml[slot * tree::kRows + r] = make_float2(mx, total);
+            else if (a.lse)
+                a.lse[(static_cast<int64_t>(p.s) * a.s.n_q + i) * a.n_heads + head] =
+                    total == 0.f ? -INFINITY : (mx + log2f(total)) * kLn2;
+        }
+    }
+    if (p.part == 1 && h == 0 && q == 0 && lane == 0) {
+        // the unit's other tiles follow the range's end
+        const int last = tree::cta_of(c.ranges, c.range_end + p.to_last);
+        a.cut[blockIdx.x] = Cut{last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), p.s, p.h, p.p, p.q.count, {0, 0}};
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&c.o_free);
+}
+
+// Whether a phase of a barrier is over, without a wait; all lanes, on the same answer.
+__device__ __forceinline__ bool done_already(uint64_t *bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(saddr(bar)), "r"(parity)
+        : "memory");
+    return __all_sync(kFull, done != 0);
+}
+
+// Softmax and read-out of half h; this thread's row is TMEM lane r of its item's row tile. A piece is read
+// out after the half's first item of the next one where the item's scores are there: the piece's last
+// product takes as long. (Read out at once: 64 sequences of 32 tokens 86 us instead of 83. After the first
+// item always: 128 sequences of one token, 32/8 heads, contexts 20 to 1500, 84 -> 100.)
 template <bool kF16>
 __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, uint32_t h, uint8_t *sv, Ctl &c, const TreeArgs &a) {
     const int r = q * 32 + lane;
     const uint32_t lane_off = static_cast<uint32_t>(q * 32) << 16;
     const uint32_t sbuf = tmem + lane_off + h * 128, obuf = tmem + lane_off + kOCol + h * 128;
-    const int tok = prefix::quotient(r, a.s.by_group), g = r - tok * a.s.group;  // the row's token in the tile, head in the group
+    const int tok = prefix::quotient(r, a.s.by_group);  // the row's token in the tile
     Walk w = c.walk;
-    Piece p;
+    Piece p{};
     uint32_t x0 = 0, kt0 = 0;  // items and key tiles of the pieces before
-    bool ok = true;
+    Noted &noted = c.noted[h * 4 + q];
+    bool ok = true, pending = false, have = next(a, c, w, p);
 #pragma unroll 1
-    for (int n = 0; ok && next(a, c, w, p); ++n) {
-        const int two = p.rt - 1, items = (p.j1 - p.j0) << two;
+    for (int n = 0; have || pending; ++n) {
+        const int two = p.rt - 1, items = have ? (p.j1 - p.j0) << two : 0;
         const int first = (h ^ x0) & 1;                       // the half's first item
         const int i = (2 * p.p + (two ? first : 0)) * a.s.tokens + tok;  // the row's query
         const bool live = tok < a.s.tokens && i < p.q.count;
         const bool any = __any_sync(kFull, live);
         const uint32_t *mask_row = a.s.chain ? nullptr : a.mask + (static_cast<int64_t>(p.s) * a.s.n_q + (live ? i : 0)) * a.words;
         float m = kF16 ? -INFINITY : 0.f, l = 0.f;
+        int it = first;
 #pragma unroll 1
-        for (int it = first; it < items; it += 2) {
-            const uint32_t x = x0 + it, kt = kt0 + (it >> two);
-            const int key = (p.j0 + (it >> two)) * tree::kRows;
-            // bits of the keys that the row sees, a word for each quarter of the tile (rows that are not
-            // stored need no mask)
-            uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
-            if (live && key + tree::kRows > p.q.len - p.q.count) {
-                if (a.s.chain) {
+        do {
+            if (it < items && (!pending || done_already(&c.s_full[h], ((x0 + it) >> 1) & 1))) {
+                const uint32_t x = x0 + it, kt = kt0 + (it >> two);
+                const int key = (p.j0 + (it >> two)) * tree::kRows;
+                // bits of the keys that the row sees, a word for each quarter of the tile (rows that are not
+                // stored need no mask)
+                uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
+                if (live && key + tree::kRows > p.q.len - p.q.count) {
+                    if (a.s.chain) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) keep[k] = tree::chain_bits(p.q, i, key + 32 * k);
-                } else {
+                        for (int k = 0; k < 4; ++k) keep[k] = tree::chain_bits(p.q, i, key + 32 * k);
+                    } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        keep[k] = tree::mask_bits(p.q, key + 32 * k, [&](int y) { return mask_row[y]; });
-                }
-            }
-            if (!warp_wait(&c.s_full[h], (x >> 1) & 1, c, a)) {
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            if (any) {
-                const uint32_t bad = c.bad[kt % 4];
-                if (bad && live) {  // a page of this row's keys does not exist: NaN
-                    uint32_t hit = 0;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint32_t of_bad = 0;
-#pragma unroll
-                        for (int b = 0; b < 32; b += 8)  // (a copy is 8 tokens at least)
-                            if (bad >> ((32 * k + b) >> a.copies.copy_log) & 1u) of_bad |= 0xffu << b;
-                        hit |= keep[k] & of_bad;
-                    }
-                    if (hit) {
-                        l = NAN;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) keep[k] = 0;
+                        for (int k = 0; k < 4; ++k)
+                            keep[k] = tree::mask_bits(p.q, key + 32 * k, [&](int y) { return mask_row[y]; });
                     }
                 }
-                const bool sees = live && (keep[0] | keep[1] | keep[2] | keep[3]) != 0;
-                // Quarters in which some row of the warp has keys that it does not see are masked and written back.
-                if (__any_sync(kFull, live && (keep[0] & keep[1] & keep[2] & keep[3]) != ~0u)) {
+                if (!warp_wait(&c.s_full[h], (x >> 1) & 1, c, a)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                if (any) {
+                    const uint32_t bad = c.bad[kt % 4];
+                    if (bad && live) {  // a page of this row's keys does not exist: NaN
+                        uint32_t hit = 0;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t word = live ? keep[k] : ~0u;
-                        if (!__any_sync(kFull, word != ~0u)) continue;
-                        uint32_t s0[32];
-                        tmem_ld32_async(sbuf + k * 32, s0);
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t of_bad = 0;
+#pragma unroll
+                            for (int b = 0; b < 32; b += 8)  // (a copy is 8 tokens at least)
+                                if (bad >> ((32 * k + b) >> a.copies.copy_log) & 1u) of_bad |= 0xffu << b;
+                            hit |= keep[k] & of_bad;
+                        }
+                        if (hit) {
+                            l = NAN;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) keep[k] = 0;
+                        }
+                    }
+                    const bool sees = live && (keep[0] | keep[1] | keep[2] | keep[3]) != 0;
+                    // Quarters in which some row of the warp has keys that it does not see are masked and written back.
+                    if (__any_sync(kFull, live && (keep[0] & keep[1] & keep[2] & keep[3]) != ~0u)) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t word = live ? keep[k] : ~0u;
+                            if (!__any_sync(kFull, word != ~0u)) continue;
+                            uint32_t s0[32];
+                            tmem_ld32_async(sbuf + k * 32, s0);
+                            tmem_wait_dep(s0);
+#pragma unroll
+                            for (int b = 0; b < 32; ++b)
+                                if (!(word >> b & 1u)) s0[b] = __float_as_uint(-INFINITY);
+                            tmem_st32_u(sbuf + k * 32, s0);
+                        }
+                        tmem_wait_st();
+                    }
+                    // P = 2^(s c - m) with the row's present reference m, 0 at first; the sum tells whether m was
+                    // good enough (P and the sums far from the ends of their types' ranges: for fp16 P, m is
+                    // within 2^15 of the largest so far). If not, m becomes the tile's largest score and P is
+                    // computed again: P is kept in registers until then, for it overwrites scores.
+                    const f2 cc = pack2(a.c, a.c);
+                    bool raise = kF16 && m == -INFINITY && sees;
+#pragma unroll 1
+                    for (int round = 0; round < 2; ++round) {
+                        if (__any_sync(kFull, raise)) {
+                            float mx8[8];
+#pragma unroll
+                            for (int b = 0; b < 8; ++b) mx8[b] = -INFINITY;
+#pragma unroll 1
+                            for (int k = 0; k < 128; k += 32) {
+                                uint32_t s0[32];
+                                tmem_ld32_async(sbuf + k, s0);
+                                tmem_wait_dep(s0);
+                                max_scores(s0, mx8);
+                            }
+                            const float tm = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
+                                                   fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]))) * a.c;
+                            raise = raise && tm > -INFINITY;
+                            const float f = raise && l != 0.f ? ex2(m - tm) : 1.f;  // (without weight so far: O is 0)
+                            if (raise) m = tm;
+                            l *= f;
+                            // the warp rescales its O together (tcgen05.ld / st are warp-wide), rows without need by
+                            // 1. The half's previous product is done: S of this item was issued after it.
+                            if (__any_sync(kFull, f != 1.f)) {
+#pragma unroll 1
+                                for (int ch = 0; ch < 8; ++ch) {
+                                    uint32_t o[16];
+                                    tmem_ld16_async(obuf + ch * 16, o);
+                                    tmem_wait_dep(o);
+#pragma unroll
+                                    for (int b = 0; b < 16; ++b) o[b] = __float_as_uint(__uint_as_float(o[b]) * f);
+                                    tmem_st16(obuf + ch * 16, o);
+                                }
+                            }
+                        }
+                        const float mr = m == -INFINITY ? 0.f : -m;
+                        const f2 mm = pack2(mr, mr);
+                        f2 lsum[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
+                        uint32_t s0[32], s1[32], s2[32], s3[32], pk[32], pk2[32];
+                        tmem_ld32_async(sbuf, s0);
+                        tmem_ld32_async(sbuf + 32, s1);
                         tmem_wait_dep(s0);
-#pragma unroll
-                        for (int b = 0; b < 32; ++b)
-                            if (!(word >> b & 1u)) s0[b] = __float_as_uint(-INFINITY);
-                        tmem_st32_u(sbuf + k * 32, s0);
+                        tmem_wait_dep(s1);
+                        exp_scores<kF16>(s0, cc, mm, lsum, pk, 0);
+                        tmem_ld32_async(sbuf + 64, s2);
+                        exp_scores<kF16>(s1, cc, mm, lsum, pk, 16);
+                        tmem_ld32_async(sbuf + 96, s3);
+                        tmem_wait_dep(s2);
+                        tmem_wait_dep(s3);
+                        exp_scores<kF16>(s2, cc, mm, lsum, pk2, 0);
+                        exp_scores<kF16>(s3, cc, mm, lsum, pk2, 16);
+                        float l0, l1;
+                        unpack2(add2(add2(lsum[0], lsum[1]), add2(lsum[2], lsum[3])), l0, l1);
+                        l0 += l1;
+                        raise = sees && (!(l0 < kMostWeight) || (!kF16 && l == 0.f && l0 < kLeastWeight));
+                        if (round == 0 && __any_sync(kFull, raise)) continue;
+                        l += l0;
+                        tmem_st32_u(sbuf, pk);
+                        tmem_st32_u(sbuf + 64, pk2);
+                        break;
                     }
                     tmem_wait_st();
                 }
-                // P = 2^(s c - m) with the row's present reference m, 0 at first; the sum tells whether m was
-                // good enough (P and the sums far from the ends of their types' ranges: for fp16 P, m is
-                // within 2^15 of the largest so far). If not, m becomes the tile's largest score and P is
-                // computed again: P is kept in registers until then, for it overwrites scores.
-                const f2 cc = pack2(a.c, a.c);
-                bool raise = kF16 && m == -INFINITY && sees;
+                if (it + 2 >= items) c.ml[n % kMlSlots][h][r] = make_float2(l == 0.f ? -INFINITY : m, l);
+                // V has to be there, too: the issuer then has one wait less. Where the sequence ends in this tile,
+                // the rows of its last page past the end are cleared (later pages' are zeros), by the row
+                // tile whose product comes first.
+                const int end = p.q.len - key, stop = min(tree::kRows, ((p.q.len + (1 << a.s.page_log) - 1) >> a.s.page_log << a.s.page_log) - key);
+                const bool clears = end < stop && (!two || (it & 1) == 0);
+                if (clears || q == 0) {
+                    const uint32_t stage = kt % kStages;
+                    if (!(ok = warp_wait(&c.v_full[stage], (kt / kStages) & 1, c, a))) break;
+                    if (clears) {
+                        uint8_t *vb = sv + stage * kTileBytes;
 #pragma unroll 1
-                for (int round = 0; round < 2; ++round) {
-                    if (__any_sync(kFull, raise)) {
-                        float mx8[8];
-#pragma unroll
-                        for (int b = 0; b < 8; ++b) mx8[b] = -INFINITY;
-#pragma unroll 1
-                        for (int k = 0; k < 128; k += 32) {
-                            uint32_t s0[32];
-                            tmem_ld32_async(sbuf + k, s0);
-                            tmem_wait_dep(s0);
-                            max_scores(s0, mx8);
+                        for (int y = r; y < (stop - max(end, 0)) * 16; y += 128) {  // 8 16-byte units in each of two chunks
+                            const int token = max(end, 0) + (y >> 4);
+                            st_shared_v4(saddr(vb + token / 8 * kGroup + (y & 8 ? kChunk : 0) + token % 8 * 128 + (y & 7) * 16),
+                                         make_uint4(0, 0, 0, 0));
                         }
-                        const float tm = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
-                                               fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]))) * a.c;
-                        raise = raise && tm > -INFINITY;
-                        const float f = raise && l != 0.f ? ex2(m - tm) : 1.f;  // (without weight so far: O is 0)
-                        if (raise) m = tm;
-                        l *= f;
-                        // the warp rescales its O together (tcgen05.ld / st are warp-wide), rows without need by
-                        // 1. The half's previous product is done: S of this item was issued after it.
-                        if (__any_sync(kFull, f != 1.f)) {
-#pragma unroll 1
-                            for (int ch = 0; ch < 8; ++ch) {
-                                uint32_t o[16];
-                                tmem_ld16_async(obuf + ch * 16, o);
-                                tmem_wait_dep(o);
-#pragma unroll
-                                for (int b = 0; b < 16; ++b) o[b] = __float_as_uint(__uint_as_float(o[b]) * f);
-                                tmem_st16(obuf + ch * 16, o);
-                            }
-                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
-                    const float mr = m == -INFINITY ? 0.f : -m;
-                    const f2 mm = pack2(mr, mr);
-                    f2 lsum[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
-                    uint32_t s0[32], s1[32], s2[32], s3[32], pk[32], pk2[32];
-                    tmem_ld32_async(sbuf, s0);
-                    tmem_ld32_async(sbuf + 32, s1);
-                    tmem_wait_dep(s0);
-                    tmem_wait_dep(s1);
-                    exp_scores<kF16>(s0, cc, mm, lsum, pk, 0);
-                    tmem_ld32_async(sbuf + 64, s2);
-                    exp_scores<kF16>(s1, cc, mm, lsum, pk, 16);
-                    tmem_ld32_async(sbuf + 96, s3);
-                    tmem_wait_dep(s2);
-                    tmem_wait_dep(s3);
-                    exp_scores<kF16>(s2, cc, mm, lsum, pk2, 0);
-                    exp_scores<kF16>(s3, cc, mm, lsum, pk2, 16);
-                    float l0, l1;
-                    unpack2(add2(add2(lsum[0], lsum[1]), add2(lsum[2], lsum[3])), l0, l1);
-                    l0 += l1;
-                    raise = sees && (!(l0 < kMostWeight) || (!kF16 && l == 0.f && l0 < kLeastWeight));
-                    if (round == 0 && __any_sync(kFull, raise)) continue;
-                    l += l0;
-                    tmem_st32_u(sbuf, pk);
-                    tmem_st32_u(sbuf + 64, pk2);
-                    break;
                 }
-                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&c.p_full[h]);
+                it += 2;
             }
-            if (it + 2 >= items) c.ml[n & 1][h][r] = make_float2(l == 0.f ? -INFINITY : m, l);
-            // V has to be there, too: the issuer then has one wait less. Where the sequence ends in this tile,
-            // the rows of its last page past the end are cleared (later pages' are zeros), by the row
-            // tile whose product comes first.
-            const int end = p.q.len - key, stop = min(tree::kRows, ((p.q.len + (1 << a.s.page_log) - 1) >> a.s.page_log << a.s.page_log) - key);
-            const bool clears = end < stop && (!two || (it & 1) == 0);
-            if (clears || q == 0) {
-                const uint32_t stage = kt % kStages;
-                if (!(ok = warp_wait(&c.v_full[stage], (kt / kStages) & 1, c, a))) break;
-                if (clears) {
-                    uint8_t *vb = sv + stage * kTileBytes;
-#pragma unroll 1
-                    for (int y = r; y < (stop - max(end, 0)) * 16; y += 128) {  // 8 16-byte units in each of two chunks
-                        const int token = max(end, 0) + (y >> 4);
-                        st_shared_v4(saddr(vb + token / 8 * kGroup + (y & 8 ? kChunk : 0) + token % 8 * 128 + (y & 7) * 16),
-                                     make_uint4(0, 0, 0, 0));
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
+            if (pending) {
+                if (!(ok = warp_wait(&c.o_ready, (n - 1) & 1, c, a))) break;
+                tc_fence_after();
+                read_out<kF16>(tmem, q, lane, h, n - 1, noted, c, a);
+                pending = false;
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c.p_full[h]);
-        }
+        } while (it < items);
         if (!ok) break;
-        // ---- read-out: of a pair each half its own row tile, else each half 64 columns of both accumulators
-        if (!(ok = warp_wait(&c.o_ready, n & 1, c, a))) break;
-        tc_fence_after();
-        const bool both = !two && items > 1;
-        const int only = two ? h : x0 & 1;  // the half that has the (other) sums
-        if (any) {
-            const bool whole = p.part < 0;
-            const int head = p.h * a.s.group + g;
-            const int64_t slot = (2ll * blockIdx.x + max(p.part, 0)) * 2 + (two ? first : 0);
-            const uint64_t row = reinterpret_cast<uint64_t>(a.out) + 2 * (p.s * a.out_seq + i * a.out_token + head * a.out_head);
-            const float2 e = c.ml[n & 1][both ? 0 : only][r];
-            const float2 f = both ? c.ml[n & 1][1][r] : make_float2(-INFINITY, 0.f);
-            const float mx = fmaxf(e.x, f.x), mr = mx == -INFINITY ? 0.f : mx;
-            float w0 = e.y == 0.f ? 0.f : ex2(e.x - mr), w1 = f.y == 0.f ? 0.f : ex2(f.x - mr);
-            const float total = w0 * e.y + w1 * f.y;  // (NaN stays)
-            if (whole) {
-                const float inv = total == 0.f ? 0.f : __fdividef(1.f, total);
-                w0 *= inv;
-                w1 *= inv;
-            }
-            // (what has no weight may hold anything, NaN too: its bits are cleared)
-            const uint32_t keep0 = w0 == 0.f ? 0u : ~0u, keep1 = w1 == 0.f ? 0u : ~0u;
-            const uint32_t at0 = tmem + lane_off + kOCol + (both ? 0 : only * 128), at1 = tmem + lane_off + kOCol + 128;
-            // 32 columns at a time, the next on their way: of a pair all four quarters, else two with both halves' sums
-            uint32_t o[32], o1[32];
-            const int from = two ? 0 : static_cast<int>(h) * 64;
-            tmem_ld32_async(at0 + from, o);
-            tmem_ld32_async(two ? at0 + 32 : at1 + from, o1);
-#pragma unroll 1
-            for (int ch = from;; ch += 32) {
-                tmem_wait_dep(o);
-                tmem_wait_dep(o1);
-                if (both) {
-#pragma unroll
-                    for (int b = 0; b < 32; ++b)
-                        o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0 + __uint_as_float(o1[b] & keep1) * w1);
-                } else {
-#pragma unroll
-                    for (int b = 0; b < 32; ++b) o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0);
-                }
-                if (live) store_columns<kF16>(a, slot, row, r, ch, whole, o);
-                if (two) {
-                    ch += 32;
-#pragma unroll
-                    for (int b = 0; b < 32; ++b) o[b] = __float_as_uint(__uint_as_float(o1[b] & keep0) * w0);
-                    if (live) store_columns<kF16>(a, slot, row, r, ch, whole, o);
-                }
-                if (ch + 32 >= (two ? 128 : from + 64)) break;
-                tmem_ld32_async(at0 + ch + 32, o);
-                tmem_ld32_async(two ? at0 + ch + 64 : at1 + ch + 32, o1);
-            }
-            if (live && (two || h == 0)) {
-                if (!whole)
-                    a.part_ml[slot * tree::kRows + r] = make_float2(mx, total);
-                else if (a.lse)
-                    a.lse[(static_cast<int64_t>(p.s) * a.s.n_q + i) * a.n_heads + head] =
-                        total == 0.f ? -INFINITY : (mx + log2f(total)) * kLn2;
-            }
+        if (have) {
+            __syncwarp();
+            if (lane == 0) noted = Noted{p, x0};
+            __syncwarp();
+            pending = true;
+            x0 += items;
+            kt0 += p.j1 - p.j0;
+            have = next(a, c, w, p);
         }
-        if (p.part == 1 && h == 0 && q == 0 && lane == 0) {
-            // the unit's other tiles follow the range's end
-            const int last = tree::cta_of(c.ranges, c.range_end + p.to_last);
-            a.cut[blockIdx.x] = Cut{last - static_cast<int>(blockIdx.x) + 1, static_cast<int>(blockIdx.x), p.s, p.h, p.p, p.q.count, {0, 0}};
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&c.o_free);
-        x0 += items;
-        kt0 += p.j1 - p.j0;
     }
 }
 
