@@ -232,14 +232,19 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
     };
     // A piece ahead: its first pages' ids are on their way while the piece before is copied, and its
     // queries in L2 (a change of units took 4.5 us, of which the lookups were 2).
-    bool some = next(a, c, w, following);
-    int token = 0, id = some ? page_of(following, following.j0 + half, token) : -1;
+    bool some = true;
+    int token = 0, id = -1;
 #pragma unroll 1
-    for (int n = 0; ok && some; ++n) {
+    for (int n = -1; ok && some; ++n) {
         p = following;
         some = next(a, c, w, following);
         int first_token = 0;
         const int first_id = some ? page_of(following, following.j0 + half, first_token) : -1;
+        if (n < 0) {  // (p is none yet)
+            id = first_id;
+            token = first_token;
+            continue;
+        }
         if (is_k && some && elect_one())
 #pragma unroll 1
             for (int r = 0; r < 2 * following.rt; ++r)
@@ -481,33 +486,20 @@ __device__ __forceinline__ void read_out(uint32_t tmem, int q, int lane, uint32_
         // (what has no weight may hold anything, NaN too: its bits are cleared)
         const uint32_t keep0 = w0 == 0.f ? 0u : ~0u, keep1 = w1 == 0.f ? 0u : ~0u;
         const uint32_t at0 = tmem + lane_off + kOCol + (both ? 0 : only * 128), at1 = tmem + lane_off + kOCol + 128;
-        // 32 columns at a time, the next on their way: of a pair all four quarters, else two with both halves' sums
-        uint32_t o[32], o1[32];
-        const int from = two ? 0 : static_cast<int>(h) * 64;
-        tmem_ld32_async(at0 + from, o);
-        tmem_ld32_async(two ? at0 + 32 : at1 + from, o1);
+        // 32 columns at a time, of a pair all four quarters, else two with both halves' sums (one body for all,
+        // for the instruction cache: read-outs of 16 rows took 3 us)
+        const int from = two ? 0 : static_cast<int>(h) * 64, to = two ? 128 : from + 64;
 #pragma unroll 1
-        for (int ch = from;; ch += 32) {
+        for (int ch = from; ch < to; ch += 32) {
+            uint32_t o[32], o1[32];
+            tmem_ld32_async(at0 + ch, o);
+            tmem_ld32_async(at1 + ch, o1);
             tmem_wait_dep(o);
             tmem_wait_dep(o1);
-            if (both) {
 #pragma unroll
-                for (int b = 0; b < 32; ++b)
-                    o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0 + __uint_as_float(o1[b] & keep1) * w1);
-            } else {
-#pragma unroll
-                for (int b = 0; b < 32; ++b) o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0);
-            }
+            for (int b = 0; b < 32; ++b)
+                o[b] = __float_as_uint(__uint_as_float(o[b] & keep0) * w0 + __uint_as_float(o1[b] & keep1) * w1);
             if (live) store_columns<kF16>(a, slot, row, r, ch, whole, o);
-            if (two) {
-                ch += 32;
-#pragma unroll
-                for (int b = 0; b < 32; ++b) o[b] = __float_as_uint(__uint_as_float(o1[b] & keep0) * w0);
-                if (live) store_columns<kF16>(a, slot, row, r, ch, whole, o);
-            }
-            if (ch + 32 >= (two ? 128 : from + 64)) break;
-            tmem_ld32_async(at0 + ch + 32, o);
-            tmem_ld32_async(two ? at0 + ch + 64 : at1 + ch + 32, o1);
         }
         if (live && (two || h == 0)) {
             if (!whole)
@@ -554,9 +546,11 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, uint32_t
     Piece p{};
     uint32_t x0 = 0, kt0 = 0;  // items and key tiles of the pieces before
     Noted &noted = c.noted[h * 4 + q];
-    bool ok = true, pending = false, have = next(a, c, w, p);
+    bool ok = true, pending = false;
 #pragma unroll 1
-    for (int n = 0; have || pending; ++n) {
+    for (int n = 0;; ++n) {
+        const bool have = next(a, c, w, p);
+        if (!have && !pending) break;
         const int two = p.rt - 1, items = have ? (p.j1 - p.j0) << two : 0;
         const int first = (h ^ x0) & 1;                       // the half's first item
         const int i = (2 * p.p + (two ? first : 0)) * a.s.tokens + tok;  // the row's query
@@ -570,58 +564,41 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, uint32_t
             if (it < items && (!pending || done_already(&c.s_full[h], ((x0 + it) >> 1) & 1))) {
                 const uint32_t x = x0 + it, kt = kt0 + (it >> two);
                 const int key = (p.j0 + (it >> two)) * tree::kRows;
-                // bits of the keys that the row sees, a word for each quarter of the tile (rows that are not
-                // stored need no mask)
-                uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
-                if (live && key + tree::kRows > p.q.len - p.q.count) {
-                    if (a.s.chain) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) keep[k] = tree::chain_bits(p.q, i, key + 32 * k);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            keep[k] = tree::mask_bits(p.q, key + 32 * k, [&](int y) { return mask_row[y]; });
-                    }
-                }
                 if (!warp_wait(&c.s_full[h], (x >> 1) & 1, c, a)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
                 if (any) {
+                    // Keys that a row does not see take no weight: a word of 32 keys at a time, quarters in which some
+                    // row of the warp has such keys are masked and written back. (Rows that are not stored need
+                    // no mask.)
                     const uint32_t bad = c.bad[kt % 4];
-                    if (bad && live) {  // a page of this row's keys does not exist: NaN
-                        uint32_t hit = 0;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            uint32_t of_bad = 0;
-#pragma unroll
-                            for (int b = 0; b < 32; b += 8)  // (a copy is 8 tokens at least)
-                                if (bad >> ((32 * k + b) >> a.copies.copy_log) & 1u) of_bad |= 0xffu << b;
-                            hit |= keep[k] & of_bad;
-                        }
-                        if (hit) {
-                            l = NAN;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) keep[k] = 0;
-                        }
-                    }
-                    const bool sees = live && (keep[0] | keep[1] | keep[2] | keep[3]) != 0;
-                    // Quarters in which some row of the warp has keys that it does not see are masked and written back.
-                    if (__any_sync(kFull, live && (keep[0] & keep[1] & keep[2] & keep[3]) != ~0u)) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t word = live ? keep[k] : ~0u;
+                    bool sees = live;
+                    if (bad || key + tree::kRows > p.q.len - p.q.count) {
+                        uint32_t some = 0, hit = 0;
+#pragma unroll 1
+                        for (int k = 0; k < tree::kRows; k += 32) {
+                            uint32_t word = ~0u;
+                            if (live) word = a.s.chain ? tree::chain_bits(p.q, i, key + k)
+                                                       : tree::mask_bits(p.q, key + k, [&](int y) { return mask_row[y]; });
+                            some |= word;
+                            if (bad)
+#pragma unroll 1
+                                for (int b = 0; b < 32; b += 8)  // (a copy is 8 tokens at least)
+                                    if (bad >> ((k + b) >> a.copies.copy_log) & 1u) hit |= word >> b & 0xffu;
                             if (!__any_sync(kFull, word != ~0u)) continue;
                             uint32_t s0[32];
-                            tmem_ld32_async(sbuf + k * 32, s0);
+                            tmem_ld32_async(sbuf + k, s0);
                             tmem_wait_dep(s0);
 #pragma unroll
                             for (int b = 0; b < 32; ++b)
                                 if (!(word >> b & 1u)) s0[b] = __float_as_uint(-INFINITY);
-                            tmem_st32_u(sbuf + k * 32, s0);
+                            tmem_st32_u(sbuf + k, s0);
                         }
                         tmem_wait_st();
+                        if (live && hit) l = NAN;  // a page of this row's keys does not exist: NaN
+                        sees = live && some != 0 && !hit;
                     }
                     // P = 2^(s c - m) with the row's present reference m, 0 at first; the sum tells whether m was
                     // good enough (P and the sums far from the ends of their types' ranges: for fp16 P, m is
@@ -730,7 +707,6 @@ __device__ __forceinline__ void softmax(uint32_t tmem, int q, int lane, uint32_t
             pending = true;
             x0 += items;
             kt0 += p.j1 - p.j0;
-            have = next(a, c, w, p);
         }
     }
 }
