@@ -234,6 +234,59 @@ def test_as_many_units_as_ctas(n_seq, Hk):
         c.check(*c.run())
 
 
+LONG_AMONG_SHORT = [[30 + i % 50] for i in range(50)] + [[20000]] + [[30 + i % 50] for i in range(50)]
+
+
+@pytest.mark.parametrize("n_q,H", [(1, 2), (5, 8), (40, 8)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_a_long_sequence_among_short_ones(n_q, H, dtype):
+    """A unit in many parts beside whole ones, row tiles single and in pairs."""
+    c = Tree(41, LONG_AMONG_SHORT, n_q, H, 1, 64, dtype=dtype)
+    out, lse = c.run()
+    c.check(out, lse)
+    for _ in range(5):
+        again = c.run()
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("fill", [0, 1, 255, 0x5a, None])
+def test_a_workspace_of_any_content(fill):
+    """Whatever the workspace holds before a call, and between calls."""
+    c = Tree(42, LONG_AMONG_SHORT[40:], 3, 4, 1, 16)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    first = None
+    for i in range(4):
+        if fill is None:
+            c.ws.random_(0, 256, generator=g)
+        else:
+            c.ws.fill_(fill)
+        out, lse = c.run()
+        twice = c.run()  # (the workspace as the call left it)
+        first = first if first is not None else out
+        assert torch.equal(out, first) and torch.equal(twice[0], first)
+    c.check(out, lse)
+
+
+def test_calls_of_other_shapes_and_graphs_share_a_workspace():
+    a, b = Tree(43, LONG_AMONG_SHORT[40:], 3, 4, 1, 16), Tree(44, [[9000]] + [[70]] * 70, 2, 8, 1, 64, sees="chain")
+    b.ws = a.ws = a.ws if a.ws.numel() >= b.ws.numel() else b.ws
+    want = [x.run()[0].clone() for x in (a, b)]
+    side, graphs = torch.cuda.Stream(), []
+    side.wait_stream(torch.cuda.current_stream())
+    outs = [torch.zeros_like(w) for w in want]
+    for x, out in zip((a, b), outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            x.run(out, lse=False)
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 0, 1):
+        outs[i].zero_()
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i], want[i])
+        assert torch.equal((a, b)[1 - i].run()[0], want[1 - i])
+
+
 def test_no_sequence_at_all():
     c = Tree(37, [[-1], [-1]], 3, 2, 1, 16)
     c.check(*c.run())
@@ -267,8 +320,9 @@ def test_repeats_bit_for_bit_on_a_side_stream_and_from_a_graph():
     c.check(out, None)
 
 
-def test_wait_timeout_is_reported_and_the_next_launch_works():
-    c = Tree(39, [[300], [290]], 4, 2, 1, 16)
+@pytest.mark.parametrize("lens", [[[300], [290]], LONG_AMONG_SHORT])
+def test_wait_timeout_is_reported_and_the_next_launch_works(lens):
+    c = Tree(39, lens, 4, 2, 1, 16)
     torch.cuda.synchronize()
     rps.rps_debug_set_ring_wait_ns(0)
     try:
