@@ -820,12 +820,16 @@ assert _HEADS.size == C.sizeof(RpsHeads) and _TREE_ATTENTION.size == C.sizeof(Rp
 
 def _heads(name: str, src: torch.Tensor, dst: torch.Tensor) -> bytes:
     """``[n_seq][n_tok][heads][D]`` rows, and where they go."""
-    shape, st, to = src.shape, src.stride(), dst.stride()
-    if dst.shape != shape or st[3] != 1 or to[3] != 1:
-        raise ValueError(f"{name}: source and destination of one shape, head dim contiguous")
+    shape = src.shape
+    if dst.shape != shape:
+        raise ValueError(f"{name}: source and destination of one shape")
     if dst.dtype is not src.dtype:
         raise TypeError(f"{name}: source and destination of one dtype")
-    return _HEADS.pack(src.data_ptr(), dst.data_ptr(), shape[2], st[0], st[1], st[2], to[0], to[1], to[2])
+    s0, s1, s2, s3 = src.stride()
+    t0, t1, t2, t3 = dst.stride()
+    if s3 != 1 or t3 != 1:
+        raise ValueError(f"{name}: head dim contiguous")
+    return _HEADS.pack(src.data_ptr(), dst.data_ptr(), shape[2], s0, s1, s2, t0, t1, t2)
 
 
 def rps_rope_heads(rope: Rope, q: torch.Tensor, q_out: torch.Tensor, k: Optional[torch.Tensor] = None,
@@ -833,18 +837,21 @@ def rps_rope_heads(rope: Rope, q: torch.Tensor, q_out: torch.Tensor, k: Optional
     """Queries (and keys) ``[n_seq][n_tok][heads][D]`` with their norms and positions; ``q_out`` may be ``q``. ``pos``:
     int32 ``[n_seq][n_tok]`` (None: token i of its sequence is at position i)."""
     handle = _here(stream, q, q_out, k, k_out, pos, rope.any)
-    shape, dtype = q.shape, q.dtype
-    if len(shape) != 4 or dtype not in _KV_DTYPES:
+    dtype, code = q.dtype, _KV_DTYPES.get(q.dtype)
+    if q.dim() != 4 or code is None:
         raise ValueError("q: [n_seq][n_tok][heads][head dim], bf16 or fp16")
-    if (k is None) != (k_out is None):
-        raise ValueError("k comes with k_out")
-    n_seq, n_tok, _, d = shape
-    b = None
-    if k is not None:
-        if len(k.shape) != 4 or k.shape[:2] != shape[:2] or k.shape[3] != d or k.dtype is not dtype:
+    n_seq, n_tok, _, d = q.shape
+    a, b = _heads("q", q, q_out), None
+    if k is not None or k_out is not None:
+        if k is None or k_out is None:
+            raise ValueError("k comes with k_out")
+        if k.dim() != 4 or k.dtype is not dtype:
+            raise ValueError("k: [n_seq][n_tok][heads][head dim], as q")
+        k0, k1, _, k3 = k.shape
+        if k0 != n_seq or k1 != n_tok or k3 != d:
             raise ValueError("k: [n_seq][n_tok][heads][head dim], as q")
         b = _heads("k", k, k_out)
-    _check(_lib.rps_rope_heads(rope._c(d, dtype), _heads("q", q, q_out), b, _KV_DTYPES[dtype], d, n_seq, n_tok,
+    _check(_lib.rps_rope_heads(rope._c(d, dtype), a, b, code, d, n_seq, n_tok,
                                None if pos is None else _ints("pos", pos, n_seq * n_tok), handle), "rps_rope_heads")
 
 
