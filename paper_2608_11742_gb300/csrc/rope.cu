@@ -6,8 +6,8 @@
 // weights, else y = x; then each pair (y0, y1) of the first R elements is turned by
 // its angle a = 2 pi f t, t the position: A (y0 cos a - y1 sin a), A (y1 cos a + y0 sin a).
 // The frequency f of a pair is given in turns per position as a fraction of 2^64, so
-// t f modulo 2^64 is the fraction of a turn exactly, whatever the position: what is
-// left to fp32 is half a turn at most. All in fp32, rounded once at the end.
+// t f modulo 2^64 is the fraction of a turn exactly, whatever the position: of it 32 bits
+// (1.5e-9 of a radian), half a turn at most, are left to fp32. All in fp32, rounded once at the end.
 //
 // Bound by HBM: 4 D bytes a row (16-bit elements read and written once), as long as a pass
 // of a warp over 1024 bytes takes less than about 170 instructions (at twice as many, 576 x 32
@@ -197,9 +197,9 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
     if (a.R) {
         const int64_t t = a.pos ? a.pos[x] : token;
         for (int p = lane; p < a.R / 2; p += 32) {
-            const int64_t turn = static_cast<int64_t>(static_cast<uint64_t>(t) * a.turns[p]);
+            const int32_t turn = static_cast<int32_t>(static_cast<uint64_t>(t) * a.turns[p] >> 32);
             float sn, cs;
-            sincospif(static_cast<float>(turn) * 0x1p-63f, &sn, &cs);
+            sincospif(static_cast<float>(turn) * 0x1p-31f, &sn, &cs);
             turned[warp][p] = make_float2(cs * a.amplitude, sn * a.amplitude);
         }
         __syncwarp();

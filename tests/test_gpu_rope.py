@@ -4,7 +4,7 @@
 Tolerance, from the arithmetic: one rounding to the heads' type, at most e = half a step
 relative (bf16 2^-8, fp16 2^-11; below fp16's normal range 2^-25 absolute), of a value whose
 fp32 terms are measured by the size s = amplitude * hypot of the pair (or |y| itself):
-the angle, half a turn at most, is off by 2^-25 relative before and 2 ulp after the sine, 3e-7;
+the angle, half a turn at most, is off by 2^-32 of a turn and 2^-25 relative before and 2 ulp after the sine, 3e-7;
 three roundings of the products 1.8e-7; the norm's sum of at most 256 squares takes 20
 roundings of which the root halves the effect, and the reciprocal root 2 ulp: 7e-7. Together
 below 2^-19 s.
