@@ -32,9 +32,9 @@ namespace rps {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kAhead = 4;     // rows of a lane in flight
-constexpr int kPasses = 8;    // rows of a lane in a task, at most
+constexpr int kAhead = 4;  // passes of a warp in shared memory
 constexpr int kMaxDim = 256;
+constexpr int kFullWarps = 24;  // of an SM
 
 // (A division of 32 bits where they are enough.)
 __device__ __forceinline__ int64_t divide(int64_t x, int32_t d) {
@@ -56,7 +56,8 @@ struct RotateArgs {
     float amplitude, eps, inv_d;
     int32_t D, n_tok;
     const int32_t *pos;
-    int32_t passes, chunks_q, chunks_k, chunks;  // passes of a task; tasks of a token's queries, of its keys, of all
+    int32_t passes_q, passes_k, passes_all;  // passes of a token's queries, of its keys, of all its rows
+    int32_t passes, chunks;                  // of a task; tasks of a token
     int64_t tasks;
     // append: the values, and where keys and values go
     Side v;
@@ -113,11 +114,24 @@ __device__ __forceinline__ void narrow16(const f2 (&y0)[4], const f2 (&y1)[4], b
     }
 }
 
-// kLanes lanes to a row (16 elements each), 32 / kLanes rows of a token's side at a time, up to eight
-// such passes a task, four of them in flight.
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
+// kLanes lanes to a row (16 elements each), 32 / kLanes rows of a token at a time: a pass. A warp's task is
+// the passes of a token's queries, then of its keys and its values, or a part of them where tokens are few.
+// Rows come through shared memory, three passes ahead (seven: 54 us instead of 45 for 16222 tokens of 28 and
+// 4 heads). In registers they took a loop unrolled by four in which no side could follow the other, so
+// that a task was one side's, and the few keys' warps had a pass in flight (54 us).
 template <bool kF16, int kLanes, bool kPaged>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
     __shared__ float2 turned[kWarps][kMaxDim / 2];
+    __shared__ uint4 ring[kWarps][kAhead][64];  // the rows of a pass one after another
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kAt = 32 / kLanes;
     const int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
@@ -125,7 +139,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
     pdl_launch_next();
     if (task >= a.tasks) return;
     const int64_t x = divide(task, a.chunks);
-    int chunk = static_cast<int>(task - x * a.chunks);
+    const int p_lo = static_cast<int>(task - x * a.chunks) * a.passes, p_hi = min(p_lo + a.passes, a.passes_all);
     const int64_t s = divide(x, a.n_tok);
     const int i = static_cast<int>(x - s * a.n_tok);
     int token = i;
@@ -140,61 +154,67 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
         token = len - count + i;
         if (token < 0) return;  // (a row without a place)
     }
-    const bool is_q = chunk < a.chunks_q, is_v = kPaged && chunk >= a.chunks_q + a.chunks_k;
-    const Side &d = is_q ? a.q : is_v ? a.v : a.k;
-    chunk -= is_q ? 0 : is_v ? a.chunks_q + a.chunks_k : a.chunks_q;
-    const int row0 = chunk * a.passes * kAt, end = min(d.heads, row0 + a.passes * kAt);  // the task's rows
-
     // this lane's 16-byte units of a row
-    const int l = lane % kLanes, mine = row0 + lane / kLanes;
+    const int l = lane % kLanes, of_pass = lane / kLanes;
     const bool rotates = l < a.R / 16, there = l < a.D / 16;
     const bool halves = rotates && !a.interleaved;
     const int u0 = (halves ? l : 2 * l) * 16, u1 = (halves ? l + a.R / 16 : 2 * l + 1) * 16;
-    const char *from = d.src + s * d.src_seq + i * d.src_token + mine * d.src_head;
-    uint4 raw0[kAhead], raw1[kAhead];
-    const auto load = [&](int p, int u) {
-        if (!there || mine + p * kAt >= end) return;
-        const char *at = from + p * (kAt * d.src_head);
-        raw0[u] = __ldcs(reinterpret_cast<const uint4 *>(at + u0));
-        raw1[u] = __ldcs(reinterpret_cast<const uint4 *>(at + u1));
+
+    // The side of a pass, and the pass that the side begins with.
+    const auto side_of = [&](int p, int &begin) -> const Side & {
+        if (p < a.passes_q) {
+            begin = 0;
+            return a.q;
+        }
+        if (!kPaged || p < a.passes_q + a.passes_k) {
+            begin = a.passes_q;
+            return a.k;
+        }
+        begin = a.passes_q + a.passes_k;
+        return a.v;
     };
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) load(u, u);
-    char *to = d.dst + mine * (kPaged && !is_q ? a.head_stride : d.dst_head);
-    int64_t step = kAt * d.dst_head;
-    if (kPaged && !is_q) {
+    constexpr uint32_t kSlot = sizeof ring[0][0];
+    const uint32_t slots = saddr(&ring[warp][0][0]) + of_pass * 2 * a.D;
+    // The units that this lane copies: its own, or (interleaved) side by side with its neighbours', for its
+    // own would be fetched by half sectors (16222 tokens of 64 heads: 115 us)
+    const int near = a.interleaved ? l * 16 : u0, far = a.interleaved ? near + a.D : u1;
+    int begin;
+    const Side *in = &side_of(p_lo, begin);
+    const char *from = in->src + s * in->src_seq + i * in->src_token + ((p_lo - begin) * kAt + of_pass) * in->src_head;
+    int row = (p_lo - begin) * kAt + of_pass;  // of the next pass to be copied
+    const auto copy = [&](int p) {
+        if (p < p_hi) {
+            if (p != p_lo && (p == a.passes_q || (kPaged && p == a.passes_q + a.passes_k))) {  // another side begins
+                in = &side_of(p, begin);
+                row = of_pass;
+                from = in->src + s * in->src_seq + i * in->src_token + row * in->src_head;
+            }
+            if (there && row < in->heads) {
+                const uint32_t to = slots + p % kAhead * kSlot;
+                copy_async(to + near, from + near);
+                copy_async(to + far, from + far);
+            }
+            row += kAt;
+            from += kAt * in->src_head;
+        }
+        copies_commit();
+    };
+#pragma unroll 1
+    for (int p = p_lo; p < p_lo + kAhead - 1; ++p) copy(p);
+
+    // the token's place, and its sines and cosines while the rows are on their way
+    int64_t place = -1;
+    if (kPaged && p_hi > a.passes_q) {
         const int page = a.table[s * a.width + (token >> a.page_log)];
         if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.n_pages)) {
             if (lane == 0) flag_error(a.err, RPS_DEVERR_PAGE);
-            return;
-        }
-        if (a.ref[page] > 1) {  // others read this page too
+        } else if (a.ref[page] > 1) {  // others read this page too
             if (lane == 0) flag_error(a.err, RPS_DEVERR_SHARED);
-            return;
+        } else {
+            place = page * a.page_stride + (token & ((1 << a.page_log) - 1)) * a.token_stride;
         }
-        to += page * a.page_stride + (token & ((1 << a.page_log) - 1)) * a.token_stride;
-        step = kAt * a.head_stride;
-    } else {
-        to += s * d.dst_seq + i * d.dst_token;
     }
-    const auto store = [&](int p, int u) {
-        if (!there || mine + p * kAt >= end) return;
-        char *at = to + p * step;
-        *reinterpret_cast<uint4 *>(at + u0) = raw0[u];
-        *reinterpret_cast<uint4 *>(at + u1) = raw1[u];
-    };
-    if (is_v) {
-#pragma unroll 1
-        for (int p0 = 0; row0 + p0 * kAt < end; p0 += kAhead)
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                store(p0 + u, u);
-                load(p0 + u + kAhead, u);
-            }
-        return;
-    }
-    // the token's sines and cosines, and this lane's with its weights, while the rows are on their way
-    if (a.R) {
+    if (a.R && p_lo < a.passes_q + a.passes_k) {
         const int64_t t = a.pos ? a.pos[x] : token;
         for (int p = lane; p < a.R / 2; p += 32) {
             const int32_t turn = static_cast<int32_t>(static_cast<uint64_t>(t) * a.turns[p] >> 32);
@@ -206,29 +226,49 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
     }
     const f2 one = pack2(1.f, 1.f), minus = pack2(-1.f, -1.f);
     f2 c0[4], c1[4], s0[4], s1[4];  // w0 cos, w1 cos, w0 sin, -w1 sin
-    {
-        f2 w0[4] = {one, one, one, one}, w1[4] = {one, one, one, one};
-        if (d.weight && there)
-            widen16<kF16>(*reinterpret_cast<const uint4 *>(static_cast<const char *>(d.weight) + u0),
-                          *reinterpret_cast<const uint4 *>(static_cast<const char *>(d.weight) + u1), !halves, w0, w1);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float4 f = rotates ? *reinterpret_cast<const float4 *>(&turned[warp][8 * l + 2 * j]) : make_float4(1.f, 0.f, 1.f, 0.f);
-            const f2 cs = pack2(f.x, f.z), sn = pack2(f.y, f.w);
-            c0[j] = mul2(w0[j], cs);
-            c1[j] = mul2(w1[j], cs);
-            s0[j] = mul2(w0[j], sn);
-            s1[j] = mul2(mul2(w1[j], sn), minus);
-        }
-    }
-    const bool normed = d.weight != nullptr;
+    const Side *d = nullptr;
+    char *to = nullptr;
+    int at = 0;
+    int64_t step = 0;
+    bool normed = false, value = false, stored = false;
 #pragma unroll 1
-    for (int p0 = 0; row0 + p0 * kAt < end; p0 += kAhead) {
+    for (int p = p_lo; p < p_hi; ++p) {
+        if (a.interleaved) __syncwarp();  // (all lanes have taken the pass before, whose place is free)
+        copy(p + kAhead - 1);
+        if (p == p_lo || p == a.passes_q || (kPaged && p == a.passes_q + a.passes_k)) {  // another side begins
+            int first;
+            d = &side_of(p, first);
+            const bool to_cache = kPaged && p >= a.passes_q;
+            value = kPaged && p >= a.passes_q + a.passes_k;
+            normed = d->weight != nullptr;
+            at = (p - first) * kAt + of_pass;
+            stored = there && (!to_cache || place >= 0);
+            const int64_t head = to_cache ? a.head_stride : d->dst_head;
+            to = d->dst + at * head + (to_cache ? place : s * d->dst_seq + i * d->dst_token);
+            step = kAt * head;
+            if (!value) {
+                f2 w0[4] = {one, one, one, one}, w1[4] = {one, one, one, one};
+                if (normed && there)
+                    widen16<kF16>(*reinterpret_cast<const uint4 *>(static_cast<const char *>(d->weight) + u0),
+                                  *reinterpret_cast<const uint4 *>(static_cast<const char *>(d->weight) + u1), !halves, w0, w1);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (row0 + (p0 + u) * kAt >= end) break;  // (the same for the whole warp)
+                for (int j = 0; j < 4; ++j) {
+                    const float4 f = rotates ? *reinterpret_cast<const float4 *>(&turned[warp][8 * l + 2 * j]) : make_float4(1.f, 0.f, 1.f, 0.f);
+                    const f2 cs = pack2(f.x, f.z), sn = pack2(f.y, f.w);
+                    c0[j] = mul2(w0[j], cs);
+                    c1[j] = mul2(w1[j], cs);
+                    s0[j] = mul2(w0[j], sn);
+                    s1[j] = mul2(mul2(w1[j], sn), minus);
+                }
+            }
+        }
+        copies_wait<kAhead - 1>();
+        if (a.interleaved) __syncwarp();
+        const uint32_t slot = slots + p % kAhead * kSlot;
+        uint4 raw0 = ld_shared_v4(slot + u0), raw1 = ld_shared_v4(slot + u1);
+        if (!value) {
             f2 y0[4], y1[4];
-            widen16<kF16>(raw0[u], raw1[u], !halves, y0, y1);
+            widen16<kF16>(raw0, raw1, !halves, y0, y1);
             float r = 1.f;
             if (normed) {
                 f2 sum = pack2(0.f, 0.f);
@@ -252,10 +292,14 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
                 y0[j] = z0;
                 y1[j] = z1;
             }
-            narrow16<kF16>(y0, y1, !halves, raw0[u], raw1[u]);
-            store(p0 + u, u);
-            load(p0 + u + kAhead, u);
+            narrow16<kF16>(y0, y1, !halves, raw0, raw1);
         }
+        if (stored && at < d->heads) {
+            *reinterpret_cast<uint4 *>(to + u0) = raw0;
+            *reinterpret_cast<uint4 *>(to + u1) = raw1;
+        }
+        at += kAt;
+        to += step;
     }
 }
 
@@ -310,15 +354,19 @@ rps_status launch_rotate(RotateArgs &a, int32_t n_seq, bool f16, cudaStream_t st
     if (sms < 1) return RPS_ERR_CUDA;
     const int lanes = a.D <= 64 ? 4 : a.D <= 128 ? 8 : 16, at = 32 / lanes;
     const int64_t tokens = static_cast<int64_t>(n_seq) * a.n_tok;
-    // Few rows are spread over more warps: a warp's passes come one after another.
-    const auto chunks = [&](int heads) { return (heads + a.passes * at - 1) / (a.passes * at); };
-    for (a.passes = kPasses;; a.passes /= 2) {
-        a.chunks_q = chunks(a.q.heads);
-        a.chunks_k = chunks(a.k.heads);
-        a.chunks = a.chunks_q + a.chunks_k + (kPaged ? chunks(a.v.heads) : 0);
-        a.tasks = tokens * a.chunks;
-        if (a.passes == 1 || a.tasks >= sms * (a.passes > kAhead ? 64 : 8)) break;
-    }
+    const auto passes = [&](int heads) { return (heads + at - 1) / at; };
+    a.passes_q = passes(a.q.heads);
+    a.passes_k = passes(a.k.heads);
+    a.passes_all = a.passes_q + a.passes_k + (kPaged ? passes(a.v.heads) : 0);
+    // Tokens are split where there are too few: down to single passes until the card is full, for they come one
+    // after another, and to eight, which carry a token's sines and cosines, until there are eight tasks for each
+    // warp, so that the last ones of the call are short.
+    const int64_t warps = static_cast<int64_t>(sms) * kFullWarps;
+    const int64_t fill = std::min<int64_t>(a.passes_all, warps / tokens), even = std::min<int64_t>(a.passes_all / 8, 8 * warps / tokens);
+    a.chunks = static_cast<int32_t>(std::max<int64_t>({1, fill, even}));
+    a.passes = (a.passes_all + a.chunks - 1) / a.chunks;
+    a.chunks = (a.passes_all + a.passes - 1) / a.passes;
+    a.tasks = tokens * a.chunks;
     const int64_t blocks = (a.tasks + kWarps - 1) / kWarps;
     if (blocks > INT32_MAX) return RPS_ERR_UNSUPPORTED;
     const auto kernel = lanes == 4   ? (f16 ? rotate_kernel<true, 4, kPaged> : rotate_kernel<false, 4, kPaged>)
