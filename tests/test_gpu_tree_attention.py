@@ -214,7 +214,7 @@ def test_lengths_beyond_the_table():
     assert bool(torch.isfinite(out[0]).all())
 
 
-@pytest.mark.parametrize("n_seq", [383, 384, 385, 1000])
+@pytest.mark.parametrize("n_seq", [383, 384, 385, 639, 640, 641, 1000])
 def test_more_sequences_than_a_block_has_threads(n_seq):
     rng = np.random.default_rng(35)
     lens = rng.integers(1, 40, (n_seq, 1))
