@@ -77,7 +77,7 @@ typedef enum {
 #define RPS_DEVERR_NO_PAGES 0x80u  /* not enough free pages: a sequence was not grown */
 #define RPS_DEVERR_SHARED 0x100u   /* a write into a page that several sequences hold was left out */
 
-typedef enum { RPS_F32 = 0, RPS_BF16 = 1, RPS_F16 = 2 /* K/V cache and its attention only */ } rps_dtype;
+typedef enum { RPS_F32 = 0, RPS_BF16 = 1, RPS_F16 = 2 /* K/V cache, its attention, positions only */ } rps_dtype;
 
 /* Per-request state after rps_select_pivots. */
 typedef enum {
@@ -731,8 +731,8 @@ rps_status rps_tree_masks(const int32_t *d_parent, const int32_t *d_n_tok, const
  * token len - m + d, d < d_n_keep[s], in every layer. d_path [n_req * n_branch][n_path] ascends.
  * d_new_len (or NULL) takes len - m + n_keep, -1 for absent sequences: the lengths for
  * rps_kv_resize, which gives the other tokens' pages back; len itself stays. A path that does not
- * ascend or leaves 0..m-1, and more kept tokens than n_path or m, set RPS_DEVERR_ROW_INDEX,
- * move nothing of their sequence and keep its length. A row whose new page has a count above 1
+ * ascend or leaves 0..m-1, more kept tokens than n_path or m, and a sequence of fewer than m tokens
+ * set RPS_DEVERR_ROW_INDEX, move nothing of their sequence and keep its length. A row whose new page has a count above 1
  * is left out and sets RPS_DEVERR_SHARED, a page id outside the cache RPS_DEVERR_PAGE. n_path and n_q at most
  * RPS_TREE_MAX_TOKENS, at most 65535 sequences. One launch.
  */
@@ -779,7 +779,7 @@ typedef struct {
  * that can overlap. */
 size_t rps_tree_attention_workspace_bytes(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads);
 
-/* Two launches on `stream`. Errors: RPS_ERR_INVALID_ARG for NULL or misaligned pointers,
+/* One or two launches on `stream`. Errors: RPS_ERR_INVALID_ARG for NULL or misaligned pointers,
  * sizes or strides out of range, or a small workspace; RPS_ERR_UNSUPPORTED beyond the limits
  * above; RPS_ERR_CUDA when the tensor-map encoder is not available. A bounded device
  * wait that gives up reports RPS_DEVERR_TIMEOUT (the output is then incomplete). */

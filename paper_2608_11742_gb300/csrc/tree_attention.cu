@@ -27,6 +27,19 @@
 //               handed on, V's rows past the sequence's end are cleared (they may hold
 //               anything, and 0 * NaN would reach the sums). At a piece's end the same warps
 //               read the accumulators out.
+//
+// What bounds it, at the figures measured (times of both launches, warm, from a graph):
+//   64 sequences x 1 token, 28 / 4 heads, contexts 200 to 8000: 90 us, 5.97 TB/s, 0.88 of a copy's
+//     bandwidth. 64 x 1, 32 / 32 heads, context 1000: 167 us, 0.93.
+//   2 sequences x 64 tokens, 32 / 8 heads, contexts 24000 to 32700, fp16: 60 us, 3.9 TB/s; 64 x 1 to 32
+//     tokens, 32 / 4 heads, contexts 500 to 4000: 75 us, 4.2 TB/s. A pair's key tile takes 1.6 to 1.85 us,
+//     1.47 at HBM's rate: its products read 192 KB of shared memory and the copies write 64 (2048 cycles),
+//     and a half's next scores wait for its softmax (1580 cycles), P V and their own product. Slower: S and P
+//     in halves of 64 keys (65 -> 71), two warps to 32 rows in the softmax (60 -> 63).
+//   Start and end: the range is known 1.9 us after the launch before has ended, the first scores are there
+//     2.7 to 4.3 later, the last CTA ends 4 to 6 us after the median one, the joining launch takes 4 to 8.
+//   200 sequences x 4 tokens, 32 / 8 heads, contexts 20 to 300: 57 us, 10 units a CTA of two key tiles each; 77 with
+//     a third more code in the roles, which have to fit the instruction cache together.
 // Every wait is bounded; a role whose wait runs out flags RPS_DEVERR_TIMEOUT and raises the
 // CTA's abort flag, copies and MMAs in flight are drained and TMEM is freed before the CTA
 // exits.
