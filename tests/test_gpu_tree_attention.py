@@ -267,6 +267,31 @@ def test_a_workspace_of_any_content(fill):
     c.check(out, lse)
 
 
+@pytest.mark.parametrize("sees", ["tree", "chain"])
+def test_the_largest_trees(sees):
+    """1024 drafted tokens, 32 words a mask: eight pairs of row tiles; 64 with groups of 128 heads: 32 pairs of one token."""
+    c = Tree(45, [[1100], [1024], [300]], 1024, 2, 1, 64, sees=sees, count=[1024, 1001, 300])
+    c.check(*c.run())
+    c = Tree(46, [[150], [64]], 64, 128, 1, 16, sees=sees)
+    c.check(*c.run())
+
+
+def test_two_calls_at_once():
+    """On two streams, each with its workspace: as one after the other."""
+    a, b = Tree(47, LONG_AMONG_SHORT, 3, 4, 1, 64), Tree(48, [[9000]] + [[70]] * 70, 40, 8, 1, 64)
+    want = [x.run()[0].clone() for x in (a, b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.zeros_like(w) for _ in range(6)] for w in want]
+    torch.cuda.synchronize()
+    for k in range(6):
+        for x, s, out in zip((a, b), streams, outs):
+            with torch.cuda.stream(s):
+                x.run(out[k], lse=False, stream=s)
+    torch.cuda.synchronize()
+    assert rps.rps_poll_device_status()[0] == rps.RPS_OK
+    assert all(torch.equal(o, w) for w, out in zip(want, outs) for o in out)
+
+
 def test_calls_of_other_shapes_and_graphs_share_a_workspace():
     a, b = Tree(43, LONG_AMONG_SHORT[40:], 3, 4, 1, 16), Tree(44, [[9000]] + [[70]] * 70, 2, 8, 1, 64, sees="chain")
     b.ws = a.ws = a.ws if a.ws.numel() >= b.ws.numel() else b.ws
