@@ -75,7 +75,9 @@ constexpr int kDeep = 8;  // rows of a half warp in flight
 
 // Block (slice of the layers' heads, sequence): the places of the path's tokens are looked
 // up once, then a half warp moves a head's rows, in order and 8 at a time. The path ascends,
-// so its d-th entry is d at least: no row is written before it is read.
+// so its d-th entry is d at least: no row is written before it is read. Bound by HBM, by rows of
+// 256 bytes scattered over the cache (64 sequences, 32 layers of 8 heads, up to 17 of 64 tokens:
+// 27 us, 4.9 TB/s read and written).
 __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const KeepArgs a) {
     __shared__ int64_t from[RPS_TREE_MAX_TOKENS], to[RPS_TREE_MAX_TOKENS];
     __shared__ int32_t bad;

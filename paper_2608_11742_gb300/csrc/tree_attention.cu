@@ -811,18 +811,25 @@ __global__ void __launch_bounds__(kJoinThreads, 4) tree_combine_kernel(const Tre
     pdl_wait();
     pdl_launch_next();
     // (a call that gave up may not have written its entries: the parts are kept inside the workspace)
-    Cut mine{};
-    if (static_cast<int>(threadIdx.x) < ctas) mine = a.cut[threadIdx.x];
-    const bool is = mine.parts > 0 && mine.cta == static_cast<int>(threadIdx.x) && mine.parts <= ctas - mine.cta;
-    const uint32_t in_warp = __ballot_sync(kFull, is);
-    if (lane == 0) found[warp] = __popc(in_warp);
-    __syncthreads();
-    int rank = __popc(in_warp & ((1u << lane) - 1));
+    const auto sane = [&](const Cut &x, int cta) { return x.parts > 0 && x.cta == cta && x.parts <= ctas - cta; };
+    if (static_cast<int>(gridDim.x) == ctas) {  // a block for each CTA
+        if (threadIdx.x == 0) cut = a.cut[blockIdx.x];
+        __syncthreads();
+        if (!sane(cut, blockIdx.x)) return;
+    } else {
+        Cut mine{};
+        if (static_cast<int>(threadIdx.x) < ctas) mine = a.cut[threadIdx.x];
+        const bool is = sane(mine, threadIdx.x);
+        const uint32_t in_warp = __ballot_sync(kFull, is);
+        if (lane == 0) found[warp] = __popc(in_warp);
+        __syncthreads();
+        int rank = __popc(in_warp & ((1u << lane) - 1));
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) rank += w < warp ? found[w] : 0;
-    if (is && rank == static_cast<int>(blockIdx.x)) cut = mine;
-    __syncthreads();
-    if (cut.parts == 0) return;
+        for (int w = 0; w < kJoinWarps; ++w) rank += w < warp ? found[w] : 0;
+        if (is && rank == static_cast<int>(blockIdx.x)) cut = mine;
+        __syncthreads();
+        if (cut.parts == 0) return;
+    }
     // the warp's task: its 32 rows (of up to 256), its 16 columns
     const int task = blockIdx.y * (kJoinWarps / split) + warp / split, which = warp % split;
     const int group = task % (kD / kJoinCols) * kJoinGroups, row2 = task / (kD / kJoinCols) * 32 + lane;
