@@ -177,26 +177,31 @@ __device__ __forceinline__ void find_range(const TreeArgs &a, Ctl &c) {
         if (e < n_seq && n_seq <= kStagedSeqs) c.seq[e] = q;
         places = tree::places_of(a.s, q, &longest);
     };
+    // The CTA's unit by its number. (A thread has its sequence.)
+    const auto take_unit = [&](int me) {
+        const int pairs = tree::pairs_of(a.s, q), units = pairs * a.s.heads;
+        const int first = static_cast<int>(scan_block(units, c.scan, &total));
+        if (me >= first && me < first + units) {
+            const int u = me - first, h = u / pairs, p = u - h * pairs;
+            c.walk = Walk{static_cast<int>(threadIdx.x), h, p, 0, tree::cost_of(a.s, q, p)};
+        }
+    };
+    const int grid = gridDim.x, me = blockIdx.x;
+    if (a.whole) {
+        look(threadIdx.x);
+        return take_unit(me);
+    }
 #pragma unroll 1
     for (int base = 0; base < n_seq; base += kThreads) {
         look(base + threadIdx.x);
         before = scan_block(places, c.scan, &total);
         work += total;
     }
-    const int grid = gridDim.x, me = blockIdx.x;
-    if (a.few) {  // (a thread has its sequence)
+    if (a.few) {
         const int most = __reduce_max_sync(kFull, longest);
         if ((threadIdx.x & 31) == 0 && most) atomicMax(&c.longest, most);
         __syncthreads();
-        if (a.whole || c.longest <= tree::divide(work, grid) + tree::kCutCost) {
-            const int pairs = tree::pairs_of(a.s, q), units = pairs * a.s.heads;
-            const int first = static_cast<int>(scan_block(units, c.scan, &total));
-            if (me >= first && me < first + units) {
-                const int u = me - first, h = u / pairs, p = u - h * pairs;
-                c.walk = Walk{static_cast<int>(threadIdx.x), h, p, 0, tree::cost_of(a.s, q, p)};
-            }
-            return;
-        }
+        if (c.longest <= tree::divide(work, grid) + tree::kCutCost) return take_unit(me);
     }
     if (work == 0) return;
     const int n = work < static_cast<int64_t>(grid) * tree::kPairCost ? max(1, static_cast<int>(work) / tree::kPairCost) : grid;
