@@ -300,9 +300,9 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
                     int4 at = from[0];
 #pragma unroll 1
                     for (int i = 1; i <= copies; ++i, dst += kGroup / 8 << a.copies.copy_log) {
-                        const int4 following = from[i & 15];
+                        const int4 after = from[i & 15];
                         tma_load_5d(dst, tm, 0, at.x, 0, at.y, at.z, &full[s]);
-                        at = following;
+                        at = after;
                     }
                     if (is_k && j + done == p.j0) {
                         // Q, once the scores of the buffer's last piece are computed

@@ -100,6 +100,19 @@ def test_types_layers_and_layouts(dtype, tokens_first):
     assert bool((wide[..., 2 * D:] == 7.0).all()) and torch.equal(view(wide, 0).cpu(), c.q)
 
 
+@pytest.mark.parametrize("n_q", [5, 40])
+def test_rows_off_the_sectors(n_q):
+    """Queries and outputs whose rows begin 16 bytes off the 32-byte bounds: bit for bit as others; units whole and cut."""
+    c = Tree(49, [[90], [5000]], n_q, 8, 2, 16)
+    first, z = c.run()
+    wide = torch.full((2, 1, n_q, 8, D + 8), 7.0, dtype=c.dtype, device="cuda")
+    wide[..., 8:] = c.dq
+    c.dq = wide[..., 8:]
+    to = torch.full_like(wide, 7.0)
+    out, lse = c.run(to[..., 8:])
+    assert torch.equal(out, first) and torch.equal(lse, z) and bool((to[..., :8] == 7.0).all())
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("ps", [16, 256])
 def test_pages_at_odd_strides(ps, dtype):
