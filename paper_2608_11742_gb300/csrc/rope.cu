@@ -17,13 +17,15 @@
 // side, so its lanes compute the token's sines and cosines once, share them through shared
 // memory, and multiply them with the weights once:
 //   z0 = r ((w0 cos) y0 - (w1 sin) y1),  z1 = r ((w1 cos) y1 + (w0 sin) y0),  r = 1 / sqrt(..),
-// two pairs to an instruction (packed fp32).
+// two pairs to an instruction (packed fp32). A lane whose elements are not rotated leaves the sines' products
+// out (0 times an infinity is NaN), and without a norm its elements go through bit for bit.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "rps_internal.cuh"
 #include "tc_device.cuh"
@@ -114,6 +116,13 @@ __device__ __forceinline__ void narrow16(const f2 (&y0)[4], const f2 (&y1)[4], b
     }
 }
 
+// c += a b in the lanes where `is` (a predicate; as a branch: 45.5 us instead of 44.2 for the append below)
+__device__ __forceinline__ void fma2_if(f2 &c, f2 a, f2 b, bool is) {
+    asm("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\t@p fma.rn.f32x2 %0, %1, %2, %0;\n\t}"
+        : "+l"(c)
+        : "l"(a), "l"(b), "r"(static_cast<uint32_t>(is)));
+}
+
 __device__ __forceinline__ void copy_async(uint32_t to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
@@ -128,7 +137,10 @@ __device__ __forceinline__ void copies_wait() {
 // Rows come through shared memory, three passes ahead (seven: 54 us instead of 45 for 16222 tokens of 28 and
 // 4 heads). In registers they took a loop unrolled by four in which no side could follow the other, so
 // that a task was one side's, and the few keys' warps had a pass in flight (54 us).
-template <bool kF16, int kLanes, bool kPaged>
+// kAll: all elements of a head are rotated. Where some are not, leaving them alone costs 1 to 2 % on sides with a norm
+// (16222 tokens of 64 heads, R 96: 81.7 -> 82.9 us; without one 81.0 -> 80.5) and as much in the cache's kernel
+// (576 x 1 to 32 tokens of 32/8 heads, R 64, no norm: 43.7 -> 44.2).
+template <bool kF16, int kLanes, bool kPaged, bool kAll>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
     __shared__ float2 turned[kWarps][kMaxDim / 2];
     __shared__ uint4 ring[kWarps][kAhead][64];  // the rows of a pass one after another
@@ -230,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
     char *to = nullptr;
     int at = 0;
     int64_t step = 0;
-    bool normed = false, value = false, stored = false;
+    bool normed = false, as_is = false, stored = false;
 #pragma unroll 1
     for (int p = p_lo; p < p_hi; ++p) {
         if (a.interleaved) __syncwarp();  // (all lanes have taken the pass before, whose place is free)
@@ -239,14 +251,15 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
             int first;
             d = &side_of(p, first);
             const bool to_cache = kPaged && p >= a.passes_q;
-            value = kPaged && p >= a.passes_q + a.passes_k;
             normed = d->weight != nullptr;
+            // values, and what has neither norm nor rotation, without arithmetic (all lanes alike on a normed side)
+            as_is = kPaged && (p >= a.passes_q + a.passes_k || (!kAll && !normed && !rotates));
             at = (p - first) * kAt + of_pass;
             stored = there && (!to_cache || place >= 0);
             const int64_t head = to_cache ? a.head_stride : d->dst_head;
             to = d->dst + at * head + (to_cache ? place : s * d->dst_seq + i * d->dst_token);
             step = kAt * head;
-            if (!value) {
+            if (!as_is) {
                 f2 w0[4] = {one, one, one, one}, w1[4] = {one, one, one, one};
                 if (normed && there)
                     widen16<kF16>(*reinterpret_cast<const uint4 *>(static_cast<const char *>(d->weight) + u0),
@@ -266,7 +279,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
         if (a.interleaved) __syncwarp();
         const uint32_t slot = slots + p % kAhead * kSlot;
         uint4 raw0 = ld_shared_v4(slot + u0), raw1 = ld_shared_v4(slot + u1);
-        if (!value) {
+        if (!as_is) {
             f2 y0[4], y1[4];
             widen16<kF16>(raw0, raw1, !halves, y0, y1);
             float r = 1.f;
@@ -284,7 +297,15 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
             const f2 rr = pack2(r, r);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                f2 z0 = fma2(s1[j], y1[j], mul2(c0[j], y0[j])), z1 = fma2(s0[j], y0[j], mul2(c1[j], y1[j]));
+                f2 z0, z1;
+                if (kAll) {
+                    z0 = fma2(s1[j], y1[j], mul2(c0[j], y0[j])), z1 = fma2(s0[j], y0[j], mul2(c1[j], y1[j]));
+                } else {
+                    z0 = mul2(c0[j], y0[j]);
+                    fma2_if(z0, s1[j], y1[j], rotates);
+                    z1 = mul2(c1[j], y1[j]);
+                    fma2_if(z1, s0[j], y0[j], rotates);
+                }
                 if (normed) {
                     z0 = mul2(z0, rr);
                     z1 = mul2(z1, rr);
@@ -293,6 +314,12 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs a) {
                 y1[j] = z1;
             }
             narrow16<kF16>(y0, y1, !halves, raw0, raw1);
+        }
+        // (from tensor to tensor such lanes go along and take their elements again: a jump around the arithmetic took
+        // 83.9 us instead of 82.9 for the 16222 tokens above; in the cache's kernel this took 50.2 instead of 44.2)
+        if (!kPaged && !kAll && !normed && !rotates) {
+            raw0 = ld_shared_v4(slot + u0);
+            raw1 = ld_shared_v4(slot + u1);
         }
         if (stored && at < d->heads) {
             *reinterpret_cast<uint4 *>(to + u0) = raw0;
@@ -369,9 +396,13 @@ rps_status launch_rotate(RotateArgs &a, int32_t n_seq, bool f16, cudaStream_t st
     a.tasks = tokens * a.chunks;
     const int64_t blocks = (a.tasks + kWarps - 1) / kWarps;
     if (blocks > INT32_MAX) return RPS_ERR_UNSUPPORTED;
-    const auto kernel = lanes == 4   ? (f16 ? rotate_kernel<true, 4, kPaged> : rotate_kernel<false, 4, kPaged>)
-                        : lanes == 8 ? (f16 ? rotate_kernel<true, 8, kPaged> : rotate_kernel<false, 8, kPaged>)
-                                     : (f16 ? rotate_kernel<true, 16, kPaged> : rotate_kernel<false, 16, kPaged>);
+    const auto pick = [&](auto all) {
+        constexpr bool kAll = decltype(all)::value;
+        return lanes == 4   ? (f16 ? rotate_kernel<true, 4, kPaged, kAll> : rotate_kernel<false, 4, kPaged, kAll>)
+               : lanes == 8 ? (f16 ? rotate_kernel<true, 8, kPaged, kAll> : rotate_kernel<false, 8, kPaged, kAll>)
+                            : (f16 ? rotate_kernel<true, 16, kPaged, kAll> : rotate_kernel<false, 16, kPaged, kAll>);
+    };
+    const auto kernel = a.R == a.D ? pick(std::true_type{}) : pick(std::false_type{});
     return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a) == cudaSuccess ? RPS_OK
                                                                                                                 : RPS_ERR_CUDA;
 }

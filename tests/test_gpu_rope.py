@@ -269,6 +269,78 @@ def test_on_a_side_stream_and_from_a_graph():
     assert torch.equal(out, first) and int((a.kv.k != 0).sum()) > 0
 
 
+def any_bits(rng, dtype, *shape):
+    """Every kind of 16-bit pattern: zeros of both signs, the smallest, infinities, NaN with their payloads."""
+    x = rng.integers(-2 ** 15, 2 ** 15, shape).astype(np.int16)
+    x.reshape(-1)[::5] = rng.choice(np.array([0, -2 ** 15, 1, 0x7f80, -0x80, 0x7c00, -0x400, 0x7fff, 0x7f81], np.int16), x.reshape(-1)[::5].size)
+    return torch.from_numpy(x).cuda().view(dtype)
+
+
+def bits(x):
+    return x.contiguous().view(torch.int16)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,R", [(128, 96), (128, 16), (128, 0), (64, 16), (16, 0), (96, 48), (256, 208), (208, 64)])
+def test_elements_that_are_not_rotated_stay_as_they_are(D, R, interleaved, dtype):
+    """A side without norm: bit for bit past the rotated elements, whatever they hold, which also changes no rotated one."""
+    rng = np.random.default_rng(39)
+    rope, _, _ = make_rope(rng, D, R, dtype, (False, False), interleaved)
+    for heads in (1, 5, 40):
+        q, k, pos = normal(rng, dtype, 2, 3, heads, D), normal(rng, dtype, 2, 3, 2, D), i32(rng.integers(0, 9999, (2, 3)))
+        clean = torch.empty_like(q)
+        rps.rps_rope_heads(rope, q, clean, pos=pos)
+        q[..., R:], k[..., R:] = any_bits(rng, dtype, 2, 3, heads, D - R), any_bits(rng, dtype, 2, 3, 2, D - R)
+        out, k_out = torch.empty_like(q), torch.empty_like(k)
+        rps.rps_rope_heads(rope, q, out, k, k_out, pos)
+        assert torch.equal(bits(out[..., R:]), bits(q[..., R:])) and torch.equal(bits(k_out[..., R:]), bits(k[..., R:]))
+        assert torch.equal(bits(out[..., :R]), bits(clean[..., :R]))
+        # the other side's norm is no matter
+        half, _, (wq, _) = make_rope(rng, D, R, dtype, (True, False), interleaved)
+        rps.rps_rope_heads(half, clean, out, k, k_out, pos)
+        assert torch.equal(bits(k_out[..., R:]), bits(k[..., R:]))
+        check(out, clean, wq, half._made_of[0], interleaved, pos.cpu().numpy(), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("R", [0, 16, 64, 112])
+def test_normed_elements_that_are_not_rotated_take_nothing_from_others(R, interleaved, dtype):
+    """With a norm an infinity is NaN and the finite elements are zeros, by the formula x w / inf; zeros keep their signs."""
+    rng = np.random.default_rng(40)
+    D = 128
+    rope, _, (w, _) = make_rope(rng, D, R, dtype, (True, True), interleaved)
+    assert bool((w > 0).any()) and bool(torch.isfinite(w).all())
+    for at in (R, R + 1, R + 8, (R + D) // 2, D - 1):
+        q = normal(rng, dtype, 1, 2, 5, D)
+        q[0, 0, 1, at], q[0, 1, 3, at] = float("inf"), -float("inf")
+        q[0, 0, 2, at] = -0.0
+        out = torch.empty_like(q)
+        rps.rps_rope_heads(rope, q, out)
+        assert bool(torch.isnan(out[0, 0, 1, at])) and bool(torch.isnan(out[0, 1, 3, at]))
+        rest = [i for i in range(D) if i != at]
+        assert bool((out[0, 0, 1, rest] == 0).all()) and bool((out[0, 1, 3, rest] == 0).all())
+        assert bool(out[0, 0, 2, at] == 0) and bool(torch.signbit(out[0, 0, 2, at]) != torch.signbit(w[at]))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("R", [None, 0, 64])
+def test_append_of_rows_that_hold_anything(R, dtype):
+    """Without rotation and norm, keys, values and queries bit for bit, as rps_kv_write has them; with R, past it."""
+    rng = np.random.default_rng(41)
+    a, b = (Append(42, [[60, 33], [20, 90]], 6, 2, 16, 7, dtype) for _ in range(2))
+    rope = None if R is None else make_rope(rng, 128, R, dtype, (False, False))[0]
+    r = R or 0
+    a.rows[..., r:] = any_bits(rng, dtype, *a.rows.shape[:-1], 128 - r)
+    out = torch.empty_like(a.q)
+    rps.rps_kv_append(a.kv, 1, rope, a.kn, a.vn, a.q, out)
+    rps.rps_kv_write(b.kv, 1, a.kn.contiguous(), a.vn.contiguous())
+    assert rps.rps_poll_device_status()[0] == rps.RPS_OK
+    assert torch.equal(bits(out[..., r:]), bits(a.q[..., r:]))
+    assert torch.equal(bits(a.kv.k[..., r:]), bits(b.kv.k[..., r:])) and torch.equal(bits(a.kv.v), bits(b.kv.v))
+
+
 def test_refusals_of_the_binding():
     rng = np.random.default_rng(37)
     bf16 = torch.bfloat16
