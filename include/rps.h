@@ -774,9 +774,9 @@ typedef struct {
     float scale;
 } rps_tree_attention;
 
-/* Workspace bytes of rps_tree_attention_fwd (0 for invalid arguments). The workspace needs
- * no initialisation and keeps nothing between calls; one workspace must not serve two calls
- * that can overlap. */
+/* Workspace bytes of rps_tree_attention_fwd (0 for invalid arguments). The workspace begins on
+ * a 16-byte bound, needs no initialisation and keeps nothing between calls; one workspace must
+ * not serve two calls that can overlap. */
 size_t rps_tree_attention_workspace_bytes(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads);
 
 /* One or two launches on `stream`. Errors: RPS_ERR_INVALID_ARG for NULL or misaligned pointers,

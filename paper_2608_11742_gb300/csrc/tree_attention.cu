@@ -920,13 +920,6 @@ rps_status check_tree_shape(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads
     return RPS_OK;
 }
 
-size_t tree_part_bytes(const Shape &s, size_t *ml_at, size_t *o_at) {
-    const size_t slots = 2 * kMaxCtas * 2 * tree::kRows;
-    *ml_at = (sizeof(Cut) * kMaxCtas + 255) / 256 * 256;
-    *o_at = *ml_at + sizeof(float2) * slots;
-    return *o_at + sizeof(float) * slots * kD;
-}
-
 }  // namespace
 }  // namespace rps
 
@@ -935,8 +928,7 @@ using namespace rps;
 extern "C" size_t rps_tree_attention_workspace_bytes(const rps_kv_cache *kv, int32_t n_q, int32_t n_heads) {
     Shape s;
     if (check_tree_shape(kv, n_q, n_heads, 0, &s) != RPS_OK) return 0;
-    size_t ml, o;
-    return tree_part_bytes(s, &ml, &o);
+    return tree::workspace_at(0, sizeof(Cut), kD).bytes;
 }
 
 extern "C" rps_status rps_tree_attention_fwd(const rps_tree_attention *p, const rps_kv_cache *kv, void *d_ws, size_t ws_bytes,
@@ -954,9 +946,8 @@ extern "C" rps_status rps_tree_attention_fwd(const rps_tree_attention *p, const 
     const int64_t os[3] = {p->out_head_stride, p->out_token_stride, p->out_seq_stride};
     for (int i = 0; i < 3; ++i)
         if (ext[i] > 1 && (qs[i] <= 0 || os[i] <= 0 || qs[i] % 8 || os[i] % 8)) return RPS_ERR_INVALID_ARG;
-    size_t ml_at, o_at;
-    if (!d_ws || reinterpret_cast<uintptr_t>(d_ws) % 16 || ws_bytes < tree_part_bytes(a.s, &ml_at, &o_at))
-        return RPS_ERR_INVALID_ARG;
+    const tree::Workspace w = tree::workspace_at(reinterpret_cast<uintptr_t>(d_ws), sizeof(Cut), kD);
+    if (!d_ws || reinterpret_cast<uintptr_t>(d_ws) % tree::kBaseAlign || ws_bytes < w.bytes) return RPS_ERR_INVALID_ARG;
     int sms = 0;
     if ((st = tree_setup(&sms)) != RPS_OK) return st;
     const Encoder encode = tensor_map_encoder();
@@ -982,9 +973,9 @@ extern "C" rps_status rps_tree_attention_fwd(const rps_tree_attention *p, const 
     a.paired = p->n_q > a.s.tokens;
     a.sectors = (reinterpret_cast<uintptr_t>(p->out) | static_cast<uintptr_t>(2 * (a.out_seq | a.out_token | a.out_head))) % 32 == 0;
     char *ws = static_cast<char *>(d_ws);
-    a.cut = reinterpret_cast<Cut *>(ws);
-    a.part_ml = reinterpret_cast<float2 *>(ws + ml_at);
-    a.part_o = reinterpret_cast<float *>(ws + o_at);
+    a.cut = reinterpret_cast<Cut *>(ws + w.cut);
+    a.part_ml = reinterpret_cast<float2 *>(ws + w.ml);
+    a.part_o = reinterpret_cast<float *>(ws + w.o);
     a.tries = static_cast<uint32_t>(std::min<uint64_t>((ring_wait_limit_ns() + 999) / 1000, 1u << 30));
 
     // CTAs: as many as there can be key tiles

@@ -13,6 +13,7 @@
 // several CTAs, whose partial results are joined afterwards.
 #pragma once
 
+#include <stddef.h>
 #include <stdint.h>
 
 #include "prefix_split.h"
@@ -221,6 +222,23 @@ PREFIX_HD int64_t places_of(const Shape &s, const Seq &q, int *longest) {
         head += cost;
     }
     return head * s.heads;
+}
+
+// A call's workspace, as offsets from its base: the cuts, maximum and sum of the partial results' rows, their
+// columns. Columns are written and read 32 bytes at a time, and the base is a multiple of 16 only: the layout
+// begins on the next 32-byte bound, for which `bytes` has room whatever the base.
+constexpr size_t kPartAlign = 32, kBaseAlign = 16;
+struct Workspace {
+    size_t cut, ml, o, bytes;
+};
+inline Workspace workspace_at(uintptr_t base, size_t cut_bytes, int columns) {
+    const size_t slots = 2 * kMaxCtas * 2 * kRows;
+    Workspace w;
+    w.cut = (kPartAlign - base % kPartAlign) % kPartAlign;
+    w.ml = w.cut + (cut_bytes * kMaxCtas + 255) / 256 * 256;
+    w.o = w.ml + 2 * sizeof(float) * slots;
+    w.bytes = w.o - w.cut + sizeof(float) * slots * columns + kPartAlign - kBaseAlign;
+    return w;
 }
 
 }  // namespace tree

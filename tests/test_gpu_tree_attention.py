@@ -280,6 +280,23 @@ def test_a_workspace_of_any_content(fill):
     c.check(out, lse)
 
 
+@pytest.mark.parametrize("n_q", [3, 40])
+def test_a_workspace_on_any_16_byte_bound(n_q):
+    """Cut units in a workspace that begins 0, 16 and 48 bytes past a bound of 256: the same bits, nothing written around it."""
+    c = Tree(51, LONG_AMONG_SHORT[40:], n_q, 8, 1, 64)
+    first, z = c.run()
+    c.check(first, z)
+    n = c.ws.numel()
+    for at in (0, 16, 48):
+        arena = torch.full((n + 512,), 0x5a, dtype=torch.uint8, device="cuda")
+        at += 256 - arena.data_ptr() % 256
+        c.ws = arena[at:at + n]
+        out, lse = c.run()
+        assert rps.rps_poll_device_status()[0] == rps.RPS_OK
+        assert torch.equal(out, first) and torch.equal(lse, z)
+        assert bool((arena[:at] == 0x5a).all()) and bool((arena[at + n:] == 0x5a).all())
+
+
 @pytest.mark.parametrize("sees", ["tree", "chain"])
 def test_the_largest_trees(sees):
     """1024 drafted tokens, 32 words a mask: eight pairs of row tiles; 64 with groups of 128 heads: 32 pairs of one token."""

@@ -125,6 +125,32 @@ int main(int argc, char **argv) {
 }
 """
 
+LAYOUT = r"""
+#include <cstdio>
+#include "tree_split.h"
+using namespace rps::tree;
+int main() {
+    for (uintptr_t base = 1 << 20; base < (1 << 20) + 512; base += kBaseAlign) {
+        const Workspace w = workspace_at(base, 32, 128), zero = workspace_at(0, 32, 128);
+        const size_t slots = 2 * kMaxCtas * 2 * kRows;
+        const bool good = (base + w.o) % kPartAlign == 0 && (base + w.ml) % 8 == 0 && (base + w.cut) % 16 == 0 &&
+                          w.cut + 32 * kMaxCtas <= w.ml && w.ml + 8 * slots <= w.o && w.o + 4 * slots * 128 <= w.bytes &&
+                          w.bytes == zero.bytes;
+        if (!good) return 1;
+    }
+    std::puts("ok");
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_the_parts_of_a_workspace_lie_on_their_bounds(tmp_path):
+    """Partial results are moved 32 bytes at a time, wherever a workspace begins (16-byte bounds), and lie inside it."""
+    src, exe = tmp_path / "layout.cc", tmp_path / "layout"
+    src.write_text(LAYOUT)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", f"-I{CSRC}", str(src), "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)], capture_output=True, text=True).stdout.strip() == "ok"
+
 
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
 def test_every_tile_is_taken_once(tmp_path):
