@@ -241,12 +241,12 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
     uint64_t *full = is_k ? c.k_full : c.v_full, *empty = is_k ? c.k_empty : c.v_empty;
     const int copies = tree::kRows >> a.copies.copy_log;  // of a tile, 16 at most
     const int half = lane >> 4;
-    // the page of copy lane % 16 of key tile j of a piece (-1: not a token of the sequence)
-    const auto page_of = [&](const Piece &x, int j, int &token) {
+    // the page of copy lane % 16 of key tile j of a piece (-1: not a token of the sequence; n_pages: an id outside the cache)
+    const auto page_of = [&](const Piece &x, int j, int &token) -> int {
         token = j * tree::kRows + ((lane & 15) << a.copies.copy_log);
         if ((lane & 15) >= copies || j >= x.j1 || token >= x.q.len) return -1;
-        // (a negative id is told from a token that is not there)
-        return a.table[static_cast<int64_t>(x.s) * a.s.max_pages + (token >> a.s.page_log)] & 0x7fffffff;
+        return min(static_cast<uint32_t>(a.table[static_cast<int64_t>(x.s) * a.s.max_pages + (token >> a.s.page_log)]),
+                   static_cast<uint32_t>(a.s.n_pages));
     };
     // A piece ahead: its first pages' ids are on their way while the piece before is copied, and its
     // queries in L2 (a change of units took 4.5 us, of which the lookups were 2).
@@ -270,7 +270,7 @@ __device__ __forceinline__ void produce(bool is_k, const CUtensorMap *tm, const 
 #pragma unroll 1
         for (int j = p.j0; ok && j < p.j1; j += 2) {
             const int two = min(2, p.j1 - j);
-            const bool there = id >= 0, bad_page = id >= a.s.n_pages;
+            const bool there = id >= 0, bad_page = id == a.s.n_pages;
             const int in_page = token & ((1 << a.s.page_log) - 1);
             const bool none = !there || bad_page;  // (a coordinate whose copy is all zeros)
             c.copy_at[is_k][lane] = a.copies.by_groups

@@ -216,6 +216,30 @@ def test_bad_pages_give_nan_to_the_rows_that_see_them(n_q):
         assert torch.equal(out[1, 0, :first], whole[1, 0, :first])
 
 
+@pytest.mark.parametrize("n_q", [3, 70])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_page_ids_far_outside_the_cache(n_q, pad):
+    """Ids whose low bits are those of a page of the cache are outside it, too; pages in groups of eight tokens, and one by one."""
+    for bad in (-2 ** 31, -2 ** 31 + 1, -1, 2 ** 31 - 1, 2 ** 30):
+        c = Tree(50, [[200, 190], [100, 90]], n_q, 4, 2, 16, sees="chain")
+        if pad:
+            for name in ("k", "v"):
+                t = getattr(c.kv, name)
+                to = torch.full((*t.shape[:2], t.shape[2] * 16 + pad, D), float("nan"), dtype=c.dtype, device="cuda")
+                view = to.as_strided(t.shape, (to.stride(0), to.stride(1), 16 * D, D, 1))
+                view.copy_(t)
+                setattr(c.kv, name, view)
+        whole = c.run()[0].clone()
+        c.kv.table[0, 1, 2] = bad  # tokens 32.. of 190
+        c.kv.table[1, 0, 6] = bad  # tokens 96.. of 100: drafted ones
+        out, lse = c.run()
+        assert rps.rps_poll_device_status() == (rps.RPS_ERR_DEVICE, rps.DEVERR_PAGE)
+        assert torch.equal(out[0, 0], whole[0, 0]) and torch.equal(out[1, 1], whole[1, 1])
+        assert bool(torch.isnan(out[0, 1]).all()) and bool(torch.isnan(lse[0, 1]).all())
+        first = max(0, n_q - 4)  # the query that is token 96
+        assert bool(torch.isnan(out[1, 0, first:]).all()) and torch.equal(out[1, 0, :first], whole[1, 0, :first])
+
+
 def test_lengths_beyond_the_table():
     c = Tree(34, [[100], [64]], 4, 2, 1, 16)
     width = c.table.shape[2]
