@@ -261,6 +261,41 @@ def test_more_sequences_than_a_block_has_threads(n_seq):
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("sees", ["tree", "chain"])
+@pytest.mark.parametrize("n_q", [4, 70])
+def test_lengths_beyond_the_table_count_as_its_capacity(n_q, sees):
+    """All rows, and the positions of the drafted tokens among them: bit for bit as a full table, in single row tiles and pairs."""
+    c = Tree(52, [[100], [320], [256], [320]], n_q, 4, 1, 16, sees=sees, count=[n_q, n_q - 1, n_q, 2])
+    width = c.table.shape[2] - 1  # (the case's own spare column)
+    assert width == 20
+    c.kv = rps.KvCacheBuf(c.kv.k, c.kv.v, c.kv.page_ref, c.kv.table[..., :width].contiguous(), c.kv.length)
+    first, z = c.run()
+    c.check(first, z)
+    for beyond in (321, 1000, 2 ** 31 - 1):
+        c.kv.length[1], c.kv.length[3] = beyond, beyond
+        out, lse = c.run()
+        c.check(out, lse)
+        assert torch.equal(out, first) and torch.equal(lse, z)
+
+
+@pytest.mark.parametrize("n_seq", [1023, 1024, 1025, 1500, 5000])
+@pytest.mark.parametrize("sees", ["tree", "chain"])
+def test_more_sequences_than_are_staged(n_seq, sees):
+    """Beyond 1024 every role reads the lengths and counts itself: ragged counts, absent and empty sequences, a long one."""
+    rng = np.random.default_rng(53)
+    lens = rng.integers(0, 40, (n_seq, 1))
+    lens[rng.random((n_seq, 1)) < 0.1] = -1
+    lens[400:520] = -1
+    lens[n_seq - 3], lens[n_seq - 1] = 3000, -1
+    count = rng.integers(0, 4, n_seq)
+    count[n_seq - 3] = 3
+    c = Tree(53, lens, 3, 2, 2, 16, sees=sees, count=count)
+    out, lse = c.run()
+    c.check(out, lse)
+    again = c.run()
+    assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
 @pytest.mark.parametrize("n_seq,Hk", [(150, 1), (151, 1), (152, 1), (153, 1), (154, 1), (76, 2), (77, 2)])
 def test_as_many_units_as_ctas(n_seq, Hk):
     """On both sides of the card's CTAs, units of one length and one that is longer."""
