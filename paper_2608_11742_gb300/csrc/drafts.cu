@@ -20,8 +20,11 @@ struct MaskArgs {
 
 // A block per sequence, a thread per token: it walks up to the context. A parent comes
 // before its children, so the walk goes through the words of the token's mask from the
-// last to the first, and each is written once. Bound by the walk: a step is one access
-// to shared memory, about 30 cycles.
+// last to the first, and each is written once. Bound by the walk, one dependent access to shared
+// memory an ancestor, and by its instructions: in a deep tree each step ends a word in some lane
+// of the warp, whose store the others wait for, and a block's 32 warps walk together. 500 trees of up
+// to 253 tokens with fans of 2 and 3 (depths about 8): 4.3 us; chains: 1 x 32 tokens 3.2, 1 x 253 36,
+// 500 x 253 44, 1 x 1024 190.
 __global__ void __launch_bounds__(RPS_TREE_MAX_TOKENS) tree_masks_kernel(const MaskArgs a) {
     __shared__ int32_t parent[RPS_TREE_MAX_TOKENS];
     const int i = threadIdx.x;

@@ -6,8 +6,9 @@
 // weights, else y = x; then each pair (y0, y1) of the first R elements is turned by
 // its angle a = 2 pi f t, t the position: A (y0 cos a - y1 sin a), A (y1 cos a + y0 sin a).
 // The frequency f of a pair is given in turns per position as a fraction of 2^64, so
-// t f modulo 2^64 is the fraction of a turn exactly, whatever the position: of it 32 bits
-// (1.5e-9 of a radian), half a turn at most, are left to fp32. All in fp32, rounded once at the end.
+// t f modulo 2^64 is the fraction of a turn exactly, whatever the position. It is cut to 32 bits, half a turn
+// at most (1.5e-9 of a radian), and rounded to fp32's 24: 1e-7 of a radian at most near half a turn, relative to
+// smaller angles 2^-24, as every fp32 step behind it. All in fp32, rounded once at the end.
 //
 // Bound by HBM: 4 D bytes a row (16-bit elements read and written once), as long as a pass
 // of a warp over 1024 bytes takes less than about 170 instructions (at twice as many, 576 x 32

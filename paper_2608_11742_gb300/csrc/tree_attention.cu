@@ -23,7 +23,10 @@
 //   warps 4-7   softmax of even items, 8-11 of odd ones: thread = row. One pass with a
 //               standing base-2 reference, which is changed only where a tile's sum is far
 //               out of range. P is rounded to the cache's type (the product takes no other);
-//               its sum is taken before the rounding, in fp32. Before the last key tile's P is
+//               its sum is taken before the rounding, in fp32. The output's error is 1.4 times that of
+//               its own rounding so (bf16 0.0023 instead of 0.0017, root mean square); P in two parts
+//               brings it back, at 101 us instead of 98 for 64 single tokens and 208 instead of 172 for
+//               64 x 1, 32 / 32 heads, context 1000. Before the last key tile's P is
 //               handed on, V's rows past the sequence's end are cleared (they may hold
 //               anything, and 0 * NaN would reach the sums). At a piece's end the same warps
 //               read the accumulators out.
@@ -982,7 +985,7 @@ extern "C" rps_status rps_tree_attention_fwd(const rps_tree_attention *p, const 
     const int64_t tiles = ((static_cast<int64_t>(a.s.max_pages) << a.s.page_log) + tree::kRows - 1) / tree::kRows;
     const int64_t units = static_cast<int64_t>(a.s.n_seq) * a.s.heads * a.s.pairs;
     // Where units are no more than CTAs and cannot be long, none is cut, and there is nothing to join: one launch
-    // (one sequence, 32 heads, 344 tokens: 11.5 us with two, 9 with one).
+    // (one sequence, 32 heads, 16 drafted of 344 tokens: 11.0 to 11.8 us with two, 8.9 to 9.7 with one, by the inputs).
     a.few = units <= std::min(sms, kThreads);  // (so there are no more sequences)
     a.whole = a.few && tiles <= kWholeTiles;
     const int grid = static_cast<int>(std::min<int64_t>(a.whole ? units : units * tiles, sms));
